@@ -257,7 +257,154 @@ int river_get_debug(river_ctx *ctx, int32_t what, void *dst, size_t bytes);
  * canary for slots that are read before they are written).  Asynchronous. */
 int river_fill_cache(river_ctx *ctx, int32_t value);
 
-const char *river_last_error(const river_ctx *ctx); /* ctx may be NULL: last create error */
+/* ------------------------------------------------------------------------------------------
+ * Paged key-value cache: operators over a cache of the caller that is kept in pages.
+ *
+ * A page holds page_size positions of one sequence, in every layer; a sequence's row of a page
+ * table names its pages in the order of their positions.  Sequences grow page by page, share the
+ * pages of what they have in common, and give back what a window has left behind.  The
+ * operators below need no context: they run on the stream they are given, of the device that is
+ * current, keep nothing from one call for the next, allocate nothing on the device and can be captured
+ * into a HIP graph.  (river_rope_store, river_paged_attention: the graph reads the table, the lengths and
+ * q_start anew at every replay.  river_copy_pages, river_pool_flush: page numbers are baked in.)
+ *
+ * Errors of calls without a context: river_last_error(NULL), per host thread.
+ * ------------------------------------------------------------------------------------------ */
+
+/* A cache.  HOST struct, read during the call only.  In a page the layout is
+ * [n_kv_heads][page_size][head_dim] (a head's positions are neighbours: what attention streams), for k and v alike;
+ * pages and layers may lie in either order and with gaps (k and v may be halves of one array).
+ * k, v and both strides are multiples of 16 bytes; no two pages of k, or of v, may overlap. */
+typedef struct {
+  void *k, *v;            /* DEVICE */
+  int64_t layer_stride;   /* elements from a layer's pages to the next layer's */
+  int64_t page_stride;    /* elements from a page to the next page */
+  int32_t n_layers, n_pages;
+  int32_t page_size;      /* positions of a page, 1..65536, not necessarily a power of two */
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* 64 or 128 */
+  int32_t dtype;          /* RIVER_F32 or RIVER_BF16: queries, new keys and values, outputs */
+  int32_t kv_dtype;       /* RIVER_KV_*: the pages hold dtype, or IEEE half (RIVER_BF16 only) */
+} river_pages;
+
+/* The sequences of a call and their new tokens.  HOST struct of DEVICE arrays that the kernels read.
+ * Sequence s has lens[s] positions with its new tokens, which are the tokens q_start[s] ..
+ * q_start[s+1] - 1 of the call; the last of them is at position lens[s] - 1.  Tokens from
+ * q_start[n_seq] on (a padded batch) belong to no sequence: their rows are neither read nor
+ * written.  So do tokens whose position would be negative, except that attention gives them zeros.
+ * A table entry outside [0, n_pages) is a page that is not there: its positions are not stored and not
+ * seen.  Positions from max_pages * page_size on have no page.  The q_start of a call ascends. */
+typedef struct {
+  const int32_t *table;   /* [n_seq][table_stride], the first max_pages entries of a row are used */
+  const int32_t *lens;    /* [n_seq] */
+  const int32_t *q_start; /* [n_seq + 1], or NULL: one token each (n_tokens == n_seq) */
+  int32_t n_seq, n_tokens;
+  int32_t max_pages, table_stride;
+  int32_t max_new;        /* no sequence has more new tokens (further ones would be left out) */
+  int32_t max_len;        /* no sequence has more positions: by this the work is divided (longer ones are
+                             still right, but slow) */
+} river_batch;
+
+/* Rotary positions: the first rot_dim elements of a head are pairs (x, y) that position p turns by
+ * p * inv_freq[i], times mscale: HALF pairs (i, i + rot_dim/2), INTERLEAVED (2i, 2i + 1).
+ * The other elements stay as they are. */
+enum { RIVER_ROPE_HALF = 0, RIVER_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  const double *inv_freq; /* DEVICE [rot_dim/2] radians per position: in 64 bits, because p * f of a far position
+                             needs them */
+  int32_t rot_dim;        /* even, 2..head_dim */
+  int32_t layout;         /* RIVER_ROPE_HALF or RIVER_ROPE_INTERLEAVED */
+  float mscale;           /* 1 unless a scaling wants another (river_rope_frequencies says which) */
+} river_rope;
+
+/* Frequencies of rotary positions, host arithmetic in 64 bits: f_i = base^(-2i/rot_dim), scaled for contexts
+ * `factor` times longer than original_len:
+ *   PLAIN   f_i
+ *   LINEAR  f_i / factor (positions interpolated)
+ *   BASE    base * factor^(rot_dim/(rot_dim-2)) in base's place (the slowest pair turns factor times slower; rot_dim > 2)
+ *   BANDS   by turns n_i = original_len f_i / 2 pi: f_i where n_i >= high, f_i / factor where n_i <= low,
+ *           between them f_i s + f_i/factor (1-s) with s = (n_i - low)/(high - low)
+ *   RAMP    by index: f_i (1-t) + f_i/factor t with t = clamp((i - a)/(b - a), 0, 1), a and b the indices
+ *           rot_dim ln(original_len / (2 pi n)) / (2 ln base) for n = high (rounded down, not below 0) and n = low (rounded up,
+ *           not above rot_dim - 1; b - a at least 0.001); *mscale = 0.1 ln(factor) + 1
+ * factor >= 1; low < high are numbers of turns.  PLAIN ignores factor and what follows it, LINEAR and BASE what
+ * follows factor.  inv_freq: HOST [rot_dim/2].  mscale: HOST, nullable (1 but for RAMP). */
+enum { RIVER_ROPE_PLAIN = 0, RIVER_ROPE_LINEAR = 1, RIVER_ROPE_BASE = 2, RIVER_ROPE_BANDS = 3, RIVER_ROPE_RAMP = 4 };
+int river_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                           double low, double high, double *inv_freq, float *mscale);
+
+/* Rotates the new tokens' queries and keys at their positions and writes keys and values, rounded to
+ * the cache's type, to their slots in `layer`.
+ * q: DEVICE [n_tokens][n_q_heads][head_dim], k, v: [n_tokens][n_kv_heads][head_dim], of pages->dtype, the strides in
+ * elements from a token to the next (slices of one stacked row will do; they may be any multiple of one
+ * element, but those of 16 bytes at aligned pointers are faster).  q_out: rotated queries, may be q itself with q's stride.
+ * Pages that several sequences share must not be written: river_pool_extend sees to that. */
+int river_rope_store(const river_pages *pages, int32_t layer, const river_batch *batch, const river_rope *rope,
+                     int32_t n_q_heads, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                     const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride, void *hip_stream);
+
+/* Attention of the new tokens over their sequences' pages of `layer` (the new positions' rows among them:
+ * river_rope_store comes first).  A token at position p sees j <= p; with window > 0 of these only
+ * j > p - window, and j < sinks.  out = sum_j softmax_j(scale q.k_j) v_j; a row that sees nothing, or only scores of
+ * -infinity, is zero.  What is not seen has no influence, whatever its bits (NaN, infinities).
+ * Query heads h * (n_q_heads / n_kv_heads) .. share key head h.
+ * scale: > 0, or 0 = 1/sqrt(head_dim).  window: 0 = none.  sinks: used with a window only.
+ * q, out: DEVICE [n_tokens][n_q_heads][head_dim], pages->dtype, strides in elements, multiples of 16 bytes, 16-byte aligned;
+ * out must not overlap q.  At most 2^22 tokens and sequences a call (river_rope_store too).
+ * workspace: DEVICE, 16-byte aligned, of at least the bytes that river_paged_attention_workspace gives for the
+ * same arguments (0 bytes: may be NULL); its contents mean nothing before and after the call. */
+int river_paged_attention_workspace(const river_pages *pages, const river_batch *batch, int32_t n_q_heads,
+                                    int32_t window, int32_t sinks, size_t *bytes);
+int river_paged_attention(const river_pages *pages, int32_t layer, const river_batch *batch, int32_t n_q_heads,
+                          const void *q, int64_t q_stride, float scale, int32_t window, int32_t sinks, void *out,
+                          int64_t out_stride, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Copies pages src[i] to dst[i] in every layer, keys and values, as if one pair after the other (a page may be
+ * copied several times, and be the source of a later pair; pairs that depend on each other cost a launch).
+ * src, dst: HOST [n], copied by the call, each in [0, n_pages). */
+int river_copy_pages(const river_pages *pages, const int32_t *src, const int32_t *dst, int32_t n, void *hip_stream);
+
+/*
+ * Bookkeeping of pages: which sequence has which, how many share one, which are free.  HOST only but for
+ * river_pool_flush: the other calls change the pool's records, and flush brings page copies and
+ * table up to date on the device, in stream order.  Not thread-safe.  Pages are given out lowest number first.
+ */
+typedef struct river_pool river_pool; /* opaque */
+int river_pool_create(int32_t n_pages, int32_t page_size, int32_t max_seqs, int32_t max_pages, river_pool **out);
+int river_pool_destroy(river_pool *pool); /* NULL is a no-op */
+/* n_new positions more for sequence seq.  Its last page, if it is shared and not full, becomes its own (a copy
+ * is queued).  RIVER_ENOSPC (nothing changed) if there are no pages, or the row has no room. */
+int river_pool_extend(river_pool *pool, int32_t seq, int32_t n_new);
+/* Sequence dst, which must have no positions, becomes src's twin: all pages shared. */
+int river_pool_fork(river_pool *pool, int32_t src, int32_t dst);
+/* The sequence keeps its first new_len positions (0: none; its row is empty then).  What trim gave back stays gone:
+ * RIVER_ESTATE where the last page to be kept, not full, is such a one. */
+int river_pool_rewind(river_pool *pool, int32_t seq, int32_t new_len);
+/* Gives back the pages of which no position is seen by the sequence's last position or a later one, with this window
+ * and these sinks: their entries become -1.  A page that holds the last position stays. */
+int river_pool_trim(river_pool *pool, int32_t seq, int32_t window, int32_t sinks);
+/* Moves pages (copies are queued) so that those in use are 0 .. used-1; returns the number of moves or an error. */
+int river_pool_compact(river_pool *pool);
+/* Enqueues the queued copies in `pages` and the changed lengths and table entries in `state`.
+ * state: DEVICE int32 [max_seqs] lengths, then [max_seqs][max_pages] the table, kept by the caller from the first flush on
+ * (the first one writes all of it).  pages: its n_pages and page_size must be the pool's; may be NULL if no copy is queued. */
+int river_pool_flush(river_pool *pool, const river_pages *pages, int32_t *state, void *hip_stream);
+int river_pool_length(const river_pool *pool, int32_t seq);         /* positions, or a negative error */
+int river_pool_free_pages(const river_pool *pool);                  /* pages nobody has, or a negative error */
+int river_pool_row(const river_pool *pool, int32_t seq, int32_t *row); /* HOST [max_pages]: the sequence's entries */
+
+/* Copies positions first .. first + n - 1 of a context's sequence, in all layers, to the pages that `row` (DEVICE
+ * [max_pages]) names, rotated keys as the context keeps them; the pages' shape and types must be the context's.  A prompt that
+ * was prefilled once can then be given to other sequences and contexts with river_load_pages.  Runs on the context's stream. */
+int river_save_pages(river_ctx *ctx, int32_t seq, int32_t first, int32_t n, const river_pages *pages,
+                     const int32_t *row, int32_t max_pages);
+/* The reverse: positions 0 .. n - 1 of sequence seq come from pages, and the sequence has n positions afterwards,
+ * as after a prefill that produced next_token.  Pages that are not there leave their positions' rows as they were.
+ * Clears a device-side time-out as a prefill does. */
+int river_load_pages(river_ctx *ctx, int32_t seq, int32_t n, int32_t next_token, const river_pages *pages,
+                     const int32_t *row, int32_t max_pages);
+
+const char *river_last_error(const river_ctx *ctx); /* ctx may be NULL: last error of a call without a context */
 int river_destroy(river_ctx *ctx);                  /* NULL is a no-op */
 
 #ifdef __cplusplus

@@ -23,7 +23,13 @@ EXIT_PER_SEQUENCE, EXIT_BATCH_MIN = 0, 1
 EXPORTS = ("river_quantize_w4", "river_workspace_bytes", "river_create", "river_create_static", "river_prefill",
            "river_decode_step", "river_decode_batch", "river_read_batch_records", "river_read_records",
            "river_rewind", "river_position", "river_seq_position",
-           "river_get_debug", "river_fill_cache", "river_last_error", "river_destroy")
+           "river_get_debug", "river_fill_cache", "river_last_error", "river_destroy",
+           "river_rope_frequencies", "river_rope_store", "river_paged_attention_workspace", "river_paged_attention",
+           "river_copy_pages", "river_pool_create", "river_pool_destroy", "river_pool_extend", "river_pool_fork",
+           "river_pool_rewind", "river_pool_trim", "river_pool_compact", "river_pool_flush", "river_pool_length",
+           "river_pool_free_pages", "river_pool_row", "river_save_pages", "river_load_pages")
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
 
 class RiverError(RuntimeError):
@@ -53,6 +59,20 @@ class river_weights(C.Structure):
 
 class river_qweights(C.Structure):
     _fields_ = [("codes", _PP * 7), ("scale", _PP * 7), ("zero", _PP * 7)]
+
+
+class river_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("page_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "kv_dtype")]
+
+
+class river_batch(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("lens", C.c_void_p), ("q_start", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_seq", "n_tokens", "max_pages", "table_stride", "max_new", "max_len")]
+
+
+class river_rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("mscale", C.c_float)]
 
 
 _lib = None
@@ -92,6 +112,18 @@ def load():
     L.river_last_error.argtypes = [C.c_void_p]
     L.river_last_error.restype = C.c_char_p
     L.river_destroy.argtypes = [C.c_void_p]
+    i32, i64, f64, ptr, pages, batch = C.c_int32, C.c_int64, C.c_double, C.c_void_p, C.POINTER(river_pages), C.POINTER(river_batch)
+    L.river_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, ptr, C.POINTER(C.c_float)]
+    L.river_rope_store.argtypes = [pages, i32, batch, C.POINTER(river_rope), i32, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr]
+    L.river_paged_attention_workspace.argtypes = [pages, batch, i32, i32, i32, C.POINTER(C.c_size_t)]
+    L.river_paged_attention.argtypes = [pages, i32, batch, i32, ptr, i64, C.c_float, i32, i32, ptr, i64, ptr, C.c_size_t, ptr]
+    L.river_copy_pages.argtypes = [pages, ptr, ptr, i32, ptr]
+    L.river_pool_create.argtypes = [i32, i32, i32, i32, C.POINTER(ptr)]
+    for name, more in (("destroy", []), ("extend", [i32, i32]), ("fork", [i32, i32]), ("rewind", [i32, i32]), ("trim", [i32, i32, i32]),
+                       ("compact", []), ("flush", [pages, ptr, ptr]), ("length", [i32]), ("free_pages", []), ("row", [i32, ptr])):
+        getattr(L, "river_pool_" + name).argtypes = [ptr, *more]
+    L.river_save_pages.argtypes = [ptr, i32, i32, i32, pages, ptr, i32]
+    L.river_load_pages.argtypes = [ptr, i32, i32, i32, pages, ptr, i32]
     _lib = L
     return L
 
@@ -293,6 +325,18 @@ class River:
         self._check(load().river_get_debug(self._h, DBG_BATCH_LOGITS, out.ctypes.data, out.nbytes))
         return out
 
+    def save_pages(self, pages: "Pages", row: torch.Tensor, n: int, first: int = 0, seq: int = 0):
+        """Positions first .. first + n - 1 of the sequence to the pages that `row` (device int32) names."""
+        _check_on(pages.device, torch.int32, row=row)
+        assert row.dim() == 1 and row.is_contiguous()
+        self._check(load().river_save_pages(self._h, seq, first, n, pages.ref, row.data_ptr(), row.numel()))
+
+    def load_pages(self, pages: "Pages", row: torch.Tensor, n: int, next_token: int, seq: int = 0):
+        """Positions 0 .. n - 1 of the sequence from pages; next_token is what its next step consumes by default."""
+        _check_on(pages.device, torch.int32, row=row)
+        assert row.dim() == 1 and row.is_contiguous()
+        self._check(load().river_load_pages(self._h, seq, n, int(next_token), pages.ref, row.data_ptr(), row.numel()))
+
     def read_records(self, n: int):
         toks = np.empty(n, dtype=np.int32)
         es = np.empty(n, dtype=np.int32)
@@ -348,6 +392,235 @@ class River:
 
     def fill_cache(self, byte: int):
         self._check(load().river_fill_cache(self._h, byte))
+
+
+# ------------------------------------------------------------------ paged key-value cache
+
+def _check_call(rc: int):
+    if rc < 0:
+        raise RiverError(rc, load().river_last_error(None).decode())
+    return rc
+
+
+def _check_on(device, dtype, **tensors):
+    for name, t in tensors.items():
+        if t.device != device or t.dtype != dtype:
+            raise ValueError(f"{name}: {dtype} on {device} is needed, not {t.dtype} on {t.device}")
+
+
+def _on_stream(device, call, *args):
+    """The call on the device's current torch stream (the library takes the stream of the current device)."""
+    if device.index == torch.cuda.current_device():
+        return _check_call(call(*args, torch.cuda.current_stream().cuda_stream))
+    with torch.cuda.device(device):
+        return _check_call(call(*args, torch.cuda.current_stream().cuda_stream))
+
+
+class Pages:
+    """A paged cache: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (the last three dimensions
+    contiguous, the strides of k and v alike), in the dtype of the activations (fp32, bf16) or, with bf16 ones, fp16."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, dtype: torch.dtype | None = None):
+        dtype = k.dtype if dtype is None else dtype
+        if not k.is_cuda or k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or v.device != k.device or v.dtype != k.dtype:
+            raise ValueError("k and v: device tensors [layers, pages, heads, page_size, head_dim] of one shape, type and layout")
+        layers, pages, heads, size, hd = k.shape
+        if k.stride()[2:] != (size * hd, hd, 1):
+            raise ValueError("a page's heads, positions and elements must be contiguous")
+        if (dtype, k.dtype) not in ((torch.float32,) * 2, (torch.bfloat16,) * 2, (torch.bfloat16, torch.float16)):
+            raise ValueError(f"no cache of {k.dtype} for {dtype}")
+        self.k, self.v, self.dtype, self.device = k, v, dtype, k.device
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.c = river_pages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), layers, pages, size, heads, hd,
+                             0 if dtype == torch.float32 else 1, 1 if k.dtype == torch.float16 else 0)
+        self.ref = C.byref(self.c)
+        self.shape_key = (heads, size, hd, dtype)
+
+
+class Batch:
+    """The sequences of a call: table [n_seq, max_pages], lens [n_seq] and q_start [n_seq + 1] (None: one new token per
+    sequence), int32 on the device and read there at every call; max_new and max_len (default: what the table holds) bound
+    the new tokens and the lengths."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor | None = None, max_new: int = 1,
+                 max_len: int | None = None):
+        _check_on(table.device, torch.int32, table=table, lens=lens, **({} if q_start is None else {"q_start": q_start}))
+        n = lens.numel()
+        if not table.is_cuda or table.dim() != 2 or table.shape[0] != n or table.shape[1] < 1 or lens.dim() != 1:
+            raise ValueError("table [n_seq, max_pages] and lens [n_seq] on the device")
+        if (table.shape[1] > 1 and table.stride(1) != 1) or (n > 1 and table.stride(0) < table.shape[1]) or not lens.is_contiguous():
+            raise ValueError("rows of the table and lens must be contiguous")
+        if q_start is not None and (q_start.shape != (n + 1,) or not q_start.is_contiguous()):
+            raise ValueError("q_start [n_seq + 1]")
+        if q_start is None and max_new != 1:
+            raise ValueError("without q_start every sequence has one new token")
+        self.table, self.lens, self.q_start, self.device, self.n_seq = table, lens, q_start, table.device, n
+        self.max_len, self.max_new = max_len, max_new
+        self._calls, self._bytes = {}, {}       # the C struct, and the workspace, of a shape of call
+
+    def bind(self, n_tokens: int, pages: Pages):
+        """The call's C struct (one per number of tokens and page size: never changed once made)."""
+        if pages.device != self.device:
+            raise ValueError("pages and batch are on different devices")
+        got = self._calls.get((n_tokens, pages.page_size))
+        if got is None:
+            most = self.table.shape[1]
+            c = river_batch(self.table.data_ptr(), self.lens.data_ptr(), None if self.q_start is None else self.q_start.data_ptr(), self.n_seq,
+                            n_tokens, most, self.table.stride(0) if self.n_seq > 1 else most, self.max_new,
+                            min(2**31 - 1, most * pages.page_size) if self.max_len is None else self.max_len)
+            if len(self._calls) >= 256:
+                self._calls, self._bytes = {}, {}
+            got = self._calls[(n_tokens, pages.page_size)] = C.byref(c)
+        return got
+
+
+class Rope:
+    """Rotary positions: inv_freq float64 [rot_dim / 2] on the device (see rope_frequencies), layout "half" or "interleaved"."""
+
+    def __init__(self, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0):
+        if not inv_freq.is_cuda or inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq: float64 [rot_dim / 2] on the device")
+        self.inv_freq, self.device = inv_freq, inv_freq.device
+        self.c = river_rope(inv_freq.data_ptr(), 2 * inv_freq.numel(), ROPE_LAYOUTS[layout], mscale)
+        self.ref = C.byref(self.c)
+
+
+def river_rope_frequencies(rot_dim: int, base: float, scaling: str = "plain", factor: float = 1.0, original_len: float = 0.0,
+                           low: float = 1.0, high: float = 32.0):
+    """(frequencies as a numpy array of float64, what cosines and sines are multiplied with)."""
+    f, m = np.empty(max(rot_dim // 2, 1), dtype=np.float64), C.c_float()
+    _check_call(load().river_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, original_len, low, high, f.ctypes.data,
+                                              C.byref(m)))
+    return f, m.value
+
+
+def _rows(name: str, t: torch.Tensor, pages: Pages, heads: int | None = None) -> int:
+    """[n_tokens, heads, head_dim] with contiguous heads: the stride between tokens."""
+    if t.dtype != pages.dtype or t.device != pages.device or t.dim() != 3 or t.shape[2] != pages.head_dim:
+        raise ValueError(f"{name}: {pages.dtype} [n_tokens, heads, {pages.head_dim}] on {pages.device}")
+    n, h, hd = t.shape
+    if (heads is not None and h != heads) or t.stride(2) != 1 or (h > 1 and t.stride(1) != hd):
+        raise ValueError(f"{name}: wrong number of heads, or a token's heads are not contiguous")
+    return t.stride(0) if n > 1 else h * hd
+
+
+def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope: Rope,
+                     out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rotates q and k [n_tokens, heads, head_dim] at the new tokens' positions and stores k and v in the pages.  Returns the
+    rotated queries: `out`, which may be q, or a new tensor (rows of tokens that belong to no sequence are not written)."""
+    n = q.shape[0]
+    qs, ks, vs = _rows("q", q, pages), _rows("k", k, pages, pages.n_kv_heads), _rows("v", v, pages, pages.n_kv_heads)
+    if k.shape[0] != n or v.shape[0] != n or rope.device != pages.device:
+        raise ValueError("q, k and v must have the same tokens, and the frequencies their device")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    os_ = _rows("out", out, pages, q.shape[1])
+    if out.shape[0] != n:
+        raise ValueError("out must have q's shape")
+    _on_stream(pages.device, load().river_rope_store, pages.ref, layer, batch.bind(n, pages), rope.ref, q.shape[1], q.data_ptr(), qs,
+               k.data_ptr(), ks, v.data_ptr(), vs, out.data_ptr(), os_)
+    return out
+
+
+def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, window: int = 0, sinks: int = 0,
+                          scale: float = 0.0, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of the new tokens' queries [n_tokens, heads, head_dim] over their sequences' pages.  Rows of `out` (or of the new
+    tensor that is returned) whose tokens belong to no sequence are not written."""
+    qs = _rows("q", q, pages)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    os_ = _rows("out", out, pages, q.shape[1])
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    L, heads = load(), q.shape[1]
+    ref = batch.bind(q.shape[0], pages)
+    key = (pages.shape_key, q.shape[0], heads, window, sinks)
+    nbytes = batch._bytes.get(key)
+    if nbytes is None:
+        got = C.c_size_t()
+        _check_call(L.river_paged_attention_workspace(pages.ref, ref, heads, window, sinks, C.byref(got)))
+        nbytes = batch._bytes[key] = got.value
+    # (from torch's allocator, call by call: the memory of a captured call belongs to its graph, and no two streams share it)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=pages.device) if nbytes else None
+    _on_stream(pages.device, L.river_paged_attention, pages.ref, layer, ref, heads, q.data_ptr(), qs, scale, window, sinks,
+               out.data_ptr(), os_, ws.data_ptr() if nbytes else None, nbytes)
+    return out
+
+
+def _page_list(x) -> np.ndarray:
+    a = np.ascontiguousarray(x)
+    if a.ndim != 1 or (a.size and a.dtype.kind not in "iu"):
+        raise ValueError("a list of page numbers")
+    if a.size and (a.min() < -2**31 or a.max() >= 2**31):
+        raise ValueError("page number out of range")
+    return a.astype(np.int32, copy=False)
+
+
+def river_copy_pages(pages: Pages, src, dst):
+    """Copies pages src[i] -> dst[i] (host lists) in every layer, as if one after the other."""
+    s, d = _page_list(src), _page_list(dst)
+    if s.size != d.size:
+        raise ValueError("as many destinations as sources")
+    _on_stream(pages.device, load().river_copy_pages, pages.ref, s.ctypes.data, d.ctypes.data, s.size)
+
+
+class PagePool:
+    """Which sequence has which pages (river_pool_*).  lens and table are views of `state`, which flush keeps current on
+    the device; a Batch over their rows serves every step."""
+
+    def __init__(self, n_pages: int, page_size: int, max_seqs: int, max_pages: int, device="cuda:0"):
+        h = C.c_void_p()
+        _check_call(load().river_pool_create(n_pages, page_size, max_seqs, max_pages, C.byref(h)))
+        self._h, self.max_seqs, self.max_pages = h, max_seqs, max_pages
+        self.state = torch.empty(max_seqs * (max_pages + 1), dtype=torch.int32, device=device)
+        self.lens, self.table = self.state[:max_seqs], self.state[max_seqs:].view(max_seqs, max_pages)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            load().river_pool_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def extend(self, seq: int, n_new: int):
+        _check_call(load().river_pool_extend(self._h, seq, n_new))
+
+    def fork(self, src: int, dst: int):
+        _check_call(load().river_pool_fork(self._h, src, dst))
+
+    def rewind(self, seq: int, new_len: int):
+        _check_call(load().river_pool_rewind(self._h, seq, new_len))
+
+    def free(self, seq: int):
+        self.rewind(seq, 0)
+
+    def trim(self, seq: int, window: int, sinks: int = 0):
+        _check_call(load().river_pool_trim(self._h, seq, window, sinks))
+
+    def compact(self) -> int:
+        return _check_call(load().river_pool_compact(self._h))
+
+    def flush(self, pages: Pages | None = None):
+        """Queued copies and changed entries, on the device's current stream."""
+        if pages is not None and pages.device != self.state.device:
+            raise ValueError("pages and pool are on different devices")
+        _on_stream(self.state.device, load().river_pool_flush, self._h, None if pages is None else pages.ref, self.state.data_ptr())
+
+    def length(self, seq: int) -> int:
+        return _check_call(load().river_pool_length(self._h, seq))
+
+    @property
+    def free_pages(self) -> int:
+        return _check_call(load().river_pool_free_pages(self._h))
+
+    def row(self, seq: int) -> np.ndarray:
+        out = np.empty(self.max_pages, dtype=np.int32)
+        _check_call(load().river_pool_row(self._h, seq, out.ctypes.data))
+        return out
 
 
 # The C entry points under their own names (the class above is the same calls with

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "river_device.h"
+#include "river_host.h"
 #include "river_prefill.h"
 
 using namespace river;
@@ -515,8 +516,6 @@ struct river_ctx {
   bd::SeqState st_b{};
 };
 
-static thread_local std::string g_create_err;
-
 // Rows of d_model and n_q * head_dim columns of at most four 1 KiB granules (see Shape).  Sections of four bf16
 // blocks of head size 64, d_model 512 / 1024 / 1536 / 2048 / 2304 / 2560 / 3072 / 4096, us per step with the
 // narrow shapes and without: backbone 108 / 119 / 142 / 168 / 207 / 228 / 262 / 368 and 108 / 123 / 145 / 171 / 200 / 218 /
@@ -742,14 +741,14 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
                        void *workspace, size_t workspace_bytes, void *hip_stream, river_ctx **out,
                        bool use_static) {
   std::string why;
-  if (!out) { g_create_err = "null out"; return RIVER_EINVAL; }
+  if (!out) { call_error() = "null out"; return RIVER_EINVAL; }
   *out = nullptr;
-  if (!valid_cfg(cfg, &why)) { g_create_err = why; return RIVER_EINVAL; }
-  if (!w || !workspace) { g_create_err = "null weights or workspace"; return RIVER_EINVAL; }
-  if (((uintptr_t)workspace) % 256) { g_create_err = "workspace must be 256-byte aligned"; return RIVER_EINVAL; }
+  if (!valid_cfg(cfg, &why)) { call_error() = why; return RIVER_EINVAL; }
+  if (!w || !workspace) { call_error() = "null weights or workspace"; return RIVER_EINVAL; }
+  if (((uintptr_t)workspace) % 256) { call_error() = "workspace must be 256-byte aligned"; return RIVER_EINVAL; }
   if (!w->tok_emb || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wq || !w->wk || !w->wv ||
       !w->wo || !w->ffn_norm || !w->w_gate || !w->w_up || !w->w_down) {
-    g_create_err = "null weight table";
+    call_error() = "null weight table";
     return RIVER_EINVAL;
   }
   const int L = cfg->n_layers;
@@ -758,11 +757,11 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
   for (int l = 0; l < L; ++l)
     for (int t = 0; t < 9; ++t)
       if (!tabs[t][l] || ((uintptr_t)tabs[t][l]) % 16) {
-        g_create_err = "null or misaligned (16 B) layer weight";
+        call_error() = "null or misaligned (16 B) layer weight";
         return RIVER_EINVAL;
       }
   Layout lay = make_layout(cfg);
-  if (workspace_bytes < lay.total) { g_create_err = "workspace too small"; return RIVER_ENOSPC; }
+  if (workspace_bytes < lay.total) { call_error() = "workspace too small"; return RIVER_ENOSPC; }
 
   river_ctx *x = new river_ctx();
   x->cfg = *cfg;
@@ -793,7 +792,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
         hqs[(size_t)l * 7 + m] = q->scale[m][l];
         hqz[(size_t)l * 7 + m] = q->zero[m][l];
         if (((uintptr_t)d.qc[m]) % 16) {
-          g_create_err = "misaligned (16 B) river codes";
+          call_error() = "misaligned (16 B) river codes";
           delete x;
           return RIVER_EINVAL;
         }
@@ -805,7 +804,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
     for (int l = std::max(cfg->min_exit_layer, 0); l < L; ++l)
       for (int m = 0; m < 7; ++m)
         if (!hl[l].qc[m] || !hqs[(size_t)l * 7 + m] || !hqz[(size_t)l * 7 + m]) {
-          g_create_err = "river twin missing for a block above min_exit_layer";
+          call_error() = "river twin missing for a block above min_exit_layer";
           delete x;
           return RIVER_EINVAL;
         }
@@ -813,7 +812,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
   int dev_id = 0;
   hipDeviceProp_t prop;
   if (hipGetDevice(&dev_id) != hipSuccess || hipGetDeviceProperties(&prop, dev_id) != hipSuccess) {
-    g_create_err = "no HIP device";
+    call_error() = "no HIP device";
     delete x;
     return RIVER_EHIP;
   }
@@ -837,7 +836,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
   if (use_static) {
     const size_t need = lay.qsz - lay.hidden;
     if (need > kStaticScratchBytes) {
-      g_create_err = "configuration needs " + std::to_string(need) + " bytes of scratch; the static scratch of "
+      call_error() = "configuration needs " + std::to_string(need) + " bytes of scratch; the static scratch of "
                      "river_create_static holds " + std::to_string(kStaticScratchBytes) + " (use river_create)";
       delete x;
       return RIVER_ENOSPC;
@@ -845,7 +844,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
     char *sp = nullptr;
     std::string why2;
     const int rc = static_scratch_ptr(dev_id, &sp, &why2);
-    if (rc != RIVER_OK) { g_create_err = why2; delete x; return rc; }
+    if (rc != RIVER_OK) { call_error() = why2; delete x; return rc; }
     bool busy;
     {
       std::lock_guard<std::mutex> lk(g_bar_mu);
@@ -853,7 +852,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
       if (!busy) g_static_live[dev_id] = true;
     }
     if (busy) {                 // (the context's destructor takes the same lock)
-      g_create_err = "the static scratch of this device is in use by a live context";
+      call_error() = "the static scratch of this device is in use by a live context";
       delete x;
       return RIVER_ESTATE;
     }
@@ -894,7 +893,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
     std::string why2;
     x->bar_device = dev_id;
     const int rc = bar_acquire(dev_id, &x->bar_slot, &bp, &why2);
-    if (rc != RIVER_OK) { g_create_err = why2; delete x; return rc; }
+    if (rc != RIVER_OK) { call_error() = why2; delete x; return rc; }
     D.bar = (unsigned long long *)bp;
     D.bar_vector_poll = 0;
     const size_t words = cfg->max_batch > 1 ? (size_t)cfg->max_batch * (2 + L) : (size_t)kRecHead + L;
@@ -915,7 +914,7 @@ static int create_impl(const river_config *cfg, const river_weights *w, const ri
     }
   }
   auto fail = [&](const char *what, hipError_t e) {
-    g_create_err = std::string(what) + ": " + hipGetErrorString(e);
+    call_error() = std::string(what) + ": " + hipGetErrorString(e);
     delete x;
     return RIVER_EHIP;
   };
@@ -1891,8 +1890,62 @@ extern "C" int river_fill_cache(river_ctx *x, int32_t value) {
   return RIVER_OK;
 }
 
+// A paged cache of the caller that has the context's shape, a sequence and its row.
+static int check_move(river_ctx *x, int seq, const river_pages *p, const int32_t *row, int max_pages) {
+  if (check_pages(p, &x->err)) return RIVER_EINVAL;
+  const river_config &c = x->cfg;
+  if (p->n_layers != c.n_layers || p->n_kv_heads != c.n_kv_heads || p->head_dim != c.head_dim || p->dtype != c.dtype || p->kv_dtype != c.kv_dtype) {
+    x->err = "the pages' layers, heads or types are not the context's";
+    return RIVER_EINVAL;
+  }
+  if (seq < 0 || seq >= c.max_batch || !row || (uintptr_t)row % 4 || max_pages < 1) {
+    x->err = "bad sequence or row of pages";
+    return RIVER_EINVAL;
+  }
+  return RIVER_OK;
+}
+static int move_seq(river_ctx *x, int seq, const river_pages *p, const int32_t *row, int max_pages, int first, int n, bool to_pages) {
+  const size_t at = x->lay.cache_bytes * (size_t)seq;
+  HIP_TRY(x, move_rows(*p, row, max_pages, (char *)x->dev.kcache + at, (char *)x->dev.vcache + at, x->cfg.max_seq, first, n, to_pages, x->stream));
+  return RIVER_OK;
+}
+
+extern "C" int river_save_pages(river_ctx *x, int32_t seq, int32_t first, int32_t n, const river_pages *pages,
+                                const int32_t *row, int32_t max_pages) {
+  CHECK_CTX(x);
+  if (const int rc = check_move(x, seq, pages, row, max_pages)) return rc;
+  const int have = x->cfg.max_batch > 1 ? x->pos_b[seq] : x->pos;
+  if (first < 0 || n < 0 || n > have || first > have - n) { x->err = "positions that the sequence does not have"; return RIVER_EINVAL; }
+  if ((long long)first + n > (long long)max_pages * pages->page_size) { x->err = "more positions than the row has pages for"; return RIVER_ENOSPC; }
+  return n ? move_seq(x, seq, pages, row, max_pages, first, n, true) : RIVER_OK;
+}
+
+extern "C" int river_load_pages(river_ctx *x, int32_t seq, int32_t n, int32_t next_token, const river_pages *pages,
+                                const int32_t *row, int32_t max_pages) {
+  if (!x) return RIVER_EINVAL;
+  if (const int rc = check_move(x, seq, pages, row, max_pages)) return rc;
+  if (n < 1 || next_token < 0 || next_token >= x->cfg.vocab) { x->err = "no positions, or token id out of range"; return RIVER_EINVAL; }
+  if (n > x->cfg.max_seq) { x->err = "more positions than max_seq"; return RIVER_ENOSPC; }
+  if ((long long)n > (long long)max_pages * pages->page_size) { x->err = "more positions than the row has pages for"; return RIVER_ENOSPC; }
+  x->broken = false;                                   // (a new sequence, as in a prefill)
+  const bool many = x->cfg.max_batch > 1;
+  if (!many) {
+    const int rc = reset_state(x);
+    if (rc) return rc;
+  }
+  if (const int rc = move_seq(x, seq, pages, row, max_pages, 0, n, false)) return rc;
+  HIP_TRY(x, set_word(many ? x->st_b.token + seq : &x->dev.st->cur_token, next_token, x->stream));
+  if (many) {
+    x->pos_b[seq] = n;
+  } else {
+    x->pos = n;
+    x->have_token = true;
+  }
+  return RIVER_OK;
+}
+
 extern "C" const char *river_last_error(const river_ctx *x) {
-  return x ? x->err.c_str() : g_create_err.c_str();
+  return x ? x->err.c_str() : call_error().c_str();
 }
 
 extern "C" int river_destroy(river_ctx *x) {
