@@ -9,6 +9,7 @@ namespace river {
 namespace pg {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 // n / d for 0 <= n < 2^31 and 1 <= d <= 2^16 as a product: with 2^s >= d and m = ceil(2^(31+s) / d) the error m d - 2^(31+s)
 // is below d <= 2^s, so (n m) >> (31+s) is exact (Granlund and Montgomery, 1994).
@@ -135,50 +136,459 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope_store(Cache c, Batch b, R
 }
 
 // ------------------------------------------------------------------ attention
+//
+// Rows.  The new tokens of a sequence and the rep query heads that share a key head make count * rep rows of one product:
+// row R is head R % rep of new token R / rep.  Sixteen neighbouring rows are a tile.
+// Keys.  What any row of a tile can see is [0, hs) and [low, end): its keys are counted through both, i = 0 .. hs + end - low - 1.
 
 struct AttnArgs {
   const void *q;
   void *out;
   long long q_stride, out_stride;
   int nq, rep;                            // query heads, and how many of them share a key head
+  Div by_rep;
   float scale2;                           // scale * log2 e
-  int window, sinks;
+  int window, sinks;                      // (no window: sinks is 0)
+  int n_splits, split_len, tiles;         // of the keys, and tiles of rows per sequence and key head
+  float *part_o;                          // [n_tokens][nq][n_splits][HD], where a tile has several splits
+  float2 *part_ml;                        // [n_tokens][nq][n_splits] maximum (base 2) and sum
 };
 
-// One wavefront per (token, query head), one position after the other.
+struct Span {                             // the keys of a tile of rows
+  int first, last;                        // positions of its first and its last row's token
+  int hs, low, n;
+  __device__ __forceinline__ int pos(int i) const { return i < hs ? i : i - hs + low; }
+};
+// rows r0 .. r1 of a sequence with `count` new tokens
+__device__ __forceinline__ Span span_of(const Batch &b, const AttnArgs &a, int len, int count, int r0, int r1) {
+  Span s;
+  s.first = len - count + a.by_rep.quot(r0);
+  s.last = len - count + a.by_rep.quot(r1);
+  const int end = min(s.last + 1, b.cap);
+  s.low = a.window ? max(0, s.first - a.window + 1) : 0;
+  s.hs = max(0, min(min(a.sinks, s.low), end));
+  s.n = s.hs + max(0, end - s.low);
+  return s;
+}
+// Splits of a tile that have keys, at least one; the last split of a launch takes what is left.
+__device__ __forceinline__ int splits_of(const AttnArgs &a, int n) { return min(a.n_splits, max(1, (n + a.split_len - 1) / a.split_len)); }
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+
+// What a type of pages is multiplied with.  16-bit: D[16 x 16] += A[16 x 32] B[32 x 16], lane l has A's row l % 16 and B's
+// column l % 16, in both the contraction's elements 8 (l / 16) .. + 7, and D's rows 4 (l / 16) .. + 3 of column l % 16.  fp32: four
+// elements of the contraction, one in each quarter of the wavefront.
+template <class C> struct Mat;
+template <> struct Mat<__bf16> {
+  static constexpr int kKeys = 32;        // keys of a step
+  static constexpr float kBias = 0.f;
+  static constexpr bool kSplitP = true;   // probabilities as a sum of two bf16 numbers (see Step)
+  static __device__ __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float x, float y) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y}); }
+  static __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+  static __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+  static constexpr uint32_t kExp = 0x7f80u;
+};
+template <> struct Mat<_Float16> {
+  static constexpr int kKeys = 32;
+  // probabilities times 2^15: fp16's normal numbers then reach down to 2^-29 of the most likely key's
+  static constexpr float kBias = 15.f;
+  static constexpr bool kSplitP = false;  // (their 11 bits are eight times finer than the result's)
+  static __device__ __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float x, float y) { return __builtin_bit_cast(uint32_t, half2v{(_Float16)x, (_Float16)y}); }
+  static __device__ __forceinline__ float low(uint32_t w) { return (float)__builtin_bit_cast(half2v, w).x; }
+  static __device__ __forceinline__ float high(uint32_t w) { return (float)__builtin_bit_cast(half2v, w).y; }
+  static constexpr uint32_t kExp = 0x7c00u;
+};
+template <> struct Mat<float> {
+  static constexpr int kKeys = 16;
+  static constexpr float kBias = 0.f;
+  static __device__ __forceinline__ f32x4 mul1(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+};
+
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+// a 32-bit word of the pages' type with its elements that are not finite as zeros
+template <class C>
+__device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+  if constexpr (sizeof(C) == 4) return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+  else {
+    constexpr uint32_t e = Mat<C>::kExp;
+    if ((w & e) == e) w &= 0xffff0000u;
+    if ((w & (e << 16)) == (e << 16)) w &= 0xffffu;
+    return w;
+  }
+}
+
+struct False { static constexpr bool value = false; };
+struct True { static constexpr bool value = true; };
+
+// E neighbouring elements of a row that is divided by its sum (which is zero where nothing was seen), rounded once
+template <class T, int E>
+__device__ __forceinline__ void store_row(T *to, const float (&v)[E], float sum) {
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  T x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = (T)(v[e] * f);
+  if constexpr (sizeof(x) >= 16) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(x) / 16; ++i) ((u32x4 *)to)[i] = ((const u32x4 *)x)[i];
+  } else {
+    *(u32x2 *)to = *(const u32x2 *)x;
+  }
+}
+
+// Attention of a tile of 16 rows over one split of its keys: one workgroup of four wavefronts, which take steps of
+// Mat::kKeys keys in turn and join at the end.
+//
+// Bound: the stream of keys and values (a key head's are read once for the rows that share it).  A lane loads whole 16-byte pieces
+// in the order in which the matrix instruction wants keys: row l % 16, pieces l / 16 + 4 j (the order of the contraction is free as
+// long as the queries have the same), the next step's while this one is worked on; no barrier, each wavefront for itself.
+// The product is S^T = K Q^T, so that a row's scores lie along a lane's registers: its running maximum moves seldom, and only then are the
+// lanes of a row asked and O rescaled.  P^T is then in the order that O^T += V^T P^T wants its right operand in; V^T comes out of
+// the wavefront's own LDS, whose transposing read gives a lane four keys of one element.
+// LDS pieces lie in an order by row (swizzle), so that neither side meets in one bank.
+template <class C, int HD>
+struct Tile {
+  typedef Mat<C> M;
+  static constexpr int KB = M::kKeys / 16;               // blocks of 16 keys in a step
+  static constexpr int ES = sizeof(C), PER = 16 / ES;    // elements of a 16-byte piece
+  static constexpr int NP = HD / PER / 4;                // pieces of a lane in a row
+  static constexpr int ROW = HD * ES;                    // bytes
+  static constexpr int LDS = M::kKeys * ROW;             // of a wavefront
+  static constexpr int ND = HD / 16;
+  struct Data { u32x4 k[KB][NP], v[KB][NP]; };
+  static __device__ __forceinline__ int swizzle(int row, int piece) {
+    if constexpr (ES == 4) return piece ^ (((row >> 2) & 3) << 2);
+    else if constexpr (HD == 128) return piece ^ (((row & 7) << 1) | ((row >> 3) & 1));
+    else return piece ^ ((((row >> 1) & 3) << 1) | ((row >> 3) & 1));
+  }
+  static __device__ __forceinline__ int at(int row, int piece) { return row * ROW + swizzle(row, piece) * 16; }
+};
+
+constexpr int kAttnThreads = 256;
+
+template <class C, int HD>
+constexpr int attn_lds() {                               // the wavefronts' values, then their results
+  return 4 * (Tile<C, HD>::LDS > 16 * (HD + 4) * 4 ? Tile<C, HD>::LDS : 16 * (HD + 4) * 4);
+}
+
 template <class T, class C, int HD>
-__global__ __launch_bounds__(256) void k_attn_rows(Cache c, Batch b, AttnArgs a) {
-  constexpr int E = HD / 64;
-  const long long w = (long long)blockIdx.x * 4 + threadIdx.x / 64;
-  const int lane = threadIdx.x % 64;
+__global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
+  typedef Tile<C, HD> W;
+  typedef Mat<C> M;
+  constexpr int KB = W::KB, NP = W::NP, ND = W::ND, PER = W::PER;
+  __shared__ __align__(16) char lds[attn_lds<C, HD>()];
+  // workgroup -> (sequence, key head, split, tile); the tiles of the same keys are a multiple of the grid's other
+  // dimension apart, on one XCD where that is a multiple of 8
+  const int per = c.n_kv_heads * a.n_splits;
+  const int tile = blockIdx.y, s = blockIdx.x / per, x = blockIdx.x % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
+  int first_token, count;
+  seq_tokens(b, s, first_token, count);
+  const int rows = count * a.rep, r0 = tile * 16;
+  if (r0 >= rows) return;
+  const int r1 = min(r0 + 15, rows - 1);
+  const Span sp = span_of(b, a, b.lens[s], count, r0, r1);
+  const int parts = splits_of(a, sp.n);
+  if (z >= parts) return;
+  const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
+
+  // this lane's row: its query in the order of the contraction, its position
+  const int r = min(r0 + col, r1), tok = a.by_rep.quot(r), qh = head * a.rep + (r - tok * a.rep);
+  const int mypos = b.lens[s] - count + tok;
+  const T *qrow = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)qh * HD;
+  u32x4 qf[NP];
+  float sc = a.scale2;
+  if constexpr (sizeof(T) == sizeof(C) && !(sizeof(C) == 2 && M::kBias != 0.f)) {
+#pragma unroll
+    for (int j = 0; j < NP; ++j) qf[j] = *(const u32x4 *)(qrow + (g + 4 * j) * PER);
+  } else {
+    // bf16 queries over fp16 pages: a row is divided by a power of two so that its largest element is below 2 (what
+    // gets below fp16's numbers is below 2^-24 of that), which goes into the row's scale
+    u32x4 w[NP];
+    float big = 0.f;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      w[j] = *(const u32x4 *)(qrow + (g + 4 * j) * PER);
+      for (int e = 0; e < 4; ++e)
+        big = fmaxf(big, fmaxf(fabsf(Mat<__bf16>::low(w[j][e])), fabsf(Mat<__bf16>::high(w[j][e]))));
+    }
+    big = fmaxf(big, __shfl_xor(big, 16));
+    big = fmaxf(big, __shfl_xor(big, 32));
+    const int ex = big > 0.f && !not_finite(big) ? ilogbf(big) : 0;
+    sc = ldexpf(sc, ex);
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+      for (int e = 0; e < 4; ++e)
+        qf[j][e] = M::pack(ldexpf(Mat<__bf16>::low(w[j][e]), -ex), ldexpf(Mat<__bf16>::high(w[j][e]), -ex));
+  }
+
+  const C *kp = (const C *)c.k + (long long)head * c.page_size * HD, *vp = (const C *)c.v + (long long)head * c.page_size * HD;
+  char *mine = lds + wave * W::LDS;
+  f32x4 o[ND];
+  float m, l;
+
+  // The entries of step `it`'s keys, a step ahead of the loads that need them
+  const int steps = (i1 - i0 + 4 * M::kKeys - 1) / (4 * M::kKeys);
+  auto key_of = [&](int it, int kb) { return i0 + (it * 4 + wave) * M::kKeys + kb * 16 + col; };
+  auto entries = [&](int it, int (&e)[KB]) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      e[kb] = b.table[(long long)s * b.table_stride + c.by_page.quot(sp.pos(min(key_of(it, kb), i1 - 1)))];
+  };
+  // Rows without a page, or behind the split's end, are page 0's first (any memory of the cache will do)
+  auto fetch = [&](int it, const int (&e)[KB], typename W::Data &d, uint32_t &there) {
+    there = 0;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int i = key_of(it, kb), p = sp.pos(min(i, i1 - 1));
+      const bool ok = i < i1 && (unsigned)e[kb] < (unsigned)c.n_pages;
+      const long long at = ok ? (long long)e[kb] * c.page_stride + (long long)(p - c.by_page.quot(p) * c.page_size) * HD : 0;
+      there |= (uint32_t)(__ballot(ok) & 0xffffu) << (16 * kb);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) d.k[kb][j] = *(const u32x4 *)(kp + at + (g + 4 * j) * PER);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) d.v[kb][j] = *(const u32x4 *)(vp + at + (g + 4 * j) * PER);
+    }
+  };
+
+  // CAREFUL: values that are not finite stand where some rows see them and others do not (0 times them would be NaN):
+  // they are taken out of the product and added to the rows that see them.  Everything else has the same bits.
+  auto work = [&](auto careful_, int it, typename W::Data &d, uint32_t there) {
+    constexpr bool CAREFUL = decltype(careful_)::value;
+    f32x4 sc_[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      sc_[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        if constexpr (W::ES == 2) sc_[kb] = M::mul(d.k[kb][j], qf[j], sc_[kb]);
+        else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc_[kb] = M::mul1(__uint_as_float(d.k[kb][j][e]), __uint_as_float(qf[j][e]), sc_[kb]);
+        }
+      }
+    }
+    // does every row see every key of this step?
+    const int base = i0 + (it * 4 + wave) * M::kKeys, lo = sp.pos(base), hi = sp.pos(min(base + M::kKeys, i1) - 1);
+    const bool all = __popc(there) == M::kKeys && hi <= sp.first && (!a.window || lo > sp.last - a.window || hi < a.sinks);
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        float v = sc_[kb][n] * sc;
+        if (!all) {
+          const int key = kb * 16 + 4 * g + n, p = sp.pos(base + key);
+          const bool ok = (there >> key & 1) && p <= mypos && (!a.window || p > mypos - a.window || p < a.sinks);
+          v = ok ? v : -INFINITY;
+        }
+        sc_[kb][n] = v;
+        top = fmaxf(top, v);
+      }
+    if (__any(top > m)) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < ND; ++t) o[t] *= f;
+    }
+    const float off = (m == -INFINITY ? 0.f : m) - M::kBias;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const float p = __builtin_amdgcn_exp2f(sc_[kb][n] - off);
+        sc_[kb][n] = p;
+        l += p;
+      }
+    // values: rows that no row of the tile sees are zeros, whatever their bits
+    if (!all) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const int p = sp.pos(base + kb * 16 + col);
+        const bool some = (there >> (kb * 16 + col) & 1) && p <= sp.last && (!a.window || p > sp.first - a.window || p < a.sinks);
+#pragma unroll
+        for (int j = 0; j < NP; ++j) d.v[kb][j] = some ? d.v[kb][j] : u32x4{0, 0, 0, 0};
+      }
+    }
+    auto put = [&] {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) *(u32x4 *)(mine + W::at(kb * 16 + col, g + 4 * j)) = d.v[kb][j];
+      __builtin_amdgcn_wave_barrier();
+    };
+    put();
+    if constexpr (CAREFUL) {
+      for (int key = 0; key < M::kKeys; ++key) {
+        const int p = sp.pos(base + key);
+        const bool ok = (there >> key & 1) && p <= mypos && (!a.window || p > mypos - a.window || p < a.sinks);
+        for (int t = 0; t < ND; ++t)
+          for (int n = 0; n < 4; ++n) {
+            const int e = t * 16 + 4 * g + n;
+            const float v = (float)*(const C *)(mine + W::at(key, e / PER) + e % PER * W::ES);
+            if (ok && not_finite(v)) o[t][n] += v;
+          }
+      }
+      __builtin_amdgcn_wave_barrier();
+      for (int kb = 0; kb < KB; ++kb)
+        for (int j = 0; j < NP; ++j)
+          for (int e = 0; e < 4; ++e) d.v[kb][j][e] = finite_only<C>(d.v[kb][j][e]);
+      put();
+    }
+    if constexpr (W::ES == 2) {
+      // P^T: the keys 4 g .. of both blocks.  A bf16 probability leaves out 2^-9 of itself, as much as the result's own rounding
+      // does; what it leaves out is a second product, which costs nothing beside the stream
+      u32x4 hi, rest;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float p0 = sc_[w / 2][2 * (w & 1)], p1 = sc_[w / 2][2 * (w & 1) + 1];
+        hi[w] = M::pack(p0, p1);
+        if constexpr (M::kSplitP) rest[w] = M::pack(p0 - M::low(hi[w]), p1 - M::high(hi[w]));
+      }
+#pragma unroll
+      for (int t = 0; t < ND; ++t) {
+        u32x4 v;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const int row = kb * 16 + 4 * g + col / 4;
+          const s16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4 *)(mine + W::at(row, 2 * t + (col >> 1 & 1)) + (col & 1) * 8));
+          const u32x2 w2 = __builtin_bit_cast(u32x2, four);
+          v[2 * kb] = w2.x;
+          v[2 * kb + 1] = w2.y;
+        }
+        o[t] = M::mul(v, hi, o[t]);
+        if constexpr (M::kSplitP) o[t] = M::mul(v, rest, o[t]);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const int row = 4 * g + n, e = t * 16 + col;
+          o[t] = M::mul1(*(const float *)(mine + W::at(row, e / 4) + e % 4 * 4), sc_[0][n], o[t]);
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+  };
+
+  auto pass = [&](auto careful_) {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < ND; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // (a wavefront whose keys are beyond the end works on none that any row sees)
+    if (steps == 0) return;
+    int e[KB], e1[KB];
+    typename W::Data d, d1;
+    uint32_t there, there1;
+    entries(0, e);
+    entries(1, e1);
+    fetch(0, e, d, there);
+    for (int it = 0; it + 1 < steps; ++it) {
+      entries(it + 2, e);
+      fetch(it + 1, e1, d1, there1);
+      work(careful_, it, d, there);
+      d = d1;
+      there = there1;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) e1[kb] = e[kb];
+    }
+    work(careful_, steps - 1, d, there);
+  };
+  pass(False{});
+  float sick = 0.f;
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) sick += o[t][n] * 0.f;
+  if (__any(sick != 0.f)) pass(True{});
+
+  // the four wavefronts' results: [row][HD + 4] with maximum and sum behind the row
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  __syncthreads();
+  constexpr int LD = HD + 4;
+  float *res = (float *)lds;
+#pragma unroll
+  for (int t = 0; t < ND; ++t) *(f32x4 *)(res + (wave * 16 + col) * LD + t * 16 + 4 * g) = o[t];
+  if (g == 0) {
+    res[(wave * 16 + col) * LD + HD] = m;
+    res[(wave * 16 + col) * LD + HD + 1] = l;
+  }
+  __syncthreads();
+  constexpr int E = HD / 16;                             // elements of a thread
+  const int row = threadIdx.x / 16, e0 = threadIdx.x % 16 * E;
+  if (r0 + row > r1) return;
+  float mw[4], big = -INFINITY, sum = 0.f, v[E];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) { mw[w] = res[(w * 16 + row) * LD + HD]; big = fmaxf(big, mw[w]); }
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw[w] - big);
+    sum += f * res[(w * 16 + row) * LD + HD + 1];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] += f * res[(w * 16 + row) * LD + e0 + e];
+  }
+  const int to = a.by_rep.quot(r0 + row), oh = head * a.rep + (r0 + row - to * a.rep);
+  const long long t = first_token + to;
+  if (parts == 1) {
+    store_row<T, E>((T *)a.out + t * a.out_stride + (long long)oh * HD + e0, v, sum);
+  } else {
+    const long long part = (t * a.nq + oh) * a.n_splits + z;
+#pragma unroll
+    for (int e = 0; e < E; e += 4) *(f32x4 *)(a.part_o + part * HD + e0 + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    if (e0 == 0) a.part_ml[part] = make_float2(big, sum);
+  }
+}
+
+// The splits of a row joined, in their order: 16 lanes a row.
+template <class T, int HD>
+__global__ __launch_bounds__(256) void k_attn_join(Batch b, AttnArgs a) {
+  constexpr int E = HD / 16;
+  const long long w = (long long)blockIdx.x * 16 + threadIdx.x / 16;
   if (w >= (long long)b.n_tokens * a.nq) return;
-  const int t = (int)(w / a.nq), h = (int)(w % a.nq);
+  const int t = (int)(w / a.nq), h = (int)(w % a.nq), e0 = threadIdx.x % 16 * E;
   const int s = seq_of(b, t);
   if (s < 0) return;
-  const int p = position_of(b, s, t);
-  float q[E], o[E];
-  for (int e = 0; e < E; ++e) { q[e] = (float)((const T *)a.q)[t * a.q_stride + h * HD + lane * E + e]; o[e] = 0.f; }
-  float m = -INFINITY, l = 0.f;
-  const int low = a.window ? max(0, p - a.window + 1) : 0;
-  const int end = min(p + 1, b.cap);
-  for (int j = a.window && a.sinks ? 0 : low; j < end; ++j) {
-    if (j < low && j >= a.sinks) { j = low - 1; continue; }
-    int slot;
-    const int page = page_of(c, b, s, j, slot);
-    if (page < 0) continue;
-    const long long at = (long long)page * c.page_stride + ((long long)(h / a.rep) * c.page_size + slot) * HD + lane * E;
-    float x = 0.f;
-    for (int e = 0; e < E; ++e) x += q[e] * (float)((const C *)c.k)[at + e];
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-    x *= a.scale2;
-    const float n = fmaxf(m, x), mm = n == -INFINITY ? 0.f : n;
-    const float r = exp2f(m - mm), pr = exp2f(x - mm);
-    l = l * r + pr;
-    for (int e = 0; e < E; ++e) o[e] = o[e] * r + pr * (float)((const C *)c.v)[at + e];
-    m = n;
+  int first, count;
+  seq_tokens(b, s, first, count);
+  const int r = (t - first) * a.rep + h % a.rep, r0 = r & ~15;
+  if (t < first || t - first >= count || r0 >= a.tiles * 16) return;
+  const Span sp = span_of(b, a, b.lens[s], count, r0, min(r0 + 15, count * a.rep - 1));
+  const int parts = splits_of(a, sp.n);
+  if (parts == 1) return;
+  const float2 *ml = a.part_ml + w * a.n_splits;
+  const float *po = a.part_o + w * a.n_splits * HD + e0;
+  float big = -INFINITY, sum = 0.f, v[E];
+  for (int z = 0; z < parts; ++z) big = fmaxf(big, ml[z].x);
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = 0.f;
+  for (int z = 0; z < parts; ++z) {
+    const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[z].x - big);
+    sum += f * ml[z].y;
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const f32x4 x = *(const f32x4 *)(po + (long long)z * HD + e);
+      for (int n = 0; n < 4; ++n) v[e + n] += f * x[n];
+    }
   }
-  for (int e = 0; e < E; ++e)
-    ((T *)a.out)[t * a.out_stride + h * HD + lane * E + e] = (T)(l == 0.f ? 0.f : o[e] / l);
+  store_row<T, E>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, v, sum);
 }
 
 // ------------------------------------------------------------------ copies

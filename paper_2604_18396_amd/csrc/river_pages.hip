@@ -188,13 +188,39 @@ static const char *bad_attention(const river_pages *pages, const river_batch *ba
   return nullptr;
 }
 
+// How a call is divided.  Workgroups without a split of the keys: sequences x key heads x tiles of 16 rows; splits so that the
+// CUs have two each, of at least 128 keys (a step for each of the four wavefronts).
+struct AttnPlan {
+  int tiles, n_splits, split_len;
+  size_t o_bytes, bytes;                                         // of the partial results
+};
+static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
+  AttnPlan y{};
+  const int rep = nq / p->n_kv_heads;
+  const long long rows = (long long)(b->q_start ? std::min(b->max_new, b->n_tokens) : 1) * rep;
+  y.tiles = (int)((rows + 15) / 16);
+  long long keys = std::min<long long>(b->max_len, (long long)b->max_pages * p->page_size);
+  if (window) keys = std::min<long long>(keys, (long long)window + sinks + 15 / rep);
+  const long long groups = (long long)b->n_seq * p->n_kv_heads * y.tiles;
+  const long long want = std::max(1ll, std::min({(512 + groups - 1) / std::max(1ll, groups), (keys + 127) / 128, 256ll}));
+  y.split_len = (int)std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30);
+  y.split_len = std::max(y.split_len, 128);
+  y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
+  if (y.n_splits > 1) {
+    const size_t parts = (size_t)b->n_tokens * nq * y.n_splits;
+    y.o_bytes = parts * p->head_dim * 4;
+    y.bytes = y.o_bytes + parts * 8;
+  }
+  return y;
+}
+
 extern "C" int river_paged_attention_workspace(const river_pages *pages, const river_batch *batch, int32_t n_q_heads,
                                                int32_t window, int32_t sinks, size_t *bytes) {
   return guarded([&]() -> int {
     std::string why;
     if (!bytes) return refuse("null bytes");
     if (const char *m = bad_attention(pages, batch, n_q_heads, window, sinks, &why)) return refuse(m);
-    *bytes = 0;
+    *bytes = plan_attention(pages, batch, n_q_heads, window, sinks).bytes;
     return RIVER_OK;
   });
 }
@@ -213,16 +239,26 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
     if (q_stride < qw || out_stride < qw) return refuse("a stride is smaller than its row");
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || q_stride * es % 16 || out_stride * es % 16)
       return refuse("queries, output and their strides must be multiples of 16 bytes");
-    if (batch->n_tokens == 0 || batch->n_seq == 0) return RIVER_OK;
+    const AttnPlan y = plan_attention(pages, batch, n_q_heads, window, sinks);
+    if (y.bytes && (!workspace || (uintptr_t)workspace % 16)) return refuse("null or misaligned (16 B) workspace");
+    if (workspace_bytes < y.bytes) return refuse("workspace too small", RIVER_ENOSPC);
+    if (batch->n_tokens == 0 || batch->n_seq == 0 || y.tiles == 0) return RIVER_OK;
     const Cache c = layer_cache(pages, layer);
     const Batch b = device_batch(batch, pages->page_size);
     if (scale == 0.f) scale = 1.f / std::sqrt((float)pages->head_dim);
-    const AttnArgs a{q, out, q_stride, out_stride, n_q_heads, n_q_heads / pages->n_kv_heads, scale * 1.44269504088896340736f, window, sinks};
-    const long long waves = (long long)b.n_tokens * n_q_heads;
-    if (waves > (1ll << 32)) return refuse("too many tokens and heads");
-    const hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
-      return launch(k_attn_rows<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, (hipStream_t)hip_stream, c, b, a);
+    const int rep = n_q_heads / pages->n_kv_heads;
+    AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale * 1.44269504088896340736f, window, window ? sinks : 0,
+               y.n_splits, y.split_len, y.tiles, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes)};
+    const long long groups = (long long)b.n_seq * c.n_kv_heads * y.n_splits;
+    if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * n_q_heads >= (1ll << 28)) return refuse("too many sequences, tokens and heads");
+    const hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
+      return launch(k_attn_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups, y.tiles), dim3(kAttnThreads), 0, st, c, b, a);
     });
+    if (e == hipSuccess && y.n_splits > 1)
+      e = by_types(pages, [&](auto t, auto, auto hd) {
+        return launch(k_attn_join<decltype(t), decltype(hd)::v>, dim3((unsigned)(((long long)b.n_tokens * n_q_heads + 15) / 16)), dim3(256), 0, st, b, a);
+      });
     return e == hipSuccess ? RIVER_OK : hip_failed("river_paged_attention", e);
   });
 }
