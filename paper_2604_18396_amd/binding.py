@@ -410,10 +410,11 @@ def _check_on(device, dtype, **tensors):
 
 def _on_stream(device, call, *args):
     """The call on the device's current torch stream (the library takes the stream of the current device)."""
+    # (the stream's handle without the torch.cuda.Stream object around it, which takes longer than the rest of a small call)
     if device.index == torch.cuda.current_device():
-        return _check_call(call(*args, torch.cuda.current_stream().cuda_stream))
+        return _check_call(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
     with torch.cuda.device(device):
-        return _check_call(call(*args, torch.cuda.current_stream().cuda_stream))
+        return _check_call(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
 
 
 class Pages:
@@ -496,12 +497,24 @@ def river_rope_frequencies(rot_dim: int, base: float, scaling: str = "plain", fa
 
 def _rows(name: str, t: torch.Tensor, pages: Pages, heads: int | None = None) -> int:
     """[n_tokens, heads, head_dim] with contiguous heads: the stride between tokens."""
-    if t.dtype != pages.dtype or t.device != pages.device or t.dim() != 3 or t.shape[2] != pages.head_dim:
+    shape = t.shape
+    if t.dtype != pages.dtype or t.device != pages.device or len(shape) != 3 or shape[2] != pages.head_dim:
         raise ValueError(f"{name}: {pages.dtype} [n_tokens, heads, {pages.head_dim}] on {pages.device}")
-    n, h, hd = t.shape
-    if (heads is not None and h != heads) or t.stride(2) != 1 or (h > 1 and t.stride(1) != hd):
+    n, h, hd = shape
+    between, head, one = t.stride()
+    if (heads is not None and h != heads) or one != 1 or (h > 1 and head != hd):
         raise ValueError(f"{name}: wrong number of heads, or a token's heads are not contiguous")
-    return t.stride(0) if n > 1 else h * hd
+    return between if n > 1 else h * hd
+
+
+def _out(q: torch.Tensor, out: torch.Tensor | None, pages: Pages):
+    """The place of the result (a new tensor where none is given) and the stride between its tokens."""
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        return out, q.shape[1] * q.shape[2]
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    return out, _rows("out", out, pages)
 
 
 def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope: Rope,
@@ -512,11 +525,7 @@ def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k:
     qs, ks, vs = _rows("q", q, pages), _rows("k", k, pages, pages.n_kv_heads), _rows("v", v, pages, pages.n_kv_heads)
     if k.shape[0] != n or v.shape[0] != n or rope.device != pages.device:
         raise ValueError("q, k and v must have the same tokens, and the frequencies their device")
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    os_ = _rows("out", out, pages, q.shape[1])
-    if out.shape[0] != n:
-        raise ValueError("out must have q's shape")
+    out, os_ = _out(q, out, pages)
     _on_stream(pages.device, load().river_rope_store, pages.ref, layer, batch.bind(n, pages), rope.ref, q.shape[1], q.data_ptr(), qs,
                k.data_ptr(), ks, v.data_ptr(), vs, out.data_ptr(), os_)
     return out
@@ -527,14 +536,10 @@ def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tenso
     """Attention of the new tokens' queries [n_tokens, heads, head_dim] over their sequences' pages.  Rows of `out` (or of the new
     tensor that is returned) whose tokens belong to no sequence are not written."""
     qs = _rows("q", q, pages)
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    os_ = _rows("out", out, pages, q.shape[1])
-    if out.shape != q.shape:
-        raise ValueError("out must have q's shape")
-    L, heads = load(), q.shape[1]
-    ref = batch.bind(q.shape[0], pages)
-    key = (pages.shape_key, q.shape[0], heads, window, sinks)
+    out, os_ = _out(q, out, pages)
+    L, (n, heads, _) = load(), q.shape
+    ref = batch.bind(n, pages)
+    key = (pages.shape_key, n, heads, window, sinks)
     nbytes = batch._bytes.get(key)
     if nbytes is None:
         got = C.c_size_t()
@@ -548,6 +553,8 @@ def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tenso
 
 
 def _page_list(x) -> np.ndarray:
+    if isinstance(x, np.ndarray) and x.dtype == np.int32 and x.ndim == 1 and x.flags.c_contiguous:
+        return x
     a = np.ascontiguousarray(x)
     if a.ndim != 1 or (a.size and a.dtype.kind not in "iu"):
         raise ValueError("a list of page numbers")

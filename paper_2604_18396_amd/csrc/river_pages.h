@@ -149,7 +149,7 @@ struct AttnArgs {
   Div by_rep;
   float scale2;                           // scale * log2 e
   int window, sinks;                      // (no window: sinks is 0)
-  int n_splits, split_len, tiles;         // of the keys, and tiles of rows per sequence and key head
+  int n_splits, split_len, tiles, tile_rows;   // of the keys; tiles of rows per sequence and key head
   float *part_o;                          // [n_tokens][nq][n_splits][HD], where a tile has several splits
   float2 *part_ml;                        // [n_tokens][nq][n_splits] maximum (base 2) and sum
 };
@@ -557,6 +557,338 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
   }
 }
 
+// ------------------------------------------------------------------ attention of many rows (16-bit pages)
+//
+// Bound: the matrix cores, and beside them as long, the exponentials (a 32 x 32 x 16 product takes 32 cycles, the softmax of the 32 keys x
+// 64 rows of a step 900 against the 1024 of its products at HD 128).  A wavefront holds 64 rows, so that an operand
+// fetched from LDS is used twice (with 32 rows the fetches alone take as long as the products), one wavefront per SIMD with 512
+// registers, four of them 256 rows on the same keys.  What would wait for each other is taken from different steps: step n
+// multiplies S(n+1) = K Q^T, takes the exponentials of S(n), and adds P(n-1) V, three things that do not depend on each other.
+// O is therefore rescaled one step after the maximum has moved (pend).
+// Keys and values travel global -> registers -> LDS, rings of two and four steps; one barrier a step.
+template <class C, int HD>
+struct Many {
+  typedef Mat<C> M;
+  static constexpr int KEYS = 32, RB = 2, WROWS = 32 * RB, ROWS = 4 * WROWS, VRING = 4, KRING = 2;
+  static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
+  static constexpr int KS = HD / 16, DB = HD / 32;
+  static constexpr int STAGE = KEYS * ROW, LDS = (KRING + VRING) * STAGE + 4 * VRING;
+  static constexpr int PER = 256 / PIECES, NL = KEYS / PER;    // rows of a round of loads, and rounds
+  // Pieces of a row lie in an order by row: eight neighbouring rows of keys, and the four rows of a transposing read of
+  // values, meet in different banks
+  static __device__ __forceinline__ int k_at(int row, int piece) {
+    return row * ROW + (piece ^ (HD == 128 ? row & 15 : row & 7)) * 16;
+  }
+  static __device__ __forceinline__ int v_at(int row, int piece) {
+    return row * ROW + (piece ^ (HD == 128 ? ((row & 7) << 1) | ((row >> 3) & 1) : ((row & 3) << 1) | ((row >> 2) & 1))) * 16;
+  }
+  // bit of a step's word of pages that are there for key k: a wavefront's rows of a round are a byte
+  static constexpr __device__ __forceinline__ int there_bit(int k) { return NL == 1 ? k : (k % PER / 4) * 8 + k / PER * 4 + k % 4; }
+};
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <class C>
+__device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (Mat<C>::kSplitP)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+
+template <class T, class C, int HD>
+__global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs a) {
+  typedef Many<C, HD> W;
+  typedef Mat<C> M;
+  constexpr int RB = W::RB, KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
+  extern __shared__ __align__(16) char lds[];
+  char *const klds = lds, *const vlds = lds + W::KRING * W::STAGE;
+  uint8_t *const there_lds = (uint8_t *)(lds + (W::KRING + W::VRING) * W::STAGE);
+  // workgroup -> (sequence, key head, split), tile: the last tile, which sees most keys, first; a key head's tiles on one XCD
+  // where their distance in the grid is a multiple of 8
+  const int per = c.n_kv_heads * a.n_splits;
+  const int tile = a.tiles - 1 - blockIdx.y, s = blockIdx.x / per, x = blockIdx.x % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
+  int first_token, count;
+  seq_tokens(b, s, first_token, count);
+  const int rows = count * a.rep, r0 = tile * W::ROWS;
+  if (r0 >= rows) return;
+  const int r1 = min(r0 + W::ROWS - 1, rows - 1), len = b.lens[s];
+  const Span sp = span_of(b, a, len, count, r0, r1);
+  const int parts = splits_of(a, sp.n);
+  if (z >= parts) return;
+  const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, h = lane / 32;
+  const int steps = (i1 - i0 + KEYS - 1) / KEYS;
+
+  // this wavefront's rows: their queries in the operand's order, positions; rows behind the last repeat it
+  const int w0 = min(r0 + wave * W::WROWS, r1), w1 = min(w0 + W::WROWS - 1, r1);
+  const int first = len - count + a.by_rep.quot(w0), last = len - count + a.by_rep.quot(w1);
+  u32x4 qf[KS][RB];
+  float sc[RB];
+  int mypos[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = min(r0 + wave * W::WROWS + rb * 32 + col, r1), tok = a.by_rep.quot(r);
+    mypos[rb] = len - count + tok;
+    const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
+    sc[rb] = a.scale2;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks][rb] = *(const u32x4 *)(q + (2 * ks + h) * 8);
+    if constexpr (!M::kSplitP) {                         // fp16 pages: see k_attn_split
+      float big = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        for (int e = 0; e < 4; ++e)
+          big = fmaxf(big, fmaxf(fabsf(Mat<__bf16>::low(qf[ks][rb][e])), fabsf(Mat<__bf16>::high(qf[ks][rb][e]))));
+      big = fmaxf(big, __shfl_xor(big, 32));
+      const int ex = big > 0.f && !not_finite(big) ? ilogbf(big) : 0;
+      sc[rb] = ldexpf(sc[rb], ex);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        for (int e = 0; e < 4; ++e)
+          qf[ks][rb][e] = M::pack(ldexpf(Mat<__bf16>::low(qf[ks][rb][e]), -ex), ldexpf(Mat<__bf16>::high(qf[ks][rb][e]), -ex));
+    }
+    sc[rb] = fmaxf(sc[rb], 1e-37f);                      // (-infinity times it stays one)
+  }
+
+  const C *kp = (const C *)c.k + (long long)head * c.page_size * HD, *vp = (const C *)c.v + (long long)head * c.page_size * HD;
+  const int my_row = threadIdx.x / W::PIECES, my_piece = threadIdx.x % W::PIECES;
+  auto entries = [&](int n, int (&e)[NL]) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j)
+      e[j] = b.table[(long long)s * b.table_stride + c.by_page.quot(sp.pos(min(i0 + n * KEYS + j * W::PER + my_row, i1 - 1)))];
+  };
+  auto fetch = [&](int n, const int (&e)[NL], u32x4 (&k)[NL], u32x4 (&v)[NL], uint32_t &ok_) {
+    ok_ = 0;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int i = i0 + n * KEYS + j * W::PER + my_row, p = sp.pos(min(i, i1 - 1));
+      const bool ok = i < i1 && (unsigned)e[j] < (unsigned)c.n_pages;
+      const long long at = ok ? (long long)e[j] * c.page_stride + (long long)(p - c.by_page.quot(p) * c.page_size) * HD : 0;
+      k[j] = *(const u32x4 *)(kp + at + my_piece * 8);
+      v[j] = *(const u32x4 *)(vp + at + my_piece * 8);
+      ok_ |= (uint32_t)ok << j;
+    }
+  };
+  auto stage = [&](int n, const u32x4 (&k)[NL], const u32x4 (&v)[NL], uint32_t ok_) {
+    const int slot = n % W::VRING;
+    uint32_t byte = 0;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const bool ok = ok_ >> j & 1;
+      *(u32x4 *)(klds + n % W::KRING * W::STAGE + W::k_at(j * W::PER + my_row, my_piece)) = k[j];
+      // (a value that nobody sees is zero, whatever its bits)
+      *(u32x4 *)(vlds + slot * W::STAGE + W::v_at(j * W::PER + my_row, my_piece)) = ok ? v[j] : u32x4{0, 0, 0, 0};
+      const unsigned long long all = __ballot(ok);
+#pragma unroll
+      for (int q = 0; q < 64 / W::PIECES; ++q) byte |= (uint32_t)(all >> (q * W::PIECES) & 1) << (j * 4 + q);
+    }
+    if (lane == 0) there_lds[slot * 4 + wave] = (uint8_t)byte;
+  };
+  auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  f32x16 o[DB][RB], sx[RB];
+  u32x4 pr[2][RB];
+  float m[RB], l[RB], off[RB], fac[RB];
+  bool pend;
+
+  // scores of step n as they count: what a row does not see is -infinity, and the maximum where that moves it
+  auto settle = [&](int n, float (&top)[RB]) {
+    const uint32_t there = __builtin_amdgcn_readfirstlane(*(const uint32_t *)(there_lds + n % W::VRING * 4));
+    const int base = i0 + n * KEYS, lo = sp.pos(base), hi = sp.pos(min(base + KEYS, i1) - 1);
+    const bool all = n < steps && there == 0xffffffffu && hi <= first && (!a.window || lo > last - a.window || hi < a.sinks);
+    if (!all) {
+      const uint32_t mine = n < steps ? there >> (NL == 1 ? 4 * h : 8 * h) : 0;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        top[rb] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int p = sp.pos(base + 8 * (i / 4) + 4 * h + i % 4);
+          const bool ok = (mine >> W::there_bit(8 * (i / 4) + i % 4) & 1) && p <= mypos[rb] && (!a.window || p > mypos[rb] - a.window || p < a.sinks);
+          sx[rb][i] = ok ? sx[rb][i] : -INFINITY;
+          top[rb] = fmaxf(top[rb], sx[rb][i]);
+        }
+      }
+    }
+    if (pend) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) o[d][rb] *= fac[rb];
+    }
+    pend = __any(top[0] > m[0] || top[1] > m[1]);
+    if (pend) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float now = fmaxf(m[rb], fmaxf(top[rb], __shfl_xor(top[rb], 32)));
+        const float to = (now == -INFINITY ? 0.f : now * sc[rb]) - M::kBias;
+        fac[rb] = m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[rb] - to);
+        if (now == m[rb]) fac[rb] = 1.f;
+        m[rb] = now;
+        off[rb] = to;
+        l[rb] *= fac[rb];
+      }
+    }
+  };
+
+  auto pass = [&](auto careful_) {
+    constexpr bool CAREFUL = decltype(careful_)::value;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      m[rb] = -INFINITY;
+      l[rb] = 0.f;
+      off[rb] = -M::kBias;
+      fac[rb] = 1.f;
+      pr[0][rb] = pr[1][rb] = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][rb][i] = 0.f;
+    }
+    pend = false;
+    if (steps == 0) return;
+    int e[NL];
+    u32x4 kr[NL], vr[NL];
+    uint32_t ok_;
+    // the values of step -1 are zeros; steps 0 and 1 into the ring, step 2 on the way
+    for (int i = threadIdx.x; i < W::STAGE / 16; i += 256) *(u32x4 *)(vlds + (W::VRING - 1) * W::STAGE + i * 16) = u32x4{0, 0, 0, 0};
+    entries(0, e);
+    fetch(0, e, kr, vr, ok_);
+    stage(0, kr, vr, ok_);
+    entries(1, e);
+    fetch(1, e, kr, vr, ok_);
+    stage(1, kr, vr, ok_);
+    entries(2, e);
+    fetch(2, e, kr, vr, ok_);
+    entries(3, e);
+    barrier();
+    auto scores = [&](int n, f32x16 (&to)[RB]) {
+      const char *at = klds + n % W::KRING * W::STAGE;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[rb][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 kf = *(const u32x4 *)(at + W::k_at(col, 2 * ks + h));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) to[rb] = mul32<C>(kf, qf[ks][rb], to[rb]);
+      }
+    };
+    auto maxima = [&](const f32x16 (&of)[RB], float (&top)[RB]) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        top[rb] = of[rb][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top[rb] = fmaxf(top[rb], of[rb][i]);
+      }
+    };
+    float top[RB];
+    scores(0, sx);
+    maxima(sx, top);
+    settle(0, top);
+    // step `steps` only adds what the last one left
+    for (int n = 0; n <= steps; ++n) {
+      stage(n + 2, kr, vr, ok_);
+      fetch(n + 3, e, kr, vr, ok_);
+      entries(n + 4, e);
+      f32x16 sn[RB];
+      scores(n + 1, sn);
+      u32x4 pn[2][RB];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sx[rb][i], sc[rb], -off[rb])), p1 = __builtin_amdgcn_exp2f(fmaf(sx[rb][i + 1], sc[rb], -off[rb]));
+          l[rb] += p0;
+          l[rb] += p1;
+          pn[i / 8][rb][i % 8 / 2] = M::pack(p0, p1);
+        }
+      const char *at = vlds + (n + W::VRING - 1) % W::VRING * W::STAGE;
+      if constexpr (CAREFUL) {
+        if (n > 0) {
+          const uint32_t there = *(const uint32_t *)(there_lds + (n + W::VRING - 1) % W::VRING * 4);
+          for (int key = 0; key < KEYS; ++key) {
+            const int p = sp.pos(i0 + (n - 1) * KEYS + key);
+            for (int rb = 0; rb < RB; ++rb) {
+              const bool ok = (there >> W::there_bit(key) & 1) && p <= mypos[rb] && (!a.window || p > mypos[rb] - a.window || p < a.sinks);
+              for (int d = 0; d < DB; ++d)
+                for (int i = 0; i < 16; ++i) {
+                  const int el = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
+                  const float v = (float)*(const C *)(at + W::v_at(key, el / 8) + el % 8 * 2);
+                  if (ok && not_finite(v)) o[d][rb][i] += v;
+                }
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          u32x4 vf;
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            // four keys 16 t + 8 u + 4 h .. of the element d * 32 + lane % 32
+            const int row = 16 * t + 8 * u + 4 * h + lane % 16 / 4, el = d * 32 + (lane % 32 / 16) * 16 + lane % 4 * 4;
+            const s16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4 *)(at + W::v_at(row, el / 8) + el % 8 * 2));
+            const u32x2 w2 = __builtin_bit_cast(u32x2, four);
+            vf[2 * u] = w2.x;
+            vf[2 * u + 1] = w2.y;
+          }
+          if constexpr (CAREFUL)
+            for (int w = 0; w < 4; ++w) vf[w] = finite_only<C>(vf[w]);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) o[d][rb] = mul32<C>(vf, pr[t][rb], o[d][rb]);
+        }
+      maxima(sn, top);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        sx[rb] = sn[rb];
+        pr[0][rb] = pn[0][rb];
+        pr[1][rb] = pn[1][rb];
+      }
+      settle(n + 1, top);
+      barrier();
+    }
+  };
+  pass(False{});
+  float sick = 0.f;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sick += o[d][rb][i] * 0.f;
+  if (__syncthreads_or(sick != 0.f)) pass(True{});
+
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    l[rb] += __shfl_xor(l[rb], 32);
+    const int r = r0 + wave * W::WROWS + rb * 32 + col;
+    if (r > r1) continue;
+    const int tok = a.by_rep.quot(r), qh = head * a.rep + r - tok * a.rep;
+    const long long t = first_token + tok;
+    if (parts == 1) {
+      const float f = l[rb] == 0.f ? 0.f : 1.f / l[rb];
+      T *to = (T *)a.out + t * a.out_stride + (long long)qh * HD + 4 * h;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *(u32x2 *)(to + d * 32 + 2 * i) = u32x2{Mat<__bf16>::pack(o[d][rb][i] * f, o[d][rb][i + 1] * f), Mat<__bf16>::pack(o[d][rb][i + 2] * f, o[d][rb][i + 3] * f)};
+    } else {
+      const long long part = (t * a.nq + qh) * a.n_splits + z;
+      float *to = a.part_o + part * HD + 4 * h;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) *(f32x4 *)(to + d * 32 + 2 * i) = f32x4{o[d][rb][i], o[d][rb][i + 1], o[d][rb][i + 2], o[d][rb][i + 3]};
+      // (maxima in base 2, as k_attn_split has them)
+      if (h == 0) a.part_ml[part] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kBias, l[rb]);
+    }
+  }
+}
+
 // The splits of a row joined, in their order: 16 lanes a row.
 template <class T, int HD>
 __global__ __launch_bounds__(256) void k_attn_join(Batch b, AttnArgs a) {
@@ -568,9 +900,9 @@ __global__ __launch_bounds__(256) void k_attn_join(Batch b, AttnArgs a) {
   if (s < 0) return;
   int first, count;
   seq_tokens(b, s, first, count);
-  const int r = (t - first) * a.rep + h % a.rep, r0 = r & ~15;
-  if (t < first || t - first >= count || r0 >= a.tiles * 16) return;
-  const Span sp = span_of(b, a, b.lens[s], count, r0, min(r0 + 15, count * a.rep - 1));
+  const int r = (t - first) * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
+  if (t < first || t - first >= count || r0 >= a.tiles * a.tile_rows) return;
+  const Span sp = span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, count * a.rep) - 1);
   const int parts = splits_of(a, sp.n);
   if (parts == 1) return;
   const float2 *ml = a.part_ml + w * a.n_splits;

@@ -188,23 +188,27 @@ static const char *bad_attention(const river_pages *pages, const river_batch *ba
   return nullptr;
 }
 
-// How a call is divided.  Workgroups without a split of the keys: sequences x key heads x tiles of 16 rows; splits so that the
-// CUs have two each, of at least 128 keys (a step for each of the four wavefronts).
+// How a call is divided: which kernel, tiles of rows, splits of the keys.
 struct AttnPlan {
-  int tiles, n_splits, split_len;
+  bool many;                                                     // k_attn_many, else k_attn_split
+  int tiles, tile_rows, n_splits, split_len;
   size_t o_bytes, bytes;                                         // of the partial results
 };
+constexpr int kManyRows = 128;
 static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
   AttnPlan y{};
   const int rep = nq / p->n_kv_heads;
   const long long rows = (long long)(b->q_start ? std::min(b->max_new, b->n_tokens) : 1) * rep;
-  y.tiles = (int)((rows + 15) / 16);
+  y.many = p->dtype == RIVER_BF16 && rows >= kManyRows;
+  y.tile_rows = y.many ? 256 : 16;
+  y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
   long long keys = std::min<long long>(b->max_len, (long long)b->max_pages * p->page_size);
-  if (window) keys = std::min<long long>(keys, (long long)window + sinks + 15 / rep);
-  const long long groups = (long long)b->n_seq * p->n_kv_heads * y.tiles;
-  const long long want = std::max(1ll, std::min({(512 + groups - 1) / std::max(1ll, groups), (keys + 127) / 128, 256ll}));
-  y.split_len = (int)std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30);
-  y.split_len = std::max(y.split_len, 128);
+  if (window) keys = std::min<long long>(keys, (long long)window + sinks + (y.tile_rows - 1) / rep);
+  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many, two of
+  // k_attn_split, of at least 128 keys (there a step for each of four wavefronts)
+  const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles), goal = y.many ? 256 : 512, least = y.many ? 256 : 128;
+  const long long want = std::max(1ll, std::min({goal / groups, (keys + least - 1) / least, 256ll}));
+  y.split_len = (int)std::max(128ll, std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30));
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
   if (y.n_splits > 1) {
     const size_t parts = (size_t)b->n_tokens * nq * y.n_splits;
@@ -248,11 +252,15 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
     if (scale == 0.f) scale = 1.f / std::sqrt((float)pages->head_dim);
     const int rep = n_q_heads / pages->n_kv_heads;
     AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale * 1.44269504088896340736f, window, window ? sinks : 0,
-               y.n_splits, y.split_len, y.tiles, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes)};
+               y.n_splits, y.split_len, y.tiles, y.tile_rows, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes)};
     const long long groups = (long long)b.n_seq * c.n_kv_heads * y.n_splits;
     if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * n_q_heads >= (1ll << 28)) return refuse("too many sequences, tokens and heads");
     const hipStream_t st = (hipStream_t)hip_stream;
     hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
+      if constexpr (sizeof(t) == 2)
+        if (y.many)
+          return launch(k_attn_many<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups, y.tiles), dim3(256),
+                        Many<decltype(ct), decltype(hd)::v>::LDS, st, c, b, a);
       return launch(k_attn_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups, y.tiles), dim3(kAttnThreads), 0, st, c, b, a);
     });
     if (e == hipSuccess && y.n_splits > 1)
