@@ -274,19 +274,19 @@ struct Tile {
   static __device__ __forceinline__ int at(int row, int piece) { return row * ROW + swizzle(row, piece) * 16; }
 };
 
-constexpr int kAttnThreads = 256;
-
-template <class C, int HD>
-constexpr int attn_lds() {                               // the wavefronts' values, then their results
-  return 4 * (Tile<C, HD>::LDS > 16 * (HD + 4) * 4 ? Tile<C, HD>::LDS : 16 * (HD + 4) * 4);
-}
+constexpr int kAttnWaves = 4, kAttnThreads = 64 * kAttnWaves;
+// a wavefront's result in its LDS: 16 rows of HD fp32 numbers, 16-byte pieces in an order by row
+template <int HD>
+__device__ __forceinline__ int res_at(int row, int piece) { return row * HD + (piece ^ row) * 4; }
 
 template <class T, class C, int HD>
 __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
   typedef Tile<C, HD> W;
   typedef Mat<C> M;
   constexpr int KB = W::KB, NP = W::NP, ND = W::ND, PER = W::PER;
-  __shared__ __align__(16) char lds[attn_lds<C, HD>()];
+  constexpr int AREA = W::LDS > 64 * HD ? W::LDS : 64 * HD;     // of a wavefront: its values, then its result
+  __shared__ __align__(16) char lds[kAttnWaves * AREA];
+  __shared__ float2 res_ml[kAttnWaves][16];
   // workgroup -> (sequence, key head, split, tile); the tiles of the same keys are a multiple of the grid's other
   // dimension apart, on one XCD where that is a multiple of 8
   const int per = c.n_kv_heads * a.n_splits;
@@ -333,13 +333,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
   }
 
   const C *kp = (const C *)c.k + (long long)head * c.page_size * HD, *vp = (const C *)c.v + (long long)head * c.page_size * HD;
-  char *mine = lds + wave * W::LDS;
+  char *mine = lds + wave * AREA;
   f32x4 o[ND];
   float m, l;
 
   // The entries of step `it`'s keys, a step ahead of the loads that need them
-  const int steps = (i1 - i0 + 4 * M::kKeys - 1) / (4 * M::kKeys);
-  auto key_of = [&](int it, int kb) { return i0 + (it * 4 + wave) * M::kKeys + kb * 16 + col; };
+  const int steps = (i1 - i0 + kAttnWaves * M::kKeys - 1) / (kAttnWaves * M::kKeys);
+  auto key_of = [&](int it, int kb) { return i0 + (it * kAttnWaves + wave) * M::kKeys + kb * 16 + col; };
   auto entries = [&](int it, int (&e)[KB]) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
       }
     }
     // does every row see every key of this step?
-    const int base = i0 + (it * 4 + wave) * M::kKeys, lo = sp.pos(base), hi = sp.pos(min(base + M::kKeys, i1) - 1);
+    const int base = i0 + (it * kAttnWaves + wave) * M::kKeys, lo = sp.pos(base), hi = sp.pos(min(base + M::kKeys, i1) - 1);
     const bool all = __popc(there) == M::kKeys && hi <= sp.first && (!a.window || lo > sp.last - a.window || hi < a.sinks);
     float top = -INFINITY;
 #pragma unroll
@@ -517,33 +517,34 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
     for (int n = 0; n < 4; ++n) sick += o[t][n] * 0.f;
   if (__any(sick != 0.f)) pass(True{});
 
-  // the four wavefronts' results: [row][HD + 4] with maximum and sum behind the row
+  // the wavefronts' results, added in their order
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  __syncthreads();
-  constexpr int LD = HD + 4;
   float *res = (float *)lds;
+  constexpr int LD = AREA / 4;
 #pragma unroll
-  for (int t = 0; t < ND; ++t) *(f32x4 *)(res + (wave * 16 + col) * LD + t * 16 + 4 * g) = o[t];
-  if (g == 0) {
-    res[(wave * 16 + col) * LD + HD] = m;
-    res[(wave * 16 + col) * LD + HD + 1] = l;
-  }
+  for (int t = 0; t < ND; ++t) *(f32x4 *)(res + wave * LD + res_at<HD>(col, 4 * t + g)) = o[t];
+  if (g == 0) res_ml[wave][col] = make_float2(m, l);
   __syncthreads();
-  constexpr int E = HD / 16;                             // elements of a thread
-  const int row = threadIdx.x / 16, e0 = threadIdx.x % 16 * E;
-  if (r0 + row > r1) return;
-  float mw[4], big = -INFINITY, sum = 0.f, v[E];
+  constexpr int E = HD / 32 > 4 ? HD / 32 : 4, LANES = HD / E;   // elements of a thread, threads of a row
+  const int row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
+  if (row >= 16 || r0 + row > r1) return;
+  float big = -INFINITY, sum = 0.f, v[E];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) { mw[w] = res[(w * 16 + row) * LD + HD]; big = fmaxf(big, mw[w]); }
+  for (int w = 0; w < kAttnWaves; ++w) big = fmaxf(big, res_ml[w][row].x);
 #pragma unroll
   for (int e = 0; e < E; ++e) v[e] = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw[w] - big);
-    sum += f * res[(w * 16 + row) * LD + HD + 1];
+  for (int w = 0; w < kAttnWaves; ++w) {
+    const float2 ml = res_ml[w][row];
+    const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - big);
+    sum += f * ml.y;
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] += f * res[(w * 16 + row) * LD + e0 + e];
+    for (int e = 0; e < E; e += 4) {
+      const f32x4 x4 = *(const f32x4 *)(res + w * LD + res_at<HD>(row, (e0 + e) / 4));
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[e + n] += f * x4[n];
+    }
   }
   const int to = a.by_rep.quot(r0 + row), oh = head * a.rep + (r0 + row - to * a.rep);
   const long long t = first_token + to;
@@ -889,38 +890,60 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   }
 }
 
-// The splits of a row joined, in their order: 16 lanes a row.
-template <class T, int HD>
+// The splits of a row joined.  HD / 4 lanes have a row's elements, the others take other splits; WAVES wavefronts a row, their
+// sums added in their order.
+template <class T, int HD, int WAVES>
 __global__ __launch_bounds__(256) void k_attn_join(Batch b, AttnArgs a) {
-  constexpr int E = HD / 16;
-  const long long w = (long long)blockIdx.x * 16 + threadIdx.x / 16;
-  if (w >= (long long)b.n_tokens * a.nq) return;
-  const int t = (int)(w / a.nq), h = (int)(w % a.nq), e0 = threadIdx.x % 16 * E;
-  const int s = seq_of(b, t);
-  if (s < 0) return;
-  int first, count;
-  seq_tokens(b, s, first, count);
-  const int r = (t - first) * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
-  if (t < first || t - first >= count || r0 >= a.tiles * a.tile_rows) return;
-  const Span sp = span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, count * a.rep) - 1);
-  const int parts = splits_of(a, sp.n);
-  if (parts == 1) return;
+  constexpr int LANES = HD / 4, GROUPS = WAVES * 64 / LANES;
+  const long long w = (long long)blockIdx.x * (4 / WAVES) + threadIdx.x / (64 * WAVES);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64 % WAVES, e0 = lane % LANES * 4, group = wave * (64 / LANES) + lane / LANES;
+  int parts = 0, s = -1, t = 0, h = 0;
+  if (w < (long long)b.n_tokens * a.nq) {
+    t = (int)(w / a.nq);
+    h = (int)(w % a.nq);
+    s = seq_of(b, t);
+  }
+  if (s >= 0) {
+    int first, count;
+    seq_tokens(b, s, first, count);
+    const int r = (t - first) * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
+    if (t >= first && t - first < count && r0 < a.tiles * a.tile_rows)
+      parts = splits_of(a, span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, count * a.rep) - 1).n);
+  }
+  if (parts <= 1 && WAVES == 1) return;                          // (the row is done, or no row)
   const float2 *ml = a.part_ml + w * a.n_splits;
   const float *po = a.part_o + w * a.n_splits * HD + e0;
-  float big = -INFINITY, sum = 0.f, v[E];
-  for (int z = 0; z < parts; ++z) big = fmaxf(big, ml[z].x);
+  float big = -INFINITY, sum = 0.f;
+  for (int z = lane; z < parts; z += 64) big = fmaxf(big, ml[z].x);
 #pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = 0.f;
-  for (int z = 0; z < parts; ++z) {
+  for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int z = group; z < parts; z += GROUPS) {
     const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[z].x - big);
     sum += f * ml[z].y;
-#pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      const f32x4 x = *(const f32x4 *)(po + (long long)z * HD + e);
-      for (int n = 0; n < 4; ++n) v[e + n] += f * x[n];
-    }
+    v += f * *(const f32x4 *)(po + (long long)z * HD);
   }
-  store_row<T, E>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, v, sum);
+#pragma unroll
+  for (int d = LANES; d < 64; d <<= 1) {
+    sum += __shfl_xor(sum, d);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) v[n] += __shfl_xor(v[n], d);
+  }
+  if constexpr (WAVES > 1) {
+    __shared__ f32x4 part[WAVES][LANES];
+    __shared__ float part_sum[WAVES];
+    if (lane < LANES) part[wave][lane] = v;
+    if (lane == 0) part_sum[wave] = sum;
+    __syncthreads();
+    if (parts <= 1 || wave || lane >= LANES) return;
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) { v += part[i][lane]; sum += part_sum[i]; }
+  }
+  if (lane < LANES) {
+    const float x[4] = {v[0], v[1], v[2], v[3]};
+    store_row<T, 4>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, x, sum);
+  }
 }
 
 // ------------------------------------------------------------------ copies

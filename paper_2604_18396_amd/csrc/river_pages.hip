@@ -195,6 +195,7 @@ struct AttnPlan {
   size_t o_bytes, bytes;                                         // of the partial results
 };
 constexpr int kManyRows = 128;
+
 static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
   AttnPlan y{};
   const int rep = nq / p->n_kv_heads;
@@ -265,7 +266,9 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
     });
     if (e == hipSuccess && y.n_splits > 1)
       e = by_types(pages, [&](auto t, auto, auto hd) {
-        return launch(k_attn_join<decltype(t), decltype(hd)::v>, dim3((unsigned)(((long long)b.n_tokens * n_q_heads + 15) / 16)), dim3(256), 0, st, b, a);
+        const unsigned rows = (unsigned)(b.n_tokens * n_q_heads);
+        return y.n_splits <= 16 ? launch(k_attn_join<decltype(t), decltype(hd)::v, 1>, dim3((rows + 3) / 4), dim3(256), 0, st, b, a)
+                                : launch(k_attn_join<decltype(t), decltype(hd)::v, 4>, dim3(rows), dim3(256), 0, st, b, a);
       });
     return e == hipSuccess ? RIVER_OK : hip_failed("river_paged_attention", e);
   });
