@@ -526,7 +526,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
   for (int t = 0; t < ND; ++t) *(f32x4 *)(res + wave * LD + res_at<HD>(col, 4 * t + g)) = o[t];
   if (g == 0) res_ml[wave][col] = make_float2(m, l);
   __syncthreads();
-  constexpr int E = HD / 32 > 4 ? HD / 32 : 4, LANES = HD / E;   // elements of a thread, threads of a row
+  constexpr int E = HD * 16 / kAttnThreads > 4 ? HD * 16 / kAttnThreads : 4, LANES = HD / E;   // elements of a thread, threads of a row
   const int row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
   if (row >= 16 || r0 + row > r1) return;
   float big = -INFINITY, sum = 0.f, v[E];
