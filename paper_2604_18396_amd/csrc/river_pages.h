@@ -22,6 +22,7 @@ struct Div {
 struct Cache {
   void *k, *v;
   long long page_stride;                  // elements
+  uint32_t page_pieces;                   // the same in pieces of 16 bytes
   int n_pages, page_size, n_kv_heads;
   Div by_page;
 };
@@ -158,6 +159,15 @@ struct Span {                             // the keys of a tile of rows
   int first, last;                        // positions of its first and its last row's token
   int hs, low, n;
   __device__ __forceinline__ int pos(int i) const { return i < hs ? i : i - hs + low; }
+  // Index of position p >= low.
+  __device__ __forceinline__ int at(int p) const { return p - low + hs; }
+};
+// What the row of a token at position p sees of a tile's keys, by index: those up to `to`, of these from `from` on and below
+// `sinks` (the same for all rows).  As bits of the 32 keys from index `base` on:
+struct Sight {
+  int to, from, sinks;
+  static __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+  __device__ __forceinline__ uint32_t bits(int base) const { return below(to + 1 - base) & (~below(from - base) | below(sinks - base)); }
 };
 // rows r0 .. r1 of a sequence with `count` new tokens
 __device__ __forceinline__ Span span_of(const Batch &b, const AttnArgs &a, int len, int count, int r0, int r1) {
@@ -169,6 +179,9 @@ __device__ __forceinline__ Span span_of(const Batch &b, const AttnArgs &a, int l
   s.hs = max(0, min(min(a.sinks, s.low), end));
   s.n = s.hs + max(0, end - s.low);
   return s;
+}
+__device__ __forceinline__ Sight sight_of(const AttnArgs &a, const Span &s, int p) {
+  return Sight{s.at(p), a.window ? max(0, s.at(p - a.window + 1)) : 0, max(s.hs, s.at(a.sinks))};
 }
 // Splits of a tile that have keys, at least one; the last split of a launch takes what is left.
 __device__ __forceinline__ int splits_of(const AttnArgs &a, int n) { return min(a.n_splits, max(1, (n + a.split_len - 1) / a.split_len)); }
@@ -186,7 +199,7 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 template <class C> struct Mat;
 template <> struct Mat<__bf16> {
   static constexpr int kKeys = 32;        // keys of a step
-  static constexpr float kBias = 0.f;
+  static constexpr float kBias = 0.f, kLazy = 8.f, kLazyBias = 0.f;
   static constexpr bool kSplitP = true;   // probabilities as a sum of two bf16 numbers (see Step)
   static __device__ __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -194,12 +207,17 @@ template <> struct Mat<__bf16> {
   static __device__ __forceinline__ uint32_t pack(float x, float y) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y}); }
   static __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
   static __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+  static __device__ __forceinline__ float add_pair(uint32_t w, float c) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), bf16x2{(__bf16)1.f, (__bf16)1.f}, c, false);
+  }
   static constexpr uint32_t kExp = 0x7f80u;
 };
 template <> struct Mat<_Float16> {
   static constexpr int kKeys = 32;
   // probabilities times 2^15: fp16's normal numbers then reach down to 2^-29 of the most likely key's
   static constexpr float kBias = 15.f;
+  // (where the maximum may lag behind by kLazy)
+  static constexpr float kLazy = 5.f, kLazyBias = 10.f;
   static constexpr bool kSplitP = false;  // (their 11 bits are eight times finer than the result's)
   static __device__ __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
@@ -207,6 +225,9 @@ template <> struct Mat<_Float16> {
   static __device__ __forceinline__ uint32_t pack(float x, float y) { return __builtin_bit_cast(uint32_t, half2v{(_Float16)x, (_Float16)y}); }
   static __device__ __forceinline__ float low(uint32_t w) { return (float)__builtin_bit_cast(half2v, w).x; }
   static __device__ __forceinline__ float high(uint32_t w) { return (float)__builtin_bit_cast(half2v, w).y; }
+  static __device__ __forceinline__ float add_pair(uint32_t w, float c) {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w), half2v{(_Float16)1.f, (_Float16)1.f}, c, false);
+  }
   static constexpr uint32_t kExp = 0x7c00u;
 };
 template <> struct Mat<float> {
@@ -560,32 +581,43 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)
 //
-// Bound: the matrix cores, and beside them as long, the exponentials (a 32 x 32 x 16 product takes 32 cycles, the softmax of the 32 keys x
-// 64 rows of a step 900 against the 1024 of its products at HD 128).  A wavefront holds 64 rows, so that an operand
-// fetched from LDS is used twice (with 32 rows the fetches alone take as long as the products), one wavefront per SIMD with 512
-// registers, four of them 256 rows on the same keys.  What would wait for each other is taken from different steps: step n
-// multiplies S(n+1) = K Q^T, takes the exponentials of S(n), and adds P(n-1) V, three things that do not depend on each other.
-// O is therefore rescaled one step after the maximum has moved (pend).
-// Keys and values travel global -> registers -> LDS, rings of two and four steps; one barrier a step.
+// Bound: the matrix cores, and beside them as long, the vector instructions (exponentials above all).  A wavefront holds 64
+// rows, so that an operand fetched from LDS is used twice (with 32 rows the fetches alone take as long as the products), one
+// wavefront per SIMD with 512 registers, four of them 256 rows on the same keys.  What would wait for each other is taken from
+// different steps of 32 keys: step n multiplies S(n+1) = K Q^T, takes the exponentials of S(n), and adds P(n-1) V, three things
+// that do not depend on each other.
+// O is therefore rescaled one step after the maximum has moved (pend); it moves when a score is 2^kLazy times as likely as
+// what was the maximum (one of 64 rows has a new maximum in most steps, and rescaling takes as long as the step).
+// Keys and values go from memory straight into LDS (no registers, four steps in flight), in rings of four and eight steps, one barrier
+// a step; where a key's row lies is looked up for 32 steps at once.
 template <class C, int HD>
 struct Many {
   typedef Mat<C> M;
-  static constexpr int KEYS = 32, RB = 2, WROWS = 32 * RB, ROWS = 4 * WROWS, VRING = 4, KRING = 2;
+  static constexpr int KEYS = 32, RB = 2, WROWS = 32 * RB, ROWS = 4 * WROWS;
+  static constexpr int AHEAD = 4, KRING = 4, VRING = 8, CHUNK = 32;      // in steps; CHUNK: rows looked up at once
   static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
   static constexpr int KS = HD / 16, DB = HD / 32;
-  static constexpr int STAGE = KEYS * ROW, LDS = (KRING + VRING) * STAGE + 4 * VRING;
-  static constexpr int PER = 256 / PIECES, NL = KEYS / PER;    // rows of a round of loads, and rounds
+  static constexpr int STAGE = KEYS * ROW;
+  static constexpr int V = KRING * STAGE, PLACES = V + VRING * STAGE, THERE = PLACES + 2 * CHUNK * KEYS * 8, LDS = THERE + 2 * CHUNK * 4;
+  static constexpr int PER = 64 / PIECES, NL = 8 / PER;  // a wavefront loads eight rows, PER of them at a time
   // Pieces of a row lie in an order by row: eight neighbouring rows of keys, and the four rows of a transposing read of
   // values, meet in different banks
-  static __device__ __forceinline__ int k_at(int row, int piece) {
-    return row * ROW + (piece ^ (HD == 128 ? row & 15 : row & 7)) * 16;
+  static __device__ __forceinline__ int k_swizzle(int row) { return HD == 128 ? row & 15 : row & 7; }
+  static __device__ __forceinline__ int v_swizzle(int row) {
+    return HD == 128 ? ((row & 7) << 1) | ((row >> 3) & 1) : ((row & 3) << 1) | ((row >> 2) & 1);
   }
-  static __device__ __forceinline__ int v_at(int row, int piece) {
-    return row * ROW + (piece ^ (HD == 128 ? ((row & 7) << 1) | ((row >> 3) & 1) : ((row & 3) << 1) | ((row >> 2) & 1))) * 16;
-  }
-  // bit of a step's word of pages that are there for key k: a wavefront's rows of a round are a byte
-  static constexpr __device__ __forceinline__ int there_bit(int k) { return NL == 1 ? k : (k % PER / 4) * 8 + k / PER * 4 + k % 4; }
+  static __device__ __forceinline__ int k_at(int row, int piece) { return row * ROW + (piece ^ k_swizzle(row)) * 16; }
+  static __device__ __forceinline__ int v_at(int row, int piece) { return row * ROW + (piece ^ v_swizzle(row)) * 16; }
 };
+// 16 bytes a lane from memory to LDS, the lanes' one after the other from byte `lds` on.  Counts on vmcnt; no register is written.
+__device__ __forceinline__ void load_lds16(uint32_t lds, const void *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from));
+}
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {        // all but the last N loads done, by every wavefront
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+__device__ const u32x4 g_zero_row[16] = {};
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <class C>
 __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
@@ -599,9 +631,10 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   typedef Many<C, HD> W;
   typedef Mat<C> M;
   constexpr int RB = W::RB, KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
-  extern __shared__ __align__(16) char lds[];
-  char *const klds = lds, *const vlds = lds + W::KRING * W::STAGE;
-  uint8_t *const there_lds = (uint8_t *)(lds + (W::KRING + W::VRING) * W::STAGE);
+  extern __shared__ __align__(1024) char lds[];
+  char *const vlds = lds + W::V;
+  long long *const places = (long long *)(lds + W::PLACES);
+  uint32_t *const there_of = (uint32_t *)(lds + W::THERE);
   // workgroup -> (sequence, key head, split), tile: the last tile, which sees most keys, first; a key head's tiles on one XCD
   // where their distance in the grid is a multiple of 8
   const int per = c.n_kv_heads * a.n_splits;
@@ -623,11 +656,11 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   const int first = len - count + a.by_rep.quot(w0), last = len - count + a.by_rep.quot(w1);
   u32x4 qf[KS][RB];
   float sc[RB];
-  int mypos[RB];
+  Sight sight[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int r = min(r0 + wave * W::WROWS + rb * 32 + col, r1), tok = a.by_rep.quot(r);
-    mypos[rb] = len - count + tok;
+    sight[rb] = sight_of(a, sp, len - count + tok);
     const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
     sc[rb] = a.scale2;
 #pragma unroll
@@ -649,63 +682,62 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     sc[rb] = fmaxf(sc[rb], 1e-37f);                      // (-infinity times it stays one)
   }
 
-  const C *kp = (const C *)c.k + (long long)head * c.page_size * HD, *vp = (const C *)c.v + (long long)head * c.page_size * HD;
-  const int my_row = threadIdx.x / W::PIECES, my_piece = threadIdx.x % W::PIECES;
-  auto entries = [&](int n, int (&e)[NL]) {
+  const u32x4 *kp = (const u32x4 *)((const C *)c.k + (long long)head * c.page_size * HD), *vp = (const u32x4 *)((const C *)c.v + (long long)head * c.page_size * HD);
+  const int *row_of_table = b.table + (long long)s * b.table_stride;
+  constexpr int CK = W::CHUNK * KEYS;
+  // Where the rows of CHUNK steps lie (in pieces from kp and vp), -1 without a page or behind the end; and a bit a key
+  auto look_up = [&](int chunk) {
 #pragma unroll
-    for (int j = 0; j < NL; ++j)
-      e[j] = b.table[(long long)s * b.table_stride + c.by_page.quot(sp.pos(min(i0 + n * KEYS + j * W::PER + my_row, i1 - 1)))];
-  };
-  auto fetch = [&](int n, const int (&e)[NL], u32x4 (&k)[NL], u32x4 (&v)[NL], uint32_t &ok_) {
-    ok_ = 0;
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int i = i0 + n * KEYS + j * W::PER + my_row, p = sp.pos(min(i, i1 - 1));
-      const bool ok = i < i1 && (unsigned)e[j] < (unsigned)c.n_pages;
-      const long long at = ok ? (long long)e[j] * c.page_stride + (long long)(p - c.by_page.quot(p) * c.page_size) * HD : 0;
-      k[j] = *(const u32x4 *)(kp + at + my_piece * 8);
-      v[j] = *(const u32x4 *)(vp + at + my_piece * 8);
-      ok_ |= (uint32_t)ok << j;
-    }
-  };
-  auto stage = [&](int n, const u32x4 (&k)[NL], const u32x4 (&v)[NL], uint32_t ok_) {
-    const int slot = n % W::VRING;
-    uint32_t byte = 0;
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const bool ok = ok_ >> j & 1;
-      *(u32x4 *)(klds + n % W::KRING * W::STAGE + W::k_at(j * W::PER + my_row, my_piece)) = k[j];
-      // (a value that nobody sees is zero, whatever its bits)
-      *(u32x4 *)(vlds + slot * W::STAGE + W::v_at(j * W::PER + my_row, my_piece)) = ok ? v[j] : u32x4{0, 0, 0, 0};
+    for (int j = 0; j < CK / 256; ++j) {
+      const int k = j * 256 + (int)threadIdx.x, i = chunk * CK + k, p = sp.pos(min(i0 + i, i1 - 1)), page = c.by_page.quot(p);
+      const int e = row_of_table[page];
+      const bool ok = i0 + i < i1 && (unsigned)e < (unsigned)c.n_pages;
+      const unsigned long long at = (unsigned long long)(uint32_t)e * c.page_pieces + (uint32_t)((p - page * c.page_size) * W::PIECES);
+      places[(chunk & 1) * CK + k] = ok ? (long long)at : -1;
       const unsigned long long all = __ballot(ok);
-#pragma unroll
-      for (int q = 0; q < 64 / W::PIECES; ++q) byte |= (uint32_t)(all >> (q * W::PIECES) & 1) << (j * 4 + q);
+      if (lane < 2) there_of[(chunk & 1) * W::CHUNK + (j * 256 + wave * 64) / KEYS + lane] = (uint32_t)(all >> (32 * lane));
     }
-    if (lane == 0) there_lds[slot * 4 + wave] = (uint8_t)byte;
   };
-  auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // a lane's piece of a row: in LDS it lies where the swizzle puts it
+  const int my_row = wave * 8 + lane / W::PIECES, my_slot = lane % W::PIECES;
+  int k_piece[NL], v_piece[NL];
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    k_piece[j] = my_slot ^ W::k_swizzle(my_row + j * W::PER);
+    v_piece[j] = my_slot ^ W::v_swizzle(my_row + j * W::PER);
+  }
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds, lds0 = lds_base + wave * 8 * W::ROW;
+  auto fetch = [&](int n) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const long long at = places[n % (2 * W::CHUNK) * KEYS + my_row + j * W::PER];
+      const bool ok = at >= 0;
+      // (what has no row: keys of page 0, which no score counts, and values of zeros, whatever the bits of the cache there)
+      const u32x4 *k = kp + (ok ? at : 0) + k_piece[j], *v = (ok ? vp + at : g_zero_row) + v_piece[j];
+      load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, k);
+      load_lds16(lds0 + W::V + n % W::VRING * W::STAGE + j * W::PER * W::ROW, v);
+    }
+  };
 
   f32x16 o[DB][RB], sx[RB];
   u32x4 pr[2][RB];
-  float m[RB], l[RB], off[RB], fac[RB];
+  float m[RB], lim[RB], l[RB], off[RB], fac[RB];
   bool pend;
 
-  // scores of step n as they count: what a row does not see is -infinity, and the maximum where that moves it
+  // Step n's scores as they count: what a row does not see is -infinity.  The maximum, where that moves it.
   auto settle = [&](int n, float (&top)[RB]) {
-    const uint32_t there = __builtin_amdgcn_readfirstlane(*(const uint32_t *)(there_lds + n % W::VRING * 4));
+    const uint32_t there = __builtin_amdgcn_readfirstlane(there_of[n % (2 * W::CHUNK)]);
     const int base = i0 + n * KEYS, lo = sp.pos(base), hi = sp.pos(min(base + KEYS, i1) - 1);
     const bool all = n < steps && there == 0xffffffffu && hi <= first && (!a.window || lo > last - a.window || hi < a.sinks);
     if (!all) {
-      const uint32_t mine = n < steps ? there >> (NL == 1 ? 4 * h : 8 * h) : 0;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
+        const uint32_t see = n < steps ? (sight[rb].bits(base) & there) >> (4 * h) : 0u;
         top[rb] = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int p = sp.pos(base + 8 * (i / 4) + 4 * h + i % 4);
-          const bool ok = (mine >> W::there_bit(8 * (i / 4) + i % 4) & 1) && p <= mypos[rb] && (!a.window || p > mypos[rb] - a.window || p < a.sinks);
-          sx[rb][i] = ok ? sx[rb][i] : -INFINITY;
-          top[rb] = fmaxf(top[rb], sx[rb][i]);
+          sx[rb][i] = (see >> (8 * (i / 4) + i % 4) & 1) ? sx[rb][i] : -INFINITY;
+          top[rb] = __builtin_elementwise_maximum(top[rb], sx[rb][i]);
         }
       }
     }
@@ -715,28 +747,32 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) o[d][rb] *= fac[rb];
     }
-    pend = __any(top[0] > m[0] || top[1] > m[1]);
+    pend = __any(top[0] > lim[0] || top[1] > lim[1]);
     if (pend) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const float now = fmaxf(m[rb], fmaxf(top[rb], __shfl_xor(top[rb], 32)));
-        const float to = (now == -INFINITY ? 0.f : now * sc[rb]) - M::kBias;
+        // (each row by its own scores alone, whatever the others did)
+        const float high = fmaxf(top[rb], __shfl_xor(top[rb], 32)), now = high > lim[rb] ? high : m[rb];
+        const float to = (now == -INFINITY ? 0.f : now * sc[rb]) - M::kLazyBias;
         fac[rb] = m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[rb] - to);
         if (now == m[rb]) fac[rb] = 1.f;
         m[rb] = now;
+        lim[rb] = now + M::kLazy / sc[rb];
         off[rb] = to;
         l[rb] *= fac[rb];
       }
     }
   };
 
-  auto pass = [&](auto careful_) {
-    constexpr bool CAREFUL = decltype(careful_)::value;
+  // Careful: a value that is not finite stands where some rows see it and others do not (0 times it would be NaN).  Such
+  // values are left out of what is multiplied and added to the rows that see them; everything else has the same bits.
+  bool careful = false;
+  for (;;) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      m[rb] = -INFINITY;
+      m[rb] = lim[rb] = -INFINITY;
       l[rb] = 0.f;
-      off[rb] = -M::kBias;
+      off[rb] = -M::kLazyBias;
       fac[rb] = 1.f;
       pr[0][rb] = pr[1][rb] = u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -745,103 +781,101 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
         for (int i = 0; i < 16; ++i) o[d][rb][i] = 0.f;
     }
     pend = false;
-    if (steps == 0) return;
-    int e[NL];
-    u32x4 kr[NL], vr[NL];
-    uint32_t ok_;
-    // the values of step -1 are zeros; steps 0 and 1 into the ring, step 2 on the way
-    for (int i = threadIdx.x; i < W::STAGE / 16; i += 256) *(u32x4 *)(vlds + (W::VRING - 1) * W::STAGE + i * 16) = u32x4{0, 0, 0, 0};
-    entries(0, e);
-    fetch(0, e, kr, vr, ok_);
-    stage(0, kr, vr, ok_);
-    entries(1, e);
-    fetch(1, e, kr, vr, ok_);
-    stage(1, kr, vr, ok_);
-    entries(2, e);
-    fetch(2, e, kr, vr, ok_);
-    entries(3, e);
-    barrier();
-    auto scores = [&](int n, f32x16 (&to)[RB]) {
-      const char *at = klds + n % W::KRING * W::STAGE;
+    if (steps == 0) break;
+    // (careful: this wavefront's own rows of step n, which have arrived)
+    auto clean = [&](int n) {
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+      for (int j = 0; j < NL; ++j) {
+        uint32_t *at = (uint32_t *)(vlds + n % W::VRING * W::STAGE + (my_row + j * W::PER) * W::ROW + my_slot * 16);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) to[rb][i] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 kf = *(const u32x4 *)(at + W::k_at(col, 2 * ks + h));
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) to[rb] = mul32<C>(kf, qf[ks][rb], to[rb]);
+        for (int w = 0; w < 4; ++w) at[w] = finite_only<C>(at[w]);
       }
     };
-    auto maxima = [&](const f32x16 (&of)[RB], float (&top)[RB]) {
+    look_up(0);
+    // the values of step -1 are zeros
+    for (int i = threadIdx.x; i < W::STAGE / 16; i += 256) *(u32x4 *)(vlds + (W::VRING - 1) * W::STAGE + i * 16) = u32x4{0, 0, 0, 0};
+    wait_and_meet<0>();
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        top[rb] = of[rb][0];
+    for (int n = 0; n < W::AHEAD; ++n) fetch(n);
+    if (careful) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      for (int n = 0; n < W::AHEAD; ++n) clean(n);
+    }
+    wait_and_meet<(W::AHEAD - 2) * 2 * NL>();
+    // The operands of a step, one after the other: keys of S(n + 1), then values of step n - 1.  The swizzle's part that
+    // depends on the operand is an exclusive or with a constant, the rest is the lane's.
+    const uint32_t k0 = lds_base + W::k_at(col, h);
+    const uint32_t v0 = lds_base + W::V + W::v_at(4 * h + lane % 16 / 4, (lane % 32 / 16) * 2 + lane % 4 / 2) + lane % 2 * 8;
+    auto operand = [&](int g, uint32_t k_step, uint32_t v_step) {
+      if (g < KS) return *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(k_step ^ (uint32_t)(g * 32));
+      // four keys 16 t + 8 u + 4 h .. of the element d * 32 + lane % 32
+      const int t = (g - KS) / DB, d = (g - KS) % DB;
+      u32x4 f;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top[rb] = fmaxf(top[rb], of[rb][i]);
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t at = (v_step ^ (uint32_t)(d * 64 + (HD == 128 ? u * 16 : 0))) + (16 * t + 8 * u) * W::ROW;
+        const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)at));
+        f[2 * u] = w.x;
+        f[2 * u + 1] = w.y;
       }
+      return f;
     };
     float top[RB];
-    scores(0, sx);
-    maxima(sx, top);
+    {
+      const uint32_t k_step = k0;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 f = operand(ks, k_step, 0);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) sx[rb] = mul32<C>(f, qf[ks][rb], ks ? sx[rb] : f32x16{});
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        top[rb] = sx[rb][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top[rb] = __builtin_elementwise_maximum(top[rb], sx[rb][i]);
+      }
+    }
     settle(0, top);
     // step `steps` only adds what the last one left
     for (int n = 0; n <= steps; ++n) {
-      stage(n + 2, kr, vr, ok_);
-      fetch(n + 3, e, kr, vr, ok_);
-      entries(n + 4, e);
+      // Sixteen groups (HD 64: eight) of two products, the operand of the third group after it, and a share of the vector
+      // instructions.  The compiler must not mix the groups: left alone it fetches each operand right in front of its
+      // products and waits for it, and takes the exponentials past the branches below.
+      constexpr int G = KS + 2 * DB, PAIRS = 16 / G, PRE = 3;
+      const uint32_t k_step = k0 + (n + 1) % W::KRING * W::STAGE, v_step = v0 + (n + W::VRING - 1) % W::VRING * W::STAGE;
       f32x16 sn[RB];
-      scores(n + 1, sn);
-      u32x4 pn[2][RB];
+      u32x4 f[PRE + 1], pn[2][RB];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+      for (int g = 0; g < PRE; ++g) f[g] = operand(g, k_step, v_step);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
+      for (int g = 0; g < G; ++g) {
+        if (g + PRE < G) f[(g + PRE) % (PRE + 1)] = operand(g + PRE, k_step, v_step);
+        if (g == 1) fetch(n + W::AHEAD);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          if (g < KS) sn[rb] = mul32<C>(f[g % (PRE + 1)], qf[g][rb], g ? sn[rb] : f32x16{});
+          else o[(g - KS) % DB][rb] = mul32<C>(f[g % (PRE + 1)], pr[(g - KS) / DB][rb], o[(g - KS) % DB][rb]);
+        }
+#pragma unroll
+        for (int q = g * PAIRS; q < (g + 1) * PAIRS; ++q) {      // pair q % 8 of row block q / 8
+          const int rb = q / 8, i = 2 * (q % 8);
           const float p0 = __builtin_amdgcn_exp2f(fmaf(sx[rb][i], sc[rb], -off[rb])), p1 = __builtin_amdgcn_exp2f(fmaf(sx[rb][i + 1], sc[rb], -off[rb]));
-          l[rb] += p0;
-          l[rb] += p1;
-          pn[i / 8][rb][i % 8 / 2] = M::pack(p0, p1);
+          uint32_t w = M::pack(p0, p1);
+          asm volatile("" : "+v"(w));
+          l[rb] = M::add_pair(w, l[rb]);                         // (the sum of what is multiplied: rounded alike)
+          pn[i / 8][rb][i % 8 / 2] = w;
         }
-      const char *at = vlds + (n + W::VRING - 1) % W::VRING * W::STAGE;
-      if constexpr (CAREFUL) {
-        if (n > 0) {
-          const uint32_t there = *(const uint32_t *)(there_lds + (n + W::VRING - 1) % W::VRING * 4);
-          for (int key = 0; key < KEYS; ++key) {
-            const int p = sp.pos(i0 + (n - 1) * KEYS + key);
-            for (int rb = 0; rb < RB; ++rb) {
-              const bool ok = (there >> W::there_bit(key) & 1) && p <= mypos[rb] && (!a.window || p > mypos[rb] - a.window || p < a.sinks);
-              for (int d = 0; d < DB; ++d)
-                for (int i = 0; i < 16; ++i) {
-                  const int el = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
-                  const float v = (float)*(const C *)(at + W::v_at(key, el / 8) + el % 8 * 2);
-                  if (ok && not_finite(v)) o[d][rb][i] += v;
-                }
-            }
-          }
+        // (the maximum that is NaN where one of its arguments is: two of it are one instruction.  A row with such a score is NaN anyway)
+        if (g == KS) top[0] = top[1] = -INFINITY;
+        if (g >= KS) {
+#pragma unroll
+          for (int q = (g - KS) * (32 / (2 * DB)); q < (g - KS + 1) * (32 / (2 * DB)); ++q)
+            top[q / 16] = __builtin_elementwise_maximum(top[q / 16], sn[q / 16][q % 16]);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          u32x4 vf;
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            // four keys 16 t + 8 u + 4 h .. of the element d * 32 + lane % 32
-            const int row = 16 * t + 8 * u + 4 * h + lane % 16 / 4, el = d * 32 + (lane % 32 / 16) * 16 + lane % 4 * 4;
-            const s16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4 *)(at + W::v_at(row, el / 8) + el % 8 * 2));
-            const u32x2 w2 = __builtin_bit_cast(u32x2, four);
-            vf[2 * u] = w2.x;
-            vf[2 * u + 1] = w2.y;
-          }
-          if constexpr (CAREFUL)
-            for (int w = 0; w < 4; ++w) vf[w] = finite_only<C>(vf[w]);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) o[d][rb] = mul32<C>(vf, pr[t][rb], o[d][rb]);
-        }
-      maxima(sn, top);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         sx[rb] = sn[rb];
@@ -849,18 +883,42 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
         pr[1][rb] = pn[1][rb];
       }
       settle(n + 1, top);
-      barrier();
+      if ((n + W::AHEAD + 1) % W::CHUNK == 0) look_up((n + W::AHEAD + 1) / W::CHUNK);
+      if (careful) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        clean(n + W::AHEAD);
+      }
+      wait_and_meet<(W::AHEAD - 2) * 2 * NL>();
     }
-  };
-  pass(False{});
-  float sick = 0.f;
+    wait_and_meet<0>();                                          // (nothing may land in LDS behind the end)
+    if (careful) {
+      for (int i = i0; i < i1; ++i) {
+        int slot;
+        const int page = page_of(c, b, s, sp.pos(i), slot);
+        if (page < 0) continue;
+        const C *row = (const C *)vp + (long long)page * c.page_stride + (long long)slot * HD + 4 * h;
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+          for (int e4 = 0; e4 < 16; ++e4) {
+            const float v = (float)row[d * 32 + 8 * (e4 / 4) + e4 % 4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sick += o[d][rb][i] * 0.f;
-  if (__syncthreads_or(sick != 0.f)) pass(True{});
+            for (int rb = 0; rb < RB; ++rb)
+              if ((sight[rb].bits(i) & 1) && not_finite(v)) o[d][rb][e4] += v;
+          }
+      }
+      break;
+    }
+    float sick = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sick += o[d][rb][i] * 0.f;
+    if (!__syncthreads_or(sick != 0.f)) break;
+    careful = true;
+  }
 
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -885,7 +943,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
 #pragma unroll
         for (int i = 0; i < 16; i += 4) *(f32x4 *)(to + d * 32 + 2 * i) = f32x4{o[d][rb][i], o[d][rb][i + 1], o[d][rb][i + 2], o[d][rb][i + 3]};
       // (maxima in base 2, as k_attn_split has them)
-      if (h == 0) a.part_ml[part] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kBias, l[rb]);
+      if (h == 0) a.part_ml[part] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kLazyBias, l[rb]);
     }
   }
 }

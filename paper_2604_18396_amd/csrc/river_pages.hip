@@ -2,6 +2,7 @@
 #include "river.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <climits>
 #include <cstdint>
@@ -45,6 +46,21 @@ hipError_t launch(void (*k)(A...), dim3 grid, dim3 block, size_t lds, hipStream_
   return hipLaunchKernel((const void *)k, grid, block, args, lds, s);
 }
 
+// The same with more than 64 KiB of dynamic LDS, which each kernel asks for once per device.
+template <auto K, class... A>
+hipError_t launch_lds(dim3 grid, dim3 block, size_t lds, hipStream_t s, A... a) {
+  static std::atomic<uint64_t> asked{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(asked.load(std::memory_order_relaxed) & bit)) {
+    if ((e = hipFuncSetAttribute((const void *)K, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) != hipSuccess) return e;
+    asked.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch(K, grid, block, lds, s, a...);
+}
+
 Div div_by(int d) {
   uint32_t s = 0;
   while ((1ll << s) < d) ++s;
@@ -58,7 +74,7 @@ constexpr int kMostTokens = 1 << 22;
 
 Cache layer_cache(const river_pages *p, int layer) {
   const size_t at = (size_t)layer * p->layer_stride * elem_bytes(p);
-  return Cache{(char *)p->k + at, (char *)p->v + at, p->page_stride, p->n_pages, p->page_size, p->n_kv_heads, div_by(p->page_size)};
+  return Cache{(char *)p->k + at, (char *)p->v + at, p->page_stride, (uint32_t)(p->page_stride * elem_bytes(p) / 16), p->n_pages, p->page_size, p->n_kv_heads, div_by(p->page_size)};
 }
 
 const char *bad_batch(const river_batch *b) {
@@ -105,6 +121,7 @@ int river::check_pages(const river_pages *p, std::string *why) {
   const int es = elem_bytes(p);
   if ((((uintptr_t)p->k | (uintptr_t)p->v) & 15) || p->page_stride * es % 16 || p->layer_stride * es % 16)
     return bad("pages and their strides must be multiples of 16 bytes");
+  if ((__int128)p->page_stride * es >= ((__int128)1 << 36)) return bad("page_stride must be below 64 GiB");
   // no two pages may overlap: the nearer stride holds a page, the further one all that the nearer one strides over
   const __int128 x = page_elems(p), ps = p->page_stride, ls = p->layer_stride;
   if (x > (1ll << 40) || ps < 0 || ls < 0) return bad("bad page size or strides");
@@ -260,8 +277,8 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
     hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
       if constexpr (sizeof(t) == 2)
         if (y.many)
-          return launch(k_attn_many<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups, y.tiles), dim3(256),
-                        Many<decltype(ct), decltype(hd)::v>::LDS, st, c, b, a);
+          return launch_lds<k_attn_many<decltype(t), decltype(ct), decltype(hd)::v>>(dim3((unsigned)groups, y.tiles), dim3(256),
+                                                                                    Many<decltype(ct), decltype(hd)::v>::LDS, st, c, b, a);
       return launch(k_attn_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups, y.tiles), dim3(kAttnThreads), 0, st, c, b, a);
     });
     if (e == hipSuccess && y.n_splits > 1)
