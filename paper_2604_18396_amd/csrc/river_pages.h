@@ -217,7 +217,7 @@ template <> struct Mat<_Float16> {
   // probabilities times 2^15: fp16's normal numbers then reach down to 2^-29 of the most likely key's
   static constexpr float kBias = 15.f;
   // (where the maximum may lag behind by kLazy)
-  static constexpr float kLazy = 5.f, kLazyBias = 10.f;
+  static constexpr float kLazy = 8.f, kLazyBias = 7.f;
   static constexpr bool kSplitP = false;  // (their 11 bits are eight times finer than the result's)
   static __device__ __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
@@ -598,7 +598,7 @@ struct Many {
   static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
   static constexpr int KS = HD / 16, DB = HD / 32;
   static constexpr int STAGE = KEYS * ROW;
-  static constexpr int V = KRING * STAGE, PLACES = V + VRING * STAGE, THERE = PLACES + 2 * CHUNK * KEYS * 8, LDS = THERE + 2 * CHUNK * 4;
+  static constexpr int V = KRING * STAGE, PLACES = V + VRING * STAGE, THERE = PLACES + 2 * CHUNK * KEYS * 16, LDS = THERE + 2 * CHUNK * 4;
   static constexpr int PER = 64 / PIECES, NL = 8 / PER;  // a wavefront loads eight rows, PER of them at a time
   // Pieces of a row lie in an order by row: eight neighbouring rows of keys, and the four rows of a transposing read of
   // values, meet in different banks
@@ -633,7 +633,8 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   constexpr int RB = W::RB, KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
   extern __shared__ __align__(1024) char lds[];
   char *const vlds = lds + W::V;
-  long long *const places = (long long *)(lds + W::PLACES);
+  typedef unsigned long long Place __attribute__((ext_vector_type(2)));
+  Place *const places = (Place *)(lds + W::PLACES);
   uint32_t *const there_of = (uint32_t *)(lds + W::THERE);
   // workgroup -> (sequence, key head, split), tile: the last tile, which sees most keys, first; a key head's tiles on one XCD
   // where their distance in the grid is a multiple of 8
@@ -651,9 +652,13 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, h = lane / 32;
   const int steps = (i1 - i0 + KEYS - 1) / KEYS;
 
-  // this wavefront's rows: their queries in the operand's order, positions; rows behind the last repeat it
+  // this wavefront's rows: rows behind the last repeat it
   const int w0 = min(r0 + wave * W::WROWS, r1), w1 = min(w0 + W::WROWS - 1, r1);
   const int first = len - count + a.by_rep.quot(w0), last = len - count + a.by_rep.quot(w1);
+  const int my_slot = lane % W::PIECES;
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+  // Their queries in the operand's order.  (Through LDS, in whole rows of memory, they take as long: 4500 cycles, on the way with
+  // the table's entries.)
   u32x4 qf[KS][RB];
   float sc[RB];
   Sight sight[RB];
@@ -662,30 +667,36 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     const int r = min(r0 + wave * W::WROWS + rb * 32 + col, r1), tok = a.by_rep.quot(r);
     sight[rb] = sight_of(a, sp, len - count + tok);
     const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
-    sc[rb] = a.scale2;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks][rb] = *(const u32x4 *)(q + (2 * ks + h) * 8);
-    if constexpr (!M::kSplitP) {                         // fp16 pages: see k_attn_split
-      float big = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        for (int e = 0; e < 4; ++e)
-          big = fmaxf(big, fmaxf(fabsf(Mat<__bf16>::low(qf[ks][rb][e])), fabsf(Mat<__bf16>::high(qf[ks][rb][e]))));
-      big = fmaxf(big, __shfl_xor(big, 32));
-      const int ex = big > 0.f && !not_finite(big) ? ilogbf(big) : 0;
-      sc[rb] = ldexpf(sc[rb], ex);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        for (int e = 0; e < 4; ++e)
-          qf[ks][rb][e] = M::pack(ldexpf(Mat<__bf16>::low(qf[ks][rb][e]), -ex), ldexpf(Mat<__bf16>::high(qf[ks][rb][e]), -ex));
-    }
-    sc[rb] = fmaxf(sc[rb], 1e-37f);                      // (-infinity times it stays one)
   }
+  auto queries = [&] {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      sc[rb] = a.scale2;
+      if constexpr (!M::kSplitP) {                       // fp16 pages: see k_attn_split
+        float big = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          for (int e = 0; e < 4; ++e)
+            big = fmaxf(big, fmaxf(fabsf(Mat<__bf16>::low(qf[ks][rb][e])), fabsf(Mat<__bf16>::high(qf[ks][rb][e]))));
+        big = fmaxf(big, __shfl_xor(big, 32));
+        const int ex = big > 0.f && !not_finite(big) ? ilogbf(big) : 0;
+        sc[rb] = ldexpf(sc[rb], ex);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          for (int e = 0; e < 4; ++e)
+            qf[ks][rb][e] = M::pack(ldexpf(Mat<__bf16>::low(qf[ks][rb][e]), -ex), ldexpf(Mat<__bf16>::high(qf[ks][rb][e]), -ex));
+      }
+      sc[rb] = fmaxf(sc[rb], 1e-37f);                    // (-infinity times it stays one)
+    }
+  };
 
   const u32x4 *kp = (const u32x4 *)((const C *)c.k + (long long)head * c.page_size * HD), *vp = (const u32x4 *)((const C *)c.v + (long long)head * c.page_size * HD);
   const int *row_of_table = b.table + (long long)s * b.table_stride;
   constexpr int CK = W::CHUNK * KEYS;
-  // Where the rows of CHUNK steps lie (in pieces from kp and vp), -1 without a page or behind the end; and a bit a key
+  // Where the rows of CHUNK steps lie, and a bit a key.  What has no row (no page, behind the end): keys of page 0, which no
+  // score counts, and values of zeros, whatever the bits of the cache there
   auto look_up = [&](int chunk) {
 #pragma unroll
     for (int j = 0; j < CK / 256; ++j) {
@@ -693,46 +704,46 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       const int e = row_of_table[page];
       const bool ok = i0 + i < i1 && (unsigned)e < (unsigned)c.n_pages;
       const unsigned long long at = (unsigned long long)(uint32_t)e * c.page_pieces + (uint32_t)((p - page * c.page_size) * W::PIECES);
-      places[(chunk & 1) * CK + k] = ok ? (long long)at : -1;
+      places[(chunk & 1) * CK + k] = Place{(uintptr_t)(kp + (ok ? at : 0)), (uintptr_t)(ok ? vp + at : g_zero_row)};
       const unsigned long long all = __ballot(ok);
       if (lane < 2) there_of[(chunk & 1) * W::CHUNK + (j * 256 + wave * 64) / KEYS + lane] = (uint32_t)(all >> (32 * lane));
     }
   };
   // a lane's piece of a row: in LDS it lies where the swizzle puts it
-  const int my_row = wave * 8 + lane / W::PIECES, my_slot = lane % W::PIECES;
+  const int my_row = wave * 8 + lane / W::PIECES;
   int k_piece[NL], v_piece[NL];
 #pragma unroll
   for (int j = 0; j < NL; ++j) {
     k_piece[j] = my_slot ^ W::k_swizzle(my_row + j * W::PER);
     v_piece[j] = my_slot ^ W::v_swizzle(my_row + j * W::PER);
   }
-  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds, lds0 = lds_base + wave * 8 * W::ROW;
+  const uint32_t lds0 = lds_base + wave * 8 * W::ROW;
   auto fetch = [&](int n) {
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const long long at = places[n % (2 * W::CHUNK) * KEYS + my_row + j * W::PER];
-      const bool ok = at >= 0;
-      // (what has no row: keys of page 0, which no score counts, and values of zeros, whatever the bits of the cache there)
-      const u32x4 *k = kp + (ok ? at : 0) + k_piece[j], *v = (ok ? vp + at : g_zero_row) + v_piece[j];
-      load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, k);
-      load_lds16(lds0 + W::V + n % W::VRING * W::STAGE + j * W::PER * W::ROW, v);
+      const Place at = places[n % (2 * W::CHUNK) * KEYS + my_row + j * W::PER];
+      load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at.x + k_piece[j]);
+      load_lds16(lds0 + W::V + n % W::VRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at.y + v_piece[j]);
     }
   };
 
-  f32x16 o[DB][RB], sx[RB];
-  u32x4 pr[2][RB];
-  float m[RB], lim[RB], l[RB], off[RB], fac[RB];
+  typedef float Scores[RB][16];
+  typedef u32x4 Probs[2][RB];
+  f32x16 o[DB][RB];
+  float m[RB], lim[RB], l[RB], off[RB], fac[RB], top[RB];
   bool pend;
+  // Steps of which every row of this wavefront sees every key (where all pages are there): their last key is at most all_to,
+  // and their first is at least all_from or their last below all_sinks, by index in the split
+  const int all_to = sp.at(first) - i0, all_from = (a.window ? max(0, sp.at(last - a.window + 1)) : 0) - i0, all_sinks = sight[0].sinks - i0;
 
   // Step n's scores as they count: what a row does not see is -infinity.  The maximum, where that moves it.
-  auto settle = [&](int n, float (&top)[RB]) {
-    const uint32_t there = __builtin_amdgcn_readfirstlane(there_of[n % (2 * W::CHUNK)]);
-    const int base = i0 + n * KEYS, lo = sp.pos(base), hi = sp.pos(min(base + KEYS, i1) - 1);
-    const bool all = n < steps && there == 0xffffffffu && hi <= first && (!a.window || lo > last - a.window || hi < a.sinks);
-    if (!all) {
+  auto settle = [&](int n, Scores &sx, uint32_t there_) {
+    const uint32_t there = __builtin_amdgcn_readfirstlane(there_);
+    const int base = n * KEYS;
+    if (there != 0xffffffffu || base + KEYS - 1 > all_to || (base < all_from && base + KEYS > all_sinks)) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const uint32_t see = n < steps ? (sight[rb].bits(base) & there) >> (4 * h) : 0u;
+        const uint32_t see = (sight[rb].bits(i0 + base) & there) >> (4 * h);
         top[rb] = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -745,7 +756,10 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) o[d][rb] *= fac[rb];
+        for (int rb = 0; rb < RB; ++rb) {
+          o[d][rb] *= fac[rb];
+          __builtin_amdgcn_sched_barrier(0);             // (one after the other: few registers)
+        }
     }
     pend = __any(top[0] > lim[0] || top[1] > lim[1]);
     if (pend) {
@@ -774,7 +788,6 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       l[rb] = 0.f;
       off[rb] = -M::kLazyBias;
       fac[rb] = 1.f;
-      pr[0][rb] = pr[1][rb] = u32x4{0, 0, 0, 0};
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -800,6 +813,8 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     if (careful) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       for (int n = 0; n < W::AHEAD; ++n) clean(n);
+    } else {
+      queries();
     }
     wait_and_meet<(W::AHEAD - 2) * 2 * NL>();
     // The operands of a step, one after the other: keys of S(n + 1), then values of step n - 1.  The swizzle's part that
@@ -820,75 +835,104 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       }
       return f;
     };
-    float top[RB];
-    {
-      const uint32_t k_step = k0;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 f = operand(ks, k_step, 0);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) sx[rb] = mul32<C>(f, qf[ks][rb], ks ? sx[rb] : f32x16{});
-      }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        top[rb] = sx[rb][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top[rb] = __builtin_elementwise_maximum(top[rb], sx[rb][i]);
-      }
-    }
-    settle(0, top);
-    // step `steps` only adds what the last one left
-    for (int n = 0; n <= steps; ++n) {
-      // Sixteen groups (HD 64: eight) of two products, the operand of the third group after it, and a share of the vector
-      // instructions.  The compiler must not mix the groups: left alone it fetches each operand right in front of its
-      // products and waits for it, and takes the exponentials past the branches below.
-      constexpr int G = KS + 2 * DB, PAIRS = 16 / G, PRE = 3;
+    // Step n with the scores s (of step n) and probabilities p (of step n - 1); leaves those of the next in s1 and p1.
+    // In slots of one product, the operand of the third product pair after it, and a share of the vector instructions, each
+    // from another stage of its chain (argument, exponential, rounding and sum), so that nothing waits.  The compiler must not mix
+    // the slots: left alone it fetches each operand right in front of its products and waits for it, and takes the
+    // exponentials past the branches that follow.
+    auto step = [&](int n, Scores &s, Probs &p, Scores &s1, Probs &p1) {
+      constexpr int G = KS + 2 * DB, SLOTS = G * RB, PRE = 3, EACH = 32 / SLOTS;     // EACH: halves of a pair of exponentials
+      constexpr int FROM = KS * RB + 2, PER_SLOT = (16 * RB + SLOTS - FROM - 1) / (SLOTS - FROM);
       const uint32_t k_step = k0 + (n + 1) % W::KRING * W::STAGE, v_step = v0 + (n + W::VRING - 1) % W::VRING * W::STAGE;
       f32x16 sn[RB];
-      u32x4 f[PRE + 1], pn[2][RB];
+      u32x4 f[PRE + 1];
+      float x[2][2], y[2][2];                            // arguments and exponentials of a pair, by its parity
+      const uint32_t there = there_of[(n + 1) % (2 * W::CHUNK)];
 #pragma unroll
       for (int g = 0; g < PRE; ++g) f[g] = operand(g, k_step, v_step);
+      auto arguments = [&](int q) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[q % 2][e] = fmaf(s[q / 8][2 * (q % 8) + e], sc[q / 8], -off[q / 8]);
+      };
+      auto round_and_add = [&](int q) {
+        const int rb = q / 8, i = q % 8;
+        uint32_t w = M::pack(y[q % 2][0], y[q % 2][1]);
+        l[rb] = M::add_pair(w, l[rb]);                           // (the sum of what is multiplied: rounded alike)
+        asm volatile("" : "+v"(w), "+v"(l[rb]));
+        p1[i / 4][rb][i % 4] = w;
+      };
+      arguments(0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        if (g + PRE < G) f[(g + PRE) % (PRE + 1)] = operand(g + PRE, k_step, v_step);
-        if (g == 1) fetch(n + W::AHEAD);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          if (g < KS) sn[rb] = mul32<C>(f[g % (PRE + 1)], qf[g][rb], g ? sn[rb] : f32x16{});
-          else o[(g - KS) % DB][rb] = mul32<C>(f[g % (PRE + 1)], pr[(g - KS) / DB][rb], o[(g - KS) % DB][rb]);
+      for (int slot = 0; slot < SLOTS; ++slot) {
+        const int g = slot / RB, rb = slot % RB;
+        if (rb == 0 && g + PRE < G) f[(g + PRE) % (PRE + 1)] = operand(g + PRE, k_step, v_step);
+        if (g < KS) {
+          asm volatile("" : "+a"(qf[g][rb]));                    // (products read it there; vector instructions need the other half)
+          sn[rb] = mul32<C>(f[g % (PRE + 1)], qf[g][rb], g ? sn[rb] : f32x16{});
+        } else {
+          o[(g - KS) % DB][rb] = mul32<C>(f[g % (PRE + 1)], p[(g - KS) / DB][rb], o[(g - KS) % DB][rb]);
         }
 #pragma unroll
-        for (int q = g * PAIRS; q < (g + 1) * PAIRS; ++q) {      // pair q % 8 of row block q / 8
-          const int rb = q / 8, i = 2 * (q % 8);
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(sx[rb][i], sc[rb], -off[rb])), p1 = __builtin_amdgcn_exp2f(fmaf(sx[rb][i + 1], sc[rb], -off[rb]));
-          uint32_t w = M::pack(p0, p1);
-          asm volatile("" : "+v"(w));
-          l[rb] = M::add_pair(w, l[rb]);                         // (the sum of what is multiplied: rounded alike)
-          pn[i / 8][rb][i % 8 / 2] = w;
+        for (int e = slot * EACH; e < (slot + 1) * EACH; ++e) {
+          const int q = e / 2;
+          if (e % 2 == 0 && q + 1 < 16) arguments(q + 1);
+          y[q % 2][e % 2] = __builtin_amdgcn_exp2f(x[q % 2][e % 2]);
+          asm volatile("" : "+v"(y[q % 2][e % 2]));
+          if (e % 2 == 0 && q > 0) round_and_add(q - 1);
         }
-        // (the maximum that is NaN where one of its arguments is: two of it are one instruction.  A row with such a score is NaN anyway)
-        if (g == KS) top[0] = top[1] = -INFINITY;
-        if (g >= KS) {
+        if (slot == 4) fetch(n + W::AHEAD);
+        // The new scores and their maxima (the one that is NaN where one of its arguments is: two of it are one instruction.  A
+        // row with such a score is NaN anyway)
+        if (slot >= FROM) {
 #pragma unroll
-          for (int q = (g - KS) * (32 / (2 * DB)); q < (g - KS + 1) * (32 / (2 * DB)); ++q)
-            top[q / 16] = __builtin_elementwise_maximum(top[q / 16], sn[q / 16][q % 16]);
+          for (int e = (slot - FROM) * PER_SLOT; e < (slot - FROM + 1) * PER_SLOT && e < 16 * RB; ++e) {
+            float v = sn[e / 16][e % 16];
+            asm volatile("" : "+v"(v));
+            s1[e / 16][e % 16] = v;
+            top[e / 16] = e % 16 ? __builtin_elementwise_maximum(top[e / 16], v) : v;
+          }
+          asm volatile("" : "+v"(top[0]), "+v"(top[1]));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        sx[rb] = sn[rb];
-        pr[0][rb] = pn[0][rb];
-        pr[1][rb] = pn[1][rb];
-      }
-      settle(n + 1, top);
+      round_and_add(15);
+      settle(n + 1, s1, there);
       if ((n + W::AHEAD + 1) % W::CHUNK == 0) look_up((n + W::AHEAD + 1) / W::CHUNK);
       if (careful) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         clean(n + W::AHEAD);
       }
       wait_and_meet<(W::AHEAD - 2) * 2 * NL>();
+    };
+    Scores s0, s1;
+    Probs p0, p1;
+    {
+      f32x16 sn[RB];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 f = operand(ks, k0, 0);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) sn[rb] = mul32<C>(f, qf[ks][rb], ks ? sn[rb] : f32x16{});
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float v = sn[rb][i];
+          asm volatile("" : "+v"(v));
+          s0[rb][i] = v;
+          top[rb] = i ? __builtin_elementwise_maximum(top[rb], v) : v;
+        }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) p0[0][rb] = p0[1][rb] = u32x4{0, 0, 0, 0};
+    }
+    settle(0, s0, there_of[0]);
+    // step `steps` only adds what the last one left
+    for (int n = 0; n <= steps; n += 2) {
+      step(n, s0, p0, s1, p1);
+      if (n == steps) break;
+      step(n + 1, s1, p1, s0, p0);
     }
     wait_and_meet<0>();                                          // (nothing may land in LDS behind the end)
     if (careful) {
@@ -909,42 +953,79 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       }
       break;
     }
-    float sick = 0.f;
+    float sick = 0.f;                                            // (not finite if one of them is not)
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sick += o[d][rb][i] * 0.f;
-    if (!__syncthreads_or(sick != 0.f)) break;
+        for (int i = 0; i < 16; ++i) sick = __builtin_elementwise_maximum(sick, fabsf(o[d][rb][i]));
+    const bool any_sick = __any(not_finite(sick));
+    if (lane == 0) there_of[wave] = any_sick;
+    wait_and_meet<0>();
+    if (!(there_of[0] | there_of[1] | there_of[2] | there_of[3])) break;
+    wait_and_meet<0>();                                          // (read before it is written again)
     careful = true;
   }
 
+  // Results.  A lane has four neighbouring elements of its row at a time: the rows of a block of 32 go through this wavefront's
+  // part of LDS, pieces of 16 bytes in an order by row, so that memory gets whole rows (written as they are: 10000 cycles instead of 1500).
+  char *const mine = lds + wave * (W::STAGE * 2 * (parts == 1 ? 1 : 2));
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     l[rb] += __shfl_xor(l[rb], 32);
-    const int r = r0 + wave * W::WROWS + rb * 32 + col;
-    if (r > r1) continue;
-    const int tok = a.by_rep.quot(r), qh = head * a.rep + r - tok * a.rep;
-    const long long t = first_token + tok;
+    const int from = r0 + wave * W::WROWS + rb * 32;             // the block's first row
+    if (from > r1) break;
+    // row `row` of the block in memory
+    auto place = [&](int row, long long &t, int &qh) {
+      const int r = min(from + row, r1), tok = a.by_rep.quot(r);
+      t = first_token + tok;
+      qh = head * a.rep + r - tok * a.rep;
+      return from + row <= r1;
+    };
+    long long t;
+    int qh;
     if (parts == 1) {
       const float f = l[rb] == 0.f ? 0.f : 1.f / l[rb];
-      T *to = (T *)a.out + t * a.out_stride + (long long)qh * HD + 4 * h;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *(u32x2 *)(to + d * 32 + 2 * i) = u32x2{Mat<__bf16>::pack(o[d][rb][i] * f, o[d][rb][i + 1] * f), Mat<__bf16>::pack(o[d][rb][i + 2] * f, o[d][rb][i + 3] * f)};
+        for (int i = 0; i < 16; i += 4) {
+          const int piece = 4 * d + i / 4;
+          *(u32x2 *)(mine + col * W::ROW + (piece ^ (col % W::PIECES)) * 16 + 8 * h) =
+              u32x2{Mat<__bf16>::pack(o[d][rb][i] * f, o[d][rb][i + 1] * f), Mat<__bf16>::pack(o[d][rb][i + 2] * f, o[d][rb][i + 3] * f)};
+        }
+      __builtin_amdgcn_wave_barrier();
+      u32x4 v[32 / W::PER];
+#pragma unroll
+      for (int j = 0; j < 32 / W::PER; ++j) {
+        const int row = j * W::PER + lane / W::PIECES;
+        v[j] = *(const u32x4 *)(mine + row * W::ROW + (my_slot ^ (row % W::PIECES)) * 16);
+      }
+#pragma unroll
+      for (int j = 0; j < 32 / W::PER; ++j)
+        if (place(j * W::PER + lane / W::PIECES, t, qh)) *(u32x4 *)((T *)a.out + t * a.out_stride + (long long)qh * HD + my_slot * 8) = v[j];
     } else {
-      const long long part = (t * a.nq + qh) * a.n_splits + z;
-      float *to = a.part_o + part * HD + 4 * h;
+      constexpr int P = 2 * W::PIECES;                           // fp32: twice as many pieces
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) *(f32x4 *)(to + d * 32 + 2 * i) = f32x4{o[d][rb][i], o[d][rb][i + 1], o[d][rb][i + 2], o[d][rb][i + 3]};
+        for (int i = 0; i < 16; i += 4) {
+          const int piece = 8 * d + i / 2 + h;
+          *(f32x4 *)(mine + col * (2 * W::ROW) + (piece ^ (col % P)) * 16) = f32x4{o[d][rb][i], o[d][rb][i + 1], o[d][rb][i + 2], o[d][rb][i + 3]};
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < 32 * P / 64; ++j) {
+        const int row = j * (64 / P) + lane / P, piece = lane % P;
+        const f32x4 v = *(const f32x4 *)(mine + row * (2 * W::ROW) + (piece ^ (row % P)) * 16);
+        if (place(row, t, qh)) *(f32x4 *)(a.part_o + ((t * a.nq + qh) * a.n_splits + z) * HD + piece * 4) = v;
+      }
       // (maxima in base 2, as k_attn_split has them)
-      if (h == 0) a.part_ml[part] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kLazyBias, l[rb]);
+      if (h == 0 && place(col, t, qh))
+        a.part_ml[(t * a.nq + qh) * a.n_splits + z] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kLazyBias, l[rb]);
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
