@@ -718,12 +718,15 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     v_piece[j] = my_slot ^ W::v_swizzle(my_row + j * W::PER);
   }
   const uint32_t lds0 = lds_base + wave * 8 * W::ROW;
-  auto fetch = [&](int n) {
+  auto find = [&](int n, Place (&at)[NL]) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j) at[j] = places[n % (2 * W::CHUNK) * KEYS + my_row + j * W::PER];
+  };
+  auto fetch = [&](int n, const Place (&at)[NL]) {
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const Place at = places[n % (2 * W::CHUNK) * KEYS + my_row + j * W::PER];
-      load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at.x + k_piece[j]);
-      load_lds16(lds0 + W::V + n % W::VRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at.y + v_piece[j]);
+      load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].x + k_piece[j]);
+      load_lds16(lds0 + W::V + n % W::VRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].y + v_piece[j]);
     }
   };
 
@@ -809,7 +812,11 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     for (int i = threadIdx.x; i < W::STAGE / 16; i += 256) *(u32x4 *)(vlds + (W::VRING - 1) * W::STAGE + i * 16) = u32x4{0, 0, 0, 0};
     wait_and_meet<0>();
 #pragma unroll
-    for (int n = 0; n < W::AHEAD; ++n) fetch(n);
+    for (int n = 0; n < W::AHEAD; ++n) {
+      Place at[NL];
+      find(n, at);
+      fetch(n, at);
+    }
     if (careful) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       for (int n = 0; n < W::AHEAD; ++n) clean(n);
@@ -848,6 +855,8 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       u32x4 f[PRE + 1];
       float x[2][2], y[2][2];                            // arguments and exponentials of a pair, by its parity
       const uint32_t there = there_of[(n + 1) % (2 * W::CHUNK)];
+      Place at[NL];
+      find(n + W::AHEAD, at);
 #pragma unroll
       for (int g = 0; g < PRE; ++g) f[g] = operand(g, k_step, v_step);
       auto arguments = [&](int q) {
@@ -881,7 +890,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
           asm volatile("" : "+v"(y[q % 2][e % 2]));
           if (e % 2 == 0 && q > 0) round_and_add(q - 1);
         }
-        if (slot == 4) fetch(n + W::AHEAD);
+        if (slot == 4) fetch(n + W::AHEAD, at);
         // The new scores and their maxima (the one that is NaN where one of its arguments is: two of it are one instruction.  A
         // row with such a score is NaN anyway)
         if (slot >= FROM) {
