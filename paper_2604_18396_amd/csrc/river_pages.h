@@ -136,6 +136,106 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope_store(Cache c, Batch b, R
   }
 }
 
+// The same by 16-byte pieces, where rows, strides and the rotated part allow it.  Bound: memory (a token's row in, its queries and
+// cache rows out).  A unit is a piece, or the two pieces whose elements are pairs; a thread has kRopeUnits of them in flight (its loads
+// stand in front of its stores, which the compiler may not move them past: the queries may be rotated in place).
+constexpr int kRopeUnits = 2;
+template <class T, class C, int HD>
+__global__ __launch_bounds__(kRopeThreads) void k_rope_store_wide(Cache c, Batch b, RopeArgs a, Div by_units) {
+  constexpr int PER = 16 / sizeof(T), P = HD / PER;
+  const int t = blockIdx.x;
+  const int s = seq_of(b, t);
+  if (s < 0) return;
+  const int p = position_of(b, s, t);
+  if (p < 0) return;
+  __shared__ float2 cs[HD / 2];
+  const T *q = (const T *)a.q + t * a.q_stride, *k = (const T *)a.k + t * a.k_stride, *v = (const T *)a.v + t * a.v_stride;
+  T *qo = (T *)a.q_out + t * a.q_out_stride;
+  int slot = 0;
+  const int page = page_of(c, b, s, p, slot);
+  const long long row = (long long)page * c.page_stride + (long long)slot * HD, head = (long long)c.page_size * HD;
+  C *ko = (C *)c.k + row, *vo = (C *)c.v + row;
+  const int pairs = a.interleaved ? 0 : a.rot / (2 * PER);       // units of two pieces a head; the others are of one
+  const int turned = (a.nq + c.n_kv_heads) * (int)by_units.d;    // units of queries and keys
+  const int all = page < 0 ? a.nq * (int)by_units.d : turned + c.n_kv_heads * P;
+  struct Unit { const T *from; int h, e; bool two, rot; };       // h: head, of the queries, the keys, then the values
+  auto unit = [&](int i) {
+    Unit u;
+    if (i >= turned) {
+      u.h = a.nq + c.n_kv_heads + (i - turned) / P;
+      u.e = (i - turned) % P * PER;
+      u.two = u.rot = false;
+      u.from = v + (u.h - a.nq - c.n_kv_heads) * HD + u.e;
+      return u;
+    }
+    u.h = by_units.quot(i);
+    const int j = i - u.h * (int)by_units.d;
+    u.two = j < pairs;
+    u.e = (j < pairs ? j : j + pairs) * PER;
+    u.rot = u.two || (a.interleaved && u.e < a.rot);
+    u.from = (u.h < a.nq ? q + u.h * HD : k + (u.h - a.nq) * HD) + u.e;
+    return u;
+  };
+  auto store = [&](const Unit &u, int e, const float (&x)[PER]) {
+    if (u.h < a.nq) {
+      T y[PER];
+#pragma unroll
+      for (int n = 0; n < PER; ++n) y[n] = (T)x[n];
+      *(u32x4 *)(qo + u.h * HD + e) = *(const u32x4 *)y;
+    } else {
+      const bool key = u.h < a.nq + c.n_kv_heads;
+      C y[PER];
+#pragma unroll
+      for (int n = 0; n < PER; ++n) y[n] = (C)x[n];
+      *(u32x4 *)((key ? ko : vo) + (u.h - a.nq - (key ? 0 : c.n_kv_heads)) * head + e) = *(const u32x4 *)y;
+    }
+  };
+  const int apart = a.rot / 2;
+  bool first = true;
+  for (int i = threadIdx.x; i < all || first; i += kRopeThreads * kRopeUnits) {
+    Unit u[kRopeUnits];
+    u32x4 w[kRopeUnits][2];
+#pragma unroll
+    for (int n = 0; n < kRopeUnits; ++n)
+      if (i + n * kRopeThreads < all) {
+        u[n] = unit(i + n * kRopeThreads);
+        w[n][0] = *(const u32x4 *)u[n].from;
+        if (u[n].two) w[n][1] = *(const u32x4 *)(u[n].from + apart);
+      }
+    if (first) {                                                 // (the angles, while the first rows are on their way)
+      if ((int)threadIdx.x < apart) cs[threadIdx.x] = turn(p, a.inv_freq[threadIdx.x], a.mscale);
+      __syncthreads();
+      first = false;
+    }
+#pragma unroll
+    for (int n = 0; n < kRopeUnits; ++n)
+      if (i + n * kRopeThreads < all) {
+        float x[PER], y[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) { x[e] = (float)((const T *)&w[n][0])[e]; }
+        if (u[n].two) {
+#pragma unroll
+          for (int e = 0; e < PER; ++e) {
+            const float z = (float)((const T *)&w[n][1])[e];
+            const float2 f = cs[u[n].e + e];
+            y[e] = z * f.x + x[e] * f.y;
+            x[e] = x[e] * f.x - z * f.y;
+          }
+          store(u[n], u[n].e + apart, y);
+        } else if (u[n].rot) {
+#pragma unroll
+          for (int e = 0; e < PER; e += 2) {
+            const float2 f = cs[(u[n].e + e) / 2];
+            const float z = x[e + 1];
+            x[e + 1] = z * f.x + x[e] * f.y;
+            x[e] = x[e] * f.x - z * f.y;
+          }
+        }
+        store(u[n], u[n].e, x);
+      }
+  }
+}
+
 // ------------------------------------------------------------------ attention
 //
 // Rows.  The new tokens of a sequence and the rep query heads that share a key head make count * rep rows of one product:

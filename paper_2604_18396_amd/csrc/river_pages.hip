@@ -188,8 +188,19 @@ extern "C" int river_rope_store(const river_pages *pages, int32_t layer, const r
     const Cache c = layer_cache(pages, layer);
     const Batch b = device_batch(batch, pages->page_size);
     const RopeArgs a{rope->inv_freq, rope->rot_dim, rope->layout, rope->mscale, n_q_heads, q, k, v, q_out, q_stride, k_stride, v_stride, q_out_stride};
+    // by pieces of 16 bytes: 4096 tokens of the 8B shape PIECES us, element by element ELEMENTS
+    const int per = 16 / es;
+    const bool wide = (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out) & 15) == 0 &&
+                      (q_stride | k_stride | v_stride | q_out_stride) % per == 0 &&
+                      rope->rot_dim % (rope->layout == RIVER_ROPE_HALF ? 2 * per : per) == 0;
+    const int units = pages->head_dim / per - (rope->layout == RIVER_ROPE_HALF ? rope->rot_dim / (2 * per) : 0);   // of a head
     const hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
-      return launch(k_rope_store<decltype(t), decltype(ct), decltype(hd)::v>, dim3(b.n_tokens), dim3(kRopeThreads), 0, (hipStream_t)hip_stream, c, b, a);
+      typedef decltype(t) T;
+      typedef decltype(ct) C;
+      constexpr int HD = decltype(hd)::v;
+      const dim3 grid(b.n_tokens), block(kRopeThreads);
+      return wide ? launch(k_rope_store_wide<T, C, HD>, grid, block, 0, (hipStream_t)hip_stream, c, b, a, div_by(units))
+                  : launch(k_rope_store<T, C, HD>, grid, block, 0, (hipStream_t)hip_stream, c, b, a);
     });
     return e == hipSuccess ? RIVER_OK : hip_failed("river_rope_store", e);
   });
