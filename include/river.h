@@ -352,12 +352,16 @@ int river_rope_store(const river_pages *pages, int32_t layer, const river_batch 
  * q, out: DEVICE [n_tokens][n_q_heads][head_dim], pages->dtype, strides in elements, multiples of 16 bytes, 16-byte aligned;
  * out must not overlap q.  At most 2^22 tokens and sequences a call (river_rope_store too).
  * workspace: DEVICE, 16-byte aligned, of at least the bytes that river_paged_attention_workspace gives for the
- * same arguments (0 bytes: may be NULL); its contents mean nothing before and after the call. */
+ * same arguments (0 bytes: may be NULL); its contents mean nothing before and after the call.
+ * tickets: DEVICE int32 [RIVER_TICKETS], 4-byte aligned, or NULL.  All zero before the first call that has them and left zero by every call;
+ * calls that share them (captured ones among them) must not run at the same time, as calls that share a workspace must not.
+ * With them the last workgroup of a row joins the parts of a split cache; without, or where there are many, a second launch does. */
+#define RIVER_TICKETS 1024
 int river_paged_attention_workspace(const river_pages *pages, const river_batch *batch, int32_t n_q_heads,
                                     int32_t window, int32_t sinks, size_t *bytes);
 int river_paged_attention(const river_pages *pages, int32_t layer, const river_batch *batch, int32_t n_q_heads,
                           const void *q, int64_t q_stride, float scale, int32_t window, int32_t sinks, void *out,
-                          int64_t out_stride, void *workspace, size_t workspace_bytes, void *hip_stream);
+                          int64_t out_stride, void *workspace, size_t workspace_bytes, int32_t *tickets, void *hip_stream);
 
 /* Copies pages src[i] to dst[i] in every layer, keys and values, as if one pair after the other (a page may be
  * copied several times, and be the source of a later pair; pairs that depend on each other cost a launch).

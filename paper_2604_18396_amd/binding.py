@@ -7,6 +7,7 @@ been built, loading raises: there is no fallback of any kind.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -28,6 +29,7 @@ EXPORTS = ("river_quantize_w4", "river_workspace_bytes", "river_create", "river_
            "river_copy_pages", "river_pool_create", "river_pool_destroy", "river_pool_extend", "river_pool_fork",
            "river_pool_rewind", "river_pool_trim", "river_pool_compact", "river_pool_flush", "river_pool_length",
            "river_pool_free_pages", "river_pool_row", "river_save_pages", "river_load_pages")
+TICKETS = 1024
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
@@ -116,7 +118,7 @@ def load():
     L.river_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, ptr, C.POINTER(C.c_float)]
     L.river_rope_store.argtypes = [pages, i32, batch, C.POINTER(river_rope), i32, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr]
     L.river_paged_attention_workspace.argtypes = [pages, batch, i32, i32, i32, C.POINTER(C.c_size_t)]
-    L.river_paged_attention.argtypes = [pages, i32, batch, i32, ptr, i64, C.c_float, i32, i32, ptr, i64, ptr, C.c_size_t, ptr]
+    L.river_paged_attention.argtypes = [pages, i32, batch, i32, ptr, i64, C.c_float, i32, i32, ptr, i64, ptr, C.c_size_t, ptr, ptr]
     L.river_copy_pages.argtypes = [pages, ptr, ptr, i32, ptr]
     L.river_pool_create.argtypes = [i32, i32, i32, i32, C.POINTER(ptr)]
     for name, more in (("destroy", []), ("extend", [i32, i32]), ("fork", [i32, i32]), ("rewind", [i32, i32]), ("trim", [i32, i32, i32]),
@@ -396,7 +398,7 @@ class River:
 
 # ------------------------------------------------------------------ paged key-value cache
 
-def _check_call(rc: int):
+def _check_call(rc: int) -> int:
     if rc < 0:
         raise RiverError(rc, load().river_last_error(None).decode())
     return rc
@@ -408,13 +410,20 @@ def _check_on(device, dtype, **tensors):
             raise ValueError(f"{name}: {dtype} on {device} is needed, not {t.dtype} on {t.device}")
 
 
-def _on_stream(device, call, *args):
-    """The call on the device's current torch stream (the library takes the stream of the current device)."""
-    # (the stream's handle without the torch.cuda.Stream object around it, which takes longer than the rest of a small call)
-    if device.index == torch.cuda.current_device():
-        return _check_call(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
-    with torch.cuda.device(device):
-        return _check_call(call(*args, torch._C._cuda_getCurrentRawStream(device.index)))
+# (the device's number and its stream's handle without the torch.cuda objects around them, which take longer than a small call)
+_device = torch._C._cuda_getDevice
+_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _on_device(call):
+    """The call with its first argument's device current: the library takes the current device and the stream it is given."""
+    @functools.wraps(call)
+    def there(first, *args, **kw):
+        if first.index == _device():
+            return call(first, *args, **kw)
+        with torch.cuda.device(first.index):
+            return call(first, *args, **kw)
+    return there
 
 
 class Pages:
@@ -430,7 +439,7 @@ class Pages:
             raise ValueError("a page's heads, positions and elements must be contiguous")
         if (dtype, k.dtype) not in ((torch.float32,) * 2, (torch.bfloat16,) * 2, (torch.bfloat16, torch.float16)):
             raise ValueError(f"no cache of {k.dtype} for {dtype}")
-        self.k, self.v, self.dtype, self.device = k, v, dtype, k.device
+        self.k, self.v, self.dtype, self.device, self.index = k, v, dtype, k.device, k.device.index
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.c = river_pages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), layers, pages, size, heads, hd,
                              0 if dtype == torch.float32 else 1, 1 if k.dtype == torch.float16 else 0)
@@ -517,6 +526,7 @@ def _out(q: torch.Tensor, out: torch.Tensor | None, pages: Pages):
     return out, _rows("out", out, pages)
 
 
+@_on_device
 def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope: Rope,
                      out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotates q and k [n_tokens, heads, head_dim] at the new tokens' positions and stores k and v in the pages.  Returns the
@@ -526,11 +536,12 @@ def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k:
     if k.shape[0] != n or v.shape[0] != n or rope.device != pages.device:
         raise ValueError("q, k and v must have the same tokens, and the frequencies their device")
     out, os_ = _out(q, out, pages)
-    _on_stream(pages.device, load().river_rope_store, pages.ref, layer, batch.bind(n, pages), rope.ref, q.shape[1], q.data_ptr(), qs,
-               k.data_ptr(), ks, v.data_ptr(), vs, out.data_ptr(), os_)
+    _check_call(load().river_rope_store(pages.ref, layer, batch.bind(n, pages), rope.ref, q.shape[1], q.data_ptr(), qs, k.data_ptr(), ks,
+                                        v.data_ptr(), vs, out.data_ptr(), os_, _stream(pages.index)))
     return out
 
 
+@_on_device
 def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, window: int = 0, sinks: int = 0,
                           scale: float = 0.0, out: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of the new tokens' queries [n_tokens, heads, head_dim] over their sequences' pages.  Rows of `out` (or of the new
@@ -545,11 +556,28 @@ def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tenso
         got = C.c_size_t()
         _check_call(L.river_paged_attention_workspace(pages.ref, ref, heads, window, sinks, C.byref(got)))
         nbytes = batch._bytes[key] = got.value
-    # (from torch's allocator, call by call: the memory of a captured call belongs to its graph, and no two streams share it)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=pages.device) if nbytes else None
-    _on_stream(pages.device, L.river_paged_attention, pages.ref, layer, ref, heads, q.data_ptr(), qs, scale, window, sinks,
-               out.data_ptr(), os_, ws.data_ptr() if nbytes else None, nbytes)
+    stream, ws, tickets = _stream(pages.index), None, None
+    if nbytes:
+        # (from torch's allocator, call by call: the memory of a captured call belongs to its graph, and no two streams share it)
+        memory = torch.empty(nbytes, dtype=torch.uint8, device=pages.device)
+        ws, tickets = memory.data_ptr(), _tickets(pages.index, stream)
+    _check_call(L.river_paged_attention(pages.ref, layer, ref, heads, q.data_ptr(), qs, scale, window, sinks, out.data_ptr(), os_, ws, nbytes,
+                                        tickets, stream))
     return out
+
+
+_ticket_tensors = {}
+
+
+def _tickets(index: int, stream: int):
+    """The attention's tickets for a stream: its calls run one after the other, so one set serves them all.  None while a graph is
+    captured, which may be replayed on any stream at any time."""
+    if torch._C._cuda_isCurrentStreamCapturing():
+        return None
+    t = _ticket_tensors.get((index, stream))
+    if t is None:
+        t = _ticket_tensors[(index, stream)] = torch.zeros(TICKETS, dtype=torch.int32, device=f"cuda:{index}")
+    return t.data_ptr()
 
 
 def _page_list(x) -> np.ndarray:
@@ -563,12 +591,13 @@ def _page_list(x) -> np.ndarray:
     return a.astype(np.int32, copy=False)
 
 
+@_on_device
 def river_copy_pages(pages: Pages, src, dst):
     """Copies pages src[i] -> dst[i] (host lists) in every layer, as if one after the other."""
     s, d = _page_list(src), _page_list(dst)
     if s.size != d.size:
         raise ValueError("as many destinations as sources")
-    _on_stream(pages.device, load().river_copy_pages, pages.ref, s.ctypes.data, d.ctypes.data, s.size)
+    _check_call(load().river_copy_pages(pages.ref, s.ctypes.data, d.ctypes.data, s.size, _stream(pages.index)))
 
 
 class PagePool:
@@ -580,6 +609,7 @@ class PagePool:
         _check_call(load().river_pool_create(n_pages, page_size, max_seqs, max_pages, C.byref(h)))
         self._h, self.max_seqs, self.max_pages = h, max_seqs, max_pages
         self.state = torch.empty(max_seqs * (max_pages + 1), dtype=torch.int32, device=device)
+        self.index = self.state.device.index
         self.lens, self.table = self.state[:max_seqs], self.state[max_seqs:].view(max_seqs, max_pages)
 
     def close(self):
@@ -611,11 +641,12 @@ class PagePool:
     def compact(self) -> int:
         return _check_call(load().river_pool_compact(self._h))
 
+    @_on_device
     def flush(self, pages: Pages | None = None):
         """Queued copies and changed entries, on the device's current stream."""
         if pages is not None and pages.device != self.state.device:
             raise ValueError("pages and pool are on different devices")
-        _on_stream(self.state.device, load().river_pool_flush, self._h, None if pages is None else pages.ref, self.state.data_ptr())
+        _check_call(load().river_pool_flush(self._h, None if pages is None else pages.ref, self.state.data_ptr(), _stream(self.index)))
 
     def length(self, seq: int) -> int:
         return _check_call(load().river_pool_length(self._h, seq))

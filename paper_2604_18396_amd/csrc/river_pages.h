@@ -253,6 +253,8 @@ struct AttnArgs {
   int n_splits, split_len, tiles, tile_rows;   // of the keys; tiles of rows per sequence and key head
   float *part_o;                          // [n_tokens][nq][n_splits][HD], where a tile has several splits
   float2 *part_ml;                        // [n_tokens][nq][n_splits] maximum (base 2) and sum
+  unsigned int *tickets;                  // [sequences x key heads x tiles] workgroups that are done; zero between calls (null: a
+                                          // launch of its own joins the splits)
 };
 
 struct Span {                             // the keys of a tile of rows
@@ -396,9 +398,55 @@ struct Tile {
 };
 
 constexpr int kAttnWaves = 4, kAttnThreads = 64 * kAttnWaves;
+constexpr int kJoinAtOnce = 4;            // parts of a row that a thread fetches at once
+// Eight bytes at agent scope
+__device__ __forceinline__ void put_through(float *to, float x, float y) {
+  __hip_atomic_store((unsigned long long *)to, __builtin_bit_cast(unsigned long long, make_float2(x, y)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_past(const float2 *from) {
+  return __builtin_bit_cast(float2, __hip_atomic_load((const unsigned long long *)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
 // a wavefront's result in its LDS: 16 rows of HD fp32 numbers, 16-byte pieces in an order by row
 template <int HD>
 __device__ __forceinline__ int res_at(int row, int piece) { return row * HD + (piece ^ row) * 4; }
+
+// E elements of a row from its parts, in their order
+template <int HD, int E>
+__device__ __forceinline__ void join_parts(const AttnArgs &a, long long first_part, int parts, int e0, float (&v)[E], float &sum) {
+  float big = -INFINITY;
+  sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = 0.f;
+  for (int y0 = 0; y0 < parts; y0 += kJoinAtOnce) {              // (as many on their way at once)
+    float2 ml[kJoinAtOnce], x[kJoinAtOnce][E / 2];
+#pragma unroll
+    for (int y = 0; y < kJoinAtOnce; ++y) {
+      const long long part = first_part + min(y0 + y, parts - 1);
+      ml[y] = get_past(a.part_ml + part);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) x[y][e / 2] = get_past((const float2 *)(a.part_o + part * HD + e0 + e));
+    }
+    float now = big;
+#pragma unroll
+    for (int y = 0; y < kJoinAtOnce; ++y) now = fmaxf(now, ml[y].x);
+    const float before = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(big - now);
+    sum *= before;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] *= before;
+    big = now;
+#pragma unroll
+    for (int y = 0; y < kJoinAtOnce; ++y)
+      if (y0 + y < parts) {
+        const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[y].x - big);
+        sum += f * ml[y].y;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          v[e] += f * x[y][e / 2].x;
+          v[e + 1] += f * x[y][e / 2].y;
+        }
+      }
+  }
+}
 
 template <class T, class C, int HD>
 __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
@@ -649,7 +697,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
   __syncthreads();
   constexpr int E = HD * 16 / kAttnThreads > 4 ? HD * 16 / kAttnThreads : 4, LANES = HD / E;   // elements of a thread, threads of a row
   const int row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
-  if (row >= 16 || r0 + row > r1) return;
+  static_assert(16 * LANES == kAttnThreads, "every thread has a part of a row");
+  const bool have = r0 + row <= r1;
   float big = -INFINITY, sum = 0.f, v[E];
 #pragma unroll
   for (int w = 0; w < kAttnWaves; ++w) big = fmaxf(big, res_ml[w][row].x);
@@ -667,16 +716,33 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
       for (int n = 0; n < 4; ++n) v[e + n] += f * x4[n];
     }
   }
-  const int to = a.by_rep.quot(r0 + row), oh = head * a.rep + (r0 + row - to * a.rep);
+  const int to = a.by_rep.quot(min(r0 + row, r1)), oh = head * a.rep + (min(r0 + row, r1) - to * a.rep);
   const long long t = first_token + to;
+  T *const out = (T *)a.out + t * a.out_stride + (long long)oh * HD + e0;
   if (parts == 1) {
-    store_row<T, E>((T *)a.out + t * a.out_stride + (long long)oh * HD + e0, v, sum);
-  } else {
-    const long long part = (t * a.nq + oh) * a.n_splits + z;
-#pragma unroll
-    for (int e = 0; e < E; e += 4) *(f32x4 *)(a.part_o + part * HD + e0 + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-    if (e0 == 0) a.part_ml[part] = make_float2(big, sum);
+    if (have) store_row<T, E>(out, v, sum);
+    return;
   }
+  // Parts cross XCDs, whose L2s are not coherent: they are written through and read past the L2, eight bytes at a time
+  const long long first_part = (t * a.nq + oh) * a.n_splits;
+  if (have) {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) put_through(a.part_o + (first_part + z) * HD + e0 + e, v[e], v[e + 1]);
+    if (e0 == 0) put_through((float *)(a.part_ml + first_part + z), big, sum);
+  }
+  if (!a.tickets) return;
+  // The last workgroup of the tile joins the parts, in their order
+  __shared__ unsigned int order;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  unsigned int *const ticket = a.tickets + ((long long)s * c.n_kv_heads + head) * a.tiles + tile;
+  if (threadIdx.x == 0) order = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (order != (unsigned)parts - 1) return;
+  if (threadIdx.x == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (!have) return;
+  join_parts<HD, E>(a, first_part, parts, e0, v, sum);
+  store_row<T, E>(out, v, sum);
 }
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)
@@ -1138,27 +1204,40 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   }
 }
 
-// The splits of a row joined.  HD / 4 lanes have a row's elements, the others take other splits; WAVES wavefronts a row, their
-// sums added in their order.
-template <class T, int HD, int WAVES>
-__global__ __launch_bounds__(256) void k_attn_join(Batch b, AttnArgs a) {
-  constexpr int LANES = HD / 4, GROUPS = WAVES * 64 / LANES;
-  const long long w = (long long)blockIdx.x * (4 / WAVES) + threadIdx.x / (64 * WAVES);
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64 % WAVES, e0 = lane % LANES * 4, group = wave * (64 / LANES) + lane / LANES;
-  int parts = 0, s = -1, t = 0, h = 0;
-  if (w < (long long)b.n_tokens * a.nq) {
-    t = (int)(w / a.nq);
-    h = (int)(w % a.nq);
-    s = seq_of(b, t);
-  }
-  if (s >= 0) {
-    int first, count;
-    seq_tokens(b, s, first, count);
-    const int r = (t - first) * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
-    if (t >= first && t - first < count && r0 < a.tiles * a.tile_rows)
-      parts = splits_of(a, span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, count * a.rep) - 1).n);
-  }
-  if (parts <= 1 && WAVES == 1) return;                          // (the row is done, or no row)
+// Where the splits of row (t, h) are: their number (0: no row, 1: it is done already)
+__device__ __forceinline__ int parts_of(const Batch &b, const AttnArgs &a, int t, int h) {
+  const int s = seq_of(b, t);
+  if (s < 0) return 0;
+  int first, count;
+  seq_tokens(b, s, first, count);
+  const int r = (t - first) * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
+  if (t < first || t - first >= count || r0 >= a.tiles * a.tile_rows) return 0;
+  return splits_of(a, span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, count * a.rep) - 1).n);
+}
+
+// Few splits joined in a launch of their own: bit for bit what the last workgroup of k_attn_split does.
+template <class T, int HD>
+__global__ __launch_bounds__(256) void k_attn_join_few(Batch b, AttnArgs a) {
+  constexpr int E = HD * 16 / kAttnThreads > 4 ? HD * 16 / kAttnThreads : 4, LANES = HD / E;
+  const long long w = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (w >= (long long)b.n_tokens * a.nq) return;
+  const int t = (int)(w / a.nq), h = (int)(w % a.nq), e0 = threadIdx.x % LANES * E;
+  const int parts = parts_of(b, a, t, h);
+  if (parts <= 1) return;
+  float v[E], sum;
+  join_parts<HD, E>(a, w * a.n_splits, parts, e0, v, sum);
+  store_row<T, E>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, v, sum);
+}
+
+// Many splits joined, a workgroup a row: HD / 4 lanes have a row's elements, the others take other splits; the wavefronts' sums are added
+// in their order.
+template <class T, int HD>
+__global__ __launch_bounds__(256) void k_attn_join_many(Batch b, AttnArgs a) {
+  constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
+  const long long w = blockIdx.x;
+  const int t = (int)(w / a.nq), h = (int)(w % a.nq), lane = threadIdx.x % 64, wave = threadIdx.x / 64, e0 = lane % LANES * 4;
+  const int parts = parts_of(b, a, t, h);
+  if (parts <= 1) return;
   const float2 *ml = a.part_ml + w * a.n_splits;
   const float *po = a.part_o + w * a.n_splits * HD + e0;
   float big = -INFINITY, sum = 0.f;
@@ -1167,7 +1246,7 @@ __global__ __launch_bounds__(256) void k_attn_join(Batch b, AttnArgs a) {
   for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int z = group; z < parts; z += GROUPS) {
+  for (int z = threadIdx.x / LANES; z < parts; z += GROUPS) {
     const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[z].x - big);
     sum += f * ml[z].y;
     v += f * *(const f32x4 *)(po + (long long)z * HD);
@@ -1178,20 +1257,16 @@ __global__ __launch_bounds__(256) void k_attn_join(Batch b, AttnArgs a) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) v[n] += __shfl_xor(v[n], d);
   }
-  if constexpr (WAVES > 1) {
-    __shared__ f32x4 part[WAVES][LANES];
-    __shared__ float part_sum[WAVES];
-    if (lane < LANES) part[wave][lane] = v;
-    if (lane == 0) part_sum[wave] = sum;
-    __syncthreads();
-    if (parts <= 1 || wave || lane >= LANES) return;
+  __shared__ f32x4 part[4][LANES];
+  __shared__ float part_sum[4];
+  if (lane < LANES) part[wave][lane] = v;
+  if (lane == 0) part_sum[wave] = sum;
+  __syncthreads();
+  if (wave || lane >= LANES) return;
 #pragma unroll
-    for (int i = 1; i < WAVES; ++i) { v += part[i][lane]; sum += part_sum[i]; }
-  }
-  if (lane < LANES) {
-    const float x[4] = {v[0], v[1], v[2], v[3]};
-    store_row<T, 4>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, x, sum);
-  }
+  for (int i = 1; i < 4; ++i) { v += part[i][lane]; sum += part_sum[i]; }
+  const float x[4] = {v[0], v[1], v[2], v[3]};
+  store_row<T, 4>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, x, sum);
 }
 
 // ------------------------------------------------------------------ copies

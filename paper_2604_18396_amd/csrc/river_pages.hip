@@ -219,10 +219,14 @@ static const char *bad_attention(const river_pages *pages, const river_batch *ba
 // How a call is divided: which kernel, tiles of rows, splits of the keys.
 struct AttnPlan {
   bool many;                                                     // k_attn_many, else k_attn_split
+  bool fused;                                                    // its last workgroups join the splits, where they have tickets
   int tiles, tile_rows, n_splits, split_len;
   size_t o_bytes, bytes;                                         // of the partial results
 };
 constexpr int kManyRows = 128;
+// Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a
+// second launch 6.4 + 3.8; 16 sequences of up to 1201 15.8, 14.3 + 3.9; 64 splits of 131072 105, 96 + 6)
+constexpr int kFewSplits = 16;
 
 static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
   AttnPlan y{};
@@ -233,12 +237,13 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
   long long keys = std::min<long long>(b->max_len, (long long)b->max_pages * p->page_size);
   if (window) keys = std::min<long long>(keys, (long long)window + sinks + (y.tile_rows - 1) / rep);
-  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many, two of
-  // k_attn_split, of at least 128 keys (there a step for each of four wavefronts)
-  const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles), goal = y.many ? 256 : 512, least = y.many ? 256 : 128;
-  const long long want = std::max(1ll, std::min({goal / groups, (keys + least - 1) / least, 256ll}));
+  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many, four of
+  // k_attn_split (two at a time), of at least 128 keys (there a step for each of four wavefronts), at most 64 splits
+  const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles), goal = y.many ? 256 : 1024, least = y.many ? 256 : 128;
+  const long long want = std::max(1ll, std::min({goal / groups, (keys + least - 1) / least, 64ll}));
   y.split_len = (int)std::max(128ll, std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30));
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
+  y.fused = !y.many && groups <= RIVER_TICKETS && y.n_splits <= kFewSplits;
   if (y.n_splits > 1) {
     const size_t parts = (size_t)b->n_tokens * nq * y.n_splits;
     y.o_bytes = parts * p->head_dim * 4;
@@ -260,7 +265,7 @@ extern "C" int river_paged_attention_workspace(const river_pages *pages, const r
 
 extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, const river_batch *batch, int32_t n_q_heads,
                                      const void *q, int64_t q_stride, float scale, int32_t window, int32_t sinks, void *out,
-                                     int64_t out_stride, void *workspace, size_t workspace_bytes, void *hip_stream) {
+                                     int64_t out_stride, void *workspace, size_t workspace_bytes, int32_t *tickets, void *hip_stream) {
   return guarded([&]() -> int {
     std::string why;
     if (const char *m = bad_attention(pages, batch, n_q_heads, window, sinks, &why)) return refuse(m);
@@ -281,7 +286,7 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
     if (scale == 0.f) scale = 1.f / std::sqrt((float)pages->head_dim);
     const int rep = n_q_heads / pages->n_kv_heads;
     AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale * 1.44269504088896340736f, window, window ? sinks : 0,
-               y.n_splits, y.split_len, y.tiles, y.tile_rows, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes)};
+               y.n_splits, y.split_len, y.tiles, y.tile_rows, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), y.fused && tickets ? (unsigned int *)tickets : nullptr};
     const long long groups = (long long)b.n_seq * c.n_kv_heads * y.n_splits;
     if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * n_q_heads >= (1ll << 28)) return refuse("too many sequences, tokens and heads");
     const hipStream_t st = (hipStream_t)hip_stream;
@@ -292,11 +297,12 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
                                                                                     Many<decltype(ct), decltype(hd)::v>::LDS, st, c, b, a);
       return launch(k_attn_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups, y.tiles), dim3(kAttnThreads), 0, st, c, b, a);
     });
-    if (e == hipSuccess && y.n_splits > 1)
+    if (e == hipSuccess && y.n_splits > 1 && !a.tickets)
       e = by_types(pages, [&](auto t, auto, auto hd) {
-        const unsigned rows = (unsigned)(b.n_tokens * n_q_heads);
-        return y.n_splits <= 16 ? launch(k_attn_join<decltype(t), decltype(hd)::v, 1>, dim3((rows + 3) / 4), dim3(256), 0, st, b, a)
-                                : launch(k_attn_join<decltype(t), decltype(hd)::v, 4>, dim3(rows), dim3(256), 0, st, b, a);
+        constexpr int HD = decltype(hd)::v;
+        const unsigned rows = (unsigned)(b.n_tokens * n_q_heads), each = 16;            // (of 16 lanes)
+        return y.n_splits <= kFewSplits ? launch(k_attn_join_few<decltype(t), HD>, dim3((rows + each - 1) / each), dim3(256), 0, st, b, a)
+                                        : launch(k_attn_join_many<decltype(t), HD>, dim3(rows), dim3(256), 0, st, b, a);
       });
     return e == hipSuccess ? RIVER_OK : hip_failed("river_paged_attention", e);
   });

@@ -524,6 +524,45 @@ def test_captured_steps_follow_the_table():
         assert torch.equal(st.k, twin.k) and torch.equal(st.v, twin.v)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("lens,splits", [([1000, 3, 0, 640, 129], "few"), ([20000], "many")], ids=str)
+def test_splits_are_joined_alike_with_tickets_and_without(kind, lens, splits):
+    for hd in (64, 128):
+        st = Setup(kind, 2, hd, 16, lens, [1] * len(lens), seed=29, ragged=False)
+        q = st.randn(len(lens), 8, hd)
+        ref, n = st.batch.bind(len(lens), st.pages), C.c_size_t()
+        assert B.load().river_paged_attention_workspace(st.pages.ref, ref, 8, 0, 0, C.byref(n)) == 0 and n.value > 0
+        ws = torch.full((n.value,), 255, dtype=torch.uint8, device=DEV)
+        tickets = torch.zeros(B.TICKETS, dtype=torch.int32, device=DEV)
+        outs = []
+        for t in (None, tickets, tickets, None):
+            out = torch.full_like(q, 7.0)
+            assert B.load().river_paged_attention(st.pages.ref, 0, ref, 8, q.data_ptr(), 8 * hd, 0.0, 0, 0, out.data_ptr(), 8 * hd, ws.data_ptr(),
+                                                  n.value, None if t is None else t.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+            torch.cuda.synchronize()
+            outs.append(out)
+            assert int(tickets.abs().sum()) == 0             # left as they were
+        assert all(torch.equal(outs[0], o) for o in outs)
+        want, tol = attention(st, q)
+        check(outs[0], want, tol)
+
+
+def test_two_streams_at_once():
+    """Calls of one batch object on two streams, in flight together."""
+    st = Setup("bf16", 2, 128, 16, [3000, 1500, 700], [1, 1, 1], seed=30, ragged=False)
+    q = st.randn(3, 8, 128)
+    want = B.river_paged_attention(st.pages, 0, st.batch, q)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(30):
+        for s in streams:
+            with torch.cuda.stream(s):
+                outs.append(B.river_paged_attention(st.pages, 0, st.batch, q))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
 def test_captured_copies():
     st = Setup("bf16", 2, 64, 16, [160], [1], seed=21, layers=3)
     src, dst = st.host[0, :4].tolist(), [int(st.host[0, 7]), int(st.host[0, 8]), int(st.host[0, 9]), int(st.spare[0])]
@@ -816,7 +855,7 @@ def test_the_binding_refuses():
     assert B.load().river_paged_attention_workspace(big.pages.ref, ref, 4, 0, 0, C.byref(n)) == 0
     if n.value:
         ws = torch.empty(n.value, dtype=torch.uint8, device=DEV)
-        args = lambda p, b: (big.pages.ref, 0, ref, 4, qq.data_ptr(), 256, 0.0, 0, 0, torch.empty_like(qq).data_ptr(), 256, p, b, None)
+        args = lambda p, b: (big.pages.ref, 0, ref, 4, qq.data_ptr(), 256, 0.0, 0, 0, torch.empty_like(qq).data_ptr(), 256, p, b, None, None)
         assert B.load().river_paged_attention(*args(ws.data_ptr(), n.value - 1)) == B.RIVER_ENOSPC
         assert B.load().river_paged_attention(*args(None, n.value)) == B.RIVER_EINVAL
         assert B.load().river_paged_attention(*args(ws.data_ptr() + 8, n.value)) == B.RIVER_EINVAL

@@ -50,7 +50,7 @@ def store(pg=None, b=None, r=None, layer=0, nq=4, q=P, qs=256, k=P, ks=128, v=P,
 
 def attend(pg=None, b=None, layer=0, nq=4, q=P, qs=256, scale=0.0, window=0, sinks=0, out=P, os=256, ws=None, n=0):
     return B.load().river_paged_attention(C.byref(pg or pages()), layer, C.byref(b or batch()), nq, q, qs, scale, window, sinks, out, os,
-                                          ws, n, None)
+                                          ws, n, None, None)
 
 
 @pytest.mark.parametrize("bad", BAD_PAGES, ids=str)
