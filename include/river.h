@@ -293,7 +293,7 @@ typedef struct {
  * q_start[n_seq] on (a padded batch) belong to no sequence: their rows are neither read nor
  * written.  So do tokens whose position would be negative, except that attention gives them zeros.
  * A table entry outside [0, n_pages) is a page that is not there: its positions are not stored and not
- * seen.  Positions from max_pages * page_size on have no page.  The q_start of a call ascends. */
+ * seen.  Positions from max_pages * page_size on, and from 2^30 on, have no page.  The q_start of a call ascends. */
 typedef struct {
   const int32_t *table;   /* [n_seq][table_stride], the first max_pages entries of a row are used */
   const int32_t *lens;    /* [n_seq] */

@@ -7,7 +7,6 @@ been built, loading raises: there is no fallback of any kind.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
 
 import numpy as np
@@ -415,17 +414,6 @@ _device = torch._C._cuda_getDevice
 _stream = torch._C._cuda_getCurrentRawStream
 
 
-def _on_device(call):
-    """The call with its first argument's device current: the library takes the current device and the stream it is given."""
-    @functools.wraps(call)
-    def there(first, *args, **kw):
-        if first.index == _device():
-            return call(first, *args, **kw)
-        with torch.cuda.device(first.index):
-            return call(first, *args, **kw)
-    return there
-
-
 class Pages:
     """A paged cache: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (the last three dimensions
     contiguous, the strides of k and v alike), in the dtype of the activations (fp32, bf16) or, with bf16 ones, fp16."""
@@ -464,13 +452,13 @@ class Batch:
             raise ValueError("q_start [n_seq + 1]")
         if q_start is None and max_new != 1:
             raise ValueError("without q_start every sequence has one new token")
-        self.table, self.lens, self.q_start, self.device, self.n_seq = table, lens, q_start, table.device, n
+        self.table, self.lens, self.q_start, self.index, self.n_seq = table, lens, q_start, table.get_device(), n
         self.max_len, self.max_new = max_len, max_new
         self._calls, self._bytes = {}, {}       # the C struct, and the workspace, of a shape of call
 
     def bind(self, n_tokens: int, pages: Pages):
         """The call's C struct (one per number of tokens and page size: never changed once made)."""
-        if pages.device != self.device:
+        if pages.index != self.index:
             raise ValueError("pages and batch are on different devices")
         got = self._calls.get((n_tokens, pages.page_size))
         if got is None:
@@ -490,7 +478,7 @@ class Rope:
     def __init__(self, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0):
         if not inv_freq.is_cuda or inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq: float64 [rot_dim / 2] on the device")
-        self.inv_freq, self.device = inv_freq, inv_freq.device
+        self.inv_freq, self.index = inv_freq, inv_freq.get_device()
         self.c = river_rope(inv_freq.data_ptr(), 2 * inv_freq.numel(), ROPE_LAYOUTS[layout], mscale)
         self.ref = C.byref(self.c)
 
@@ -507,7 +495,7 @@ def river_rope_frequencies(rot_dim: int, base: float, scaling: str = "plain", fa
 def _rows(name: str, t: torch.Tensor, pages: Pages, heads: int | None = None) -> int:
     """[n_tokens, heads, head_dim] with contiguous heads: the stride between tokens."""
     shape = t.shape
-    if t.dtype != pages.dtype or t.device != pages.device or len(shape) != 3 or shape[2] != pages.head_dim:
+    if t.dtype is not pages.dtype or t.get_device() != pages.index or len(shape) != 3 or shape[2] != pages.head_dim:
         raise ValueError(f"{name}: {pages.dtype} [n_tokens, heads, {pages.head_dim}] on {pages.device}")
     n, h, hd = shape
     between, head, one = t.stride()
@@ -526,14 +514,16 @@ def _out(q: torch.Tensor, out: torch.Tensor | None, pages: Pages):
     return out, _rows("out", out, pages)
 
 
-@_on_device
 def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope: Rope,
                      out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotates q and k [n_tokens, heads, head_dim] at the new tokens' positions and stores k and v in the pages.  Returns the
     rotated queries: `out`, which may be q, or a new tensor (rows of tokens that belong to no sequence are not written)."""
+    if pages.index != _device():        # the library takes the current device and the stream that it is given
+        with torch.cuda.device(pages.index):
+            return river_rope_store(pages, layer, batch, q, k, v, rope, out)
     n = q.shape[0]
     qs, ks, vs = _rows("q", q, pages), _rows("k", k, pages, pages.n_kv_heads), _rows("v", v, pages, pages.n_kv_heads)
-    if k.shape[0] != n or v.shape[0] != n or rope.device != pages.device:
+    if k.shape[0] != n or v.shape[0] != n or rope.index != pages.index:
         raise ValueError("q, k and v must have the same tokens, and the frequencies their device")
     out, os_ = _out(q, out, pages)
     _check_call(load().river_rope_store(pages.ref, layer, batch.bind(n, pages), rope.ref, q.shape[1], q.data_ptr(), qs, k.data_ptr(), ks,
@@ -541,11 +531,13 @@ def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k:
     return out
 
 
-@_on_device
 def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, window: int = 0, sinks: int = 0,
                           scale: float = 0.0, out: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of the new tokens' queries [n_tokens, heads, head_dim] over their sequences' pages.  Rows of `out` (or of the new
     tensor that is returned) whose tokens belong to no sequence are not written."""
+    if pages.index != _device():
+        with torch.cuda.device(pages.index):
+            return river_paged_attention(pages, layer, batch, q, window, sinks, scale, out)
     qs = _rows("q", q, pages)
     out, os_ = _out(q, out, pages)
     L, (n, heads, _) = load(), q.shape
@@ -591,12 +583,14 @@ def _page_list(x) -> np.ndarray:
     return a.astype(np.int32, copy=False)
 
 
-@_on_device
 def river_copy_pages(pages: Pages, src, dst):
     """Copies pages src[i] -> dst[i] (host lists) in every layer, as if one after the other."""
     s, d = _page_list(src), _page_list(dst)
     if s.size != d.size:
         raise ValueError("as many destinations as sources")
+    if pages.index != _device():
+        with torch.cuda.device(pages.index):
+            return river_copy_pages(pages, s, d)
     _check_call(load().river_copy_pages(pages.ref, s.ctypes.data, d.ctypes.data, s.size, _stream(pages.index)))
 
 
@@ -641,11 +635,13 @@ class PagePool:
     def compact(self) -> int:
         return _check_call(load().river_pool_compact(self._h))
 
-    @_on_device
     def flush(self, pages: Pages | None = None):
         """Queued copies and changed entries, on the device's current stream."""
         if pages is not None and pages.device != self.state.device:
             raise ValueError("pages and pool are on different devices")
+        if self.index != _device():
+            with torch.cuda.device(self.index):
+                return self.flush(pages)
         _check_call(load().river_pool_flush(self._h, None if pages is None else pages.ref, self.state.data_ptr(), _stream(self.index)))
 
     def length(self, seq: int) -> int:

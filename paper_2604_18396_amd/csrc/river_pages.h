@@ -460,6 +460,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
   // dimension apart, on one XCD where that is a multiple of 8
   const int per = c.n_kv_heads * a.n_splits;
   const int tile = blockIdx.y, s = blockIdx.x / per, x = blockIdx.x % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
+  // Without a window the first steps' keys do not depend on the length: their entries come with it, not behind it
+  int early[2][KB];
+#pragma unroll
+  for (int it = 0; it < 2; ++it)
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      early[it][kb] = b.table[(long long)s * b.table_stride +
+                              min(c.by_page.quot(z * a.split_len + (it * kAttnWaves + wave) * M::kKeys + kb * 16 + col), b.max_pages - 1)];
   int first_token, count;
   seq_tokens(b, s, first_token, count);
   const int rows = count * a.rep, r0 = tile * 16;
@@ -469,7 +478,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
   const int parts = splits_of(a, sp.n);
   if (z >= parts) return;
   const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
 
   // this lane's row: its query in the order of the contraction, its position
   const int r = min(r0 + col, r1), tok = a.by_rep.quot(r), qh = head * a.rep + (r - tok * a.rep);
@@ -664,8 +672,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
     int e[KB], e1[KB];
     typename W::Data d, d1;
     uint32_t there, there1;
-    entries(0, e);
-    entries(1, e1);
+    if (a.window) {
+      entries(0, e);
+      entries(1, e1);
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) { e[kb] = early[0][kb]; e1[kb] = early[1][kb]; }
+    }
     fetch(0, e, d, there);
     for (int it = 0; it + 1 < steps; ++it) {
       entries(it + 2, e);

@@ -71,6 +71,7 @@ long long page_elems(const river_pages *p) { return (long long)p->n_kv_heads * p
 
 // (a launch holds fewer than 2^32 threads in a dimension; a larger one would be cut off without an error)
 constexpr int kMostTokens = 1 << 22;
+constexpr int kMostPositions = 1 << 30;                          // of a sequence: indices of keys are 32-bit numbers
 
 Cache layer_cache(const river_pages *p, int layer) {
   const size_t at = (size_t)layer * p->layer_stride * elem_bytes(p);
@@ -89,7 +90,7 @@ const char *bad_batch(const river_batch *b) {
 }
 Batch device_batch(const river_batch *b, int page_size) {
   return Batch{b->table, b->lens, b->q_start, b->n_seq, b->n_tokens, b->max_pages, b->table_stride,
-               (int)std::min<long long>((long long)b->max_pages * page_size, INT_MAX)};
+               (int)std::min<long long>((long long)b->max_pages * page_size, kMostPositions)};
 }
 
 // The kernels of a configuration: f(T{}, C{}, HD) with the activations' type, the pages' and the head size.
@@ -235,12 +236,15 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   y.many = p->dtype == RIVER_BF16 && rows >= kManyRows;
   y.tile_rows = y.many ? 256 : 16;
   y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
-  long long keys = std::min<long long>(b->max_len, (long long)b->max_pages * p->page_size);
+  long long keys = std::min<long long>({b->max_len, (long long)b->max_pages * p->page_size, kMostPositions});
   if (window) keys = std::min<long long>(keys, (long long)window + sinks + (y.tile_rows - 1) / rep);
-  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many, four of
-  // k_attn_split (two at a time), of at least 128 keys (there a step for each of four wavefronts), at most 64 splits
-  const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles), goal = y.many ? 256 : 1024, least = y.many ? 256 : 128;
-  const long long want = std::max(1ll, std::min({goal / groups, (keys + least - 1) / least, 64ll}));
+  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many of at least 256 keys.
+  // k_attn_split (two at a time on a CU): four a CU of at least 128 keys (a step for each of the four wavefronts), eight where
+  // that leaves them 512: more of them are more even where lengths differ (8B shape, 16 sequences of 2048 .. 8192 keys, us by workgroups
+  // a CU 4 / 8 / 16: 82 / 74 / 75; 16 of 300 .. 1200 with 2 / 4 / 8: 20.7 / 18.1 / 21.8).  At most 64 splits: their join
+  const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
+  auto splits = [&](long long goal, long long least) { return std::min({goal / groups, (keys + least - 1) / least, 64ll}); };
+  const long long want = std::max(1ll, y.many ? splits(256, 256) : std::max(splits(1024, 128), splits(2048, 512)));
   y.split_len = (int)std::max(128ll, std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30));
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
   y.fused = !y.many && groups <= RIVER_TICKETS && y.n_splits <= kFewSplits;
