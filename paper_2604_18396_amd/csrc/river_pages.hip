@@ -224,7 +224,12 @@ struct AttnPlan {
   int tiles, tile_rows, n_splits, split_len;
   size_t o_bytes, bytes;                                         // of the partial results
 };
-constexpr int kManyRows = 128;
+// k_attn_many from 64 rows of a sequence and key head and 6e8 rows x keys x elements of all of them on: it reads keys once for 256 rows,
+// k_attn_split for 16, but takes 10 us to begin and end (us, k_attn_many / k_attn_split; 8B shape, new tokens behind cached ones:
+// 256 behind none 20.7 / 19.1, 32 behind 4096 30.8 / 33.4, 64 behind 4096 35.4 / 56.0, 16 behind 65536 107 / 201; eight sequences, 16 behind
+// 2048 38.3 / 37.7; 1B shape: 256 behind none 15.7 / 11.4, 64 behind 4096 26.4 / 29.5, 32 behind 2048 of eight 29.9 / 36.2)
+constexpr int kManyRows = 64;
+constexpr double kManyWork = 6e8;
 // Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a
 // second launch 6.4 + 3.8; 16 sequences of up to 1201 15.8, 14.3 + 3.9; 64 splits of 131072 105, 96 + 6)
 constexpr int kFewSplits = 16;
@@ -233,11 +238,11 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   AttnPlan y{};
   const int rep = nq / p->n_kv_heads;
   const long long rows = (long long)(b->q_start ? std::min(b->max_new, b->n_tokens) : 1) * rep;
-  y.many = p->dtype == RIVER_BF16 && rows >= kManyRows;
+  long long keys = std::min<long long>({b->max_len, (long long)b->max_pages * p->page_size, kMostPositions});
+  if (window) keys = std::min<long long>(keys, (long long)window + sinks + 15 / rep);
+  y.many = p->dtype == RIVER_BF16 && rows >= kManyRows && (double)b->n_seq * rows * keys * p->n_kv_heads * p->head_dim >= kManyWork;
   y.tile_rows = y.many ? 256 : 16;
   y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
-  long long keys = std::min<long long>({b->max_len, (long long)b->max_pages * p->page_size, kMostPositions});
-  if (window) keys = std::min<long long>(keys, (long long)window + sinks + (y.tile_rows - 1) / rep);
   // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many of at least 256 keys.
   // k_attn_split (two at a time on a CU): four a CU of at least 128 keys (a step for each of the four wavefronts), eight where
   // that leaves them 512: more of them are more even where lengths differ (8B shape, 16 sequences of 2048 .. 8192 keys, us by workgroups

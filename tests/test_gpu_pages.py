@@ -28,7 +28,9 @@ def half_step(t):
 class Setup:
     """A cache of random contents, tables in random order, and the batch: lens[s] positions, new[s] of them new."""
 
-    def __init__(self, kind, nkv, hd, ps, lens, new, seed=0, spare=2, layers=1, pad=0, extra_cols=1, ragged=True, pages_first=False):
+    def __init__(self, kind, nkv, hd, ps, lens, new, seed=0, spare=2, layers=1, pad=0, extra_cols=1, ragged=True, pages_first=False, room=0):
+        # room: pages that the table has place for beyond what is used, and the bound on lengths allows: the kernel and the
+        # splits of the keys go by that bound
         self.act, self.kvt = TYPES[kind]
         self.nkv, self.hd, self.ps, self.lens, self.new = nkv, hd, ps, lens, new
         g = torch.Generator(device=DEV)
@@ -36,7 +38,7 @@ class Setup:
         self.g = g
         rng = np.random.default_rng(seed)
         need = [-(-max(n, 0) // ps) for n in lens]
-        most = max(max(need), 1) + extra_cols
+        most = max(max(need), 1) + extra_cols + room
         n_pages = sum(need) + spare
         self.host = np.full((len(lens), most), -1, dtype=np.int32)
         order, at = rng.permutation(n_pages), 0
@@ -56,7 +58,8 @@ class Setup:
         self.q_start = torch.from_numpy(self.start).to(DEV)
         self.dlens = torch.tensor(lens, dtype=torch.int32, device=DEV)
         self.pages = B.Pages(self.k, self.v, self.act)
-        self.batch = B.Batch(self.table, self.dlens, self.q_start if ragged else None, max_new=max(max(new), 1), max_len=max(max(lens), 1))
+        self.batch = B.Batch(self.table, self.dlens, self.q_start if ragged else None, max_new=max(max(new), 1),
+                             max_len=None if room else max(max(lens), 1))
 
     def randn(self, *shape, dtype=None, std=1.0):
         return torch.randn(*shape, generator=self.g, device=DEV).mul_(std).to(dtype or self.act)
@@ -239,6 +242,7 @@ def test_attention_single_tokens(kind, hd, nkv, rep, window, sinks):
 def test_attention_page_sizes(kind, ps):
     run_attention(Setup(kind, 2, 64, ps, [517, 64, 130], [1, 1, 1], seed=ps), 8, 77, 5)
     run_attention(Setup(kind, 2, 128, ps, [517, 64, 130], [40, 64, 1], seed=ps), 4)
+    run_attention(Setup(kind, 2, 128, ps, [517, 64, 130], [140, 64, 1], seed=ps, room=320000 // ps), 4)
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -246,8 +250,18 @@ def test_attention_page_sizes(kind, ps):
 @pytest.mark.parametrize("lens,new", [([5, 9, 2], [2, 3, 2]), ([40, 70], [16, 9]), ([300, 77, 1], [300, 77, 1]), ([700, 513, 64, 0], [129, 1, 64, 0]),
                                       ([1500], [257])], ids=str)
 @pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (64, 0), (90, 4), (200, 130)])
-def test_attention_prompts(kind, hd, nkv, rep, lens, new, window, sinks):
-    run_attention(Setup(kind, nkv, hd, 16, lens, new, seed=window, pad=2), nkv * rep, window, sinks)
+@pytest.mark.parametrize("room", [0, 300, 20000])
+def test_attention_prompts(kind, hd, nkv, rep, lens, new, window, sinks, room):
+    run_attention(Setup(kind, nkv, hd, 16, lens, new, seed=window, pad=2, room=room), nkv * rep, window, sinks)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "bf16-f16"])
+@pytest.mark.parametrize("hd,nkv,rep,lens,new", [(128, 8, 4, [1100, 513, 64, 0], [1100, 129, 64, 0]), (64, 8, 8, [2050, 1], [515, 1]),
+                                                 (128, 4, 1, [3000], [1025]), (128, 2, 7, [9000, 300], [70, 33]), (64, 1, 16, [20000], [40])],
+                         ids=str)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (500, 4)])
+def test_attention_large_prompts(kind, hd, nkv, rep, lens, new, window, sinks):
+    run_attention(Setup(kind, nkv, hd, 16, lens, new, seed=31, pad=1), nkv * rep, window, sinks)
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -256,15 +270,16 @@ def test_attention_long_cache(kind):
     run_attention(Setup(kind, 2, 128, 64, [9000, 31, 4097], [1, 1, 1], seed=2, ragged=False), 8, 8000, 70)
     run_attention(Setup(kind, 1, 128, 32, [6000, 2], [5, 2], seed=3), 4)
     run_attention(Setup(kind, 1, 64, 32, [5000], [130], seed=4), 2)
+    run_attention(Setup(kind, 2, 128, 32, [5000, 70], [257, 70], seed=4, room=10), 8)
 
 
 @pytest.mark.parametrize("kind", TYPES)
 def test_attention_lengths_beyond_their_bounds(kind):
     # max_len only divides the work; what is longer is still right
-    for lens, new in (([900, 40], [1, 1]), ([900, 300], [150, 90])):
+    for lens, new, bound in (([900, 40], [1, 1], 50), ([900, 300], [150, 90], 50), ([6000, 300], [600, 90], 2000)):
         st = Setup(kind, 2, 64, 16, lens, new, seed=5)
-        st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=max(new), max_len=50)
-        run_attention(st, 8)
+        st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=max(new), max_len=bound)
+        run_attention(st, 16)
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -272,13 +287,14 @@ def test_attention_lengths_beyond_their_bounds(kind):
 def test_attention_scales(kind, std, scale):
     run_attention(Setup(kind, 2, 64, 16, [300, 5], [1, 1], seed=6), 8, scale=scale, std=std)
     run_attention(Setup(kind, 1, 128, 16, [300, 200], [200, 150], seed=6), 4, scale=scale, std=std)
+    run_attention(Setup(kind, 1, 128, 16, [300, 200], [200, 150], seed=6, room=20000), 4, scale=scale, std=std)
 
 
 def test_attention_of_queries_that_half_precision_does_not_hold():
     # bf16 queries beyond fp16's largest and below its smallest number over a cache in fp16
     for mult in (2.0 ** 20, 2.0 ** -40):
-        for lens, new in (([200, 9], [1, 1]), ([200, 90], [150, 80])):
-            st = Setup("bf16-f16", 1, 64, 16, lens, new, seed=7)
+        for lens, new, room in (([200, 9], [1, 1], 0), ([200, 90], [150, 80], 0), ([200, 90], [150, 80], 20000)):
+            st = Setup("bf16-f16", 1, 64, 16, lens, new, seed=7, room=room)
             st.k.mul_(2.0 ** -10)       # fp16's normal numbers, still
             q = (st.randn(st.tokens, 4, 64) * mult)
             got = B.river_paged_attention(st.pages, 0, st.batch, q, scale=2.0 ** 10 / mult / 8)
@@ -305,11 +321,12 @@ def test_attention_of_many_small_probabilities_in_half_precision():
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("lens,new", [([1000, 63, 64, 65, 1], [1, 1, 1, 1, 1]), ([333, 200], [4, 3]), ([400, 257, 64], [300, 257, 3])], ids=str)
 @pytest.mark.parametrize("window,sinks", [(0, 0), (1, 1), (60, 0), (128, 9), (100000, 4)])
-def test_attention_sees_exactly_what_it_should(kind, hd, lens, new, window, sinks):
+@pytest.mark.parametrize("room", [0, 20000])
+def test_attention_sees_exactly_what_it_should(kind, hd, lens, new, window, sinks, room):
     # scores of zero: every visible position counts the same.  Position j has a one in element j mod hd: the row holds
     # how many of each residue are seen, divided by their number (exact before the division, which is rounded: fp32's
     # reciprocal and product, then the output's type)
-    st = Setup(kind, 2, hd, 20, lens, new, seed=11)
+    st = Setup(kind, 2, hd, 20, lens, new, seed=11, room=room)
     for s, n in enumerate(lens):
         for c0 in range(0, n, 20):
             page = int(st.host[s, c0 // 20])
@@ -331,8 +348,9 @@ def test_attention_sees_exactly_what_it_should(kind, hd, lens, new, window, sink
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("lens,new", [([130, 17, 0, 64], [1, 1, 1, 1]), ([300, 41], [5, 3]), ([300, 130], [290, 130])], ids=str)
 @pytest.mark.parametrize("window,sinks", [(0, 0), (37, 2)])
-def test_attention_does_not_look_at_what_it_does_not_see(kind, bad, lens, new, window, sinks):
-    st = Setup(kind, 2, 128, 16, lens, new, seed=12)
+@pytest.mark.parametrize("room", [0, 20000])
+def test_attention_does_not_look_at_what_it_does_not_see(kind, bad, lens, new, window, sinks, room):
+    st = Setup(kind, 2, 128, 16, lens, new, seed=12, room=room)
     q = st.randn(st.tokens, 8, 128)
     first = B.river_paged_attention(st.pages, 0, st.batch, q, window, sinks)
     # slots behind the sequences' ends, pages of nobody, and positions that every new token's window has left behind
@@ -355,10 +373,11 @@ def test_attention_does_not_look_at_what_it_does_not_see(kind, bad, lens, new, w
 @pytest.mark.parametrize("where", ["k", "v"])
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("lens,new", [([200], [6]), ([400], [390])], ids=str)
-def test_attention_a_later_token_is_no_part_of_an_earlier_row(kind, bad, where, hd, lens, new):
+@pytest.mark.parametrize("room", [0, 20000])
+def test_attention_a_later_token_is_no_part_of_an_earlier_row(kind, bad, where, hd, lens, new, room):
     # a value that is not finite in the middle of the new tokens: rows before it, and rows whose window has left it, are as
     # they were; those that see a bad value are bad in its element, those that see a bad key are NaN or without it
-    st = Setup(kind, 1, hd, 16, lens, new, seed=13)
+    st = Setup(kind, 1, hd, 16, lens, new, seed=13, room=room)
     n, m, window = lens[0], new[0], 100
     at = n - m // 2
     q = st.randn(m, 4, hd)
@@ -380,8 +399,8 @@ def test_attention_a_later_token_is_no_part_of_an_earlier_row(kind, bad, where, 
 
 @pytest.mark.parametrize("kind", TYPES)
 def test_attention_pages_that_are_not_there(kind):
-    for lens, new in (([300, 100], [1, 1]), ([300, 100], [200, 60])):
-        st = Setup(kind, 2, 64, 16, lens, new, seed=14)
+    for lens, new, room in (([300, 100], [1, 1], 0), ([300, 100], [200, 60], 0), ([300, 100], [200, 60], 20000)):
+        st = Setup(kind, 2, 64, 16, lens, new, seed=14, room=room)
         st.host[0, 0], st.host[0, 3], st.host[0, 18], st.host[1, :] = -1, 10 ** 6, -2 ** 31, -5
         st.table.copy_(torch.from_numpy(st.host))
         q, out = run_attention(st, 8, 120, 20)
@@ -394,8 +413,8 @@ def test_attention_pages_that_are_not_there(kind):
 @pytest.mark.parametrize("kind", TYPES)
 def test_attention_more_new_tokens_than_positions(kind):
     # a padded prompt whose length says that it is shorter: tokens without a position get zeros
-    for n, m in ((3, 5), (40, 100), (-4, 2)):
-        st = Setup(kind, 1, 64, 16, [n, 20], [m, 2], seed=15)
+    for n, m, room in ((3, 5, 0), (40, 100, 0), (40, 100, 20000), (-4, 2, 0)):
+        st = Setup(kind, 1, 64, 16, [n, 20], [m, 2], seed=15, room=room)
         q = st.randn(st.tokens, 4, 64)
         got = B.river_paged_attention(st.pages, 0, st.batch, q)
         lost = min(m, m - n)
@@ -409,8 +428,8 @@ def test_attention_more_new_tokens_than_positions(kind):
 
 @pytest.mark.parametrize("kind", TYPES)
 def test_attention_strides_and_layers(kind):
-    for lens, new in (([100, 45], [1, 1]), ([100, 45], [80, 45])):
-        st = Setup(kind, 2, 64, 16, lens, new, seed=16, layers=3, pages_first=True)
+    for lens, new, room in (([100, 45], [1, 1], 0), ([100, 45], [80, 45], 0), ([100, 45], [80, 45], 20000)):
+        st = Setup(kind, 2, 64, 16, lens, new, seed=16, layers=3, pages_first=True, room=room)
         wide = st.randn(st.tokens, 8 * 64 * 3)
         q = wide[:, 64 * 8:64 * 16].unflatten(1, (8, 64))
         room = torch.full((st.tokens, 12, 64), 7.0, dtype=st.act, device=DEV)
@@ -437,18 +456,20 @@ def test_attention_pages_beyond_32_bits():
         st = Setup("bf16", 1, 64, 16, [75], [m], seed=17)
         st.k, st.v = k, v
         st.host = np.array([[5, 3, 4, 0, 1, -1]], dtype=np.int32)
-        st.table = torch.from_numpy(st.host).to(DEV)
         st.pages = B.Pages(k, v)
-        st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=m, max_len=75)
-        run_attention(st, 4)
+        for room in (0, 400000):        # (both kernels)
+            st.table = torch.full((1, 6 + room), -1, dtype=torch.int32, device=DEV)
+            st.table[0, :6] = torch.from_numpy(st.host[0])
+            st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=m)
+            run_attention(st, 4)
     B.river_copy_pages(st.pages, [5], [2])
     assert torch.equal(k[0, 2], k[0, 5]) and torch.equal(v[0, 2], v[0, 5])
 
 
 def test_the_same_call_gives_the_same_bits():
     for kind in TYPES:
-        for lens, new in (([3000, 70], [1, 1]), ([700, 300], [300, 300])):
-            st = Setup(kind, 2, 128, 16, lens, new, seed=18)
+        for lens, new, room in (([3000, 70], [1, 1], 0), ([700, 300], [300, 300], 0), ([700, 300], [300, 300], 20000), ([4000], [90], 300)):
+            st = Setup(kind, 2, 128, 16, lens, new, seed=18, room=room)
             q = st.randn(st.tokens, 8, 128)
             first = B.river_paged_attention(st.pages, 0, st.batch, q)
             for _ in range(5):
