@@ -350,7 +350,8 @@ int river_rope_store(const river_pages *pages, int32_t layer, const river_batch 
  * Query heads h * (n_q_heads / n_kv_heads) .. share key head h.
  * scale: > 0, or 0 = 1/sqrt(head_dim).  window: 0 = none.  sinks: used with a window only.
  * q, out: DEVICE [n_tokens][n_q_heads][head_dim], pages->dtype, strides in elements, multiples of 16 bytes, 16-byte aligned;
- * out must not overlap q.  At most 2^22 tokens and sequences a call (river_rope_store too).
+ * out must not overlap q.  At most 2^22 tokens and sequences a call (river_rope_store too), and fewer than
+ * 2^28 tokens x heads.
  * workspace: DEVICE, 16-byte aligned, of at least the bytes that river_paged_attention_workspace gives for the
  * same arguments (0 bytes: may be NULL); its contents mean nothing before and after the call.
  * tickets: DEVICE int32 [RIVER_TICKETS], 4-byte aligned, or NULL.  All zero before the first call that has them and left zero by every call;

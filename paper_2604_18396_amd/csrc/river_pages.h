@@ -251,8 +251,9 @@ struct AttnArgs {
   float scale2;                           // scale * log2 e
   int window, sinks;                      // (no window: sinks is 0)
   int n_splits, split_len, tiles, tile_rows;   // of the keys; tiles of rows per sequence and key head
-  float *part_o;                          // [n_tokens][nq][n_splits][HD], where a tile has several splits
-  float2 *part_ml;                        // [n_tokens][nq][n_splits] maximum (base 2) and sum
+  int max_new;                            // new tokens of a sequence beyond these are left out
+  float *part_o;                          // [n_seq][max_new][nq][n_splits][HD], where a tile has several splits
+  float2 *part_ml;                        // [n_seq][max_new][nq][n_splits] maximum (base 2) and sum
   unsigned int *tickets;                  // [sequences x key heads x tiles] workgroups that are done; zero between calls (null: a
                                           // launch of its own joins the splits)
 };
@@ -456,10 +457,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
   constexpr int AREA = W::LDS > 64 * HD ? W::LDS : 64 * HD;     // of a wavefront: its values, then its result
   __shared__ __align__(16) char lds[kAttnWaves * AREA];
   __shared__ float2 res_ml[kAttnWaves][16];
-  // workgroup -> (sequence, key head, split, tile); the tiles of the same keys are a multiple of the grid's other
-  // dimension apart, on one XCD where that is a multiple of 8
-  const int per = c.n_kv_heads * a.n_splits;
-  const int tile = blockIdx.y, s = blockIdx.x / per, x = blockIdx.x % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
+  // workgroup -> (tile, sequence, split, key head); the tiles of the same keys lie sequences x splits x key heads apart, on one XCD where
+  // that is a multiple of 8
+  const unsigned per = c.n_kv_heads * a.n_splits, id = blockIdx.x % (per * b.n_seq);
+  const int tile = blockIdx.x / (per * b.n_seq), s = id / per, x = id % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
   // Without a window the first steps' keys do not depend on the length: their entries come with it, not behind it
   int early[2][KB];
@@ -471,7 +472,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
                               min(c.by_page.quot(z * a.split_len + (it * kAttnWaves + wave) * M::kKeys + kb * 16 + col), b.max_pages - 1)];
   int first_token, count;
   seq_tokens(b, s, first_token, count);
-  const int rows = count * a.rep, r0 = tile * 16;
+  const int rows = min(count, a.max_new) * a.rep, r0 = tile * 16;
   if (r0 >= rows) return;
   const int r1 = min(r0 + 15, rows - 1);
   const Span sp = span_of(b, a, b.lens[s], count, r0, r1);
@@ -737,7 +738,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b
     return;
   }
   // Parts cross XCDs, whose L2s are not coherent: they are written through and read past the L2, eight bytes at a time
-  const long long first_part = (t * a.nq + oh) * a.n_splits;
+  const long long first_part = (((long long)s * a.max_new + to) * a.nq + oh) * a.n_splits;
   if (have) {
 #pragma unroll
     for (int e = 0; e < E; e += 2) put_through(a.part_o + (first_part + z) * HD + e0 + e, v[e], v[e + 1]);
@@ -815,13 +816,13 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   typedef unsigned long long Place __attribute__((ext_vector_type(2)));
   Place *const places = (Place *)(lds + W::PLACES);
   uint32_t *const there_of = (uint32_t *)(lds + W::THERE);
-  // workgroup -> (sequence, key head, split), tile: the last tile, which sees most keys, first; a key head's tiles on one XCD
-  // where their distance in the grid is a multiple of 8
-  const int per = c.n_kv_heads * a.n_splits;
-  const int tile = a.tiles - 1 - blockIdx.y, s = blockIdx.x / per, x = blockIdx.x % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
+  // workgroup -> (tile, sequence, split, key head), the last tile, which sees most keys, first; a key head's tiles on one XCD where
+  // their distance is a multiple of 8
+  const unsigned per = c.n_kv_heads * a.n_splits, id = blockIdx.x % (per * b.n_seq);
+  const int tile = a.tiles - 1 - (int)(blockIdx.x / (per * b.n_seq)), s = id / per, x = id % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
   int first_token, count;
   seq_tokens(b, s, first_token, count);
-  const int rows = count * a.rep, r0 = tile * W::ROWS;
+  const int rows = min(count, a.max_new) * a.rep, r0 = tile * W::ROWS;
   if (r0 >= rows) return;
   const int r1 = min(r0 + W::ROWS - 1, rows - 1), len = b.lens[s];
   const Span sp = span_of(b, a, len, count, r0, r1);
@@ -1165,14 +1166,13 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     const int from = r0 + wave * W::WROWS + rb * 32;             // the block's first row
     if (from > r1) break;
     // row `row` of the block in memory
-    auto place = [&](int row, long long &t, int &qh) {
-      const int r = min(from + row, r1), tok = a.by_rep.quot(r);
-      t = first_token + tok;
+    auto place = [&](int row, int &tok, int &qh) {
+      const int r = min(from + row, r1);
+      tok = a.by_rep.quot(r);
       qh = head * a.rep + r - tok * a.rep;
       return from + row <= r1;
     };
-    long long t;
-    int qh;
+    int tok, qh;
     if (parts == 1) {
       const float f = l[rb] == 0.f ? 0.f : 1.f / l[rb];
 #pragma unroll
@@ -1192,7 +1192,8 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       }
 #pragma unroll
       for (int j = 0; j < 32 / W::PER; ++j)
-        if (place(j * W::PER + lane / W::PIECES, t, qh)) *(u32x4 *)((T *)a.out + t * a.out_stride + (long long)qh * HD + my_slot * 8) = v[j];
+        if (place(j * W::PER + lane / W::PIECES, tok, qh))
+          *(u32x4 *)((T *)a.out + (long long)(first_token + tok) * a.out_stride + (long long)qh * HD + my_slot * 8) = v[j];
     } else {
       constexpr int P = 2 * W::PIECES;                           // fp32: twice as many pieces
 #pragma unroll
@@ -1207,25 +1208,27 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       for (int j = 0; j < 32 * P / 64; ++j) {
         const int row = j * (64 / P) + lane / P, piece = lane % P;
         const f32x4 v = *(const f32x4 *)(mine + row * (2 * W::ROW) + (piece ^ (row % P)) * 16);
-        if (place(row, t, qh)) *(f32x4 *)(a.part_o + ((t * a.nq + qh) * a.n_splits + z) * HD + piece * 4) = v;
+        if (place(row, tok, qh)) *(f32x4 *)(a.part_o + ((((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z) * HD + piece * 4) = v;
       }
       // (maxima in base 2, as k_attn_split has them)
-      if (h == 0 && place(col, t, qh))
-        a.part_ml[(t * a.nq + qh) * a.n_splits + z] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kLazyBias, l[rb]);
+      if (h == 0 && place(col, tok, qh))
+        a.part_ml[(((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kLazyBias, l[rb]);
     }
     __builtin_amdgcn_wave_barrier();
   }
 }
 
-// Where the splits of row (t, h) are: their number (0: no row, 1: it is done already)
-__device__ __forceinline__ int parts_of(const Batch &b, const AttnArgs &a, int t, int h) {
-  const int s = seq_of(b, t);
-  if (s < 0) return 0;
+// Row w of the partial results: head h of new token i of sequence s.  Its number of splits (0: no row, 1: it is done already), and its
+// place in the output.
+__device__ __forceinline__ int parts_of(const Batch &b, const AttnArgs &a, long long w, int head_dim, long long &out) {
+  const int h = (int)(w % a.nq), i = (int)(w / a.nq % a.max_new), s = (int)(w / a.nq / a.max_new);
+  if (s >= b.n_seq) return 0;
   int first, count;
   seq_tokens(b, s, first, count);
-  const int r = (t - first) * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
-  if (t < first || t - first >= count || r0 >= a.tiles * a.tile_rows) return 0;
-  return splits_of(a, span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, count * a.rep) - 1).n);
+  if (i >= count) return 0;
+  const int r = i * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
+  out = (long long)(first + i) * a.out_stride + (long long)h * head_dim;
+  return splits_of(a, span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, min(count, a.max_new) * a.rep) - 1).n);
 }
 
 // Few splits joined in a launch of their own: bit for bit what the last workgroup of k_attn_split does.
@@ -1233,13 +1236,13 @@ template <class T, int HD>
 __global__ __launch_bounds__(256) void k_attn_join_few(Batch b, AttnArgs a) {
   constexpr int E = HD * 16 / kAttnThreads > 4 ? HD * 16 / kAttnThreads : 4, LANES = HD / E;
   const long long w = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (w >= (long long)b.n_tokens * a.nq) return;
-  const int t = (int)(w / a.nq), h = (int)(w % a.nq), e0 = threadIdx.x % LANES * E;
-  const int parts = parts_of(b, a, t, h);
+  const int e0 = threadIdx.x % LANES * E;
+  long long out;
+  const int parts = parts_of(b, a, w, HD, out);
   if (parts <= 1) return;
   float v[E], sum;
   join_parts<HD, E>(a, w * a.n_splits, parts, e0, v, sum);
-  store_row<T, E>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, v, sum);
+  store_row<T, E>((T *)a.out + out + e0, v, sum);
 }
 
 // Many splits joined, a workgroup a row: HD / 4 lanes have a row's elements, the others take other splits; the wavefronts' sums are added
@@ -1248,8 +1251,9 @@ template <class T, int HD>
 __global__ __launch_bounds__(256) void k_attn_join_many(Batch b, AttnArgs a) {
   constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
   const long long w = blockIdx.x;
-  const int t = (int)(w / a.nq), h = (int)(w % a.nq), lane = threadIdx.x % 64, wave = threadIdx.x / 64, e0 = lane % LANES * 4;
-  const int parts = parts_of(b, a, t, h);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, e0 = lane % LANES * 4;
+  long long out;
+  const int parts = parts_of(b, a, w, HD, out);
   if (parts <= 1) return;
   const float2 *ml = a.part_ml + w * a.n_splits;
   const float *po = a.part_o + w * a.n_splits * HD + e0;
@@ -1279,7 +1283,7 @@ __global__ __launch_bounds__(256) void k_attn_join_many(Batch b, AttnArgs a) {
 #pragma unroll
   for (int i = 1; i < 4; ++i) { v += part[i][lane]; sum += part_sum[i]; }
   const float x[4] = {v[0], v[1], v[2], v[3]};
-  store_row<T, 4>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, x, sum);
+  store_row<T, 4>((T *)a.out + out + e0, x, sum);
 }
 
 // ------------------------------------------------------------------ copies

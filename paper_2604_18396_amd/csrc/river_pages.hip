@@ -83,6 +83,7 @@ const char *bad_batch(const river_batch *b) {
   if (b->n_seq < 0 || b->n_tokens < 0 || b->max_pages < 1 || b->table_stride < b->max_pages || b->max_new < 0 || b->max_len < 0)
     return "bad batch: n_seq, n_tokens, max_new, max_len >= 0, 1 <= max_pages <= table_stride";
   if (b->n_tokens > kMostTokens || b->n_seq > kMostTokens) return "more than 2^22 tokens or sequences in a call";
+  if (b->n_seq == 0 || b->n_tokens == 0) return nullptr;         // (nothing to do: null pointers will do)
   if (!b->table || !b->lens) return "null table or lengths";
   if (((uintptr_t)b->table | (uintptr_t)b->lens | (uintptr_t)b->q_start) % 4) return "misaligned table, lengths or q_start";
   if (!b->q_start && b->n_tokens != b->n_seq) return "without q_start every sequence has one token: n_tokens must be n_seq";
@@ -178,7 +179,6 @@ extern "C" int river_rope_store(const river_pages *pages, int32_t layer, const r
     if (rope->rot_dim < 2 || rope->rot_dim % 2 || rope->rot_dim > pages->head_dim) return refuse("rot_dim must be even, in [2, head_dim]");
     if (rope->layout != RIVER_ROPE_HALF && rope->layout != RIVER_ROPE_INTERLEAVED) return refuse("bad rotary layout");
     if (n_q_heads < 1 || n_q_heads > 65536) return refuse("n_q_heads out of range");
-    if (!q || !k || !v || !q_out) return refuse("null queries, keys or values");
     const long long qw = (long long)n_q_heads * pages->head_dim, kw = (long long)pages->n_kv_heads * pages->head_dim;
     if (kw > (1 << 24)) return refuse("too many key heads");
     if (q_stride < qw || q_out_stride < qw || k_stride < kw || v_stride < kw) return refuse("a stride is smaller than its row");
@@ -186,6 +186,7 @@ extern "C" int river_rope_store(const river_pages *pages, int32_t layer, const r
     const int es = elem_bytes(pages);
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out) % es) return refuse("misaligned queries, keys or values");
     if (batch->n_tokens == 0 || batch->n_seq == 0) return RIVER_OK;
+    if (!q || !k || !v || !q_out) return refuse("null queries, keys or values");
     const Cache c = layer_cache(pages, layer);
     const Batch b = device_batch(batch, pages->page_size);
     const RopeArgs a{rope->inv_freq, rope->rot_dim, rope->layout, rope->mscale, n_q_heads, q, k, v, q_out, q_stride, k_stride, v_stride, q_out_stride};
@@ -221,7 +222,7 @@ static const char *bad_attention(const river_pages *pages, const river_batch *ba
 struct AttnPlan {
   bool many;                                                     // k_attn_many, else k_attn_split
   bool fused;                                                    // its last workgroups join the splits, where they have tickets
-  int tiles, tile_rows, n_splits, split_len;
+  int max_new, tiles, tile_rows, n_splits, split_len;
   size_t o_bytes, bytes;                                         // of the partial results
 };
 // k_attn_many from 64 rows of a sequence and key head and 6e8 rows x keys x elements of all of them on: it reads keys once for 256 rows,
@@ -237,7 +238,8 @@ constexpr int kFewSplits = 16;
 static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
   AttnPlan y{};
   const int rep = nq / p->n_kv_heads;
-  const long long rows = (long long)(b->q_start ? std::min(b->max_new, b->n_tokens) : 1) * rep;
+  y.max_new = b->q_start ? std::min(b->max_new, b->n_tokens) : 1;
+  const long long rows = (long long)y.max_new * rep;
   long long keys = std::min<long long>({b->max_len, (long long)b->max_pages * p->page_size, kMostPositions});
   if (window) keys = std::min<long long>(keys, (long long)window + sinks + 15 / rep);
   y.many = p->dtype == RIVER_BF16 && rows >= kManyRows && (double)b->n_seq * rows * keys * p->n_kv_heads * p->head_dim >= kManyWork;
@@ -254,7 +256,7 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
   y.fused = !y.many && groups <= RIVER_TICKETS && y.n_splits <= kFewSplits;
   if (y.n_splits > 1) {
-    const size_t parts = (size_t)b->n_tokens * nq * y.n_splits;
+    const size_t parts = (size_t)b->n_seq * y.max_new * nq * y.n_splits;
     y.o_bytes = parts * p->head_dim * 4;
     y.bytes = y.o_bytes + parts * 8;
   }
@@ -280,36 +282,41 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
     if (const char *m = bad_attention(pages, batch, n_q_heads, window, sinks, &why)) return refuse(m);
     if (layer < 0 || layer >= pages->n_layers) return refuse("layer out of range");
     if (!(scale >= 0.f) || !std::isfinite(scale)) return refuse("scale must be positive (0: 1 / sqrt(head_dim))");
-    if (!q || !out) return refuse("null queries or output");
     const int es = elem_bytes(pages);
     const long long qw = (long long)n_q_heads * pages->head_dim;
     if (q_stride < qw || out_stride < qw) return refuse("a stride is smaller than its row");
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || q_stride * es % 16 || out_stride * es % 16)
       return refuse("queries, output and their strides must be multiples of 16 bytes");
+    if (batch->n_tokens == 0 || batch->n_seq == 0) return RIVER_OK;
+    if (!q || !out) return refuse("null queries or output");
+    if (q == out) return refuse("the output must not overlap the queries");
+    if (scale == 0.f) scale = 1.f / std::sqrt((float)pages->head_dim);
+    const float scale2 = scale * 1.44269504088896340736f;        // (powers of two are what the hardware has)
+    if (!std::isfinite(scale2)) return refuse("scale is too large");
     const AttnPlan y = plan_attention(pages, batch, n_q_heads, window, sinks);
     if (y.bytes && (!workspace || (uintptr_t)workspace % 16)) return refuse("null or misaligned (16 B) workspace");
     if (workspace_bytes < y.bytes) return refuse("workspace too small", RIVER_ENOSPC);
-    if (batch->n_tokens == 0 || batch->n_seq == 0 || y.tiles == 0) return RIVER_OK;
+    if (tickets && (uintptr_t)tickets % 4) return refuse("misaligned tickets");
+    if (y.tiles == 0) return RIVER_OK;
     const Cache c = layer_cache(pages, layer);
     const Batch b = device_batch(batch, pages->page_size);
-    if (scale == 0.f) scale = 1.f / std::sqrt((float)pages->head_dim);
     const int rep = n_q_heads / pages->n_kv_heads;
-    AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale * 1.44269504088896340736f, window, window ? sinks : 0,
-               y.n_splits, y.split_len, y.tiles, y.tile_rows, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), y.fused && tickets ? (unsigned int *)tickets : nullptr};
-    const long long groups = (long long)b.n_seq * c.n_kv_heads * y.n_splits;
+    AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale2, window, window ? sinks : 0,
+               y.n_splits, y.split_len, y.tiles, y.tile_rows, y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), y.fused && tickets ? (unsigned int *)tickets : nullptr};
+    const long long groups = (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
     if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * n_q_heads >= (1ll << 28)) return refuse("too many sequences, tokens and heads");
     const hipStream_t st = (hipStream_t)hip_stream;
     hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
       if constexpr (sizeof(t) == 2)
         if (y.many)
-          return launch_lds<k_attn_many<decltype(t), decltype(ct), decltype(hd)::v>>(dim3((unsigned)groups, y.tiles), dim3(256),
+          return launch_lds<k_attn_many<decltype(t), decltype(ct), decltype(hd)::v>>(dim3((unsigned)groups), dim3(256),
                                                                                     Many<decltype(ct), decltype(hd)::v>::LDS, st, c, b, a);
-      return launch(k_attn_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups, y.tiles), dim3(kAttnThreads), 0, st, c, b, a);
+      return launch(k_attn_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups), dim3(kAttnThreads), 0, st, c, b, a);
     });
     if (e == hipSuccess && y.n_splits > 1 && !a.tickets)
       e = by_types(pages, [&](auto t, auto, auto hd) {
         constexpr int HD = decltype(hd)::v;
-        const unsigned rows = (unsigned)(b.n_tokens * n_q_heads), each = 16;            // (of 16 lanes)
+        const unsigned rows = (unsigned)b.n_seq * y.max_new * n_q_heads, each = 16;            // (of 16 lanes)
         return y.n_splits <= kFewSplits ? launch(k_attn_join_few<decltype(t), HD>, dim3((rows + each - 1) / each), dim3(256), 0, st, b, a)
                                         : launch(k_attn_join_many<decltype(t), HD>, dim3(rows), dim3(256), 0, st, b, a);
       });

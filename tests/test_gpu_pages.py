@@ -427,6 +427,42 @@ def test_attention_more_new_tokens_than_positions(kind):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("lens,new,bound", [([3000, 2500], [5, 3], 3), ([900, 800], [90, 33], 40), ([3000, 700], [300, 300], 131)], ids=str)
+def test_attention_new_tokens_beyond_their_bound_are_left_out(kind, lens, new, bound):
+    st = Setup(kind, 2, 64, 16, lens, new, seed=32)
+    st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=bound, max_len=max(lens))
+    q = st.randn(st.tokens, 8, 64)
+    out = torch.full_like(q, 7.0)
+    B.river_paged_attention(st.pages, 0, st.batch, q, out=out)
+    want, tol = attention(st, q)
+    for s, m in enumerate(new):
+        lo, hi, end = int(st.start[s]), int(st.start[s]) + min(m, bound), int(st.start[s + 1])
+        check(out[lo:hi], want[lo:hi], tol[lo:hi], s)
+        assert bool((out[hi:end] == 7.0).all())
+
+
+def test_attention_of_a_much_padded_batch():
+    # the workspace goes by what the sequences may have, not by the call's tokens
+    st = Setup("bf16", 1, 64, 64, [20000, 30], [1, 1], seed=33, pad=200000)
+    run_attention(st, 4)
+    run_store(st, 4, 64, "half")
+
+
+def test_calls_without_sequences_or_tokens():
+    st = Setup("bf16", 1, 64, 16, [20], [1], seed=34)
+    f, _ = freqs(64)
+    none = B.Batch(st.table[:0], st.dlens[:0], st.q_start[:1], max_new=1)
+    empty = torch.empty(0, 4, 64, dtype=torch.bfloat16, device=DEV)
+    for batch, q in ((none, empty), (st.batch, empty), (none, st.randn(3, 4, 64))):
+        before = st.k.clone()
+        out = torch.full_like(q, 7.0)
+        B.river_paged_attention(st.pages, 0, batch, q, out=out)
+        B.river_rope_store(st.pages, 0, batch, q, q[:, :1], q[:, 1:2], B.Rope(f), out=out)
+        assert bool((out == 7.0).all()) and torch.equal(st.k, before)
+    B.river_copy_pages(st.pages, [], [])
+
+
+@pytest.mark.parametrize("kind", TYPES)
 def test_attention_strides_and_layers(kind):
     for lens, new, room in (([100, 45], [1, 1], 0), ([100, 45], [80, 45], 0), ([100, 45], [80, 45], 20000)):
         st = Setup(kind, 2, 64, 16, lens, new, seed=16, layers=3, pages_first=True, room=room)

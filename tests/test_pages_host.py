@@ -48,7 +48,7 @@ def store(pg=None, b=None, r=None, layer=0, nq=4, q=P, qs=256, k=P, ks=128, v=P,
                                      qo, qos, None)
 
 
-def attend(pg=None, b=None, layer=0, nq=4, q=P, qs=256, scale=0.0, window=0, sinks=0, out=P, os=256, ws=None, n=0):
+def attend(pg=None, b=None, layer=0, nq=4, q=P, qs=256, scale=0.0, window=0, sinks=0, out=2 * P, os=256, ws=None, n=0):
     return B.load().river_paged_attention(C.byref(pg or pages()), layer, C.byref(b or batch()), nq, q, qs, scale, window, sinks, out, os,
                                           ws, n, None, None)
 
@@ -80,7 +80,8 @@ def test_store_refuses_rotary_positions(bad):
 
 @pytest.mark.parametrize("bad", [dict(layer=2), dict(nq=0), dict(nq=3), dict(q=0), dict(out=0), dict(q=P + 8), dict(out=P + 2), dict(qs=255),
                                  dict(qs=260), dict(os=128), dict(os=257), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf),
-                                 dict(window=-1), dict(sinks=-1)], ids=str)
+                                 dict(window=-1), dict(sinks=-1), dict(scale=3e38), dict(out=P, q=P),
+                                 dict(nq=2**16 + 2)], ids=str)
 def test_attention_refuses(bad):
     assert attend(**bad) == B.RIVER_EINVAL and text()
 
@@ -88,6 +89,8 @@ def test_attention_refuses(bad):
 def test_calls_without_tokens_end_at_once():
     assert store(b=batch(n_tokens=0)) == attend(b=batch(n_tokens=0)) == 0
     assert store(b=batch(n_seq=0)) == attend(b=batch(n_seq=0)) == 0
+    none = batch(n_seq=0, n_tokens=0, table=0, lens=0, q_start=0)         # (empty tensors have no address)
+    assert store(b=none, q=0, k=0, v=0, qo=0) == attend(b=none, q=0, out=0) == 0
     assert B.load().river_copy_pages(C.byref(pages()), None, None, 0, None) == 0
 
 
