@@ -450,7 +450,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, long long first_pa
 }
 
 template <class T, class C, int HD>
-__global__ __launch_bounds__(kAttnThreads, 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
   typedef Tile<C, HD> W;
   typedef Mat<C> M;
   constexpr int KB = W::KB, NP = W::NP, ND = W::ND, PER = W::PER;
