@@ -246,12 +246,14 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   y.tile_rows = y.many ? 256 : 16;
   y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
   // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many of at least 256 keys.
-  // k_attn_split (two at a time on a CU): four a CU of at least 128 keys (a step for each of the four wavefronts), eight where
-  // that leaves them 512: more of them are more even where lengths differ (8B shape, 16 sequences of 2048 .. 8192 keys, us by workgroups
-  // a CU 4 / 8 / 16: 82 / 74 / 75; 16 of 300 .. 1200 with 2 / 4 / 8: 20.7 / 18.1 / 21.8).  At most 64 splits: their join
+  // k_attn_split (two at a time on a CU at head size 128, three at 64): three a CU of at least 128 keys (a step for each of the
+  // four wavefronts), eight where that leaves them 512: more of them are more even where lengths differ.  us by workgroups a CU, 8B
+  // shape: 64 sequences of 128 .. 512 keys 2 / 3 / 4: 21.4 / 21.1 / 27.0, 16 of 300 .. 1200 18.1 / 16.2 / 20.3, 16 of 2048 .. 8192
+  // 4 / 8 / 16: 82 / 74 / 75; 1B shape, 32 windows of 1028 16.9 / 16.7 / 21.8; fp32, 8 of 1024 .. 4096 42.7 / 39.0 / 44.0.  At most 64
+  // splits: their join
   const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
   auto splits = [&](long long goal, long long least) { return std::min({goal / groups, (keys + least - 1) / least, 64ll}); };
-  const long long want = std::max(1ll, y.many ? splits(256, 256) : std::max(splits(1024, 128), splits(2048, 512)));
+  const long long want = std::max(1ll, y.many ? splits(256, 256) : std::max(splits(768, 128), splits(2048, 512)));
   y.split_len = (int)std::max(128ll, std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30));
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
   y.fused = !y.many && groups <= RIVER_TICKETS && y.n_splits <= kFewSplits;
