@@ -1117,6 +1117,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       for (int rb = 0; rb < RB; ++rb) p0[0][rb] = p0[1][rb] = u32x4{0, 0, 0, 0};
     }
     settle(0, s0, there_of[0]);
+    wait_and_meet<(W::AHEAD - 2) * 2 * NL>();                    // (step 0 fetches over the keys of S(0))
     // step `steps` only adds what the last one left
     for (int n = 0; n <= steps; n += 2) {
       step(n, s0, p0, s1, p1);
