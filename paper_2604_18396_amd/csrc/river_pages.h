@@ -773,8 +773,8 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 template <class C, int HD>
 struct Many {
   typedef Mat<C> M;
-  static constexpr int KEYS = 32, RB = 2, WROWS = 32 * RB, ROWS = 4 * WROWS;
-  static constexpr int AHEAD = 4, KRING = 4, VRING = 8, CHUNK = 32;      // in steps; CHUNK: rows looked up at once
+  static constexpr int KEYS = 32, RB = HD == 128 ? 2 : 1, WROWS = 32 * RB, ROWS = 4 * WROWS;
+  static constexpr int AHEAD = HD == 128 ? 4 : 2, KRING = AHEAD, VRING = 2 * AHEAD, CHUNK = HD == 128 ? 32 : 16;      // in steps; CHUNK: rows looked up at once
   static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
   static constexpr int KS = HD / 16, DB = HD / 32;
   static constexpr int STAGE = KEYS * ROW;
@@ -807,7 +807,7 @@ __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 template <class T, class C, int HD>
-__global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs a) {
+__global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, Batch b, AttnArgs a) {
   typedef Many<C, HD> W;
   typedef Mat<C> M;
   constexpr int RB = W::RB, KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
@@ -904,8 +904,9 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
   };
   auto fetch = [&](int n, const Place (&at)[NL]) {
 #pragma unroll
+    for (int j = 0; j < NL; ++j) load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].x + k_piece[j]);
+#pragma unroll
     for (int j = 0; j < NL; ++j) {
-      load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].x + k_piece[j]);
       load_lds16(lds0 + W::V + n % W::VRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].y + v_piece[j]);
     }
   };
@@ -944,7 +945,9 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
           __builtin_amdgcn_sched_barrier(0);             // (one after the other: few registers)
         }
     }
-    pend = __any(top[0] > lim[0] || top[1] > lim[1]);
+    bool over = false;
+    for (int rb = 0; rb < RB; ++rb) over |= top[rb] > lim[rb];
+    pend = __any(over);
     if (pend) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -1003,7 +1006,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     } else {
       queries();
     }
-    wait_and_meet<(W::AHEAD - 2) * 2 * NL>();
+    wait_and_meet<(W::AHEAD - 2) * 2 * NL + NL>();
     // The operands of a step, one after the other: keys of S(n + 1), then values of step n - 1.  The swizzle's part that
     // depends on the operand is an exclusive or with a constant, the rest is the lane's.
     const uint32_t k0 = lds_base + W::k_at(col, h);
@@ -1028,7 +1031,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
     // the slots: left alone it fetches each operand right in front of its products and waits for it, and takes the
     // exponentials past the branches that follow.
     auto step = [&](int n, Scores &s, Probs &p, Scores &s1, Probs &p1) {
-      constexpr int G = KS + 2 * DB, SLOTS = G * RB, PRE = 3, EACH = 32 / SLOTS;     // EACH: halves of a pair of exponentials
+      constexpr int G = KS + 2 * DB, SLOTS = G * RB, PRE = 3, EACH = 16 * RB / SLOTS;     // EACH: halves of a pair of exponentials
       constexpr int FROM = KS * RB + 2, PER_SLOT = (16 * RB + SLOTS - FROM - 1) / (SLOTS - FROM);
       const uint32_t k_step = k0 + (n + 1) % W::KRING * W::STAGE, v_step = v0 + (n + W::VRING - 1) % W::VRING * W::STAGE;
       f32x16 sn[RB];
@@ -1065,7 +1068,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
 #pragma unroll
         for (int e = slot * EACH; e < (slot + 1) * EACH; ++e) {
           const int q = e / 2;
-          if (e % 2 == 0 && q + 1 < 16) arguments(q + 1);
+          if (e % 2 == 0 && q + 1 < 8 * RB) arguments(q + 1);
           y[q % 2][e % 2] = __builtin_amdgcn_exp2f(x[q % 2][e % 2]);
           asm volatile("" : "+v"(y[q % 2][e % 2]));
           if (e % 2 == 0 && q > 0) round_and_add(q - 1);
@@ -1081,18 +1084,18 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
             s1[e / 16][e % 16] = v;
             top[e / 16] = e % 16 ? __builtin_elementwise_maximum(top[e / 16], v) : v;
           }
-          asm volatile("" : "+v"(top[0]), "+v"(top[1]));
+          for (int rb_ = 0; rb_ < RB; ++rb_) asm volatile("" : "+v"(top[rb_]));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      round_and_add(15);
+      round_and_add(8 * RB - 1);
       settle(n + 1, s1, there);
       if ((n + W::AHEAD + 1) % W::CHUNK == 0) look_up((n + W::AHEAD + 1) / W::CHUNK);
       if (careful) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         clean(n + W::AHEAD);
       }
-      wait_and_meet<(W::AHEAD - 2) * 2 * NL>();
+      wait_and_meet<(W::AHEAD - 2) * 2 * NL + NL>();
     };
     Scores s0, s1;
     Probs p0, p1;
@@ -1117,7 +1120,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
       for (int rb = 0; rb < RB; ++rb) p0[0][rb] = p0[1][rb] = u32x4{0, 0, 0, 0};
     }
     settle(0, s0, there_of[0]);
-    wait_and_meet<(W::AHEAD - 2) * 2 * NL>();                    // (step 0 fetches over the keys of S(0))
+    wait_and_meet<(W::AHEAD - 2) * 2 * NL + NL>();               // (step 0 fetches over the keys of S(0))
     // step `steps` only adds what the last one left
     for (int n = 0; n <= steps; n += 2) {
       step(n, s0, p0, s1, p1);
@@ -1160,7 +1163,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_many(Cache c, Batch b, AttnArgs
 
   // Results.  A lane has four neighbouring elements of its row at a time: the rows of a block of 32 go through this wavefront's
   // part of LDS, pieces of 16 bytes in an order by row, so that memory gets whole rows (written as they are: 10000 cycles instead of 1500).
-  char *const mine = lds + wave * (W::STAGE * 2 * (parts == 1 ? 1 : 2));
+  char *const mine = lds + wave * (W::STAGE * (parts == 1 ? 1 : 2));
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     l[rb] += __shfl_xor(l[rb], 32);

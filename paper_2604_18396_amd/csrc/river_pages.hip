@@ -243,7 +243,7 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   long long keys = std::min<long long>({b->max_len, (long long)b->max_pages * p->page_size, kMostPositions});
   if (window) keys = std::min<long long>(keys, (long long)window + sinks + 15 / rep);
   y.many = p->dtype == RIVER_BF16 && rows >= kManyRows && (double)b->n_seq * rows * keys * p->n_kv_heads * p->head_dim >= kManyWork;
-  y.tile_rows = y.many ? 256 : 16;
+  y.tile_rows = y.many ? (p->head_dim == 128 ? 256 : 128) : 16;
   y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
   // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many of at least 256 keys.
   // k_attn_split (two at a time on a CU at head size 128, three at 64): three a CU of at least 128 keys (a step for each of the
@@ -253,7 +253,7 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   // splits: their join
   const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
   auto splits = [&](long long goal, long long least) { return std::min({goal / groups, (keys + least - 1) / least, 64ll}); };
-  const long long want = std::max(1ll, y.many ? splits(256, 256) : std::max(splits(768, 128), splits(2048, 512)));
+  const long long want = std::max(1ll, y.many ? splits(p->head_dim == 128 ? 256 : 512, 256) : std::max(splits(768, 128), splits(2048, 512)));
   y.split_len = (int)std::max(128ll, std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30));
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
   y.fused = !y.many && groups <= RIVER_TICKETS && y.n_splits <= kFewSplits;
