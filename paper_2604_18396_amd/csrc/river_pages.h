@@ -251,6 +251,7 @@ struct AttnArgs {
   float scale2;                           // scale * log2 e
   int window, sinks;                      // (no window: sinks is 0)
   int n_splits, split_len, tiles, tile_rows;   // of the keys; tiles of rows per sequence and key head
+  int turn_s, turn_z;                     // see work_of
   int max_new;                            // new tokens of a sequence beyond these are left out
   float *part_o;                          // [n_seq][max_new][nq][n_splits][HD], where a tile has several splits
   float2 *part_ml;                        // [n_seq][max_new][nq][n_splits] maximum (base 2) and sum
@@ -288,6 +289,21 @@ __device__ __forceinline__ Sight sight_of(const AttnArgs &a, const Span &s, int 
 }
 // Splits of a tile that have keys, at least one; the last split of a launch takes what is left.
 __device__ __forceinline__ int splits_of(const AttnArgs &a, int n) { return min(a.n_splits, max(1, (n + a.split_len - 1) / a.split_len)); }
+
+// Workgroup -> (tile, sequence, split, key head): the key heads next to each other (eight of them are the eight XCDs, so that the
+// tiles of the same keys meet in one L2), then the splits, the sequences, and the tiles, the last, which sees most keys, first.
+// Workgroups go to the XCDs in turn, within one to its four shader engines in turn, and one that has no place on its engine holds up all
+// behind it.  So the order of the sequences, and of the splits in one, turns by one each time they come back to the same engines
+// (2^turn rounds): else the longest of four sequences has one engine in four, and the empty tiles and splits of short ones leave the
+// others idle (8B shape, us, without / with: prompts of 2048, 2015, 551 and 513 tokens 181 / 122, of eight of 366 .. 1024 81 / 64, single
+// tokens of 32 sequences of 1024 .. 4096 82 / 77).
+__device__ __forceinline__ void work_of(const Cache &c, const Batch &b, const AttnArgs &a, int &tile, int &s, int &z, int &head) {
+  const unsigned u = blockIdx.x / c.n_kv_heads, v = u / a.n_splits, t = v / b.n_seq;
+  head = blockIdx.x % c.n_kv_heads;
+  z = (u + (v >> a.turn_z)) % a.n_splits;
+  s = (v + (t >> a.turn_s)) % b.n_seq;
+  tile = a.tiles - 1 - t;
+}
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -457,10 +473,8 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
   constexpr int AREA = W::LDS > 64 * HD ? W::LDS : 64 * HD;     // of a wavefront: its values, then its result
   __shared__ __align__(16) char lds[kAttnWaves * AREA];
   __shared__ float2 res_ml[kAttnWaves][16];
-  // workgroup -> (tile, sequence, split, key head); the tiles of the same keys lie sequences x splits x key heads apart, on one XCD where
-  // that is a multiple of 8
-  const unsigned per = c.n_kv_heads * a.n_splits, id = blockIdx.x % (per * b.n_seq);
-  const int tile = blockIdx.x / (per * b.n_seq), s = id / per, x = id % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
+  int tile, s, z, head;
+  work_of(c, b, a, tile, s, z, head);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
   // Without a window the first steps' keys do not depend on the length: their entries come with it, not behind it
   int early[2][KB];
@@ -761,15 +775,18 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)
 //
-// Bound: the matrix cores, and beside them as long, the vector instructions (exponentials above all).  A wavefront holds 64
-// rows, so that an operand fetched from LDS is used twice (with 32 rows the fetches alone take as long as the products), one
-// wavefront per SIMD with 512 registers, four of them 256 rows on the same keys.  What would wait for each other is taken from
-// different steps of 32 keys: step n multiplies S(n+1) = K Q^T, takes the exponentials of S(n), and adds P(n-1) V, three things
-// that do not depend on each other.
+// Bound: the vector instructions (exponentials above all), then the matrix cores.  An operand that is fetched from LDS is used by a
+// wavefront's 64 rows at head size 128: one wavefront per SIMD with 512 registers, four of them 256 rows on the same keys.  At
+// 64 a wavefront has 32 rows, and two workgroups are on a CU (us, 64 rows / 32 rows: head size 128, 4096 tokens behind none
+// 163 / 187, 256 behind 65536 322 / 412; head size 64 146 / 126, 231 / 200).
+// What would wait for each other is taken from different steps of 32 keys: step n multiplies S(n+1) = K Q^T, takes the exponentials
+// of S(n), and adds P(n-1) V, three things that do not depend on each other.
 // O is therefore rescaled one step after the maximum has moved (pend); it moves when a score is 2^kLazy times as likely as
 // what was the maximum (one of 64 rows has a new maximum in most steps, and rescaling takes as long as the step).
-// Keys and values go from memory straight into LDS (no registers, four steps in flight), in rings of four and eight steps, one barrier
-// a step; where a key's row lies is looked up for 32 steps at once.
+// Keys and values go from memory straight into LDS (no registers, AHEAD steps in flight), in rings, one barrier a step; where a key's
+// row lies is looked up for CHUNK steps at once.
+// 8B shape, 4096 tokens: 163 us, 840 TFLOP/s; 2048 behind 16384 640 us, 910; a workgroup's step takes 2500 cycles (its products
+// alone 1024), its beginning and end 20000: queries 4500 (32 rows a load), table and first keys 5500, results 7000.
 template <class C, int HD>
 struct Many {
   typedef Mat<C> M;
@@ -816,10 +833,8 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
   typedef unsigned long long Place __attribute__((ext_vector_type(2)));
   Place *const places = (Place *)(lds + W::PLACES);
   uint32_t *const there_of = (uint32_t *)(lds + W::THERE);
-  // workgroup -> (tile, sequence, split, key head), the last tile, which sees most keys, first; a key head's tiles on one XCD where
-  // their distance is a multiple of 8
-  const unsigned per = c.n_kv_heads * a.n_splits, id = blockIdx.x % (per * b.n_seq);
-  const int tile = a.tiles - 1 - (int)(blockIdx.x / (per * b.n_seq)), s = id / per, x = id % per, z = x / c.n_kv_heads, head = x % c.n_kv_heads;
+  int tile, s, z, head;
+  work_of(c, b, a, tile, s, z, head);
   int first_token, count;
   seq_tokens(b, s, first_token, count);
   const int rows = min(count, a.max_new) * a.rep, r0 = tile * W::ROWS;

@@ -225,12 +225,14 @@ struct AttnPlan {
   int max_new, tiles, tile_rows, n_splits, split_len;
   size_t o_bytes, bytes;                                         // of the partial results
 };
-// k_attn_many from 64 rows of a sequence and key head and 6e8 rows x keys x elements of all of them on: it reads keys once for 256 rows,
-// k_attn_split for 16, but takes 10 us to begin and end (us, k_attn_many / k_attn_split; 8B shape, new tokens behind cached ones:
-// 256 behind none 20.7 / 19.1, 32 behind 4096 30.8 / 33.4, 64 behind 4096 35.4 / 56.0, 16 behind 65536 107 / 201; eight sequences, 16 behind
-// 2048 38.3 / 37.7; 1B shape: 256 behind none 15.7 / 11.4, 64 behind 4096 26.4 / 29.5, 32 behind 2048 of eight 29.9 / 36.2)
+// k_attn_many from 64 rows of a sequence and key head on, where all of them see enough: rows x keys (of a row in the middle) x elements,
+// 6e8 at head size 128 and 5e8 at 64.  It reads keys once for 256 or 128 rows, k_attn_split for 16, but takes 10 us to begin and end
+// (us, k_attn_many / k_attn_split; 8B shape: 512 behind none 32.0 / 25.3, 32 behind 4096 30.5 / 31.2, 64 behind 4096 35.3 / 45.8, 16 behind
+// 65536 103 / 156; sixteen sequences, 16 behind 512 30.8 / 21.2, 32 behind 512 33.1 / 34.6; 1B shape: 512 behind none 17.3 / 16.0, 64
+// behind 4096 22.0 / 24.8, sixteen sequences, 16 behind 512 15.8 / 13.5, 32 behind 512 17.9 / 19.9)
 constexpr int kManyRows = 64;
-constexpr double kManyWork = 6e8;
+static int many_rows(int head_dim) { return head_dim == 128 ? Many<__bf16, 128>::ROWS : Many<__bf16, 64>::ROWS; }
+static double many_work(int head_dim) { return head_dim == 128 ? 6e8 : 5e8; }
 // Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a
 // second launch 6.4 + 3.8; 16 sequences of up to 1201 15.8, 14.3 + 3.9; 64 splits of 131072 105, 96 + 6)
 constexpr int kFewSplits = 16;
@@ -242,10 +244,12 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   const long long rows = (long long)y.max_new * rep;
   long long keys = std::min<long long>({b->max_len, (long long)b->max_pages * p->page_size, kMostPositions});
   if (window) keys = std::min<long long>(keys, (long long)window + sinks + 15 / rep);
-  y.many = p->dtype == RIVER_BF16 && rows >= kManyRows && (double)b->n_seq * rows * keys * p->n_kv_heads * p->head_dim >= kManyWork;
-  y.tile_rows = y.many ? (p->head_dim == 128 ? 256 : 128) : 16;
+  const double seen = (double)std::min<long long>(keys, std::max(0, b->max_len - y.max_new / 2));
+  y.many = p->dtype == RIVER_BF16 && rows >= kManyRows && b->n_seq * seen * rows * p->n_kv_heads * p->head_dim >= many_work(p->head_dim);
+  y.tile_rows = y.many ? many_rows(p->head_dim) : 16;
   y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
-  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many of at least 256 keys.
+  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many (two at head size 64)
+  // of at least 256 keys.
   // k_attn_split (two at a time on a CU at head size 128, three at 64): three a CU of at least 128 keys (a step for each of the
   // four wavefronts), eight where that leaves them 512: more of them are more even where lengths differ.  us by workgroups a CU, 8B
   // shape: 64 sequences of 128 .. 512 keys 2 / 3 / 4: 21.4 / 21.1 / 27.0, 16 of 300 .. 1200 18.1 / 16.2 / 20.3, 16 of 2048 .. 8192
@@ -253,7 +257,7 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   // splits: their join
   const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
   auto splits = [&](long long goal, long long least) { return std::min({goal / groups, (keys + least - 1) / least, 64ll}); };
-  const long long want = std::max(1ll, y.many ? splits(p->head_dim == 128 ? 256 : 512, 256) : std::max(splits(768, 128), splits(2048, 512)));
+  const long long want = std::max(1ll, y.many ? splits(65536 / y.tile_rows, 256) : std::max(splits(768, 128), splits(2048, 512)));
   y.split_len = (int)std::max(128ll, std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30));
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
   y.fused = !y.many && groups <= RIVER_TICKETS && y.n_splits <= kFewSplits;
@@ -303,8 +307,11 @@ extern "C" int river_paged_attention(const river_pages *pages, int32_t layer, co
     const Cache c = layer_cache(pages, layer);
     const Batch b = device_batch(batch, pages->page_size);
     const int rep = n_q_heads / pages->n_kv_heads;
+    // Workgroups come back to the same shader engines after 32; a round of them is sequences x key heads (see work_of)
+    auto turn = [](long long round) { int k = 0; while ((round << k) % 32) ++k; return k; };
+    const int turn_z = turn((long long)y.n_splits * c.n_kv_heads), turn_s = turn((long long)b.n_seq * y.n_splits * c.n_kv_heads);
     AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale2, window, window ? sinks : 0,
-               y.n_splits, y.split_len, y.tiles, y.tile_rows, y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), y.fused && tickets ? (unsigned int *)tickets : nullptr};
+               y.n_splits, y.split_len, y.tiles, y.tile_rows, turn_s, turn_z, y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), y.fused && tickets ? (unsigned int *)tickets : nullptr};
     const long long groups = (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
     if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * n_q_heads >= (1ll << 28)) return refuse("too many sequences, tokens and heads");
     const hipStream_t st = (hipStream_t)hip_stream;
