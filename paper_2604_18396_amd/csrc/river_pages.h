@@ -73,6 +73,7 @@ __device__ __forceinline__ int page_of(const Cache &c, const Batch &b, int s, in
 // (x, y) of a pair -> (x cos a - y sin a, x sin a + y cos a) times mscale, a = p f.  The angle is taken in 64 bits and reduced to
 // turns before it is rounded (p f of a far position has its fraction in bits that fp32 does not keep); sine and
 // cosine of the reduced angle, and the products, are fp32.  One workgroup per token: its angles are shared by all its heads.
+// This kernel, element by element, takes what k_rope_store_wide cannot (odd strides, addresses, widths).
 constexpr int kRopeThreads = 256;
 
 __device__ __forceinline__ float2 turn(int p, double f, float mscale) {
@@ -138,7 +139,9 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope_store(Cache c, Batch b, R
 
 // The same by 16-byte pieces, where rows, strides and the rotated part allow it.  Bound: memory (a token's row in, its queries and
 // cache rows out).  A unit is a piece, or the two pieces whose elements are pairs; a thread has kRopeUnits of them in flight (its loads
-// stand in front of its stores, which the compiler may not move them past: the queries may be rotated in place).
+// stand in front of its stores, which the compiler may not move them past: the queries may be rotated in place).  8B shape: 4096
+// tokens, 101 MB, 17 us (element by element 29), 5.9 TB/s; 32 tokens 4.5 us, one 2.7: start, the two or three loads that find its
+// row, the angles.
 constexpr int kRopeUnits = 2;
 template <class T, class C, int HD>
 __global__ __launch_bounds__(kRopeThreads) void k_rope_store_wide(Cache c, Batch b, RopeArgs a, Div by_units) {
@@ -396,6 +399,10 @@ __device__ __forceinline__ void store_row(T *to, const float (&v)[E], float sum)
 // lanes of a row asked and O rescaled.  P^T is then in the order that O^T += V^T P^T wants its right operand in; V^T comes out of
 // the wavefront's own LDS, whose transposing read gives a lane four keys of one element.
 // LDS pieces lie in an order by row (swizzle), so that neither side meets in one bank.
+// 8B shape: one sequence of 131071 positions, 537 MB, 93 us, 5.8 TB/s (a read alone reaches 6.8; two workgroups a CU, 185 registers:
+// steps of 16 keys and three workgroups are 1 % faster there and 18 % slower for 16 sequences of 1200); 32 sequences of up to 4096 76 us,
+// 4.6 TB/s, what is missing there is that sequences differ; one of 512 8.1 us, of which the keys are 1: start, length, entries, rows,
+// tickets, partial results one after the other.  fp32 prompts: 68 TFLOP/s of 135, the L2's rate for keys that every 16 rows read again.
 template <class C, int HD>
 struct Tile {
   typedef Mat<C> M;
@@ -791,7 +798,8 @@ template <class C, int HD>
 struct Many {
   typedef Mat<C> M;
   static constexpr int KEYS = 32, RB = HD == 128 ? 2 : 1, WROWS = 32 * RB, ROWS = 4 * WROWS;
-  static constexpr int AHEAD = HD == 128 ? 4 : 2, KRING = AHEAD, VRING = 2 * AHEAD, CHUNK = HD == 128 ? 32 : 16;      // in steps; CHUNK: rows looked up at once
+  static constexpr int AHEAD = HD == 128 ? 4 : 2, KRING = AHEAD, VRING = 2 * AHEAD;      // in steps
+  static constexpr int CHUNK = HD == 128 ? 32 : 16;      // steps whose rows are looked up at once
   static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
   static constexpr int KS = HD / 16, DB = HD / 32;
   static constexpr int STAGE = KEYS * ROW;
@@ -917,6 +925,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
 #pragma unroll
     for (int j = 0; j < NL; ++j) at[j] = places[n % (2 * W::CHUNK) * KEYS + my_row + j * W::PER];
   };
+  // (a step's keys, then its values: they are needed a step later, and a wait may leave the last of them in flight)
   auto fetch = [&](int n, const Place (&at)[NL]) {
 #pragma unroll
     for (int j = 0; j < NL; ++j) load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].x + k_piece[j]);
@@ -1046,7 +1055,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
     // the slots: left alone it fetches each operand right in front of its products and waits for it, and takes the
     // exponentials past the branches that follow.
     auto step = [&](int n, Scores &s, Probs &p, Scores &s1, Probs &p1) {
-      constexpr int G = KS + 2 * DB, SLOTS = G * RB, PRE = 3, EACH = 16 * RB / SLOTS;     // EACH: halves of a pair of exponentials
+      constexpr int G = KS + 2 * DB, SLOTS = G * RB, PRE = 3, EACH = 16 * RB / SLOTS;       // EACH: halves of a pair of exponentials
       constexpr int FROM = KS * RB + 2, PER_SLOT = (16 * RB + SLOTS - FROM - 1) / (SLOTS - FROM);
       const uint32_t k_step = k0 + (n + 1) % W::KRING * W::STAGE, v_step = v0 + (n + W::VRING - 1) % W::VRING * W::STAGE;
       f32x16 sn[RB];
@@ -1099,7 +1108,8 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
             s1[e / 16][e % 16] = v;
             top[e / 16] = e % 16 ? __builtin_elementwise_maximum(top[e / 16], v) : v;
           }
-          for (int rb_ = 0; rb_ < RB; ++rb_) asm volatile("" : "+v"(top[rb_]));
+#pragma unroll
+          for (int i = 0; i < RB; ++i) asm volatile("" : "+v"(top[i]));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -1177,7 +1187,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
   }
 
   // Results.  A lane has four neighbouring elements of its row at a time: the rows of a block of 32 go through this wavefront's
-  // part of LDS, pieces of 16 bytes in an order by row, so that memory gets whole rows (written as they are: 10000 cycles instead of 1500).
+  // part of LDS, pieces of 16 bytes in an order by row, so that memory gets whole rows.
   char *const mine = lds + wave * (W::STAGE * (parts == 1 ? 1 : 2));
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -1250,7 +1260,7 @@ __device__ __forceinline__ int parts_of(const Batch &b, const AttnArgs &a, long 
   return splits_of(a, span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, min(count, a.max_new) * a.rep) - 1).n);
 }
 
-// Few splits joined in a launch of their own: bit for bit what the last workgroup of k_attn_split does.
+// Few splits joined in a launch of their own: bit for bit what the last workgroup of k_attn_split does.  Bound: latency (4 us).
 template <class T, int HD>
 __global__ __launch_bounds__(256) void k_attn_join_few(Batch b, AttnArgs a) {
   constexpr int E = HD * 16 / kAttnThreads > 4 ? HD * 16 / kAttnThreads : 4, LANES = HD / E;
@@ -1265,7 +1275,7 @@ __global__ __launch_bounds__(256) void k_attn_join_few(Batch b, AttnArgs a) {
 }
 
 // Many splits joined, a workgroup a row: HD / 4 lanes have a row's elements, the others take other splits; the wavefronts' sums are added
-// in their order.
+// in their order.  Bound: latency (8B shape, 64 splits of one token 6 us: start, length, maxima, 32 partial results a lane group).
 template <class T, int HD>
 __global__ __launch_bounds__(256) void k_attn_join_many(Batch b, AttnArgs a) {
   constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
@@ -1310,7 +1320,8 @@ __global__ __launch_bounds__(256) void k_attn_join_many(Batch b, AttnArgs a) {
 constexpr int kPairs = 448;               // of a launch: they travel as kernel arguments (below 4 KiB)
 struct Pairs { int src[kPairs], dst[kPairs]; };
 
-// One workgroup per 16 KiB of a page; grid (pieces, pairs, layers x {k, v}).
+// One workgroup per 16 KiB of a page, four 16-byte pieces a thread in flight; grid (pieces, pairs, layers x {k, v}).  Bound: memory
+// (200 pages of 2 MiB over 32 layers, 839 MB read and written, 148 .. 157 us, 5.3 .. 5.7 TB/s; a large copy reaches 5.0).
 constexpr int kCopyPiece = 16384;
 __global__ __launch_bounds__(256) void k_copy_pages(char *k, char *v, long long page_bytes, long long layer_bytes, long long used, Pairs w) {
   char *base = (blockIdx.z & 1 ? v : k) + (blockIdx.z >> 1) * layer_bytes;

@@ -190,7 +190,7 @@ extern "C" int river_rope_store(const river_pages *pages, int32_t layer, const r
     const Cache c = layer_cache(pages, layer);
     const Batch b = device_batch(batch, pages->page_size);
     const RopeArgs a{rope->inv_freq, rope->rot_dim, rope->layout, rope->mscale, n_q_heads, q, k, v, q_out, q_stride, k_stride, v_stride, q_out_stride};
-    // by pieces of 16 bytes: 4096 tokens of the 8B shape PIECES us, element by element ELEMENTS
+    // by pieces of 16 bytes where everything allows it: 4096 tokens of the 8B shape 17 us, element by element 29
     const int per = 16 / es;
     const bool wide = (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out) & 15) == 0 &&
                       (q_stride | k_stride | v_stride | q_out_stride) % per == 0 &&
