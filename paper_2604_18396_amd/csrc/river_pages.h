@@ -782,34 +782,35 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)
 //
-// Bound: the vector instructions (exponentials above all), then the matrix cores.  An operand that is fetched from LDS is used by a
-// wavefront's 64 rows at head size 128: one wavefront per SIMD with 512 registers, four of them 256 rows on the same keys.  At
-// 64 a wavefront has 32 rows, and two workgroups are on a CU (us, 64 rows / 32 rows: head size 128, 4096 tokens behind none
-// 163 / 187, 256 behind 65536 322 / 412; head size 64 146 / 126, 231 / 200).
+// Bound: the matrix cores and the vector instructions (exponentials above all) about alike, 46 % and 47 % of a SIMD's cycles, and the
+// clock that the power limit leaves, 1.6 .. 2.1 GHz.  A wavefront holds 32 rows in fewer than 256 registers, all of them general ones,
+// so that two workgroups of 128 rows are on a CU and one's waits, beginning and end lie beside the other's products.  (64 rows a
+// wavefront, one to a SIMD, read LDS half as often, but nothing runs beside their waits: us, 64 rows / 32 rows, 8B shape: 4096 tokens
+// 163 / 153, 2048 behind 16384 640 / 630, five windows of 1024 223 / 178, prompts of 2048, 2015, 551 and 513 122 / 107; 1B shape 4096
+// tokens 146 / 111.)
 // What would wait for each other is taken from different steps of 32 keys: step n multiplies S(n+1) = K Q^T, takes the exponentials
 // of S(n), and adds P(n-1) V, three things that do not depend on each other.
 // O is therefore rescaled one step after the maximum has moved (pend); it moves when a score is 2^kLazy times as likely as
-// what was the maximum (one of 64 rows has a new maximum in most steps, and rescaling takes as long as the step).
+// what was the maximum (one of 32 rows has a new maximum in most steps, and rescaling takes half as long as the step).
 // Keys and values go from memory straight into LDS (no registers, AHEAD steps in flight), in rings, one barrier a step; where a key's
 // row lies is looked up for CHUNK steps at once.
-// 8B shape, 4096 tokens: 163 us, 840 TFLOP/s; 2048 behind 16384 640 us, 910; a workgroup's step takes 2500 cycles (its products
-// alone 1024), its beginning and end 20000: queries 4500 (32 rows a load), table and first keys 5500, results 7000.
+// 8B shape, 4096 tokens: 153 us, 900 TFLOP/s; 2048 behind 16384 630 us, 930; the largest matrix products of the library reach 1250.
 template <class C, int HD>
 struct Many {
   typedef Mat<C> M;
-  static constexpr int KEYS = 32, RB = HD == 128 ? 2 : 1, WROWS = 32 * RB, ROWS = 4 * WROWS;
-  static constexpr int AHEAD = HD == 128 ? 4 : 2, KRING = AHEAD, VRING = 2 * AHEAD;      // in steps
-  static constexpr int CHUNK = HD == 128 ? 32 : 16;      // steps whose rows are looked up at once
+  static constexpr int KEYS = 32, WROWS = 32, ROWS = 4 * WROWS;
+  static constexpr int AHEAD = 2, KRING = 2, VRING = 4;  // in steps
+  static constexpr int CHUNK = 16;                       // steps whose rows are looked up at once
   static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
   static constexpr int KS = HD / 16, DB = HD / 32;
   static constexpr int STAGE = KEYS * ROW;
   static constexpr int V = KRING * STAGE, PLACES = V + VRING * STAGE, THERE = PLACES + 2 * CHUNK * KEYS * 16, LDS = THERE + 2 * CHUNK * 4;
   static constexpr int PER = 64 / PIECES, NL = 8 / PER;  // a wavefront loads eight rows, PER of them at a time
-  // Pieces of a row lie in an order by row: eight neighbouring rows of keys, and the four rows of a transposing read of
-  // values, meet in different banks
+  // Pieces of a row lie in an order by row: neighbouring rows of keys, and the four rows (of 64 bytes each) that half a wavefront's
+  // transposing read of values takes, meet in different banks (conflicts: 1 % of LDS cycles; values in pairs of pieces 30 %)
   static __device__ __forceinline__ int k_swizzle(int row) { return HD == 128 ? row & 15 : row & 7; }
   static __device__ __forceinline__ int v_swizzle(int row) {
-    return HD == 128 ? ((row & 7) << 1) | ((row >> 3) & 1) : ((row & 3) << 1) | ((row >> 2) & 1);
+    return HD == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : ((row & 3) << 1) | ((row >> 2) & 1);
   }
   static __device__ __forceinline__ int k_at(int row, int piece) { return row * ROW + (piece ^ k_swizzle(row)) * 16; }
   static __device__ __forceinline__ int v_at(int row, int piece) { return row * ROW + (piece ^ v_swizzle(row)) * 16; }
@@ -832,10 +833,10 @@ __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 template <class T, class C, int HD>
-__global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, Batch b, AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void k_attn_many(Cache c, Batch b, AttnArgs a) {
   typedef Many<C, HD> W;
   typedef Mat<C> M;
-  constexpr int RB = W::RB, KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
+  constexpr int KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
   extern __shared__ __align__(1024) char lds[];
   char *const vlds = lds + W::V;
   typedef unsigned long long Place __attribute__((ext_vector_type(2)));
@@ -862,37 +863,29 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   // Their queries in the operand's order.  (Through LDS, in whole rows of memory, they take as long: 4500 cycles, on the way with
   // the table's entries.)
-  u32x4 qf[KS][RB];
-  float sc[RB];
-  Sight sight[RB];
+  u32x4 qf[KS];
+  float sc = a.scale2;
+  const int r = min(r0 + wave * W::WROWS + col, r1), tok = a.by_rep.quot(r);
+  const Sight sight = sight_of(a, sp, len - count + tok);
+  const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = min(r0 + wave * W::WROWS + rb * 32 + col, r1), tok = a.by_rep.quot(r);
-    sight[rb] = sight_of(a, sp, len - count + tok);
-    const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks][rb] = *(const u32x4 *)(q + (2 * ks + h) * 8);
-  }
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const u32x4 *)(q + (2 * ks + h) * 8);
   auto queries = [&] {
+    if constexpr (!M::kSplitP) {                         // fp16 pages: see k_attn_split
+      float big = 0.f;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      sc[rb] = a.scale2;
-      if constexpr (!M::kSplitP) {                       // fp16 pages: see k_attn_split
-        float big = 0.f;
+      for (int ks = 0; ks < KS; ++ks)
+        for (int e = 0; e < 4; ++e)
+          big = fmaxf(big, fmaxf(fabsf(Mat<__bf16>::low(qf[ks][e])), fabsf(Mat<__bf16>::high(qf[ks][e]))));
+      big = fmaxf(big, __shfl_xor(big, 32));
+      const int ex = big > 0.f && !not_finite(big) ? ilogbf(big) : 0;
+      sc = ldexpf(sc, ex);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          for (int e = 0; e < 4; ++e)
-            big = fmaxf(big, fmaxf(fabsf(Mat<__bf16>::low(qf[ks][rb][e])), fabsf(Mat<__bf16>::high(qf[ks][rb][e]))));
-        big = fmaxf(big, __shfl_xor(big, 32));
-        const int ex = big > 0.f && !not_finite(big) ? ilogbf(big) : 0;
-        sc[rb] = ldexpf(sc[rb], ex);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          for (int e = 0; e < 4; ++e)
-            qf[ks][rb][e] = M::pack(ldexpf(Mat<__bf16>::low(qf[ks][rb][e]), -ex), ldexpf(Mat<__bf16>::high(qf[ks][rb][e]), -ex));
-      }
-      sc[rb] = fmaxf(sc[rb], 1e-37f);                    // (-infinity times it stays one)
+      for (int ks = 0; ks < KS; ++ks)
+        for (int e = 0; e < 4; ++e)
+          qf[ks][e] = M::pack(ldexpf(Mat<__bf16>::low(qf[ks][e]), -ex), ldexpf(Mat<__bf16>::high(qf[ks][e]), -ex));
     }
+    sc = fmaxf(sc, 1e-37f);                              // (-infinity times it stays one)
   };
 
   const u32x4 *kp = (const u32x4 *)((const C *)c.k + (long long)head * c.page_size * HD), *vp = (const u32x4 *)((const C *)c.v + (long long)head * c.page_size * HD);
@@ -935,56 +928,46 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
     }
   };
 
-  typedef float Scores[RB][16];
-  typedef u32x4 Probs[2][RB];
-  f32x16 o[DB][RB];
-  float m[RB], lim[RB], l[RB], off[RB], fac[RB], top[RB];
+  typedef float Scores[16];
+  typedef u32x4 Probs[2];
+  f32x16 o[DB];
+  float m, lim, l, off, fac, top;
   bool pend;
   // Steps of which every row of this wavefront sees every key (where all pages are there): their last key is at most all_to,
   // and their first is at least all_from or their last below all_sinks, by index in the split
-  const int all_to = sp.at(first) - i0, all_from = (a.window ? max(0, sp.at(last - a.window + 1)) : 0) - i0, all_sinks = sight[0].sinks - i0;
+  const int all_to = sp.at(first) - i0, all_from = (a.window ? max(0, sp.at(last - a.window + 1)) : 0) - i0, all_sinks = sight.sinks - i0;
 
   // Step n's scores as they count: what a row does not see is -infinity.  The maximum, where that moves it.
   auto settle = [&](int n, Scores &sx, uint32_t there_) {
     const uint32_t there = __builtin_amdgcn_readfirstlane(there_);
     const int base = n * KEYS;
     if (there != 0xffffffffu || base + KEYS - 1 > all_to || (base < all_from && base + KEYS > all_sinks)) {
+      const uint32_t see = (sight.bits(i0 + base) & there) >> (4 * h);
+      top = -INFINITY;
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const uint32_t see = (sight[rb].bits(i0 + base) & there) >> (4 * h);
-        top[rb] = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sx[rb][i] = (see >> (8 * (i / 4) + i % 4) & 1) ? sx[rb][i] : -INFINITY;
-          top[rb] = __builtin_elementwise_maximum(top[rb], sx[rb][i]);
-        }
+      for (int i = 0; i < 16; ++i) {
+        sx[i] = (see >> (8 * (i / 4) + i % 4) & 1) ? sx[i] : -INFINITY;
+        top = __builtin_elementwise_maximum(top, sx[i]);
       }
     }
     if (pend) {
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          o[d][rb] *= fac[rb];
-          __builtin_amdgcn_sched_barrier(0);             // (one after the other: few registers)
-        }
-    }
-    bool over = false;
-    for (int rb = 0; rb < RB; ++rb) over |= top[rb] > lim[rb];
-    pend = __any(over);
-    if (pend) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        // (each row by its own scores alone, whatever the others did)
-        const float high = fmaxf(top[rb], __shfl_xor(top[rb], 32)), now = high > lim[rb] ? high : m[rb];
-        const float to = (now == -INFINITY ? 0.f : now * sc[rb]) - M::kLazyBias;
-        fac[rb] = m[rb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off[rb] - to);
-        if (now == m[rb]) fac[rb] = 1.f;
-        m[rb] = now;
-        lim[rb] = now + M::kLazy / sc[rb];
-        off[rb] = to;
-        l[rb] *= fac[rb];
+      for (int d = 0; d < DB; ++d) {
+        o[d] *= fac;
+        __builtin_amdgcn_sched_barrier(0);               // (one after the other: few registers)
       }
+    }
+    pend = __any(top > lim);
+    if (pend) {
+      // (each row by its own scores alone, whatever the others did)
+      const float high = fmaxf(top, __shfl_xor(top, 32)), now = high > lim ? high : m;
+      const float to = (now == -INFINITY ? 0.f : now * sc) - M::kLazyBias;
+      fac = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(off - to);
+      if (now == m) fac = 1.f;
+      m = now;
+      lim = now + M::kLazy / sc;
+      off = to;
+      l *= fac;
     }
   };
 
@@ -992,17 +975,12 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
   // values are left out of what is multiplied and added to the rows that see them; everything else has the same bits.
   bool careful = false;
   for (;;) {
+    m = lim = -INFINITY;
+    l = 0.f;
+    off = -M::kLazyBias;
+    fac = 1.f;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      m[rb] = lim[rb] = -INFINITY;
-      l[rb] = 0.f;
-      off[rb] = -M::kLazyBias;
-      fac[rb] = 1.f;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][rb][i] = 0.f;
-    }
+    for (int d = 0; d < DB; ++d) o[d] = f32x16{};
     pend = false;
     if (steps == 0) break;
     // (careful: this wavefront's own rows of step n, which have arrived)
@@ -1042,7 +1020,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
       u32x4 f;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint32_t at = (v_step ^ (uint32_t)(d * 64 + (HD == 128 ? u * 16 : 0))) + (16 * t + 8 * u) * W::ROW;
+        const uint32_t at = (v_step ^ (uint32_t)(d * 64 + (HD == 128 ? u * 32 : 0))) + (16 * t + 8 * u) * W::ROW;
         const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)at));
         f[2 * u] = w.x;
         f[2 * u + 1] = w.y;
@@ -1050,15 +1028,15 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
       return f;
     };
     // Step n with the scores s (of step n) and probabilities p (of step n - 1); leaves those of the next in s1 and p1.
-    // In slots of one product, the operand of the third product pair after it, and a share of the vector instructions, each
+    // In slots of one product, the operand of the third product after it, and a share of the vector instructions, each
     // from another stage of its chain (argument, exponential, rounding and sum), so that nothing waits.  The compiler must not mix
     // the slots: left alone it fetches each operand right in front of its products and waits for it, and takes the
     // exponentials past the branches that follow.
     auto step = [&](int n, Scores &s, Probs &p, Scores &s1, Probs &p1) {
-      constexpr int G = KS + 2 * DB, SLOTS = G * RB, PRE = 3, EACH = 16 * RB / SLOTS;       // EACH: halves of a pair of exponentials
-      constexpr int FROM = KS * RB + 2, PER_SLOT = (16 * RB + SLOTS - FROM - 1) / (SLOTS - FROM);
+      constexpr int SLOTS = KS + 2 * DB, PRE = 3, EACH = 16 / SLOTS;   // EACH: exponentials
+      constexpr int FROM = KS + 2, PER_SLOT = (16 + SLOTS - FROM - 1) / (SLOTS - FROM);
       const uint32_t k_step = k0 + (n + 1) % W::KRING * W::STAGE, v_step = v0 + (n + W::VRING - 1) % W::VRING * W::STAGE;
-      f32x16 sn[RB];
+      f32x16 sn;
       u32x4 f[PRE + 1];
       float x[2][2], y[2][2];                            // arguments and exponentials of a pair, by its parity
       const uint32_t there = there_of[(n + 1) % (2 * W::CHUNK)];
@@ -1068,31 +1046,26 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
       for (int g = 0; g < PRE; ++g) f[g] = operand(g, k_step, v_step);
       auto arguments = [&](int q) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[q % 2][e] = fmaf(s[q / 8][2 * (q % 8) + e], sc[q / 8], -off[q / 8]);
+        for (int e = 0; e < 2; ++e) x[q % 2][e] = fmaf(s[2 * q + e], sc, -off);
       };
       auto round_and_add = [&](int q) {
-        const int rb = q / 8, i = q % 8;
         uint32_t w = M::pack(y[q % 2][0], y[q % 2][1]);
-        l[rb] = M::add_pair(w, l[rb]);                           // (the sum of what is multiplied: rounded alike)
-        asm volatile("" : "+v"(w), "+v"(l[rb]));
-        p1[i / 4][rb][i % 4] = w;
+        l = M::add_pair(w, l);                                   // (the sum of what is multiplied: rounded alike)
+        asm volatile("" : "+v"(w), "+v"(l));
+        p1[q / 4][q % 4] = w;
       };
       arguments(0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int slot = 0; slot < SLOTS; ++slot) {
-        const int g = slot / RB, rb = slot % RB;
-        if (rb == 0 && g + PRE < G) f[(g + PRE) % (PRE + 1)] = operand(g + PRE, k_step, v_step);
-        if (g < KS) {
-          asm volatile("" : "+a"(qf[g][rb]));                    // (products read it there; vector instructions need the other half)
-          sn[rb] = mul32<C>(f[g % (PRE + 1)], qf[g][rb], g ? sn[rb] : f32x16{});
-        } else {
-          o[(g - KS) % DB][rb] = mul32<C>(f[g % (PRE + 1)], p[(g - KS) / DB][rb], o[(g - KS) % DB][rb]);
-        }
+        if (slot + PRE < SLOTS) f[(slot + PRE) % (PRE + 1)] = operand(slot + PRE, k_step, v_step);
+        const u32x4 x0 = f[slot % (PRE + 1)];
+        if (slot < KS) sn = mul32<C>(x0, qf[slot], slot ? sn : f32x16{});
+        else o[(slot - KS) % DB] = mul32<C>(x0, p[(slot - KS) / DB], o[(slot - KS) % DB]);
 #pragma unroll
         for (int e = slot * EACH; e < (slot + 1) * EACH; ++e) {
           const int q = e / 2;
-          if (e % 2 == 0 && q + 1 < 8 * RB) arguments(q + 1);
+          if (e % 2 == 0 && q + 1 < 8) arguments(q + 1);
           y[q % 2][e % 2] = __builtin_amdgcn_exp2f(x[q % 2][e % 2]);
           asm volatile("" : "+v"(y[q % 2][e % 2]));
           if (e % 2 == 0 && q > 0) round_and_add(q - 1);
@@ -1102,18 +1075,17 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
         // row with such a score is NaN anyway)
         if (slot >= FROM) {
 #pragma unroll
-          for (int e = (slot - FROM) * PER_SLOT; e < (slot - FROM + 1) * PER_SLOT && e < 16 * RB; ++e) {
-            float v = sn[e / 16][e % 16];
+          for (int e = (slot - FROM) * PER_SLOT; e < (slot - FROM + 1) * PER_SLOT && e < 16; ++e) {
+            float v = sn[e];
             asm volatile("" : "+v"(v));
-            s1[e / 16][e % 16] = v;
-            top[e / 16] = e % 16 ? __builtin_elementwise_maximum(top[e / 16], v) : v;
+            s1[e] = v;
+            top = e ? __builtin_elementwise_maximum(top, v) : v;
           }
-#pragma unroll
-          for (int i = 0; i < RB; ++i) asm volatile("" : "+v"(top[i]));
+          asm volatile("" : "+v"(top));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      round_and_add(8 * RB - 1);
+      round_and_add(7);
       settle(n + 1, s1, there);
       if ((n + W::AHEAD + 1) % W::CHUNK == 0) look_up((n + W::AHEAD + 1) / W::CHUNK);
       if (careful) {
@@ -1125,24 +1097,17 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
     Scores s0, s1;
     Probs p0, p1;
     {
-      f32x16 sn[RB];
+      f32x16 sn;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 f = operand(ks, k0, 0);
+      for (int ks = 0; ks < KS; ++ks) sn = mul32<C>(operand(ks, k0, 0), qf[ks], ks ? sn : f32x16{});
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) sn[rb] = mul32<C>(f, qf[ks][rb], ks ? sn[rb] : f32x16{});
+      for (int i = 0; i < 16; ++i) {
+        float v = sn[i];
+        asm volatile("" : "+v"(v));
+        s0[i] = v;
+        top = i ? __builtin_elementwise_maximum(top, v) : v;
       }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float v = sn[rb][i];
-          asm volatile("" : "+v"(v));
-          s0[rb][i] = v;
-          top[rb] = i ? __builtin_elementwise_maximum(top[rb], v) : v;
-        }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) p0[0][rb] = p0[1][rb] = u32x4{0, 0, 0, 0};
+      p0[0] = p0[1] = u32x4{0, 0, 0, 0};
     }
     settle(0, s0, there_of[0]);
     wait_and_meet<(W::AHEAD - 2) * 2 * NL + NL>();               // (step 0 fetches over the keys of S(0))
@@ -1164,9 +1129,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
 #pragma unroll
           for (int e4 = 0; e4 < 16; ++e4) {
             const float v = (float)row[d * 32 + 8 * (e4 / 4) + e4 % 4];
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-              if ((sight[rb].bits(i) & 1) && not_finite(v)) o[d][rb][e4] += v;
+            if ((sight.bits(i) & 1) && not_finite(v)) o[d][e4] += v;
           }
       }
       break;
@@ -1175,9 +1138,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sick = __builtin_elementwise_maximum(sick, fabsf(o[d][rb][i]));
+      for (int i = 0; i < 16; ++i) sick = __builtin_elementwise_maximum(sick, fabsf(o[d][i]));
     const bool any_sick = __any(not_finite(sick));
     if (lane == 0) there_of[wave] = any_sick;
     wait_and_meet<0>();
@@ -1186,31 +1147,28 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
     careful = true;
   }
 
-  // Results.  A lane has four neighbouring elements of its row at a time: the rows of a block of 32 go through this wavefront's
-  // part of LDS, pieces of 16 bytes in an order by row, so that memory gets whole rows.
+  // Results.  A lane has four neighbouring elements of its row at a time: they go through this wavefront's part of LDS, pieces of 16 bytes in an order by row, so that memory gets whole rows.
   char *const mine = lds + wave * (W::STAGE * (parts == 1 ? 1 : 2));
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    l[rb] += __shfl_xor(l[rb], 32);
-    const int from = r0 + wave * W::WROWS + rb * 32;             // the block's first row
-    if (from > r1) break;
-    // row `row` of the block in memory
-    auto place = [&](int row, int &tok, int &qh) {
+  l += __shfl_xor(l, 32);
+  const int from = r0 + wave * W::WROWS;                         // this wavefront's first row
+  if (from <= r1) {
+    // row `row` of them in memory
+    int tok, qh;
+    auto place = [&](int row) {
       const int r = min(from + row, r1);
       tok = a.by_rep.quot(r);
       qh = head * a.rep + r - tok * a.rep;
       return from + row <= r1;
     };
-    int tok, qh;
     if (parts == 1) {
-      const float f = l[rb] == 0.f ? 0.f : 1.f / l[rb];
+      const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const int piece = 4 * d + i / 4;
           *(u32x2 *)(mine + col * W::ROW + (piece ^ (col % W::PIECES)) * 16 + 8 * h) =
-              u32x2{Mat<__bf16>::pack(o[d][rb][i] * f, o[d][rb][i + 1] * f), Mat<__bf16>::pack(o[d][rb][i + 2] * f, o[d][rb][i + 3] * f)};
+              u32x2{Mat<__bf16>::pack(o[d][i] * f, o[d][i + 1] * f), Mat<__bf16>::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
         }
       __builtin_amdgcn_wave_barrier();
       u32x4 v[32 / W::PER];
@@ -1221,7 +1179,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
       }
 #pragma unroll
       for (int j = 0; j < 32 / W::PER; ++j)
-        if (place(j * W::PER + lane / W::PIECES, tok, qh))
+        if (place(j * W::PER + lane / W::PIECES))
           *(u32x4 *)((T *)a.out + (long long)(first_token + tok) * a.out_stride + (long long)qh * HD + my_slot * 8) = v[j];
     } else {
       constexpr int P = 2 * W::PIECES;                           // fp32: twice as many pieces
@@ -1230,20 +1188,19 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void k_attn_many(Cache c, B
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const int piece = 8 * d + i / 2 + h;
-          *(f32x4 *)(mine + col * (2 * W::ROW) + (piece ^ (col % P)) * 16) = f32x4{o[d][rb][i], o[d][rb][i + 1], o[d][rb][i + 2], o[d][rb][i + 3]};
+          *(f32x4 *)(mine + col * (2 * W::ROW) + (piece ^ (col % P)) * 16) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
         }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int j = 0; j < 32 * P / 64; ++j) {
         const int row = j * (64 / P) + lane / P, piece = lane % P;
         const f32x4 v = *(const f32x4 *)(mine + row * (2 * W::ROW) + (piece ^ (row % P)) * 16);
-        if (place(row, tok, qh)) *(f32x4 *)(a.part_o + ((((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z) * HD + piece * 4) = v;
+        if (place(row)) *(f32x4 *)(a.part_o + ((((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z) * HD + piece * 4) = v;
       }
       // (maxima in base 2, as k_attn_split has them)
-      if (h == 0 && place(col, tok, qh))
-        a.part_ml[(((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z] = make_float2(m[rb] == -INFINITY ? -INFINITY : off[rb] + M::kLazyBias, l[rb]);
+      if (h == 0 && place(col))
+        a.part_ml[(((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z] = make_float2(m == -INFINITY ? -INFINITY : off + M::kLazyBias, l);
     }
-    __builtin_amdgcn_wave_barrier();
   }
 }
 

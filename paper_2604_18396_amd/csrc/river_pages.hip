@@ -225,14 +225,14 @@ struct AttnPlan {
   int max_new, tiles, tile_rows, n_splits, split_len;
   size_t o_bytes, bytes;                                         // of the partial results
 };
-// k_attn_many from 64 rows of a sequence and key head on, where all of them see enough: rows x keys (of a row in the middle) x elements,
-// 6e8 at head size 128 and 5e8 at 64.  It reads keys once for 256 or 128 rows, k_attn_split for 16, but takes 10 us to begin and end
-// (us, k_attn_many / k_attn_split; 8B shape: 512 behind none 32.0 / 25.3, 32 behind 4096 30.5 / 31.2, 64 behind 4096 35.3 / 45.8, 16 behind
-// 65536 103 / 156; sixteen sequences, 16 behind 512 30.8 / 21.2, 32 behind 512 33.1 / 34.6; 1B shape: 512 behind none 17.3 / 16.0, 64
-// behind 4096 22.0 / 24.8, sixteen sequences, 16 behind 512 15.8 / 13.5, 32 behind 512 17.9 / 19.9)
-constexpr int kManyRows = 64;
-static int many_rows(int head_dim) { return head_dim == 128 ? Many<__bf16, 128>::ROWS : Many<__bf16, 64>::ROWS; }
-static double many_work(int head_dim) { return head_dim == 128 ? 6e8 : 5e8; }
+// k_attn_many where the rows of a sequence and key head are more than a tile of k_attn_split and all of them see enough: rows x keys
+// (of a row in the middle) x elements, 1.3e8 at head size 128 and 3e8 at 64.  It reads keys once for 128 rows, k_attn_split for 16, but
+// takes longer to begin and end (us, k_attn_many / k_attn_split; 8B shape: 256 new tokens behind none 12.2 / 11.3, 32 behind 1024
+// 18.4 / 21.5, 16 behind 4096 18.9 / 22.8, 8 behind 65536 56 / 104; eight sequences, 8 behind 2048 31.9 / 29.0; sixteen, 16 behind 512
+// 22.2 / 24.2; 1B shape: 512 behind none 15.6 / 15.8, 32 behind 4096 17.0 / 17.3, 64 behind 4096 22.8 / 29.9, 8 behind 65536 39.5 / 47.4;
+// sixteen, 16 behind 512 16.3 / 14.8, 32 behind 512 19.3 / 21.0)
+constexpr int kSplitRows = 16;
+static double many_work(int head_dim) { return head_dim == 128 ? 1.3e8 : 3e8; }
 // Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a
 // second launch 6.4 + 3.8; 16 sequences of up to 1201 15.8, 14.3 + 3.9; 64 splits of 131072 105, 96 + 6)
 constexpr int kFewSplits = 16;
@@ -245,11 +245,11 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   long long keys = std::min<long long>({b->max_len, (long long)b->max_pages * p->page_size, kMostPositions});
   if (window) keys = std::min<long long>(keys, (long long)window + sinks + 15 / rep);
   const double seen = (double)std::min<long long>(keys, std::max(0, b->max_len - y.max_new / 2));
-  y.many = p->dtype == RIVER_BF16 && rows >= kManyRows && b->n_seq * seen * rows * p->n_kv_heads * p->head_dim >= many_work(p->head_dim);
-  y.tile_rows = y.many ? many_rows(p->head_dim) : 16;
+  y.many = p->dtype == RIVER_BF16 && rows > kSplitRows && b->n_seq * seen * rows * p->n_kv_heads * p->head_dim >= many_work(p->head_dim);
+  y.tile_rows = y.many ? Many<__bf16, 128>::ROWS : kSplitRows;
   y.tiles = (int)((rows + y.tile_rows - 1) / y.tile_rows);
-  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has one of k_attn_many (two at head size 64)
-  // of at least 256 keys.
+  // Workgroups without a split: sequences x key heads x tiles; splits so that every CU has two of k_attn_many of at least 256
+  // keys.
   // k_attn_split (two at a time on a CU at head size 128, three at 64): three a CU of at least 128 keys (a step for each of the
   // four wavefronts), eight where that leaves them 512: more of them are more even where lengths differ.  us by workgroups a CU, 8B
   // shape: 64 sequences of 128 .. 512 keys 2 / 3 / 4: 21.4 / 21.1 / 27.0, 16 of 300 .. 1200 18.1 / 16.2 / 20.3, 16 of 2048 .. 8192
@@ -257,7 +257,10 @@ static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int n
   // splits: their join
   const long long groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
   auto splits = [&](long long goal, long long least) { return std::min({goal / groups, (keys + least - 1) / least, 64ll}); };
-  const long long want = std::max(1ll, y.many ? splits(65536 / y.tile_rows, 256) : std::max(splits(768, 128), splits(2048, 512)));
+  long long want = std::max(1ll, y.many ? splits(512, 256) : std::max(splits(768, 128), splits(2048, 512)));
+  // k_attn_many: only where it saves more (48 keys take 1 us) than joining takes, 4 us and the partial results written and read (8B shape,
+  // us, split / not: 384 tokens 19.9 / 15.2, 768 29.6 / 23.1, 1024 38.9 / 29.0; sixteen sequences, 32 behind 512 27.4 / 18.5)
+  if (y.many && keys / 48. * (want - 1) / want < 4 + (double)b->n_seq * y.max_new * nq * p->head_dim * want * 8 / 5e6) want = 1;
   y.split_len = (int)std::max(128ll, std::min<long long>(((keys + want - 1) / want + 127) / 128 * 128, 1 << 30));
   y.n_splits = (int)std::max(1ll, (keys + y.split_len - 1) / y.split_len);
   y.fused = !y.many && groups <= RIVER_TICKETS && y.n_splits <= kFewSplits;
