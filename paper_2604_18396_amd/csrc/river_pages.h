@@ -784,17 +784,18 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 //
 // Bound: the matrix cores and the vector instructions (exponentials above all) about alike, 46 % and 47 % of a SIMD's cycles, and the
 // clock that the power limit leaves, 1.6 .. 2.1 GHz.  A wavefront holds 32 rows in fewer than 256 registers, all of them general ones,
-// so that two workgroups of 128 rows are on a CU and one's waits, beginning and end lie beside the other's products.  (64 rows a
+// so that two workgroups of 128 rows are on a CU (three at head size 64, whose few spilled registers lie outside the steps: 4096
+// tokens 114 / 98 us) and one's waits, beginning and end lie beside the other's products.  (64 rows a
 // wavefront, one to a SIMD, read LDS half as often, but nothing runs beside their waits: us, 64 rows / 32 rows, 8B shape: 4096 tokens
-// 163 / 153, 2048 behind 16384 640 / 630, five windows of 1024 223 / 178, prompts of 2048, 2015, 551 and 513 122 / 107; 1B shape 4096
-// tokens 146 / 111.)
+// 163 / 148, 2048 behind 16384 640 / 615, five windows of 1024 223 / 171, prompts of 2048, 2015, 551 and 513 122 / 102; 1B shape 4096
+// tokens 146 / 98.)
 // What would wait for each other is taken from different steps of 32 keys: step n multiplies S(n+1) = K Q^T, takes the exponentials
 // of S(n), and adds P(n-1) V, three things that do not depend on each other.
 // O is therefore rescaled one step after the maximum has moved (pend); it moves when a score is 2^kLazy times as likely as
 // what was the maximum (one of 32 rows has a new maximum in most steps, and rescaling takes half as long as the step).
 // Keys and values go from memory straight into LDS (no registers, AHEAD steps in flight), in rings, one barrier a step; where a key's
 // row lies is looked up for CHUNK steps at once.
-// 8B shape, 4096 tokens: 153 us, 900 TFLOP/s; 2048 behind 16384 630 us, 930; the largest matrix products of the library reach 1250.
+// 8B shape, 4096 tokens: 148 .. 153 us, 900 .. 930 TFLOP/s; 2048 behind 16384 615 us, 950; the largest matrix products of the library reach 1250.
 template <class C, int HD>
 struct Many {
   typedef Mat<C> M;
@@ -833,7 +834,7 @@ __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 template <class T, class C, int HD>
-__global__ __launch_bounds__(256, 2) void k_attn_many(Cache c, Batch b, AttnArgs a) {
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Batch b, AttnArgs a) {
   typedef Many<C, HD> W;
   typedef Mat<C> M;
   constexpr int KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
