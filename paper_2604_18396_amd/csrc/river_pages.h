@@ -782,7 +782,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)
 //
-// Bound: the matrix cores and the vector instructions (exponentials above all) about alike, 46 % and 47 % of a SIMD's cycles, and the
+// Bound: the matrix cores and the vector instructions (exponentials above all) about alike, 48 % and 49 % of a SIMD's cycles, and the
 // clock that the power limit leaves, 1.6 .. 2.1 GHz.  A wavefront holds 32 rows in fewer than 256 registers, all of them general ones,
 // so that two workgroups of 128 rows are on a CU (three at head size 64, whose few spilled registers lie outside the steps: 4096
 // tokens 114 / 98 us) and one's waits, beginning and end lie beside the other's products.  (64 rows a
