@@ -414,7 +414,18 @@ _device = torch._C._cuda_getDevice
 _stream = torch._C._cuda_getCurrentRawStream
 
 
-class Pages:
+class _Fixed:
+    """What the library was told of once stays as it is: another tensor or bound needs another object."""
+
+    _made = False
+
+    def __setattr__(self, name, value):
+        if self._made:
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be changed: make another {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+
+class Pages(_Fixed):
     """A paged cache: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (the last three dimensions
     contiguous, the strides of k and v alike), in the dtype of the activations (fp32, bf16) or, with bf16 ones, fp16."""
 
@@ -433,9 +444,10 @@ class Pages:
                              0 if dtype == torch.float32 else 1, 1 if k.dtype == torch.float16 else 0)
         self.ref = C.byref(self.c)
         self.shape_key = (heads, size, hd, dtype)
+        self._made = True
 
 
-class Batch:
+class Batch(_Fixed):
     """The sequences of a call: table [n_seq, max_pages], lens [n_seq] and q_start [n_seq + 1] (None: one new token per
     sequence), int32 on the device and read there at every call; max_new and max_len (default: what the table holds) bound
     the new tokens and the lengths."""
@@ -454,7 +466,8 @@ class Batch:
             raise ValueError("without q_start every sequence has one new token")
         self.table, self.lens, self.q_start, self.index, self.n_seq = table, lens, q_start, table.get_device(), n
         self.max_len, self.max_new = max_len, max_new
-        self._calls, self._bytes = {}, {}       # the C struct, and the workspace, of a shape of call
+        self._calls, self._bytes = {}, {}       # the C struct, and the workspace's size, of a shape of call
+        self._made = True
 
     def bind(self, n_tokens: int, pages: Pages):
         """The call's C struct (one per number of tokens and page size: never changed once made)."""
@@ -467,13 +480,14 @@ class Batch:
                             n_tokens, most, self.table.stride(0) if self.n_seq > 1 else most, self.max_new,
                             min(2**31 - 1, most * pages.page_size) if self.max_len is None else self.max_len)
             if len(self._calls) >= 256:
-                self._calls, self._bytes = {}, {}
+                self._calls.clear()
+                self._bytes.clear()
             got = self._calls[(n_tokens, pages.page_size)] = C.byref(c)
         return got
 
 
-class Rope:
-    """Rotary positions: inv_freq float64 [rot_dim / 2] on the device (see rope_frequencies), layout "half" or "interleaved"."""
+class Rope(_Fixed):
+    """Rotary positions: inv_freq float64 [rot_dim / 2] on the device (river_rope_frequencies has the usual ones), layout "half" or "interleaved"."""
 
     def __init__(self, inv_freq: torch.Tensor, layout: str = "half", mscale: float = 1.0):
         if not inv_freq.is_cuda or inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
@@ -481,6 +495,7 @@ class Rope:
         self.inv_freq, self.index = inv_freq, inv_freq.get_device()
         self.c = river_rope(inv_freq.data_ptr(), 2 * inv_freq.numel(), ROPE_LAYOUTS[layout], mscale)
         self.ref = C.byref(self.c)
+        self._made = True
 
 
 def river_rope_frequencies(rot_dim: int, base: float, scaling: str = "plain", factor: float = 1.0, original_len: float = 0.0,

@@ -265,6 +265,19 @@ def test_attention_large_prompts(kind, hd, nkv, rep, lens, new, window, sinks):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("n_seq,nkv", [(2, 8), (3, 3), (4, 8), (5, 1), (8, 2), (33, 1), (33, 8)])
+@pytest.mark.parametrize("shape", ["single tokens", "prompts", "split prompts"])
+def test_attention_of_many_ragged_sequences(kind, n_seq, nkv, shape):
+    # every sequence's tiles and splits are worked on once, whatever the order in which they are handed out
+    rng = np.random.default_rng(n_seq * 10 + nkv)
+    lens = [int(n) for n in rng.integers(1, 900, n_seq)]
+    lens[0], lens[n_seq // 2] = 1000, 0
+    new = [min(n, 1) if shape == "single tokens" else int(rng.integers(0, n + 1)) for n in lens]
+    new[0] = 1 if shape == "single tokens" else 300
+    run_attention(Setup(kind, nkv, 64, 16, lens, new, seed=n_seq, room=20000 // 16 if shape == "split prompts" else 0), nkv * 4)
+
+
+@pytest.mark.parametrize("kind", TYPES)
 def test_attention_long_cache(kind):
     run_attention(Setup(kind, 1, 64, 64, [20011], [1], seed=1, ragged=False), 4)
     run_attention(Setup(kind, 2, 128, 64, [9000, 31, 4097], [1, 1, 1], seed=2, ragged=False), 8, 8000, 70)
@@ -510,6 +523,18 @@ def test_the_same_call_gives_the_same_bits():
             first = B.river_paged_attention(st.pages, 0, st.batch, q)
             for _ in range(5):
                 assert torch.equal(first, B.river_paged_attention(st.pages, 0, st.batch, q))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "bf16-f16"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_full_card_gives_the_same_bits(kind, hd):
+    # workgroups side by side on every CU, out of step with each other
+    st = Setup(kind, 8, hd, 16, [2000, 1100, 513, 40], [2000, 900, 513, 3], seed=37)
+    q = st.randn(st.tokens, 32, hd)
+    for window, sinks in ((0, 0), (700, 4)):
+        first = B.river_paged_attention(st.pages, 0, st.batch, q, window, sinks)
+        for _ in range(5):
+            assert torch.equal(first, B.river_paged_attention(st.pages, 0, st.batch, q, window, sinks))
 
 
 # ------------------------------------------------------------------ streams and graphs
@@ -865,6 +890,14 @@ def test_attention_over_a_context_s_own_cache():
     for layer in range(2):
         run_attention(st, 8, layer=layer)
     a.close()
+
+
+def test_handles_stay_as_they_were_made():
+    st = Setup("bf16", 1, 64, 16, [20], [1], seed=38)
+    f, m = freqs(64)
+    for handle, name in ((st.pages, "k"), (st.batch, "max_len"), (st.batch, "table"), (B.Rope(f, "half", m), "inv_freq")):
+        with pytest.raises(AttributeError):
+            setattr(handle, name, getattr(handle, name))
 
 
 def test_the_binding_refuses():
