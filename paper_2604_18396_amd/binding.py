@@ -532,7 +532,8 @@ def _out(q: torch.Tensor, out: torch.Tensor | None, pages: Pages):
 def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope: Rope,
                      out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotates q and k [n_tokens, heads, head_dim] at the new tokens' positions and stores k and v in the pages.  Returns the
-    rotated queries: `out`, which may be q, or a new tensor (rows of tokens that belong to no sequence are not written)."""
+    rotated queries: `out`, which may be q, or a new tensor (rows of tokens that belong to no sequence are not written).  For inference:
+    autograd does not see it."""
     if pages.index != _device():        # the library takes the current device and the stream that it is given
         with torch.cuda.device(pages.index):
             return river_rope_store(pages, layer, batch, q, k, v, rope, out)
@@ -549,7 +550,7 @@ def river_rope_store(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, k:
 def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tensor, window: int = 0, sinks: int = 0,
                           scale: float = 0.0, out: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of the new tokens' queries [n_tokens, heads, head_dim] over their sequences' pages.  Rows of `out` (or of the new
-    tensor that is returned) whose tokens belong to no sequence are not written."""
+    tensor that is returned) whose tokens belong to no sequence are not written.  For inference: autograd does not see it."""
     if pages.index != _device():
         with torch.cuda.device(pages.index):
             return river_paged_attention(pages, layer, batch, q, window, sinks, scale, out)
