@@ -88,10 +88,10 @@ struct river_pool {
   // A later position p >= len - 1 sees j > p - window and j < sinks: pages between them are seen by none.
   void trim(int s, int window, int sinks) {
     const long long gone = (long long)len[s] - window;           // positions below this are behind the window
-    for (int i = (int)(((long long)sinks + page_size - 1) / page_size); (long long)(i + 1) * page_size <= gone; ++i)
+    for (long long i = ((long long)sinks + page_size - 1) / page_size; (i + 1) * page_size <= gone; ++i)    // (sinks: up to 2^31 - 1)
       if (row(s)[i] >= 0) {
         drop(row(s)[i]);
-        set_entry(s, i, -1);
+        set_entry(s, (int)i, -1);
       }
   }
   // Pages from `used` on move to the free ones below it.

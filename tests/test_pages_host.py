@@ -295,3 +295,15 @@ def test_pool_against_a_model(seed):
         assert p.free_pages() == len(m.free)
         for i in range(seqs):
             assert p.length(i) == m.len[i] and p.entries(i) == m.rows[i] + [-1] * (most - len(m.rows[i]))
+
+
+@pytest.mark.parametrize("ps", [1, 2, 16])
+@pytest.mark.parametrize("window", [1, 2**31 - 1])
+def test_pool_trims_nothing_where_every_position_is_a_sink(ps, window):
+    # (the first page that is no sink's is beyond every row, and beyond an int at page size 1)
+    p = Pool(64, ps, 2, 32)
+    assert p.extend(0, 20) == 0
+    before = p.entries(0)
+    for sinks in (2**31 - 1, 2**31 - 2, 2**30, 20):
+        assert p.trim(0, window, sinks) == 0 and p.entries(0) == before
+    assert p.trim(0, 2**31 - 1, 0) == 0 and p.entries(0) == before
