@@ -409,9 +409,10 @@ def _check_on(device, dtype, **tensors):
             raise ValueError(f"{name}: {dtype} on {device} is needed, not {t.dtype} on {t.device}")
 
 
-# (the device's number and its stream's handle without the torch.cuda objects around them, which take longer than a small call)
-_device = torch._C._cuda_getDevice
-_stream = torch._C._cuda_getCurrentRawStream
+# (the device's number and its stream's handle without the torch.cuda objects around them, which take longer than a small call; a torch
+# that is built without a GPU has neither, and imports this module all the same)
+_device = getattr(torch._C, "_cuda_getDevice", None)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 class _Fixed:

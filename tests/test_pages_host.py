@@ -2,7 +2,10 @@
 import ctypes as C
 import heapq
 import math
+import os
 import random
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -307,3 +310,13 @@ def test_pool_trims_nothing_where_every_position_is_a_sink(ps, window):
     for sinks in (2**31 - 1, 2**31 - 2, 2**30, 20):
         assert p.trim(0, window, sinks) == 0 and p.entries(0) == before
     assert p.trim(0, 2**31 - 1, 0) == 0 and p.entries(0) == before
+
+
+def test_the_binding_is_imported_where_torch_has_no_gpu_part():
+    # (a torch built for the CPU: the byte model, the configurations and the host calls are of use there)
+    code = ("import torch\n"
+            "for name in [n for n in dir(torch._C) if n.startswith('_cuda_')]: delattr(torch._C, name)\n"
+            "from paper_2604_18396_amd import binding as B\n"
+            "assert B.river_rope_frequencies(4, 100.0)[0].tolist() == [1.0, 0.1]\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=root, timeout=300)
