@@ -31,6 +31,7 @@ EXPORTS = ("river_quantize_w4", "river_workspace_bytes", "river_create", "river_
 TICKETS = 1024
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+ROPE_HIGH = {"bands": 4.0, "ramp": 32.0}        # turns from which on a frequency stays as it is, where models do not say otherwise
 
 
 class RiverError(RuntimeError):
@@ -500,8 +501,10 @@ class Rope(_Fixed):
 
 
 def river_rope_frequencies(rot_dim: int, base: float, scaling: str = "plain", factor: float = 1.0, original_len: float = 0.0,
-                           low: float = 1.0, high: float = 32.0):
-    """(frequencies as a numpy array of float64, what cosines and sines are multiplied with)."""
+                           low: float | None = None, high: float | None = None):
+    """(frequencies as a numpy array of float64, what cosines and sines are multiplied with).  low and high: turns between which
+    "bands" (default 1 and 4) and "ramp" (1 and 32) pass from scaled to unscaled frequencies."""
+    low, high = 1.0 if low is None else low, ROPE_HIGH.get(scaling, 32.0) if high is None else high
     f, m = np.empty(max(rot_dim // 2, 1), dtype=np.float64), C.c_float()
     _check_call(load().river_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, original_len, low, high, f.ctypes.data,
                                               C.byref(m)))

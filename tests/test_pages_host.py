@@ -148,6 +148,21 @@ def test_frequencies():
         assert m1 == 1.0
 
 
+def test_frequencies_pass_between_the_usual_turns_by_default():
+    # bands between 1 and 4 turns, the ramp between 1 and 32 (perf/operators.py has the same)
+    rot, base, factor, orig = 128, 500000.0, 8.0, 8192.0
+    for scaling, high in (("bands", 4.0), ("ramp", 32.0)):
+        got, m = B.river_rope_frequencies(rot, base, scaling, factor, orig)
+        want, m1 = B.river_rope_frequencies(rot, base, scaling, factor, orig, 1.0, high)
+        assert got.tolist() == want.tolist() and m == m1
+    f = base ** (-2.0 * np.arange(rot // 2) / rot)
+    got, _ = B.river_rope_frequencies(rot, base, "bands", factor, orig)
+    n = orig * f / (2 * math.pi)
+    s = np.clip((n - 1) / 3, 0, 1)
+    np.testing.assert_allclose(got, f * s + f / factor * (1 - s), rtol=1e-13)
+    assert B.river_rope_frequencies(rot, base, "bands", factor, orig, high=32.0)[0].tolist() != got.tolist()
+
+
 @pytest.mark.parametrize("args", [(0, 1e4), (7, 1e4), (64, 1.0), (64, math.nan), (64, 1e4, "linear", 0.5), (64, 1e4, "linear", math.inf),
                                   (2, 1e4, "base", 2.0), (64, 1e4, "bands", 2.0, 0.0), (64, 1e4, "ramp", 2.0, 8192.0, 32.0, 1.0),
                                   (64, 1e4, "ramp", 2.0, 8192.0, 0.0, 32.0)], ids=str)
