@@ -588,7 +588,8 @@ def _tickets(index: int, stream: int):
         return None
     t = _ticket_tensors.get((index, stream))
     if t is None:
-        t = _ticket_tensors[(index, stream)] = torch.zeros(TICKETS, dtype=torch.int32, device=f"cuda:{index}")
+        # (two threads that call for the first time at once get the one tensor that stays: another would be freed under a call's kernel)
+        t = _ticket_tensors.setdefault((index, stream), torch.zeros(TICKETS, dtype=torch.int32, device=f"cuda:{index}"))
     return t.data_ptr()
 
 

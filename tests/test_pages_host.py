@@ -335,3 +335,28 @@ def test_the_binding_is_imported_where_torch_has_no_gpu_part():
             "assert B.river_rope_frequencies(4, 100.0)[0].tolist() == [1.0, 0.1]\n")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     subprocess.run([sys.executable, "-c", code], check=True, cwd=root, timeout=300)
+
+
+def test_threads_of_one_stream_share_its_tickets(monkeypatch):
+    # another thread's first call comes in while this one's is making its tensor: both use the one that is kept
+    made, others = [], []
+
+    def zeros(n, dtype, device):
+        made.append(np.zeros(n, dtype=np.int32))
+        if len(made) == 1:
+            others.append(B._tickets(0, 77))
+        return Tensor(made[-1])
+
+    class Tensor:
+        def __init__(self, a):
+            self.a = a
+
+        def data_ptr(self):
+            return self.a.ctypes.data
+
+    monkeypatch.setattr(B.torch._C, "_cuda_isCurrentStreamCapturing", lambda: False, raising=False)
+    monkeypatch.setattr(B.torch, "zeros", zeros)
+    monkeypatch.setattr(B, "_ticket_tensors", {})
+    mine = B._tickets(0, 77)
+    assert others == [mine] and B._tickets(0, 77) == mine and B._ticket_tensors[(0, 77)].data_ptr() == mine
+    assert B._tickets(0, 78) != mine
