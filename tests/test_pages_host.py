@@ -342,10 +342,11 @@ def test_threads_of_one_stream_share_its_tickets(monkeypatch):
     made, others = [], []
 
     def zeros(n, dtype, device):
-        made.append(np.zeros(n, dtype=np.int32))
+        a = np.zeros(n, dtype=np.int32)
+        made.append(a)
         if len(made) == 1:
             others.append(B._tickets(0, 77))
-        return Tensor(made[-1])
+        return Tensor(a)
 
     class Tensor:
         def __init__(self, a):
