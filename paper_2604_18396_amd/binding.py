@@ -329,15 +329,19 @@ class River:
 
     def save_pages(self, pages: "Pages", row: torch.Tensor, n: int, first: int = 0, seq: int = 0):
         """Positions first .. first + n - 1 of the sequence to the pages that `row` (device int32) names."""
-        _check_on(pages.device, torch.int32, row=row)
-        assert row.dim() == 1 and row.is_contiguous()
+        self._check_pages(pages, row)
         self._check(load().river_save_pages(self._h, seq, first, n, pages.ref, row.data_ptr(), row.numel()))
 
     def load_pages(self, pages: "Pages", row: torch.Tensor, n: int, next_token: int, seq: int = 0):
         """Positions 0 .. n - 1 of the sequence from pages; next_token is what its next step consumes by default."""
+        self._check_pages(pages, row)
+        self._check(load().river_load_pages(self._h, seq, n, int(next_token), pages.ref, row.data_ptr(), row.numel()))
+
+    def _check_pages(self, pages: "Pages", row: torch.Tensor):
         _check_on(pages.device, torch.int32, row=row)
         assert row.dim() == 1 and row.is_contiguous()
-        self._check(load().river_load_pages(self._h, seq, n, int(next_token), pages.ref, row.data_ptr(), row.numel()))
+        if pages.index != self.workspace.get_device():
+            raise ValueError("pages and context are on different devices")
 
     def read_records(self, n: int):
         toks = np.empty(n, dtype=np.int32)

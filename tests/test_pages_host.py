@@ -6,6 +6,7 @@ import os
 import random
 import subprocess
 import sys
+import types
 
 import numpy as np
 import pytest
@@ -361,3 +362,15 @@ def test_threads_of_one_stream_share_its_tickets(monkeypatch):
     mine = B._tickets(0, 77)
     assert others == [mine] and B._tickets(0, 77) == mine and B._ticket_tensors[(0, 77)].data_ptr() == mine
     assert B._tickets(0, 78) != mine
+
+
+def test_a_context_refuses_pages_of_another_device():
+    # (its kernels would read another GPU's addresses; stand-ins for both, the call must not come as far as the library)
+    r = B.River.__new__(B.River)
+    r._h, r.workspace = None, B.torch.empty(1)
+    pg = types.SimpleNamespace(device=B.torch.device("meta"), index=1, ref=None)
+    row = B.torch.empty(3, dtype=B.torch.int32, device="meta")
+    with pytest.raises(ValueError, match="different devices"):
+        r.save_pages(pg, row, 1)
+    with pytest.raises(ValueError, match="different devices"):
+        r.load_pages(pg, row, 1, 0)
