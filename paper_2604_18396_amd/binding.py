@@ -6,6 +6,7 @@ been built, loading raises: there is no fallback of any kind.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -239,10 +240,11 @@ class River:
             raise RiverError(RIVER_EINVAL, "invalid configuration")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev_weights["tok_emb"].device)
         self.workspace_bytes = nbytes
+        self._stream = torch.cuda.current_stream()             # the context's, from now on
         h = C.c_void_p()
         create = L.river_create_static if static_scratch else L.river_create
         rc = create(C.byref(self._c), C.byref(w), C.byref(q) if q is not None else None,
-                    self.workspace.data_ptr(), nbytes, _stream_ptr(), C.byref(h))
+                    self.workspace.data_ptr(), nbytes, self._stream.cuda_stream, C.byref(h))
         if rc:
             raise RiverError(rc, L.river_last_error(None).decode())
         self._h = h
@@ -328,14 +330,31 @@ class River:
         return out
 
     def save_pages(self, pages: "Pages", row: torch.Tensor, n: int, first: int = 0, seq: int = 0):
-        """Positions first .. first + n - 1 of the sequence to the pages that `row` (device int32) names."""
+        """Positions first .. first + n - 1 of the sequence to the pages that `row` (device int32) names.  On the context's stream, behind
+        what the current one has queued; what is queued there afterwards comes behind the call."""
         self._check_pages(pages, row)
-        self._check(load().river_save_pages(self._h, seq, first, n, pages.ref, row.data_ptr(), row.numel()))
+        with self._in_order():
+            self._check(load().river_save_pages(self._h, seq, first, n, pages.ref, row.data_ptr(), row.numel()))
 
     def load_pages(self, pages: "Pages", row: torch.Tensor, n: int, next_token: int, seq: int = 0):
-        """Positions 0 .. n - 1 of the sequence from pages; next_token is what its next step consumes by default."""
+        """Positions 0 .. n - 1 of the sequence from pages; next_token is what its next step consumes by default.  Streams as in
+        save_pages."""
         self._check_pages(pages, row)
-        self._check(load().river_load_pages(self._h, seq, n, int(next_token), pages.ref, row.data_ptr(), row.numel()))
+        with self._in_order():
+            self._check(load().river_load_pages(self._h, seq, n, int(next_token), pages.ref, row.data_ptr(), row.numel()))
+
+    @contextlib.contextmanager
+    def _in_order(self):
+        with torch.cuda.device(self._stream.device):
+            here = torch.cuda.current_stream()
+            if here == self._stream:
+                yield
+                return
+            self._stream.wait_stream(here)
+            try:
+                yield
+            finally:
+                here.wait_stream(self._stream)
 
     def _check_pages(self, pages: "Pages", row: torch.Tensor):
         _check_on(pages.device, torch.int32, row=row)

@@ -949,3 +949,65 @@ def test_the_binding_refuses():
         assert B.load().river_paged_attention(*args(ws.data_ptr(), n.value - 1)) == B.RIVER_ENOSPC
         assert B.load().river_paged_attention(*args(None, n.value)) == B.RIVER_EINVAL
         assert B.load().river_paged_attention(*args(ws.data_ptr() + 8, n.value)) == B.RIVER_EINVAL
+
+
+def busy():
+    """Some 20 ms of work on the current stream."""
+    x = torch.ones(4096, 4096, device=DEV)
+    for _ in range(20):
+        x = x @ x
+    return x
+
+
+@pytest.mark.parametrize("max_batch", [1, 2])
+def test_contexts_and_pages_on_another_stream(max_batch):
+    """Pages and row are what the caller's stream has queued when a context loads them, and what a context saves is there for what the
+    caller's stream does next, although the context has a stream of its own."""
+    w = inputs.make_weights(SAVE, 5)
+    dw = B.upload_weights(w)
+    river = B.quantize_river(SAVE, dw)
+    prompt = inputs.make_prompt(SAVE.vocab, 45, 6)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    a = B.River(SAVE, dw, river, max_batch=max_batch)
+    with torch.cuda.stream(side):
+        b = B.River(SAVE, dw, river, max_batch=max_batch)
+    tok = a.prefill(prompt)
+    one = lambda x: x if max_batch == 1 else x[0]
+    want_k, want_v = one(a.kcache())[:, :45], one(a.vcache())[:, :45]
+    good = torch.tensor([4, 0, 8, 2, 7, 1, 5], dtype=torch.int32, device=DEV)
+
+    def cache():
+        return B.Pages(*(torch.full((SAVE.n_layers, 9, SAVE.n_kv_heads, 7, SAVE.head_dim), math.nan, dtype=torch.bfloat16, device=DEV) for _ in range(2)))
+
+    def rows(k):
+        p = np.arange(45)
+        return k.float().cpu().numpy()[:, good.cpu().numpy()[p // 7], :, p % 7].transpose(1, 0, 2, 3).reshape(SAVE.n_layers, 45, -1)
+
+    # the context's stream is behind, the caller's is not
+    pages = cache()
+    torch.cuda.synchronize()
+    x = busy()
+    with torch.cuda.stream(side):
+        a.save_pages(pages, good + 0, 45)
+        got_k, got_v = pages.k.clone(), pages.v.clone()
+    torch.cuda.synchronize()
+    assert np.array_equal(rows(got_k), want_k) and np.array_equal(rows(got_v), want_v)
+    # the caller's is behind: pages and row are not written yet
+    for context, stream in ((b, torch.cuda.current_stream()), (a, side)):
+        context.fill_cache(0)
+        late, row = cache(), torch.full_like(good, -1)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            x = busy()
+            late.k.copy_(got_k)
+            late.v.copy_(got_v)
+            row.copy_(good)
+            context.load_pages(late, row + 0, 45, tok)
+            late.k.zero_()                  # (behind the call)
+            row.fill_(-1)
+        torch.cuda.synchronize()
+        assert np.array_equal(one(context.kcache())[:, :45], want_k) and np.array_equal(one(context.vcache())[:, :45], want_v)
+    a.close()
+    b.close()
+    del x
