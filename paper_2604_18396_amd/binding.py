@@ -474,10 +474,11 @@ class Pages(_Fixed):
 
 class Batch(_Fixed):
     """The sequences of a call: table [n_seq, max_pages], lens [n_seq] and q_start [n_seq + 1] (None: one new token per
-    sequence), int32 on the device and read there at every call; max_new and max_len (default: what the table holds) bound
-    the new tokens and the lengths."""
+    sequence), int32 on the device and read there at every call.  max_new and max_len bound a sequence's new tokens (further ones
+    are left out of the attention) and positions (more are still right); the attention divides its work by them, so that bounds
+    near what is there are fastest.  Default: a call's tokens, and what the table holds."""
 
-    def __init__(self, table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor | None = None, max_new: int = 1,
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor | None = None, max_new: int | None = None,
                  max_len: int | None = None):
         _check_on(table.device, torch.int32, table=table, lens=lens, **({} if q_start is None else {"q_start": q_start}))
         n = lens.numel()
@@ -487,7 +488,7 @@ class Batch(_Fixed):
             raise ValueError("rows of the table and lens must be contiguous")
         if q_start is not None and (q_start.shape != (n + 1,) or not q_start.is_contiguous()):
             raise ValueError("q_start [n_seq + 1]")
-        if q_start is None and max_new != 1:
+        if q_start is None and max_new not in (None, 1):
             raise ValueError("without q_start every sequence has one new token")
         self.table, self.lens, self.q_start, self.index, self.n_seq = table, lens, q_start, table.get_device(), n
         self.max_len, self.max_new = max_len, max_new
@@ -502,7 +503,8 @@ class Batch(_Fixed):
         if got is None:
             most = self.table.shape[1]
             c = river_batch(self.table.data_ptr(), self.lens.data_ptr(), None if self.q_start is None else self.q_start.data_ptr(), self.n_seq,
-                            n_tokens, most, self.table.stride(0) if self.n_seq > 1 else most, self.max_new,
+                            n_tokens, most, self.table.stride(0) if self.n_seq > 1 else most,
+                            n_tokens if self.max_new is None else self.max_new,
                             min(2**31 - 1, most * pages.page_size) if self.max_len is None else self.max_len)
             if len(self._calls) >= 256:
                 self._calls.clear()

@@ -1011,3 +1011,13 @@ def test_contexts_and_pages_on_another_stream(max_batch):
     a.close()
     b.close()
     del x
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("lens,new", [([20, 7], [3, 1]), ([300, 0, 64], [290, 0, 64]), ([3000, 40], [1, 33])], ids=str)
+def test_attention_without_a_bound_on_the_new_tokens(kind, lens, new):
+    # every new token of every sequence has its row, also where the batch was made without max_new
+    st = Setup(kind, 2, 64, 16, lens, new, seed=39, pad=3)
+    st.batch = B.Batch(st.table, st.dlens, st.q_start)
+    run_attention(st, 8)
+    run_attention(st, 8, 50, 3)
