@@ -59,6 +59,10 @@ __device__ __forceinline__ int position_of(const Batch &b, int s, int t) {
   return p < 0 ? -1 : (int)p;
 }
 
+// The same for new token i of a sequence with `count` of them: -1 if it has none, and no less, so that a window of up to 2^31 - 1
+// can be taken from it.
+__device__ __forceinline__ int new_position(int len, int count, int i) { return max(max(len, 0) - count + i, -1); }
+
 // The page of position p (0 <= p) and the slot in it; -1: there is none.
 __device__ __forceinline__ int page_of(const Cache &c, const Batch &b, int s, int p, int &slot) {
   if (p >= b.cap) return -1;
@@ -279,8 +283,8 @@ struct Sight {
 // rows r0 .. r1 of a sequence with `count` new tokens
 __device__ __forceinline__ Span span_of(const Batch &b, const AttnArgs &a, int len, int count, int r0, int r1) {
   Span s;
-  s.first = len - count + a.by_rep.quot(r0);
-  s.last = len - count + a.by_rep.quot(r1);
+  s.first = new_position(len, count, a.by_rep.quot(r0));
+  s.last = new_position(len, count, a.by_rep.quot(r1));
   const int end = min(s.last + 1, b.cap);
   s.low = a.window ? max(0, s.first - a.window + 1) : 0;
   s.hs = max(0, min(min(a.sinks, s.low), end));
@@ -503,7 +507,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 
   // this lane's row: its query in the order of the contraction, its position
   const int r = min(r0 + col, r1), tok = a.by_rep.quot(r), qh = head * a.rep + (r - tok * a.rep);
-  const int mypos = b.lens[s] - count + tok;
+  const int mypos = new_position(b.lens[s], count, tok);
   const T *qrow = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)qh * HD;
   u32x4 qf[NP];
   float sc = a.scale2;
@@ -859,7 +863,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
 
   // this wavefront's rows: rows behind the last repeat it
   const int w0 = min(r0 + wave * W::WROWS, r1), w1 = min(w0 + W::WROWS - 1, r1);
-  const int first = len - count + a.by_rep.quot(w0), last = len - count + a.by_rep.quot(w1);
+  const int first = new_position(len, count, a.by_rep.quot(w0)), last = new_position(len, count, a.by_rep.quot(w1));
   const int my_slot = lane % W::PIECES;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   // Their queries in the operand's order.  (Through LDS, in whole rows of memory, they take as long: 4500 cycles, on the way with
@@ -867,7 +871,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   u32x4 qf[KS];
   float sc = a.scale2;
   const int r = min(r0 + wave * W::WROWS + col, r1), tok = a.by_rep.quot(r);
-  const Sight sight = sight_of(a, sp, len - count + tok);
+  const Sight sight = sight_of(a, sp, new_position(len, count, tok));
   const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const u32x4 *)(q + (2 * ks + h) * 8);

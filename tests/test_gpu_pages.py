@@ -1021,3 +1021,18 @@ def test_attention_without_a_bound_on_the_new_tokens(kind, lens, new):
     st.batch = B.Batch(st.table, st.dlens, st.q_start)
     run_attention(st, 8)
     run_attention(st, 8, 50, 3)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("window,sinks", [(2**31 - 1, 0), (2**31 - 1, 2**31 - 1), (2**31 - 3, 3), (2**30, 2**30), (5, 2**31 - 1)])
+@pytest.mark.parametrize("n,m,room", [(1, 5, 0), (40, 100, 0), (40, 100, 20000), (130, 300, 20000), (-2**31, 40, 0), (-2**31, 300, 20000)])
+def test_attention_of_the_widest_windows(kind, window, sinks, n, m, room):
+    # a window that holds all there is, as a number that no length reaches; new tokens that have no position among the others
+    st = Setup(kind, 1, 64, 16, [n, 20, 300], [m, 2, 150], seed=40, room=room)
+    q = st.randn(st.tokens, 4, 64)
+    got = B.river_paged_attention(st.pages, 0, st.batch, q, window, sinks)
+    lost = min(m, m - n)
+    assert bool((got[:lost] == 0).all())
+    st.new, st.start = [max(n, 0), 2, 150], np.array([lost, m, m + 2, m + 152])
+    want, tol = attention(st, q, window, sinks)
+    check(got[lost:], want[lost:], tol[lost:])
