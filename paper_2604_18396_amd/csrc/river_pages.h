@@ -378,13 +378,14 @@ __device__ __forceinline__ uint32_t finite_only(uint32_t w) {
 struct False { static constexpr bool value = false; };
 struct True { static constexpr bool value = true; };
 
-// E neighbouring elements of a row that is divided by its sum (which is zero where nothing was seen), rounded once
+// E neighbouring elements of a row that is divided by its sum, rounded once.  A sum of zero (nothing was seen, or only scores of
+// -infinity) makes a row of zeros, also where a value that counts for nothing is not finite.
 template <class T, int E>
 __device__ __forceinline__ void store_row(T *to, const float (&v)[E], float sum) {
   const float f = sum == 0.f ? 0.f : 1.f / sum;
   T x[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = (T)(v[e] * f);
+  for (int e = 0; e < E; ++e) x[e] = (T)(sum == 0.f ? 0.f : v[e] * f);
   if constexpr (sizeof(x) >= 16) {
 #pragma unroll
     for (int i = 0; i < (int)sizeof(x) / 16; ++i) ((u32x4 *)to)[i] = ((const u32x4 *)x)[i];
@@ -1166,14 +1167,15 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
       return from + row <= r1;
     };
     if (parts == 1) {
-      const float f = l == 0.f ? 0.f : 1.f / l;
+      const bool none = l == 0.f;                                // (as in store_row)
+      const float f = none ? 0.f : 1.f / l;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const int piece = 4 * d + i / 4;
           *(u32x2 *)(mine + col * W::ROW + (piece ^ (col % W::PIECES)) * 16 + 8 * h) =
-              u32x2{Mat<__bf16>::pack(o[d][i] * f, o[d][i + 1] * f), Mat<__bf16>::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
+              none ? u32x2{0, 0} : u32x2{Mat<__bf16>::pack(o[d][i] * f, o[d][i + 1] * f), Mat<__bf16>::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
         }
       __builtin_amdgcn_wave_barrier();
       u32x4 v[32 / W::PER];

@@ -1036,3 +1036,20 @@ def test_attention_of_the_widest_windows(kind, window, sinks, n, m, room):
     st.new, st.start = [max(n, 0), 2, 150], np.array([lost, m, m + 2, m + 152])
     want, tol = attention(st, q, window, sinks)
     check(got[lost:], want[lost:], tol[lost:])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("lens,new", [([300], [1]), ([20000], [1]), ([300], [5]), ([400], [290]), ([1500, 700], [200, 300])], ids=str)
+@pytest.mark.parametrize("room", [0, 20000])
+def test_attention_of_scores_of_minus_infinity_alone(kind, bad, hd, lens, new, room):
+    # keys that score -infinity count for nothing: a row that sees no others is zero, whatever their values are
+    st = Setup(kind, 1, hd, 16, lens, new, seed=41, room=room)
+    st.k[..., 0] = -math.inf
+    st.v[..., 3] = bad
+    q = torch.zeros(st.tokens, 4, hd, dtype=st.act, device=DEV)
+    q[..., 0] = 1.0
+    out = torch.full_like(q, 7.0)
+    B.river_paged_attention(st.pages, 0, st.batch, q, out=out)
+    assert bool((out == 0).all())
