@@ -592,6 +592,8 @@ def river_paged_attention(pages: Pages, layer: int, batch: Batch, q: torch.Tenso
     if nbytes is None:
         got = C.c_size_t()
         _check_call(L.river_paged_attention_workspace(pages.ref, ref, heads, window, sinks, C.byref(got)))
+        if len(batch._bytes) >= 256:
+            batch._bytes.clear()
         nbytes = batch._bytes[key] = got.value
     stream, ws, tickets = _stream(pages.index), None, None
     if nbytes:

@@ -1053,3 +1053,13 @@ def test_attention_of_scores_of_minus_infinity_alone(kind, bad, hd, lens, new, r
     out = torch.full_like(q, 7.0)
     B.river_paged_attention(st.pages, 0, st.batch, q, out=out)
     assert bool((out == 0).all())
+
+
+def test_a_batch_does_not_grow_with_its_calls():
+    # (what it remembers of shapes of calls is bounded, whatever the windows)
+    st = Setup("bf16", 1, 64, 16, [40, 9], [1, 1], seed=42, ragged=False)
+    q = st.randn(2, 4, 64)
+    for window in range(1, 700):
+        B.river_paged_attention(st.pages, 0, st.batch, q, window)
+    assert len(st.batch._bytes) <= 256 and len(st.batch._calls) <= 256
+    run_attention(st, 4, 7)
