@@ -1063,3 +1063,29 @@ def test_a_batch_does_not_grow_with_its_calls():
         B.river_paged_attention(st.pages, 0, st.batch, q, window)
     assert len(st.batch._bytes) <= 256 and len(st.batch._calls) <= 256
     run_attention(st, 4, 7)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_probabilities_of_single_tokens_are_more_than_their_type(kind, hd):
+    # Two keys of scores 0 and -d and values 1 and -1: o = tanh(d / 2).  Rounded to bf16 alone the second probability, 1 - d to the maximum's 1,
+    # would be off by up to 2^-9 (its numbers below 1 are 2^-8 apart), and o by half of that; as a sum of two such numbers it is off by
+    # 2^-17 at most, scores and exponentials by 2^-20 (the module's tolerance of a score: products of one term, and the instruction's)
+    st = Setup(kind, 1, hd, 16, [2] * 64, [1] * 64, seed=43, ragged=False)
+    st.k.zero_()
+    st.v.zero_()
+    d = (torch.arange(64, device=DEV, dtype=torch.float64) + 0.5) / 64 * 2.0 ** -7
+    q = torch.zeros(64, 1, hd, dtype=st.act, device=DEV)
+    q[:, 0, 0] = d.to(st.act)
+    d = q[:, 0, 0].double()
+    for s in range(64):
+        page = int(st.host[s, 0])
+        st.k[0, page, 0, 1, 0] = -1.0
+        st.v[0, page, 0, 0], st.v[0, page, 0, 1] = 1.0, -1.0
+    got = B.river_paged_attention(st.pages, 0, st.batch, q, scale=1.0).double()[:, 0]
+    want = torch.tanh(d / 2)[:, None].expand(64, hd)
+    tol = half_step(st.act) * want + 2.0 ** -17 + 2.0 ** -19
+    p = (-d).exp()
+    once = (1 - p.to(torch.bfloat16).double()) / (1 + p)
+    assert int(((once - want[:, 0]).abs() > tol[:, 0]).sum()) > 32        # (a single rounding would be seen)
+    check(got, want, tol)
