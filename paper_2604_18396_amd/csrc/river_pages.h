@@ -821,7 +821,8 @@ struct Many {
   static __device__ __forceinline__ int k_at(int row, int piece) { return row * ROW + (piece ^ k_swizzle(row)) * 16; }
   static __device__ __forceinline__ int v_at(int row, int piece) { return row * ROW + (piece ^ v_swizzle(row)) * 16; }
 };
-// 16 bytes a lane from memory to LDS, the lanes' one after the other from byte `lds` on.  Counts on vmcnt; no register is written.
+// 16 bytes a lane from memory to LDS, the lanes' one after the other from byte `lds` on.  Counts on vmcnt; no register is written but m0, which the
+// compiler keeps nothing in (it is reserved: it sets it in front of each use of its own, and takes no clobber of it).
 __device__ __forceinline__ void load_lds16(uint32_t lds, const void *from) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from));
 }
