@@ -59,9 +59,10 @@ __device__ __forceinline__ int position_of(const Batch &b, int s, int t) {
   return p < 0 ? -1 : (int)p;
 }
 
-// The same for new token i of a sequence with `count` of them: -1 if it has none, and no less, so that a window of up to 2^31 - 1
-// can be taken from it.
-__device__ __forceinline__ int new_position(int len, int count, int i) { return max(max(len, 0) - count + i, -1); }
+// The same from the sequence's length (length_of) for its new token i of `count`: -1 if it has none, and no less, so that a window of up
+// to 2^31 - 1 can be taken from it.
+__device__ __forceinline__ int length_of(const Batch &b, int s) { return max(b.lens[s], 0); }
+__device__ __forceinline__ int new_position(int len, int count, int i) { return max(len - count + i, -1); }
 
 // The page of position p (0 <= p) and the slot in it; -1: there is none.
 __device__ __forceinline__ int page_of(const Cache &c, const Batch &b, int s, int p, int &slot) {
@@ -292,7 +293,7 @@ __device__ __forceinline__ Span span_of(const Batch &b, const AttnArgs &a, int l
   return s;
 }
 __device__ __forceinline__ Sight sight_of(const AttnArgs &a, const Span &s, int p) {
-  return Sight{s.at(p), a.window ? max(0, s.at(p - a.window + 1)) : 0, max(s.hs, s.at(a.sinks))};
+  return Sight{s.at(p), a.window ? max(0, s.at(max(p, -1) - a.window + 1)) : 0, max(s.hs, s.at(a.sinks))};
 }
 // Splits of a tile that have keys, at least one; the last split of a launch takes what is left.
 __device__ __forceinline__ int splits_of(const AttnArgs &a, int n) { return min(a.n_splits, max(1, (n + a.split_len - 1) / a.split_len)); }
@@ -501,14 +502,14 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
   const int rows = min(count, a.max_new) * a.rep, r0 = tile * 16;
   if (r0 >= rows) return;
   const int r1 = min(r0 + 15, rows - 1);
-  const Span sp = span_of(b, a, b.lens[s], count, r0, r1);
+  const Span sp = span_of(b, a, length_of(b, s), count, r0, r1);
   const int parts = splits_of(a, sp.n);
   if (z >= parts) return;
   const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
 
   // this lane's row: its query in the order of the contraction, its position
   const int r = min(r0 + col, r1), tok = a.by_rep.quot(r), qh = head * a.rep + (r - tok * a.rep);
-  const int mypos = new_position(b.lens[s], count, tok);
+  const int mypos = new_position(length_of(b, s), count, tok);
   const T *qrow = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)qh * HD;
   u32x4 qf[NP];
   float sc = a.scale2;
@@ -855,7 +856,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   seq_tokens(b, s, first_token, count);
   const int rows = min(count, a.max_new) * a.rep, r0 = tile * W::ROWS;
   if (r0 >= rows) return;
-  const int r1 = min(r0 + W::ROWS - 1, rows - 1), len = b.lens[s];
+  const int r1 = min(r0 + W::ROWS - 1, rows - 1), len = length_of(b, s);
   const Span sp = span_of(b, a, len, count, r0, r1);
   const int parts = splits_of(a, sp.n);
   if (z >= parts) return;
@@ -865,7 +866,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
 
   // this wavefront's rows: rows behind the last repeat it
   const int w0 = min(r0 + wave * W::WROWS, r1), w1 = min(w0 + W::WROWS - 1, r1);
-  const int first = new_position(len, count, a.by_rep.quot(w0)), last = new_position(len, count, a.by_rep.quot(w1));
+  const int first = len - count + a.by_rep.quot(w0), last = len - count + a.by_rep.quot(w1);
   const int my_slot = lane % W::PIECES;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   // Their queries in the operand's order.  (Through LDS, in whole rows of memory, they take as long: 4500 cycles, on the way with
@@ -873,7 +874,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   u32x4 qf[KS];
   float sc = a.scale2;
   const int r = min(r0 + wave * W::WROWS + col, r1), tok = a.by_rep.quot(r);
-  const Sight sight = sight_of(a, sp, new_position(len, count, tok));
+  const Sight sight = sight_of(a, sp, len - count + tok);
   const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const u32x4 *)(q + (2 * ks + h) * 8);
@@ -942,7 +943,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   bool pend;
   // Steps of which every row of this wavefront sees every key (where all pages are there): their last key is at most all_to,
   // and their first is at least all_from or their last below all_sinks, by index in the split
-  const int all_to = sp.at(first) - i0, all_from = (a.window ? max(0, sp.at(last - a.window + 1)) : 0) - i0, all_sinks = sight.sinks - i0;
+  const int all_to = sp.at(first) - i0, all_from = (a.window ? max(0, sp.at(max(last, -1) - a.window + 1)) : 0) - i0, all_sinks = sight.sinks - i0;
 
   // Step n's scores as they count: what a row does not see is -infinity.  The maximum, where that moves it.
   auto settle = [&](int n, Scores &sx, uint32_t there_) {
@@ -1126,6 +1127,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
     }
     wait_and_meet<0>();                                          // (nothing may land in LDS behind the end)
     if (careful) {
+      // (a row whose scores here are all -infinity stays zero: see store_row)
+      const bool counts = l + __shfl_xor(l, 32) != 0.f;
       for (int i = i0; i < i1; ++i) {
         int slot;
         const int page = page_of(c, b, s, sp.pos(i), slot);
@@ -1136,7 +1139,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
 #pragma unroll
           for (int e4 = 0; e4 < 16; ++e4) {
             const float v = (float)row[d * 32 + 8 * (e4 / 4) + e4 % 4];
-            if ((sight.bits(i) & 1) && not_finite(v)) o[d][e4] += v;
+            if (counts && (sight.bits(i) & 1) && not_finite(v)) o[d][e4] += v;
           }
       }
       break;
@@ -1168,15 +1171,14 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
       return from + row <= r1;
     };
     if (parts == 1) {
-      const bool none = l == 0.f;                                // (as in store_row)
-      const float f = none ? 0.f : 1.f / l;
+      const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const int piece = 4 * d + i / 4;
           *(u32x2 *)(mine + col * W::ROW + (piece ^ (col % W::PIECES)) * 16 + 8 * h) =
-              none ? u32x2{0, 0} : u32x2{Mat<__bf16>::pack(o[d][i] * f, o[d][i + 1] * f), Mat<__bf16>::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
+              u32x2{Mat<__bf16>::pack(o[d][i] * f, o[d][i + 1] * f), Mat<__bf16>::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
         }
       __builtin_amdgcn_wave_barrier();
       u32x4 v[32 / W::PER];
@@ -1222,7 +1224,7 @@ __device__ __forceinline__ int parts_of(const Batch &b, const AttnArgs &a, long 
   if (i >= count) return 0;
   const int r = i * a.rep + h % a.rep, r0 = r - r % a.tile_rows;
   out = (long long)(first + i) * a.out_stride + (long long)h * head_dim;
-  return splits_of(a, span_of(b, a, b.lens[s], count, r0, min(r0 + a.tile_rows, min(count, a.max_new) * a.rep) - 1).n);
+  return splits_of(a, span_of(b, a, length_of(b, s), count, r0, min(r0 + a.tile_rows, min(count, a.max_new) * a.rep) - 1).n);
 }
 
 // Few splits joined in a launch of their own: bit for bit what the last workgroup of k_attn_split does.  Bound: latency (4 us).
