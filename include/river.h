@@ -300,9 +300,9 @@ typedef struct {
   const int32_t *q_start; /* [n_seq + 1], or NULL: one token each (n_tokens == n_seq) */
   int32_t n_seq, n_tokens;
   int32_t max_pages, table_stride;
-  int32_t max_new;        /* no sequence has more new tokens (further ones would be left out) */
-  int32_t max_len;        /* no sequence has more positions: by this the work is divided (longer ones are
-                             still right, but slow) */
+  int32_t max_new;        /* no sequence has more new tokens (further ones are left out of the attention) */
+  int32_t max_len;        /* no sequence has more positions: by these two the attention's work is divided.  Sequences longer
+                             than max_len, and bounds far above what is there, are still right, but slow */
 } river_batch;
 
 /* Rotary positions: the first rot_dim elements of a head are pairs (x, y) that position p turns by
@@ -327,7 +327,7 @@ typedef struct {
  *   RAMP    by index: f_i (1-t) + f_i/factor t with t = clamp((i - a)/(b - a), 0, 1), a and b the indices
  *           rot_dim ln(original_len / (2 pi n)) / (2 ln base) for n = high (rounded down, not below 0) and n = low (rounded up,
  *           not above rot_dim - 1; b - a at least 0.001); *mscale = 0.1 ln(factor) + 1
- * factor >= 1; low < high are numbers of turns.  PLAIN ignores factor and what follows it, LINEAR and BASE what
+ * factor >= 1; low < high are numbers of turns (models have 1 and 4 for BANDS, 1 and 32 for RAMP).  PLAIN ignores factor and what follows it, LINEAR and BASE what
  * follows factor.  inv_freq: HOST [rot_dim/2].  mscale: HOST, nullable (1 but for RAMP). */
 enum { RIVER_ROPE_PLAIN = 0, RIVER_ROPE_LINEAR = 1, RIVER_ROPE_BASE = 2, RIVER_ROPE_BANDS = 3, RIVER_ROPE_RAMP = 4 };
 int river_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
@@ -346,12 +346,14 @@ int river_rope_store(const river_pages *pages, int32_t layer, const river_batch 
 /* Attention of the new tokens over their sequences' pages of `layer` (the new positions' rows among them:
  * river_rope_store comes first).  A token at position p sees j <= p; with window > 0 of these only
  * j > p - window, and j < sinks.  out = sum_j softmax_j(scale q.k_j) v_j; a row that sees nothing, or only scores of
- * -infinity, is zero.  What is not seen has no influence, whatever its bits (NaN, infinities).
+ * -infinity, is zero, whatever its values.  What is not seen has no influence, whatever its bits (NaN, infinities).
  * Query heads h * (n_q_heads / n_kv_heads) .. share key head h.
- * scale: > 0, or 0 = 1/sqrt(head_dim).  window: 0 = none.  sinks: used with a window only.
+ * scale: > 0, or 0 = 1/sqrt(head_dim).  window: 0 = none, at most 2^31 - 1.  sinks: used with a window only.
  * q, out: DEVICE [n_tokens][n_q_heads][head_dim], pages->dtype, strides in elements, multiples of 16 bytes, 16-byte aligned;
  * out must not overlap q.  At most 2^22 tokens and sequences a call (river_rope_store too), and fewer than
  * 2^28 tokens x heads.
+ * Scores, maxima and sums are fp32.  What values are multiplied with is rounded: probabilities to 2^-17 of themselves over bf16 pages,
+ * but to bf16 where a sequence has many new tokens, and to half over half pages (bf16 queries too, scaled by row); fp32 pages: none.
  * workspace: DEVICE, 16-byte aligned, of at least the bytes that river_paged_attention_workspace gives for the
  * same arguments (0 bytes: may be NULL); its contents mean nothing before and after the call.
  * tickets: DEVICE int32 [RIVER_TICKETS], 4-byte aligned, or NULL.  All zero before the first call that has them and left zero by every call;
@@ -400,7 +402,8 @@ int river_pool_row(const river_pool *pool, int32_t seq, int32_t *row); /* HOST [
 
 /* Copies positions first .. first + n - 1 of a context's sequence, in all layers, to the pages that `row` (DEVICE
  * [max_pages]) names, rotated keys as the context keeps them; the pages' shape and types must be the context's.  A prompt that
- * was prefilled once can then be given to other sequences and contexts with river_load_pages.  Runs on the context's stream. */
+ * was prefilled once can then be given to other sequences and contexts with river_load_pages.  Runs on the context's stream: pages and
+ * row must be written before it comes to the call, and be left alone until it is behind it. */
 int river_save_pages(river_ctx *ctx, int32_t seq, int32_t first, int32_t n, const river_pages *pages,
                      const int32_t *row, int32_t max_pages);
 /* The reverse: positions 0 .. n - 1 of sequence seq come from pages, and the sequence has n positions afterwards,

@@ -405,7 +405,7 @@ __device__ __forceinline__ void store_row(T *to, const float (&v)[E], float sum)
 // lanes of a row asked and O rescaled.  P^T is then in the order that O^T += V^T P^T wants its right operand in; V^T comes out of
 // the wavefront's own LDS, whose transposing read gives a lane four keys of one element.
 // LDS pieces lie in an order by row (swizzle), so that neither side meets in one bank.
-// 8B shape: one sequence of 131071 positions, 537 MB, 93 us, 5.8 TB/s (a read alone reaches 6.8; two workgroups a CU, 185 registers:
+// 8B shape: one sequence of 131071 positions, 537 MB, 93 us, 5.8 TB/s (a read alone reaches 6.8; two workgroups a CU, all 256 registers of a lane:
 // steps of 16 keys and three workgroups are 1 % faster there and 18 % slower for 16 sequences of 1200); 32 sequences of up to 4096 76 us,
 // 4.6 TB/s, what is missing there is that sequences differ; one of 512 8.1 us, of which the keys are 1: start, length, entries, rows,
 // tickets, partial results one after the other.  fp32 prompts: 68 TFLOP/s of 135, the L2's rate for keys that every 16 rows read again.
@@ -788,8 +788,8 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)
 //
-// Bound: the matrix cores and the vector instructions (exponentials above all) about alike, 48 % and 49 % of a SIMD's cycles, and the
-// clock that the power limit leaves, 1.6 .. 2.1 GHz.  A wavefront holds 32 rows in fewer than 256 registers, all of them general ones,
+// Bound: the matrix cores and the vector instructions (exponentials above all) about alike, 48 % and 49 % of a SIMD's cycles, neither of them
+// full: its wavefronts wait for a quarter to a third of theirs.  The clock is 1.84 .. 2.07 GHz meanwhile (a decode call's 2.44 .. 2.57).  A wavefront holds 32 rows in fewer than 256 registers, all of them general ones,
 // so that two workgroups of 128 rows are on a CU (three at head size 64, whose few spilled registers lie outside the steps: 4096
 // tokens 114 / 98 us) and one's waits, beginning and end lie beside the other's products.  (64 rows a
 // wavefront, one to a SIMD, read LDS half as often, but nothing runs beside their waits: us, 64 rows / 32 rows, 8B shape: 4096 tokens
@@ -799,9 +799,11 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 // of S(n), and adds P(n-1) V, three things that do not depend on each other.
 // O is therefore rescaled one step after the maximum has moved (pend); it moves when a score is 2^kLazy times as likely as
 // what was the maximum (one of 32 rows has a new maximum in most steps, and rescaling takes half as long as the step).
+// A probability is rounded once to the pages' type, and the sum is of what is multiplied: over bf16 pages that leaves out up to half a step of the
+// result (4096 tokens: off by 2.1e-3 of the norm, 1.6e-3 with fp32 ones); a second product, as in k_attn_split, would cost a third of the time.
 // Keys and values go from memory straight into LDS (no registers, AHEAD steps in flight), in rings, one barrier a step; where a key's
 // row lies is looked up for CHUNK steps at once.
-// 8B shape, 4096 tokens: 148 .. 153 us, 900 .. 930 TFLOP/s; 2048 behind 16384 615 us, 950; the largest matrix products of the library reach 1250.
+// 8B shape, 4096 tokens: 148 .. 158 us by the box, 870 .. 930 TFLOP/s; 2048 behind 16384 615 us, 950; the largest matrix products of the library reach 1250.
 template <class C, int HD>
 struct Many {
   typedef Mat<C> M;

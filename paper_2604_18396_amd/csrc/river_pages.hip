@@ -230,7 +230,8 @@ struct AttnPlan {
 // takes longer to begin and end (us, k_attn_many / k_attn_split; 8B shape: 256 new tokens behind none 12.2 / 11.3, 32 behind 1024
 // 18.4 / 21.5, 16 behind 4096 18.9 / 22.8, 8 behind 65536 56 / 104; eight sequences, 8 behind 2048 31.9 / 29.0; sixteen, 16 behind 512
 // 22.2 / 24.2; 1B shape: 512 behind none 15.6 / 15.8, 32 behind 4096 17.0 / 17.3, 64 behind 4096 22.8 / 29.9, 8 behind 65536 39.5 / 47.4;
-// sixteen, 16 behind 512 16.3 / 14.8, 32 behind 512 19.3 / 21.0)
+// sixteen, 16 behind 512 16.3 / 14.8, 32 behind 512 19.3 / 21.0.  One product does not part all of these: 256 behind none and eight sequences
+// of 8 behind 2048 lie above the limit and are 8 .. 10 % slower there)
 constexpr int kSplitRows = 16;
 static double many_work(int head_dim) { return head_dim == 128 ? 1.3e8 : 3e8; }
 // Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a

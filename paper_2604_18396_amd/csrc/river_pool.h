@@ -23,7 +23,7 @@ struct river_pool {
       : n_pages(pages), page_size(size), max_seqs(seqs), max_pages(per_seq), refs(pages, 0), free_heap(pages), len(seqs, 0),
         table((size_t)seqs * per_seq, -1), is_dirty((size_t)seqs * (per_seq + 1), 0) {
     for (int i = 0; i < pages; ++i) free_heap[i] = i;            // (ascending: a heap)
-    // nothing below allocates: a queue that has no room is an error before anything changes (see room)
+    // nothing below allocates: a queue that has no room is an error before anything changes (extend, compact)
     dirty.reserve(is_dirty.size());
   }
   int *row(int s) { return table.data() + (size_t)s * max_pages; }
