@@ -9,8 +9,8 @@ ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "river.hip")
 # one object per source, river.hip's code object first in the library
 SOURCES = [SRC, os.path.join(HERE, "csrc", "river_pages.hip")]
-DEPS = [*SOURCES, *(os.path.join(HERE, "csrc", h) for h in ("river_device.h", "river_prefill.h", "river_host.h", "river_pages.h",
-                                                            "river_pool.h")),
+DEPS = [*SOURCES, *(os.path.join(HERE, "csrc", h) for h in ("river_copies.h", "river_device.h", "river_prefill.h", "river_host.h", "river_pages.h",
+                                                            "river_pages_host.h", "river_pool.h")),
         os.path.join(ROOT, "include", "river.h")]
 LIB = os.path.join(HERE, "libriver.so")
 

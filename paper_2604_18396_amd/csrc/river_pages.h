@@ -1,5 +1,5 @@
 // Device code of the paged key-value cache (gfx950): rotary positions with the store into the pages, attention over
-// the pages, page copies.
+// the pages.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -305,13 +305,37 @@ __device__ __forceinline__ int splits_of(const AttnArgs &a, int n) { return min(
 // (2^turn rounds): else the longest of four sequences has one engine in four, and the empty tiles and splits of short ones leave the
 // others idle (8B shape, us, without / with: prompts of 2048, 2015, 551 and 513 tokens 181 / 122, of eight of 366 .. 1024 81 / 64, single
 // tokens of 32 sequences of 1024 .. 4096 82 / 77).
-__device__ __forceinline__ void work_of(const Cache &c, const Batch &b, const AttnArgs &a, int &tile, int &s, int &z, int &head) {
-  const unsigned u = blockIdx.x / c.n_kv_heads, v = u / a.n_splits, t = v / b.n_seq;
-  head = blockIdx.x % c.n_kv_heads;
+__device__ __forceinline__ void work_of(unsigned group, const Cache &c, const Batch &b, const AttnArgs &a, int &tile, int &s, int &z, int &head) {
+  const unsigned u = group / c.n_kv_heads, v = u / a.n_splits, t = v / b.n_seq;
+  head = group % c.n_kv_heads;
   z = (u + (v >> a.turn_z)) % a.n_splits;
   s = (v + (t >> a.turn_s)) % b.n_seq;
   tile = a.tiles - 1 - t;
 }
+
+// What a workgroup of an attention kernel works on: rows r0 .. r1 (counted from the first token on, see above) and the keys
+// i0 .. i1 - 1 of their span, under one key head.
+// Keys: entry(p, i) is the table's entry i, which has position p.  Rows: position(i) is that of token first_token + i; reach(i, j, ..)
+// are the lowest and the highest of tokens i .. j (of a wavefront's rows, in k_attn_many).
+struct OneRow {
+  const int *row;
+  __device__ __forceinline__ int entry(int, int i) const { return row[i]; }
+};
+struct OfSequence {
+  int len, count;
+  __device__ __forceinline__ int position(int i) const { return new_position(len, count, i); }
+  __device__ __forceinline__ void reach(int i, int j, int &first, int &last) const { first = position(i); last = position(j); }
+};
+template <class Keys, class Rows>
+struct Unit {
+  Keys keys;
+  Rows rows;
+  Span sp;
+  int i0, i1, r0, r1, first_token, head;
+  int n_parts, part;                      // partial results of a row, and which this one is
+  long long row0;                         // the first token's place among them
+  bool whole;                             // no other part: the result is the output
+};
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -478,39 +502,31 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, long long first_pa
   }
 }
 
-template <class T, class C, int HD>
-__global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
+// Elements of a row that a thread of the joins has, and threads of a row
+template <int HD>
+struct RowPart {
+  static constexpr int E = HD * 16 / kAttnThreads > 4 ? HD * 16 / kAttnThreads : 4, LANES = HD / E;
+};
+
+// One unit of 16 rows at most: its result in the output, or as a part of it.  early: the entries of the first two steps' keys, where
+// have_early.  lds: kAttnWaves areas.  v: what thread t has of row t / LANES (see RowPart).
+template <class C, int HD>
+struct SplitLds {
+  static constexpr int AREA = Tile<C, HD>::LDS > 64 * HD ? Tile<C, HD>::LDS : 64 * HD;     // of a wavefront: its values, then its result
+};
+template <class T, class C, int HD, class Keys, class Rows>
+__device__ __forceinline__ void split_unit(const Cache &c, const AttnArgs &a, const Unit<Keys, Rows> &w, char *lds, float2 (*res_ml)[16],
+                                           bool have_early, const int (&early)[2][Tile<C, HD>::KB], float (&v)[RowPart<HD>::E]) {
   typedef Tile<C, HD> W;
   typedef Mat<C> M;
-  constexpr int KB = W::KB, NP = W::NP, ND = W::ND, PER = W::PER;
-  constexpr int AREA = W::LDS > 64 * HD ? W::LDS : 64 * HD;     // of a wavefront: its values, then its result
-  __shared__ __align__(16) char lds[kAttnWaves * AREA];
-  __shared__ float2 res_ml[kAttnWaves][16];
-  int tile, s, z, head;
-  work_of(c, b, a, tile, s, z, head);
+  constexpr int KB = W::KB, NP = W::NP, ND = W::ND, PER = W::PER, AREA = SplitLds<C, HD>::AREA;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
-  // Without a window the first steps' keys do not depend on the length: their entries come with it, not behind it
-  int early[2][KB];
-#pragma unroll
-  for (int it = 0; it < 2; ++it)
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      early[it][kb] = b.table[(long long)s * b.table_stride +
-                              min(c.by_page.quot(z * a.split_len + (it * kAttnWaves + wave) * M::kKeys + kb * 16 + col), b.max_pages - 1)];
-  int first_token, count;
-  seq_tokens(b, s, first_token, count);
-  const int rows = min(count, a.max_new) * a.rep, r0 = tile * 16;
-  if (r0 >= rows) return;
-  const int r1 = min(r0 + 15, rows - 1);
-  const Span sp = span_of(b, a, length_of(b, s), count, r0, r1);
-  const int parts = splits_of(a, sp.n);
-  if (z >= parts) return;
-  const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
-
+  const Span &sp = w.sp;
+  const int i0 = w.i0, i1 = w.i1, r0 = w.r0, r1 = w.r1;
   // this lane's row: its query in the order of the contraction, its position
-  const int r = min(r0 + col, r1), tok = a.by_rep.quot(r), qh = head * a.rep + (r - tok * a.rep);
-  const int mypos = new_position(length_of(b, s), count, tok);
-  const T *qrow = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)qh * HD;
+  const int r = min(r0 + col, r1), tok = a.by_rep.quot(r), qh = w.head * a.rep + (r - tok * a.rep);
+  const int mypos = w.rows.position(tok);
+  const T *qrow = (const T *)a.q + (long long)(w.first_token + tok) * a.q_stride + (long long)qh * HD;
   u32x4 qf[NP];
   float sc = a.scale2;
   if constexpr (sizeof(T) == sizeof(C) && !(sizeof(C) == 2 && M::kBias != 0.f)) {
@@ -519,25 +535,25 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
   } else {
     // bf16 queries over fp16 pages: a row is divided by a power of two so that its largest element is below 2 (what
     // gets below fp16's numbers is below 2^-24 of that), which goes into the row's scale
-    u32x4 w[NP];
-    float big = 0.f;
+    u32x4 qw[NP];
+    float most = 0.f;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-      w[j] = *(const u32x4 *)(qrow + (g + 4 * j) * PER);
+      qw[j] = *(const u32x4 *)(qrow + (g + 4 * j) * PER);
       for (int e = 0; e < 4; ++e)
-        big = fmaxf(big, fmaxf(fabsf(Mat<__bf16>::low(w[j][e])), fabsf(Mat<__bf16>::high(w[j][e]))));
+        most = fmaxf(most, fmaxf(fabsf(Mat<__bf16>::low(qw[j][e])), fabsf(Mat<__bf16>::high(qw[j][e]))));
     }
-    big = fmaxf(big, __shfl_xor(big, 16));
-    big = fmaxf(big, __shfl_xor(big, 32));
-    const int ex = big > 0.f && !not_finite(big) ? ilogbf(big) : 0;
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const int ex = most > 0.f && !not_finite(most) ? ilogbf(most) : 0;
     sc = ldexpf(sc, ex);
 #pragma unroll
     for (int j = 0; j < NP; ++j)
       for (int e = 0; e < 4; ++e)
-        qf[j][e] = M::pack(ldexpf(Mat<__bf16>::low(w[j][e]), -ex), ldexpf(Mat<__bf16>::high(w[j][e]), -ex));
+        qf[j][e] = M::pack(ldexpf(Mat<__bf16>::low(qw[j][e]), -ex), ldexpf(Mat<__bf16>::high(qw[j][e]), -ex));
   }
 
-  const C *kp = (const C *)c.k + (long long)head * c.page_size * HD, *vp = (const C *)c.v + (long long)head * c.page_size * HD;
+  const C *kp = (const C *)c.k + (long long)w.head * c.page_size * HD, *vp = (const C *)c.v + (long long)w.head * c.page_size * HD;
   char *mine = lds + wave * AREA;
   f32x4 o[ND];
   float m, l;
@@ -547,8 +563,10 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
   auto key_of = [&](int it, int kb) { return i0 + (it * kAttnWaves + wave) * M::kKeys + kb * 16 + col; };
   auto entries = [&](int it, int (&e)[KB]) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      e[kb] = b.table[(long long)s * b.table_stride + c.by_page.quot(sp.pos(min(key_of(it, kb), i1 - 1)))];
+    for (int kb = 0; kb < KB; ++kb) {
+      const int p = sp.pos(min(key_of(it, kb), i1 - 1));
+      e[kb] = w.keys.entry(p, c.by_page.quot(p));
+    }
   };
   // Rows without a page, or behind the split's end, are page 0's first (any memory of the cache will do)
   auto fetch = [&](int it, const int (&e)[KB], typename W::Data &d, uint32_t &there) {
@@ -700,7 +718,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
     int e[KB], e1[KB];
     typename W::Data d, d1;
     uint32_t there, there1;
-    if (a.window) {
+    if (!have_early) {
       entries(0, e);
       entries(1, e1);
     } else {
@@ -736,42 +754,73 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
   for (int t = 0; t < ND; ++t) *(f32x4 *)(res + wave * LD + res_at<HD>(col, 4 * t + g)) = o[t];
   if (g == 0) res_ml[wave][col] = make_float2(m, l);
   __syncthreads();
-  constexpr int E = HD * 16 / kAttnThreads > 4 ? HD * 16 / kAttnThreads : 4, LANES = HD / E;   // elements of a thread, threads of a row
+  constexpr int E = RowPart<HD>::E, LANES = RowPart<HD>::LANES;
   const int row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
   static_assert(16 * LANES == kAttnThreads, "every thread has a part of a row");
-  const bool have = r0 + row <= r1;
-  float big = -INFINITY, sum = 0.f, v[E];
+  float big = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int w = 0; w < kAttnWaves; ++w) big = fmaxf(big, res_ml[w][row].x);
+  for (int i = 0; i < kAttnWaves; ++i) big = fmaxf(big, res_ml[i][row].x);
 #pragma unroll
   for (int e = 0; e < E; ++e) v[e] = 0.f;
 #pragma unroll
-  for (int w = 0; w < kAttnWaves; ++w) {
-    const float2 ml = res_ml[w][row];
+  for (int i = 0; i < kAttnWaves; ++i) {
+    const float2 ml = res_ml[i][row];
     const float f = big == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - big);
     sum += f * ml.y;
 #pragma unroll
     for (int e = 0; e < E; e += 4) {
-      const f32x4 x4 = *(const f32x4 *)(res + w * LD + res_at<HD>(row, (e0 + e) / 4));
+      const f32x4 x4 = *(const f32x4 *)(res + i * LD + res_at<HD>(row, (e0 + e) / 4));
 #pragma unroll
       for (int n = 0; n < 4; ++n) v[e + n] += f * x4[n];
     }
   }
-  const int to = a.by_rep.quot(min(r0 + row, r1)), oh = head * a.rep + (min(r0 + row, r1) - to * a.rep);
-  const long long t = first_token + to;
+  const int to = a.by_rep.quot(min(r0 + row, r1)), oh = w.head * a.rep + (min(r0 + row, r1) - to * a.rep);
+  const long long t = w.first_token + to;
   T *const out = (T *)a.out + t * a.out_stride + (long long)oh * HD + e0;
-  if (parts == 1) {
+  const bool have = r0 + row <= r1;
+  if (w.whole) {
     if (have) store_row<T, E>(out, v, sum);
     return;
   }
   // Parts cross XCDs, whose L2s are not coherent: they are written through and read past the L2, eight bytes at a time
-  const long long first_part = (((long long)s * a.max_new + to) * a.nq + oh) * a.n_splits;
   if (have) {
+    const long long part = ((w.row0 + to) * a.nq + oh) * w.n_parts + w.part;
 #pragma unroll
-    for (int e = 0; e < E; e += 2) put_through(a.part_o + (first_part + z) * HD + e0 + e, v[e], v[e + 1]);
-    if (e0 == 0) put_through((float *)(a.part_ml + first_part + z), big, sum);
+    for (int e = 0; e < E; e += 2) put_through(a.part_o + part * HD + e0 + e, v[e], v[e + 1]);
+    if (e0 == 0) put_through((float *)(a.part_ml + part), big, sum);
   }
-  if (!a.tickets) return;
+}
+
+template <class T, class C, int HD>
+__global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
+  typedef Mat<C> M;
+  constexpr int KB = Tile<C, HD>::KB, E = RowPart<HD>::E, LANES = RowPart<HD>::LANES;
+  __shared__ __align__(16) char lds[kAttnWaves * SplitLds<C, HD>::AREA];
+  __shared__ float2 res_ml[kAttnWaves][16];
+  int tile, s, z, head;
+  work_of(blockIdx.x, c, b, a, tile, s, z, head);
+  const int *const row_of_table = b.table + (long long)s * b.table_stride;
+  // Without a window the first steps' keys do not depend on the length: their entries come with it, not behind it
+  int early[2][KB];
+#pragma unroll
+  for (int it = 0; it < 2; ++it)
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      early[it][kb] = row_of_table[min(c.by_page.quot(z * a.split_len + (it * kAttnWaves + (int)threadIdx.x / 64) * M::kKeys + kb * 16 + (int)threadIdx.x % 16),
+                                       b.max_pages - 1)];
+  int first_token, count;
+  seq_tokens(b, s, first_token, count);
+  const int rows = min(count, a.max_new) * a.rep, r0 = tile * 16;
+  if (r0 >= rows) return;
+  const int r1 = min(r0 + 15, rows - 1), len = length_of(b, s);
+  const Span sp = span_of(b, a, len, count, r0, r1);
+  const int parts = splits_of(a, sp.n);
+  if (z >= parts) return;
+  const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
+  const Unit<OneRow, OfSequence> w{{row_of_table}, {len, count}, sp, i0, i1, r0, r1, first_token, head, a.n_splits, z, (long long)s * a.max_new, parts == 1};
+  float v[E];
+  split_unit<T, C, HD>(c, a, w, lds, res_ml, !a.window, early, v);
+  if (parts == 1 || !a.tickets) return;
   // The last workgroup of the tile joins the parts, in their order
   __shared__ unsigned int order;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -781,9 +830,12 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
   __syncthreads();
   if (order != (unsigned)parts - 1) return;
   if (threadIdx.x == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  if (!have) return;
-  join_parts<HD, E>(a, first_part, parts, e0, v, sum);
-  store_row<T, E>(out, v, sum);
+  const int row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
+  if (r0 + row > r1) return;
+  const int to = a.by_rep.quot(r0 + row), oh = head * a.rep + (r0 + row - to * a.rep);
+  float sum;
+  join_parts<HD, E>(a, ((w.row0 + to) * a.nq + oh) * a.n_splits, parts, e0, v, sum);
+  store_row<T, E>((T *)a.out + (long long)(first_token + to) * a.out_stride + (long long)oh * HD + e0, v, sum);
 }
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)
@@ -833,7 +885,7 @@ template <int N>
 __device__ __forceinline__ void wait_and_meet() {        // all but the last N loads done, by every wavefront
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
-__device__ const u32x4 g_zero_row[16] = {};
+static __device__ const u32x4 g_zero_row[16] = {};
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <class C>
 __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
@@ -842,33 +894,25 @@ __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
   else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
 }
 
-template <class T, class C, int HD>
-__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Batch b, AttnArgs a) {
+// One unit of 128 rows at most: its result in the output, or as a part of it.
+template <class T, class C, int HD, class Keys, class Rows>
+__device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, const Unit<Keys, Rows> &w, char *lds) {
   typedef Many<C, HD> W;
   typedef Mat<C> M;
   constexpr int KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
-  extern __shared__ __align__(1024) char lds[];
   char *const vlds = lds + W::V;
   typedef unsigned long long Place __attribute__((ext_vector_type(2)));
   Place *const places = (Place *)(lds + W::PLACES);
   uint32_t *const there_of = (uint32_t *)(lds + W::THERE);
-  int tile, s, z, head;
-  work_of(c, b, a, tile, s, z, head);
-  int first_token, count;
-  seq_tokens(b, s, first_token, count);
-  const int rows = min(count, a.max_new) * a.rep, r0 = tile * W::ROWS;
-  if (r0 >= rows) return;
-  const int r1 = min(r0 + W::ROWS - 1, rows - 1), len = length_of(b, s);
-  const Span sp = span_of(b, a, len, count, r0, r1);
-  const int parts = splits_of(a, sp.n);
-  if (z >= parts) return;
-  const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
+  const Span &sp = w.sp;
+  const int i0 = w.i0, i1 = w.i1, r0 = w.r0, r1 = w.r1, head = w.head;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, h = lane / 32;
   const int steps = (i1 - i0 + KEYS - 1) / KEYS;
 
   // this wavefront's rows: rows behind the last repeat it
   const int w0 = min(r0 + wave * W::WROWS, r1), w1 = min(w0 + W::WROWS - 1, r1);
-  const int first = len - count + a.by_rep.quot(w0), last = len - count + a.by_rep.quot(w1);
+  int first, last;                                       // positions of their first and last token
+  w.rows.reach(a.by_rep.quot(w0), a.by_rep.quot(w1), first, last);
   const int my_slot = lane % W::PIECES;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   // Their queries in the operand's order.  (Through LDS, in whole rows of memory, they take as long: 4500 cycles, on the way with
@@ -876,8 +920,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   u32x4 qf[KS];
   float sc = a.scale2;
   const int r = min(r0 + wave * W::WROWS + col, r1), tok = a.by_rep.quot(r);
-  const Sight sight = sight_of(a, sp, len - count + tok);
-  const T *q = (const T *)a.q + (long long)(first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
+  const Sight sight = sight_of(a, sp, w.rows.position(tok));
+  const T *q = (const T *)a.q + (long long)(w.first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const u32x4 *)(q + (2 * ks + h) * 8);
   auto queries = [&] {
@@ -899,7 +943,6 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   };
 
   const u32x4 *kp = (const u32x4 *)((const C *)c.k + (long long)head * c.page_size * HD), *vp = (const u32x4 *)((const C *)c.v + (long long)head * c.page_size * HD);
-  const int *row_of_table = b.table + (long long)s * b.table_stride;
   constexpr int CK = W::CHUNK * KEYS;
   // Where the rows of CHUNK steps lie, and a bit a key.  What has no row (no page, behind the end): keys of page 0, which no
   // score counts, and values of zeros, whatever the bits of the cache there
@@ -907,7 +950,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
 #pragma unroll
     for (int j = 0; j < CK / 256; ++j) {
       const int k = j * 256 + (int)threadIdx.x, i = chunk * CK + k, p = sp.pos(min(i0 + i, i1 - 1)), page = c.by_page.quot(p);
-      const int e = row_of_table[page];
+      const int e = w.keys.entry(p, page);
       const bool ok = i0 + i < i1 && (unsigned)e < (unsigned)c.n_pages;
       const unsigned long long at = (unsigned long long)(uint32_t)e * c.page_pieces + (uint32_t)((p - page * c.page_size) * W::PIECES);
       places[(chunk & 1) * CK + k] = Place{(uintptr_t)(kp + (ok ? at : 0)), (uintptr_t)(ok ? vp + at : g_zero_row)};
@@ -1132,10 +1175,9 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
       // (a row whose scores here are all -infinity stays zero: see store_row)
       const bool counts = l + __shfl_xor(l, 32) != 0.f;
       for (int i = i0; i < i1; ++i) {
-        int slot;
-        const int page = page_of(c, b, s, sp.pos(i), slot);
-        if (page < 0) continue;
-        const C *row = (const C *)vp + (long long)page * c.page_stride + (long long)slot * HD + 4 * h;
+        const int p = sp.pos(i), at = c.by_page.quot(p), page = w.keys.entry(p, at);
+        if ((unsigned)page >= (unsigned)c.n_pages) continue;
+        const C *row = (const C *)vp + (long long)page * c.page_stride + (long long)(p - at * c.page_size) * HD + 4 * h;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -1160,7 +1202,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   }
 
   // Results.  A lane has four neighbouring elements of its row at a time: they go through this wavefront's part of LDS, pieces of 16 bytes in an order by row, so that memory gets whole rows.
-  char *const mine = lds + wave * (W::STAGE * (parts == 1 ? 1 : 2));
+  char *const mine = lds + wave * (W::STAGE * (w.whole ? 1 : 2));
   l += __shfl_xor(l, 32);
   const int from = r0 + wave * W::WROWS;                         // this wavefront's first row
   if (from <= r1) {
@@ -1172,7 +1214,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
       qh = head * a.rep + r - tok * a.rep;
       return from + row <= r1;
     };
-    if (parts == 1) {
+    if (w.whole) {
       const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
@@ -1192,7 +1234,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
 #pragma unroll
       for (int j = 0; j < 32 / W::PER; ++j)
         if (place(j * W::PER + lane / W::PIECES))
-          *(u32x4 *)((T *)a.out + (long long)(first_token + tok) * a.out_stride + (long long)qh * HD + my_slot * 8) = v[j];
+          *(u32x4 *)((T *)a.out + (long long)(w.first_token + tok) * a.out_stride + (long long)qh * HD + my_slot * 8) = v[j];
     } else {
       constexpr int P = 2 * W::PIECES;                           // fp32: twice as many pieces
 #pragma unroll
@@ -1207,13 +1249,31 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
       for (int j = 0; j < 32 * P / 64; ++j) {
         const int row = j * (64 / P) + lane / P, piece = lane % P;
         const f32x4 v = *(const f32x4 *)(mine + row * (2 * W::ROW) + (piece ^ (row % P)) * 16);
-        if (place(row)) *(f32x4 *)(a.part_o + ((((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z) * HD + piece * 4) = v;
+        if (place(row)) *(f32x4 *)(a.part_o + (((w.row0 + tok) * a.nq + qh) * w.n_parts + w.part) * HD + piece * 4) = v;
       }
       // (maxima in base 2, as k_attn_split has them)
       if (h == 0 && place(col))
-        a.part_ml[(((long long)s * a.max_new + tok) * a.nq + qh) * a.n_splits + z] = make_float2(m == -INFINITY ? -INFINITY : off + M::kLazyBias, l);
+        a.part_ml[((w.row0 + tok) * a.nq + qh) * w.n_parts + w.part] = make_float2(m == -INFINITY ? -INFINITY : off + M::kLazyBias, l);
     }
   }
+}
+
+template <class T, class C, int HD>
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Batch b, AttnArgs a) {
+  extern __shared__ __align__(1024) char lds[];
+  int tile, s, z, head;
+  work_of(blockIdx.x, c, b, a, tile, s, z, head);
+  int first_token, count;
+  seq_tokens(b, s, first_token, count);
+  const int rows = min(count, a.max_new) * a.rep, r0 = tile * Many<C, HD>::ROWS;
+  if (r0 >= rows) return;
+  const int r1 = min(r0 + Many<C, HD>::ROWS - 1, rows - 1), len = length_of(b, s);
+  const Span sp = span_of(b, a, len, count, r0, r1);
+  const int parts = splits_of(a, sp.n);
+  if (z >= parts) return;
+  const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
+  many_unit<T, C, HD>(c, a, Unit<OneRow, OfSequence>{{b.table + (long long)s * b.table_stride}, {len, count}, sp, i0, i1, r0, r1, first_token, head,
+                                                     a.n_splits, z, (long long)s * a.max_new, parts == 1}, lds);
 }
 
 // Row w of the partial results: head h of new token i of sequence s.  Its number of splits (0: no row, 1: it is done already), and its
@@ -1282,52 +1342,6 @@ __global__ __launch_bounds__(256) void k_attn_join_many(Batch b, AttnArgs a) {
   for (int i = 1; i < 4; ++i) { v += part[i][lane]; sum += part_sum[i]; }
   const float x[4] = {v[0], v[1], v[2], v[3]};
   store_row<T, 4>((T *)a.out + out + e0, x, sum);
-}
-
-// ------------------------------------------------------------------ copies
-
-constexpr int kPairs = 448;               // of a launch: they travel as kernel arguments (below 4 KiB)
-struct Pairs { int src[kPairs], dst[kPairs]; };
-
-// One workgroup per 16 KiB of a page, four 16-byte pieces a thread in flight; grid (pieces, pairs, layers x {k, v}).  Bound: memory
-// (200 pages of 2 MiB over 32 layers, 839 MB read and written, 148 .. 157 us, 5.3 .. 5.7 TB/s; a large copy reaches 5.0).
-constexpr int kCopyPiece = 16384;
-__global__ __launch_bounds__(256) void k_copy_pages(char *k, char *v, long long page_bytes, long long layer_bytes, long long used, Pairs w) {
-  char *base = (blockIdx.z & 1 ? v : k) + (blockIdx.z >> 1) * layer_bytes;
-  const char *src = base + w.src[blockIdx.y] * page_bytes;
-  char *dst = base + w.dst[blockIdx.y] * page_bytes;
-  const long long at = (long long)blockIdx.x * kCopyPiece + threadIdx.x * 16;
-#pragma unroll
-  for (int i = 0; i < kCopyPiece / 4096; ++i)
-    if (at + i * 4096 < used) *(u32x4 *)(dst + at + i * 4096) = *(const u32x4 *)(src + at + i * 4096);
-}
-
-__global__ void k_set_entries(int *state, int n, Pairs w) {        // state[src[i]] = dst[i]
-  for (int i = threadIdx.x; i < n; i += blockDim.x) state[w.src[i]] = w.dst[i];
-}
-__global__ void k_clear_state(int *state, int max_seqs, long long n) {     // no positions, no pages
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x)
-    state[i] = i < max_seqs ? 0 : -1;
-}
-
-// A context's cache rows [position][head][HD] <-> pages [head][slot][HD], 16 bytes a thread; grid (rows' pieces, layers).
-__global__ __launch_bounds__(256) void k_move_rows(Cache c, const int *row, int max_pages, long long layer_stride_bytes, char *kc, char *vc,
-                                                   long long ctx_layer_bytes, int head_bytes, int first, int n, int to_pages) {
-  const int per_head = head_bytes / 16, per_row = c.n_kv_heads * per_head;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (long long)n * per_row) return;
-  const int p = first + (int)(i / per_row), r = (int)(i % per_row), h = r / per_head, e = r % per_head;
-  const int at = c.by_page.quot(p);
-  if (at >= max_pages) return;
-  const int page = row[at], slot = p - at * c.page_size;
-  if ((unsigned)page >= (unsigned)c.n_pages) return;
-  const long long in_page = (long long)blockIdx.y * layer_stride_bytes + page * c.page_stride +
-                            ((long long)h * c.page_size + slot) * head_bytes + e * 16;
-  const long long in_ctx = (long long)blockIdx.y * ctx_layer_bytes + (long long)p * per_row * 16 + r * 16;
-  u32x4 *pk = (u32x4 *)((char *)c.k + in_page), *pv = (u32x4 *)((char *)c.v + in_page);
-  u32x4 *xk = (u32x4 *)(kc + in_ctx), *xv = (u32x4 *)(vc + in_ctx);
-  if (to_pages) { *pk = *xk; *pv = *xv; }
-  else { *xk = *pk; *xv = *pv; }
 }
 
 }  // namespace pg

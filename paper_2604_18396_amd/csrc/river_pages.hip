@@ -2,7 +2,6 @@
 #include "river.h"
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <climits>
 #include <cstdint>
@@ -11,100 +10,12 @@
 #include <new>
 #include <string>
 
-#include "river_host.h"
-#include "river_pages.h"
+#include "river_copies.h"
+#include "river_pages_host.h"
 #include "river_pool.h"
 
 using namespace river;
 using namespace river::pg;
-
-namespace {
-
-int refuse(const char *why, int code = RIVER_EINVAL) {
-  call_error() = why;
-  return code;
-}
-int hip_failed(const char *what, hipError_t e) {
-  call_error() = std::string(what) + ": " + hipGetErrorString(e);
-  return RIVER_EHIP;
-}
-// Every entry point: no exception leaves the library (what is left to throw is memory that runs out).
-template <class F>
-int guarded(F f) {
-  try {
-    return f();
-  } catch (...) {
-    try { call_error() = "out of host memory"; } catch (...) {}
-    return RIVER_ENOSPC;
-  }
-}
-// The launch's own result (an error of the caller's that is pending stays his).
-template <class T> struct As { typedef T type; };
-template <class... A>
-hipError_t launch(void (*k)(A...), dim3 grid, dim3 block, size_t lds, hipStream_t s, typename As<A>::type... a) {
-  void *args[] = {(void *)&a...};
-  return hipLaunchKernel((const void *)k, grid, block, args, lds, s);
-}
-
-// The same with more than 64 KiB of dynamic LDS, which each kernel asks for once per device.
-template <auto K, class... A>
-hipError_t launch_lds(dim3 grid, dim3 block, size_t lds, hipStream_t s, A... a) {
-  static std::atomic<uint64_t> asked{0};
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (!(asked.load(std::memory_order_relaxed) & bit)) {
-    if ((e = hipFuncSetAttribute((const void *)K, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) != hipSuccess) return e;
-    asked.fetch_or(bit, std::memory_order_relaxed);
-  }
-  return launch(K, grid, block, lds, s, a...);
-}
-
-Div div_by(int d) {
-  uint32_t s = 0;
-  while ((1ll << s) < d) ++s;
-  return Div{(uint32_t)d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
-}
-int elem_bytes(const river_pages *p) { return p->dtype == RIVER_F32 ? 4 : 2; }
-long long page_elems(const river_pages *p) { return (long long)p->n_kv_heads * p->page_size * p->head_dim; }
-
-// (a launch holds fewer than 2^32 threads in a dimension; a larger one would be cut off without an error)
-constexpr int kMostTokens = 1 << 22;
-constexpr int kMostPositions = 1 << 30;                          // of a sequence: indices of keys are 32-bit numbers
-
-Cache layer_cache(const river_pages *p, int layer) {
-  const size_t at = (size_t)layer * p->layer_stride * elem_bytes(p);
-  return Cache{(char *)p->k + at, (char *)p->v + at, p->page_stride, (uint32_t)(p->page_stride * elem_bytes(p) / 16), p->n_pages, p->page_size, p->n_kv_heads, div_by(p->page_size)};
-}
-
-const char *bad_batch(const river_batch *b) {
-  if (!b) return "null batch";
-  if (b->n_seq < 0 || b->n_tokens < 0 || b->max_pages < 1 || b->table_stride < b->max_pages || b->max_new < 0 || b->max_len < 0)
-    return "bad batch: n_seq, n_tokens, max_new, max_len >= 0, 1 <= max_pages <= table_stride";
-  if (b->n_tokens > kMostTokens || b->n_seq > kMostTokens) return "more than 2^22 tokens or sequences in a call";
-  if (b->n_seq == 0 || b->n_tokens == 0) return nullptr;         // (nothing to do: null pointers will do)
-  if (!b->table || !b->lens) return "null table or lengths";
-  if (((uintptr_t)b->table | (uintptr_t)b->lens | (uintptr_t)b->q_start) % 4) return "misaligned table, lengths or q_start";
-  if (!b->q_start && b->n_tokens != b->n_seq) return "without q_start every sequence has one token: n_tokens must be n_seq";
-  return nullptr;
-}
-Batch device_batch(const river_batch *b, int page_size) {
-  return Batch{b->table, b->lens, b->q_start, b->n_seq, b->n_tokens, b->max_pages, b->table_stride,
-               (int)std::min<long long>((long long)b->max_pages * page_size, kMostPositions)};
-}
-
-// The kernels of a configuration: f(T{}, C{}, HD) with the activations' type, the pages' and the head size.
-template <int N> struct Int { static constexpr int v = N; };
-template <class F>
-auto by_types(const river_pages *p, F f) {
-  const bool big = p->head_dim == 128;
-  if (p->dtype == RIVER_F32) return big ? f(float{}, float{}, Int<128>{}) : f(float{}, float{}, Int<64>{});
-  if (p->kv_dtype == RIVER_KV_F16) return big ? f(__bf16{}, _Float16{}, Int<128>{}) : f(__bf16{}, _Float16{}, Int<64>{});
-  return big ? f(__bf16{}, __bf16{}, Int<128>{}) : f(__bf16{}, __bf16{}, Int<64>{});
-}
-
-}  // namespace
 
 std::string &river::call_error() {
   static thread_local std::string text;
@@ -210,7 +121,7 @@ extern "C" int river_rope_store(const river_pages *pages, int32_t layer, const r
 
 // ------------------------------------------------------------------ attention
 
-static const char *bad_attention(const river_pages *pages, const river_batch *batch, int n_q_heads, int window, int sinks, std::string *why) {
+const char *river::pg::bad_attention(const river_pages *pages, const river_batch *batch, int n_q_heads, int window, int sinks, std::string *why) {
   if (check_pages(pages, why)) return why->c_str();
   if (const char *m = bad_batch(batch)) return m;
   if (n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % pages->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
@@ -218,13 +129,6 @@ static const char *bad_attention(const river_pages *pages, const river_batch *ba
   return nullptr;
 }
 
-// How a call is divided: which kernel, tiles of rows, splits of the keys.
-struct AttnPlan {
-  bool many;                                                     // k_attn_many, else k_attn_split
-  bool fused;                                                    // its last workgroups join the splits, where they have tickets
-  int max_new, tiles, tile_rows, n_splits, split_len;
-  size_t o_bytes, bytes;                                         // of the partial results
-};
 // k_attn_many where the rows of a sequence and key head are more than a tile of k_attn_split and all of them see enough: rows x keys
 // (of a row in the middle) x elements, 1.3e8 at head size 128 and 3e8 at 64.  It reads keys once for 128 rows, k_attn_split for 16, but
 // takes longer to begin and end (us, k_attn_many / k_attn_split; 8B shape: 256 new tokens behind none 12.2 / 11.3, 32 behind 1024
@@ -232,13 +136,12 @@ struct AttnPlan {
 // 22.2 / 24.2; 1B shape: 512 behind none 15.6 / 15.8, 32 behind 4096 17.0 / 17.3, 64 behind 4096 22.8 / 29.9, 8 behind 65536 39.5 / 47.4;
 // sixteen, 16 behind 512 16.3 / 14.8, 32 behind 512 19.3 / 21.0.  One product does not part all of these: 256 behind none and eight sequences
 // of 8 behind 2048 lie above the limit and are 8 .. 10 % slower there)
-constexpr int kSplitRows = 16;
 static double many_work(int head_dim) { return head_dim == 128 ? 1.3e8 : 3e8; }
 // Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a
 // second launch 6.4 + 3.8; 16 sequences of up to 1201 15.8, 14.3 + 3.9; 64 splits of 131072 105, 96 + 6)
 constexpr int kFewSplits = 16;
 
-static AttnPlan plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
+AttnPlan river::pg::plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
   AttnPlan y{};
   const int rep = nq / p->n_kv_heads;
   y.max_new = b->q_start ? std::min(b->max_new, b->n_tokens) : 1;
