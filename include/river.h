@@ -366,6 +366,72 @@ int river_paged_attention(const river_pages *pages, int32_t layer, const river_b
                           const void *q, int64_t q_stride, float scale, int32_t window, int32_t sinks, void *out,
                           int64_t out_stride, void *workspace, size_t workspace_bytes, int32_t *tickets, void *hip_stream);
 
+/* Prefixes that several sequences of a call have in common.  HOST struct of DEVICE arrays that the kernels read.
+ * The sequences seq_start[g] .. seq_start[g+1] - 1 of the batch are group g (there may be none; those in front of the first group
+ * and behind the last have no prefix); their positions below lens[g] are those of the prefix, whose pages table's row g names.
+ * lens is cut at max_pages * page_size and at 2^30.  seq_start ascends. */
+typedef struct {
+  const int32_t *table;     /* [n_groups][table_stride], the first max_pages entries of a row are used */
+  const int32_t *lens;      /* [n_groups] */
+  const int32_t *seq_start; /* [n_groups + 1] */
+  int32_t n_groups;         /* 0: the other fields are not used */
+  int32_t max_pages, table_stride;
+  int32_t max_len;          /* no prefix is longer, and */
+  int32_t max_seqs;         /* no group has more sequences: by these two the work is divided.  More are still right, but slow */
+} river_prefixes;
+
+/* river_paged_attention (without a window) where the positions below its group's prefix come from the prefix's pages, whose
+ * keys and values are read once for the new tokens of the whole group.  A sequence's lens and positions count the prefix; its entries
+ * of positions below lens[g] are not read (they may be -1: river_rope_store and river_store_slots do not need them for later positions
+ * either).  A prefix need not end with a page: its last page and the sequence's own entry of the same positions are two pages then, each with
+ * its own positions.  A token whose position is below the prefix's length sees what comes up to it.
+ * Arguments, roundings and errors as in river_paged_attention; no tickets.  max_new: as there; further tokens are left out.
+ * workspace: as there, of the bytes that river_prefix_attention_workspace gives. */
+int river_prefix_attention_workspace(const river_pages *pages, const river_batch *batch, const river_prefixes *prefixes,
+                                     int32_t n_q_heads, size_t *bytes);
+int river_prefix_attention(const river_pages *pages, int32_t layer, const river_batch *batch, const river_prefixes *prefixes,
+                           int32_t n_q_heads, const void *q, int64_t q_stride, float scale, void *out, int64_t out_stride,
+                           void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Writes keys and values as they are (rounded once to the cache's type) to slots of `layer`: token t's to slot slots[t] % page_size of
+ * page slots[t] / page_size.  A slot below 0, or of no page, is left out: a place of the batch without a token.  Two tokens
+ * must not have the same slot.
+ * slots: DEVICE [n_tokens], 8-byte aligned.  k, v: as in river_rope_store. */
+int river_store_slots(const river_pages *pages, int32_t layer, const int64_t *slots, int32_t n_tokens, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride, void *hip_stream);
+
+/* A page table that is kept on the device alone: for steps that are captured, and for many pages at once (a river_pool's flush sends
+ * entries from the host).  HOST struct of DEVICE arrays, all the caller's; use it or a river_pool for a cache, not both.
+ * free_pages: the first *n_free are the pages that nobody has, the last of them is given out first. */
+typedef struct {
+  int32_t *table;           /* [n_seq][table_stride], the first max_pages entries of a row are used; -1: no page */
+  const int32_t *lens;      /* [n_seq] positions before the call */
+  int32_t *lens_out;        /* [n_seq] positions after it: may be lens */
+  int32_t *free_pages;      /* [n_pages] */
+  const int32_t *n_free;    /* [1] before the call */
+  int32_t *n_free_out;      /* [1] after it: may be n_free */
+  const int32_t *n_shared;  /* [n_seq], or NULL (0): entries at a row's beginning that are somebody else's (a prefix): they are never given back */
+  int32_t n_seq;            /* at most 4096 */
+  int32_t max_pages, table_stride;
+  int32_t n_pages, page_size;
+} river_tables;
+
+/* Lays a step out from the requests' lengths.  Sequence s asks for n_new[s] positions more, or gives back its last -n_new[s] where that
+ * is negative (INT32_MIN: all).
+ * First, pages of which no position is left go back to the free list, their entries become -1; entries that name no page are skipped.
+ * Then the sequences are served in their order: each gets all that it asks for, or nothing and stays as it was.  It gets nothing where its
+ * row has no room (it counts for nothing then), where the tokens asked for up to it exceed n_tokens, and where it needs pages and
+ * those needed up to it exceed the free ones.  Pages that a call gave out lie in the free list as before once a call has
+ * given them back.
+ * q_start: DEVICE [n_seq + 1], where each sequence's new tokens begin, as river_batch has it.
+ * slots: DEVICE [n_tokens], 8-byte aligned, nullable: where the new tokens' keys and values belong (page * page_size + place
+ *   in the page; -1 where the entry names no page), -1 behind the last one.  positions: DEVICE [n_tokens], nullable: their positions, 0 behind the last one.
+ * refused: DEVICE [1], nullable: sequences that asked and got nothing.
+ * n_new: DEVICE [n_seq].  The arrays must not overlap, but for lens_out and n_free_out.  Calls on one table must not run at the same
+ * time.  A captured call reads n_new, lengths, table and free list anew at every replay. */
+int river_build_batch(const river_tables *tables, const int32_t *n_new, int32_t n_tokens, int32_t *q_start, int64_t *slots,
+                      int32_t *positions, int32_t *refused, void *hip_stream);
+
 /* Copies pages src[i] to dst[i] in every layer, keys and values, as if one pair after the other (a page may be
  * copied several times, and be the source of a later pair; pairs that depend on each other cost a launch).
  * src, dst: HOST [n], copied by the call, each in [0, n_pages). */

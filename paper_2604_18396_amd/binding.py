@@ -28,7 +28,8 @@ EXPORTS = ("river_quantize_w4", "river_workspace_bytes", "river_create", "river_
            "river_rope_frequencies", "river_rope_store", "river_paged_attention_workspace", "river_paged_attention",
            "river_copy_pages", "river_pool_create", "river_pool_destroy", "river_pool_extend", "river_pool_fork",
            "river_pool_rewind", "river_pool_trim", "river_pool_compact", "river_pool_flush", "river_pool_length",
-           "river_pool_free_pages", "river_pool_row", "river_save_pages", "river_load_pages")
+           "river_pool_free_pages", "river_pool_row", "river_save_pages", "river_load_pages",
+           "river_build_batch", "river_store_slots", "river_prefix_attention_workspace", "river_prefix_attention")
 TICKETS = 1024
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
@@ -72,6 +73,16 @@ class river_pages(C.Structure):
 class river_batch(C.Structure):
     _fields_ = [("table", C.c_void_p), ("lens", C.c_void_p), ("q_start", C.c_void_p)] + \
                [(n, C.c_int32) for n in ("n_seq", "n_tokens", "max_pages", "table_stride", "max_new", "max_len")]
+
+
+class river_prefixes(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("lens", C.c_void_p), ("seq_start", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_groups", "max_pages", "table_stride", "max_len", "max_seqs")]
+
+
+class river_tables(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("table", "lens", "lens_out", "free_pages", "n_free", "n_free_out", "n_shared")] + \
+               [(n, C.c_int32) for n in ("n_seq", "max_pages", "table_stride", "n_pages", "page_size")]
 
 
 class river_rope(C.Structure):
@@ -125,6 +136,11 @@ def load():
     for name, more in (("destroy", []), ("extend", [i32, i32]), ("fork", [i32, i32]), ("rewind", [i32, i32]), ("trim", [i32, i32, i32]),
                        ("compact", []), ("flush", [pages, ptr, ptr]), ("length", [i32]), ("free_pages", []), ("row", [i32, ptr])):
         getattr(L, "river_pool_" + name).argtypes = [ptr, *more]
+    prefixes = C.POINTER(river_prefixes)
+    L.river_build_batch.argtypes = [C.POINTER(river_tables), ptr, i32, ptr, ptr, ptr, ptr, ptr]
+    L.river_store_slots.argtypes = [pages, i32, ptr, i32, ptr, i64, ptr, i64, ptr]
+    L.river_prefix_attention_workspace.argtypes = [pages, batch, prefixes, i32, C.POINTER(C.c_size_t)]
+    L.river_prefix_attention.argtypes = [pages, i32, batch, prefixes, i32, ptr, i64, C.c_float, ptr, i64, ptr, C.c_size_t, ptr]
     L.river_save_pages.argtypes = [ptr, i32, i32, i32, pages, ptr, i32]
     L.river_load_pages.argtypes = [ptr, i32, i32, i32, pages, ptr, i32]
     _lib = L
@@ -741,3 +757,141 @@ def river_rewind(ctx: River, new_len: int):
 
 def river_destroy(ctx: River):
     ctx.close()
+
+
+# ------------------------------------------------------------------ a step laid out on the device, common prefixes
+
+class Prefixes(_Fixed):
+    """Prefixes that sequences of a Batch have in common: table [n_groups, max_pages], lens [n_groups] and seq_start [n_groups + 1], int32
+    on the device and read there at every call: sequences seq_start[g] .. seq_start[g + 1] - 1 have the first lens[g] positions in the pages of
+    row g.  max_len and max_seqs bound the prefixes' positions and a group's sequences (more are still right); the attention divides
+    its work by them.  Default: what the table holds, and all sequences of the call."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, seq_start: torch.Tensor, max_len: int | None = None, max_seqs: int | None = None):
+        _check_on(table.device, torch.int32, table=table, lens=lens, seq_start=seq_start)
+        n = lens.numel()
+        if not table.is_cuda or table.dim() != 2 or table.shape[0] != n or table.shape[1] < 1 or lens.dim() != 1:
+            raise ValueError("table [n_groups, max_pages] and lens [n_groups] on the device")
+        if (table.shape[1] > 1 and table.stride(1) != 1) or (n > 1 and table.stride(0) < table.shape[1]) or not lens.is_contiguous():
+            raise ValueError("rows of the table and lens must be contiguous")
+        if seq_start.shape != (n + 1,) or not seq_start.is_contiguous():
+            raise ValueError("seq_start [n_groups + 1]")
+        self.table, self.lens, self.seq_start, self.index, self.n_groups = table, lens, seq_start, table.get_device(), n
+        self.max_len, self.max_seqs = max_len, max_seqs
+        self._calls, self._bytes = {}, {}       # the C struct of a batch and page size, and the workspace's size of a shape of call
+        self._made = True
+
+    def bind(self, n_seq: int, page_size: int):
+        got = self._calls.get((n_seq, page_size))
+        if got is None:
+            most = self.table.shape[1]
+            if len(self._calls) >= 256:
+                self._calls.clear()
+                self._bytes.clear()
+            got = self._calls[(n_seq, page_size)] = C.byref(river_prefixes(
+                self.table.data_ptr(), self.lens.data_ptr(), self.seq_start.data_ptr(), self.n_groups, most,
+                self.table.stride(0) if self.n_groups > 1 else most,
+                min(2**31 - 1, most * page_size) if self.max_len is None else self.max_len, n_seq if self.max_seqs is None else self.max_seqs))
+        return got
+
+
+def river_prefix_attention(pages: Pages, layer: int, batch: Batch, prefixes: Prefixes, q: torch.Tensor, scale: float = 0.0,
+                           out: torch.Tensor | None = None) -> torch.Tensor:
+    """river_paged_attention, without a window, of sequences that go on from common prefixes, whose pages are read once for a group.  Rows of `out`
+    (or of the new tensor that is returned) whose tokens belong to no sequence are not written.  For inference: autograd does not see it."""
+    if pages.index != _device():
+        with torch.cuda.device(pages.index):
+            return river_prefix_attention(pages, layer, batch, prefixes, q, scale, out)
+    if prefixes.index != pages.index:
+        raise ValueError("pages and prefixes are on different devices")
+    qs = _rows("q", q, pages)
+    out, os_ = _out(q, out, pages)
+    L, (n, heads, _) = load(), q.shape
+    ref, shared = batch.bind(n, pages), prefixes.bind(batch.n_seq, pages.page_size)
+    key = (pages.shape_key, n, heads, batch.n_seq, batch.q_start is None, batch.max_new, batch.max_len, batch.table.shape[1])
+    nbytes = prefixes._bytes.get(key)
+    if nbytes is None:
+        got = C.c_size_t()
+        _check_call(L.river_prefix_attention_workspace(pages.ref, ref, shared, heads, C.byref(got)))
+        if len(prefixes._bytes) >= 256:
+            prefixes._bytes.clear()
+        nbytes = prefixes._bytes[key] = got.value
+    # (from torch's allocator, call by call: see river_paged_attention)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=pages.device).data_ptr() if nbytes else None
+    _check_call(L.river_prefix_attention(pages.ref, layer, ref, shared, heads, q.data_ptr(), qs, scale, out.data_ptr(), os_, ws, nbytes,
+                                         _stream(pages.index)))
+    return out
+
+
+def river_store_slots(pages: Pages, layer: int, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
+    """Stores k and v [n_tokens, heads, head_dim] as they are to slots [n_tokens] (int64: page * page_size + place in the page, below 0: left
+    out; none of them twice).  For inference: autograd does not see it."""
+    if pages.index != _device():
+        with torch.cuda.device(pages.index):
+            return river_store_slots(pages, layer, slots, k, v)
+    ks, vs, n = _rows("k", k, pages, pages.n_kv_heads), _rows("v", v, pages, pages.n_kv_heads), k.shape[0]
+    if v.shape[0] != n or slots.shape != (n,) or slots.dtype is not torch.int64 or slots.get_device() != pages.index or not slots.is_contiguous():
+        raise ValueError("slots: int64 [n_tokens] on the pages' device, and as many keys and values")
+    _check_call(load().river_store_slots(pages.ref, layer, slots.data_ptr(), n, k.data_ptr(), ks, v.data_ptr(), vs, _stream(pages.index)))
+
+
+class Tables(_Fixed):
+    """A page table that lives on the device alone, and its free list: table [n_seq, max_pages], lens [n_seq], free_pages [n_pages], n_free [1]
+    and, where rows begin with pages of somebody else, n_shared [n_seq]; all int32, the caller's, and changed by river_build_batch.  lens_out
+    and n_free_out: where it writes lengths and count instead (a step laid out ahead of being taken)."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int,
+                 n_shared: torch.Tensor | None = None, lens_out: torch.Tensor | None = None, n_free_out: torch.Tensor | None = None):
+        lens_out, n_free_out = lens if lens_out is None else lens_out, n_free if n_free_out is None else n_free_out
+        vectors = dict(lens=lens, lens_out=lens_out, free_pages=free_pages, n_free=n_free, n_free_out=n_free_out,
+                       **({} if n_shared is None else {"n_shared": n_shared}))
+        _check_on(table.device, torch.int32, table=table, **vectors)
+        n = lens.numel()
+        if not table.is_cuda or table.dim() != 2 or table.shape[0] != n or table.shape[1] < 1:
+            raise ValueError("table [n_seq, max_pages] and lens [n_seq] on the device")
+        if (table.shape[1] > 1 and table.stride(1) != 1) or (n > 1 and table.stride(0) < table.shape[1]):
+            raise ValueError("rows of the table must be contiguous")
+        for name, t in vectors.items():
+            if t.dim() != 1 or not t.is_contiguous() or (name in ("lens_out", "n_shared") and t.numel() != n) or (name[:6] == "n_free" and t.numel() != 1):
+                raise ValueError(f"{name}: one number, or as many as there are sequences, contiguous")
+        self.table, self.lens, self.lens_out, self.free_pages, self.n_free, self.n_free_out, self.n_shared = (
+            table, lens, lens_out, free_pages, n_free, n_free_out, n_shared)
+        self.n_seq, self.page_size, self.device, self.index = n, page_size, table.device, table.get_device()
+        self.c = river_tables(table.data_ptr(), lens.data_ptr(), lens_out.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr(),
+                              None if n_shared is None else n_shared.data_ptr(), n, table.shape[1], table.stride(0) if n > 1 else table.shape[1],
+                              free_pages.numel(), page_size)
+        self.ref = C.byref(self.c)
+        self._made = True
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, max_seqs: int, max_pages: int, device="cuda:0", n_shared: torch.Tensor | None = None) -> "Tables":
+        """No positions, all pages free, the lowest given out first."""
+        free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        return cls(torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device), torch.zeros(max_seqs, dtype=torch.int32, device=device),
+                   free, torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size, n_shared)
+
+
+def _vector(name: str, t: torch.Tensor | None, dtype: torch.dtype, n: int | None, index: int):
+    """The address of a contiguous vector on the device, of n numbers (None: of any number)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != index or t.dim() != 1 or (n is not None and t.numel() != n) or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} [{'n_tokens' if n is None else n}] on the tables' device")
+    return t.data_ptr()
+
+
+def river_build_batch(tables: Tables, n_new: torch.Tensor, q_start: torch.Tensor, slots: torch.Tensor | None = None,
+                      positions: torch.Tensor | None = None, refused: torch.Tensor | None = None, n_tokens: int | None = None):
+    """Lays a step out: sequence s gets n_new[s] positions more (or gives back -n_new[s]), all of them or none.  Written: q_start [n_seq + 1],
+    and where given slots (int64) and positions (int32) [n_tokens] of the new tokens, refused [1] (sequences that asked and got nothing).  n_tokens: no
+    more new tokens than these in the call (default: the room in slots or positions, else 2^22)."""
+    if tables.index != _device():
+        with torch.cuda.device(tables.index):
+            return river_build_batch(tables, n_new, q_start, slots, positions, refused, n_tokens)
+    if n_tokens is None:
+        n_tokens = slots.numel() if slots is not None else positions.numel() if positions is not None else 1 << 22
+    i, n = tables.index, tables.n_seq
+    _check_call(load().river_build_batch(tables.ref, _vector("n_new", n_new, torch.int32, n, i), n_tokens,
+                                         _vector("q_start", q_start, torch.int32, n + 1, i), _vector("slots", slots, torch.int64, n_tokens, i),
+                                         _vector("positions", positions, torch.int32, n_tokens, i), _vector("refused", refused, torch.int32, 1, i),
+                                         _stream(i)))

@@ -8,9 +8,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "river.hip")
 # one object per source, river.hip's code object first in the library
-SOURCES = [SRC, os.path.join(HERE, "csrc", "river_pages.hip")]
+SOURCES = [SRC, *(os.path.join(HERE, "csrc", s) for s in ("river_pages.hip", "river_prefix.hip", "river_step.hip"))]
 DEPS = [*SOURCES, *(os.path.join(HERE, "csrc", h) for h in ("river_copies.h", "river_device.h", "river_prefill.h", "river_host.h", "river_pages.h",
-                                                            "river_pages_host.h", "river_pool.h")),
+                                                            "river_pages_host.h", "river_pool.h", "river_prefix.h", "river_step.h")),
         os.path.join(ROOT, "include", "river.h")]
 LIB = os.path.join(HERE, "libriver.so")
 

@@ -1,0 +1,216 @@
+// Device code of attention over pages where groups of sequences go on from common prefixes (gfx950).
+#pragma once
+#include "river_pages.h"
+
+namespace river {
+namespace pg {
+
+// Group g is the sequences seq_start[g] .. seq_start[g + 1] - 1, whose positions below lens[g] are the group's prefix, with a row of
+// pages of its own.  A row's softmax over j <= p is the softmax over its parts, each with its own maximum m and sum l:
+//   o = sum_i 2^(m_i - m) l_i o_i / sum_i 2^(m_i - m) l_i
+// so the rows of all of a group's new tokens that share a key head are the rows of one product with the prefix's keys, which are
+// read once for a tile of them, and each sequence's rows have a product with its own keys.  One launch has the units of both kinds, the
+// prefixes' first; another joins a row's parts.
+struct Prefixes {
+  const int *table, *lens, *seq_start;
+  int n_groups, max_pages, table_stride;
+  int cap;                                // positions that a row has entries for
+  int tiles, n_splits, least;             // tiles of a group's rows (further ones are taken in turn), splits of its keys at most, keys of a split at least
+  unsigned units;                         // workgroups of the prefixes; 0: a sequence's rows go through its prefix too
+};
+
+// How many of n ascending numbers are at most x.  All lanes of a wavefront ask alike.
+__device__ __forceinline__ int count_up_to(const int *v, int n, int x) {
+  const int lane = threadIdx.x % 64;
+  int lo = 0;
+  while (n > 64) {
+    const int step = (n + 63) / 64, c = __popcll(__ballot(lane * step < n && v[lo + min(lane * step, n - 1)] <= x));
+    if (c == 0) return lo;
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  return lo + __popcll(__ballot(lane < n && v[lo + min(lane, max(n - 1, 0))] <= x));
+}
+
+__device__ __forceinline__ int group_of(const Prefixes &x, int s) {      // or -1
+  if (x.n_groups == 0) return -1;
+  const int g = __builtin_amdgcn_readfirstlane(count_up_to(x.seq_start, x.n_groups + 1, s)) - 1;
+  return g < x.n_groups ? g : -1;
+}
+__device__ __forceinline__ int prefix_len(const Prefixes &x, int g) { return g < 0 ? 0 : min(max(x.lens[g], 0), x.cap); }
+
+// Splits of n keys: whole steps of 128 keys, `least` at least and no more splits than `most`; one if there are none.
+__device__ __forceinline__ int split_len(int n, int most, int least) { return max(least, ((n + most - 1) / most + 127) / 128 * 128); }
+__device__ __forceinline__ int split_count(int n, int most, int least) {
+  const int len = split_len(n, most, least);
+  return max(1, (n + len - 1) / len);
+}
+
+// Keys that lie in the group's pages below position n, in the sequence's own from there on.
+struct TwoRows {
+  const int *common, *own;
+  int n;
+  __device__ __forceinline__ int entry(int p, int i) const { return (p < n ? common : own)[i]; }
+};
+// Rows whose positions were found before: this lane's, and the lowest and highest of its wavefront's.
+struct Found {
+  int mine, first, last;
+  __device__ __forceinline__ int position(int) const { return mine; }
+  __device__ __forceinline__ void reach(int, int, int &lo, int &hi) const { lo = first; hi = last; }
+};
+typedef Unit<TwoRows, Found> Share;
+
+constexpr int kAttnRows = 16;              // of a tile of split_unit
+constexpr int kEverything = 1 << 30;       // a position that sees every key
+template <int TR>
+__device__ __forceinline__ int my_row(int r0, int r1) {           // this lane's row of a tile of TR
+  return min(r0 + (TR == kAttnRows ? (int)threadIdx.x % 16 : (int)threadIdx.x / 64 * 32 + (int)threadIdx.x % 32), r1);
+}
+
+// Tile `tile` of group g's rows with split z of its prefix.  A token without a position (it has no result) counts as one
+// that sees all, so that it costs the others nothing.
+template <int TR>
+__device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int g, int tile, int z, int head, Share &w) {
+  const int n = prefix_len(x, g), parts = split_count(n, x.n_splits, x.least), len = split_len(n, x.n_splits, x.least);
+  if (n == 0 || z >= parts) return false;
+  const int s0 = min(max(x.seq_start[g], 0), b.n_seq), s1 = min(max(x.seq_start[g + 1], s0), b.n_seq);
+  const int t0 = b.q_start ? min(max(b.q_start[s0], 0), b.n_tokens) : s0, t1 = b.q_start ? min(max(b.q_start[s1], t0), b.n_tokens) : s1;
+  const int rows = (t1 - t0) * a.rep, r0 = tile * TR;
+  if (r0 >= rows) return false;
+  w.r0 = r0;
+  w.r1 = min(r0 + TR - 1, rows - 1);
+  const int t = t0 + a.by_rep.quot(my_row<TR>(r0, w.r1));
+  int s = t;
+  if (b.q_start) {                        // the last of the group's sequences that begins at or before the token
+    int hi = s1;
+    for (s = s0; s + 1 < hi;) {
+      const int mid = (s + hi) >> 1;
+      if (b.q_start[mid] <= t) s = mid; else hi = mid;
+    }
+  }
+  int p = position_of(b, s, t);
+  if (p < 0) p = kEverything;
+  int lo = p, hi = p;
+#pragma unroll
+  for (int d = 1; d < (TR == kAttnRows ? 16 : 32); d <<= 1) {
+    lo = min(lo, __shfl_xor(lo, d));
+    hi = max(hi, __shfl_xor(hi, d));
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  w.rows = {p, lo, hi};
+  w.sp = {lo, hi, 0, 0, n};
+  const int *row = x.table + (long long)g * x.table_stride;
+  w.keys = {row, row, n};
+  w.i0 = z * len;
+  w.i1 = z == parts - 1 ? n : w.i0 + len;
+  w.first_token = t0;
+  w.row0 = t0;
+  w.head = head;
+  w.part = z;
+  w.whole = false;
+  return true;
+}
+
+// Tile `tile` of sequence s's rows with split z of its own keys (of all that it sees, where the prefixes have no units).
+template <int TR>
+__device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int s, int tile, int z, int head, Share &w) {
+  int first_token, count;
+  seq_tokens(b, s, first_token, count);
+  const int rows = min(count, a.max_new) * a.rep, r0 = tile * TR;
+  if (r0 >= rows) return false;
+  w.r0 = r0;
+  w.r1 = min(r0 + TR - 1, rows - 1);
+  const int g = group_of(x, s), n = prefix_len(x, g), len = length_of(b, s);
+  const int lo = new_position(len, count, a.by_rep.quot(r0)), hi = new_position(len, count, a.by_rep.quot(w.r1));
+  const int low = x.units ? n : 0, keys = max(0, min(hi + 1, max(b.cap, n)) - low);
+  const int parts = split_count(keys, a.n_splits, a.split_len), each = split_len(keys, a.n_splits, a.split_len);
+  if (z >= parts) return false;
+  w.sp = {lo, hi, 0, low, keys};
+  if constexpr (TR == kAttnRows) w.rows = {new_position(len, count, a.by_rep.quot(my_row<TR>(r0, w.r1))), lo, hi};
+  else {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w0 = min(r0 + wave * 32, w.r1), w1 = min(w0 + 31, w.r1);
+    w.rows = {new_position(len, count, a.by_rep.quot(my_row<TR>(r0, w.r1))), new_position(len, count, a.by_rep.quot(w0)),
+              new_position(len, count, a.by_rep.quot(w1))};
+  }
+  w.keys = {x.table + (long long)max(g, 0) * x.table_stride, b.table + (long long)s * b.table_stride, n};
+  w.i0 = z * each;
+  w.i1 = z == parts - 1 ? keys : w.i0 + each;
+  w.first_token = first_token;
+  w.row0 = first_token;
+  w.head = head;
+  const int before = x.units ? x.n_splits : 0;
+  w.part = before + z;
+  w.whole = parts == 1 && (n == 0 || !x.units);
+  return true;
+}
+
+// Sixteen rows a unit, of either kind.  Bound and layout: see k_attn_split.
+template <class T, class C, int HD>
+__global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share_split(Cache c, Batch b, AttnArgs a, Prefixes x) {
+  __shared__ __align__(16) char lds[kAttnWaves * SplitLds<C, HD>::AREA];
+  __shared__ float2 res_ml[kAttnWaves][16];
+  const bool common = blockIdx.x < x.units;
+  int tile, s, z, head;
+  if (common) {
+    const unsigned u = blockIdx.x / c.n_kv_heads, v = u / x.tiles;
+    head = blockIdx.x % c.n_kv_heads;
+    tile = u % x.tiles;
+    z = v % x.n_splits;
+    s = v / x.n_splits;
+  } else work_of(blockIdx.x - x.units, c, b, a, tile, s, z, head);
+  Share w;
+  w.n_parts = (x.units ? x.n_splits : 0) + a.n_splits;
+  for (;;) {
+    if (!(common ? prefix_unit<kAttnRows>(x, b, a, s, tile, z, head, w) : own_unit<kAttnRows>(x, b, a, s, tile, z, head, w))) return;
+    const int early[2][Tile<C, HD>::KB] = {};
+    float v[RowPart<HD>::E];
+    split_unit<T, C, HD>(c, a, w, lds, res_ml, false, early, v);
+    if (!common) return;
+    tile += x.tiles;
+    __syncthreads();
+  }
+}
+
+// A row's parts, joined: those of its group's prefix, then its sequence's own.  A workgroup has RB heads of one token.
+template <class T, int HD, int RB>
+__global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixes x, int chunks) {
+  constexpr int LANES = HD / 4;
+  static_assert(RB * LANES == 256, "a thread has four elements of a row");
+  const int t = blockIdx.x / chunks, h = blockIdx.x % chunks * RB + threadIdx.x / LANES, e0 = threadIdx.x % LANES * 4;
+  int s = t;
+  if (b.q_start) {
+    s = __builtin_amdgcn_readfirstlane(count_up_to(b.q_start, b.n_seq + 1, t)) - 1;
+    if (s < 0 || s >= b.n_seq) return;
+  }
+  int first, count;
+  seq_tokens(b, s, first, count);
+  const int i = t - first;
+  if (i >= min(count, a.max_new)) return;
+  const int len = length_of(b, s), n = prefix_len(x, group_of(x, s)), low = x.units ? n : 0;
+  const int common = low ? split_count(n, x.n_splits, x.least) : 0;
+  // the last row of this one's tile: see own_unit
+  const int r = i * a.rep + h % a.rep, r1 = min(r - r % a.tile_rows + a.tile_rows, min(count, a.max_new) * a.rep) - 1;
+  const int keys = max(0, min(new_position(len, count, a.by_rep.quot(r1)) + 1, max(b.cap, n)) - low);
+  const int own = split_count(keys, a.n_splits, a.split_len);
+  if (common + own == 1 || h >= a.nq) return;
+  const int before = x.units ? x.n_splits : 0, n_parts = before + a.n_splits;
+  const long long row = ((long long)t * a.nq + h) * n_parts;
+  float big = -INFINITY, sum = 0.f;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int y = 0; y < common + own; ++y) {
+    const long long part = row + (y < common ? y : before + y - common);
+    const float2 ml = a.part_ml[part];
+    const f32x4 o = *(const f32x4 *)(a.part_o + part * HD + e0);
+    const float now = fmaxf(big, ml.x), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(big - now), g = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - now);
+    sum = sum * f + g * ml.y;
+    v = v * f + g * o;
+    big = now;
+  }
+  if (new_position(len, count, i) < 0) sum = 0.f;                // (a token without a position sees nothing)
+  const float out[4] = {v[0], v[1], v[2], v[3]};
+  store_row<T, 4>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, out, sum);
+}
+
+}  // namespace pg
+}  // namespace river

@@ -1,0 +1,128 @@
+// Host side of attention with common prefixes (include/river.h): checks of arguments, how a call is divided, launches.
+#include "river.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <string>
+
+#include "river_pages_host.h"
+#include "river_prefix.h"
+
+using namespace river;
+using namespace river::pg;
+
+namespace {
+
+const char *bad_prefixes(const river_prefixes *x) {
+  if (!x) return "null prefixes";
+  if (x->n_groups < 0 || x->n_groups > kMostTokens || x->max_len < 0 || x->max_seqs < 0) return "bad prefixes: n_groups in [0, 2^22], max_len, max_seqs >= 0";
+  if (x->n_groups == 0) return nullptr;
+  if (x->max_pages < 1 || x->table_stride < x->max_pages) return "bad prefixes: 1 <= max_pages <= table_stride";
+  if (!x->table || !x->lens || !x->seq_start) return "null table, lengths or seq_start of the prefixes";
+  if (((uintptr_t)x->table | (uintptr_t)x->lens | (uintptr_t)x->seq_start) % 4) return "misaligned table, lengths or seq_start of the prefixes";
+  return nullptr;
+}
+
+// How a call is divided: units of a group's rows and its prefix, units of a sequence's rows and its own keys.
+struct SharePlan {
+  int max_new, tiles, n_splits, least;                           // of the sequences
+  int p_tiles, p_splits, p_least;                                // of the prefixes
+  long long units;                                               // workgroups of the prefixes
+  size_t o_bytes, bytes;                                         // of the partial results
+};
+
+SharePlan plan_share(const river_pages *p, const river_batch *b, const river_prefixes *x, int nq) {
+  SharePlan y{};
+  const int rep = nq / p->n_kv_heads;
+  y.max_new = b->q_start ? std::min(b->max_new, b->n_tokens) : 1;
+  // Both kinds: three workgroups a CU of at least 128 keys, eight where that leaves them 512 (see plan_attention)
+  auto splits = [&](long long groups, long long keys) {
+    auto by = [&](long long goal, long long least) { return std::min({goal / std::max(1ll, groups), (keys + least - 1) / least, 64ll}); };
+    return (int)std::max(1ll, std::max(by(768, 128), by(2048, 512)));
+  };
+  const long long rows = (long long)y.max_new * rep;
+  y.tiles = (int)((rows + kAttnRows - 1) / kAttnRows);
+  const long long common = x->n_groups ? std::min<long long>({x->max_len, (long long)x->max_pages * p->page_size, kMostPositions}) : 0;
+  const long long keys = std::min<long long>({b->max_len, std::max<long long>((long long)b->max_pages * p->page_size, common), kMostPositions});
+  y.least = y.p_least = 128;
+  if (common && x->max_seqs > 1) {
+    const long long group_rows = std::min<long long>(b->n_tokens, (long long)x->max_seqs * y.max_new) * rep;
+    y.p_tiles = (int)((group_rows + kAttnRows - 1) / kAttnRows);
+    y.p_splits = splits((long long)x->n_groups * p->n_kv_heads * y.p_tiles, common);
+    y.units = (long long)x->n_groups * p->n_kv_heads * y.p_tiles * y.p_splits;
+  }
+  y.n_splits = splits((long long)b->n_seq * p->n_kv_heads * y.tiles, y.units ? std::max(1ll, keys - common) : keys);
+  if (y.units || y.n_splits > 1) {
+    const size_t parts = (size_t)b->n_tokens * nq * ((y.units ? y.p_splits : 0) + y.n_splits);
+    y.o_bytes = parts * p->head_dim * 4;
+    y.bytes = y.o_bytes + parts * 8;
+  }
+  return y;
+}
+
+}  // namespace
+
+extern "C" int river_prefix_attention_workspace(const river_pages *pages, const river_batch *batch, const river_prefixes *prefixes,
+                                                int32_t n_q_heads, size_t *bytes) {
+  return guarded([&]() -> int {
+    std::string why;
+    if (!bytes) return refuse("null bytes");
+    if (const char *m = bad_attention(pages, batch, n_q_heads, 0, 0, &why)) return refuse(m);
+    if (const char *m = bad_prefixes(prefixes)) return refuse(m);
+    *bytes = plan_share(pages, batch, prefixes, n_q_heads).bytes;
+    return RIVER_OK;
+  });
+}
+
+extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, const river_batch *batch, const river_prefixes *prefixes,
+                                      int32_t n_q_heads, const void *q, int64_t q_stride, float scale, void *out, int64_t out_stride,
+                                      void *workspace, size_t workspace_bytes, void *hip_stream) {
+  return guarded([&]() -> int {
+    std::string why;
+    if (const char *m = bad_attention(pages, batch, n_q_heads, 0, 0, &why)) return refuse(m);
+    if (const char *m = bad_prefixes(prefixes)) return refuse(m);
+    if (layer < 0 || layer >= pages->n_layers) return refuse("layer out of range");
+    if (!(scale >= 0.f) || !std::isfinite(scale)) return refuse("scale must be positive (0: 1 / sqrt(head_dim))");
+    const int es = elem_bytes(pages);
+    const long long qw = (long long)n_q_heads * pages->head_dim;
+    if (q_stride < qw || out_stride < qw) return refuse("a stride is smaller than its row");
+    if ((((uintptr_t)q | (uintptr_t)out) & 15) || q_stride * es % 16 || out_stride * es % 16)
+      return refuse("queries, output and their strides must be multiples of 16 bytes");
+    if (batch->n_tokens == 0 || batch->n_seq == 0) return RIVER_OK;
+    if (!q || !out) return refuse("null queries or output");
+    if (q == out) return refuse("the output must not overlap the queries");
+    if (scale == 0.f) scale = 1.f / std::sqrt((float)pages->head_dim);
+    const float scale2 = scale * 1.44269504088896340736f;        // (powers of two are what the hardware has)
+    if (!std::isfinite(scale2)) return refuse("scale is too large");
+    if ((long long)batch->n_tokens * n_q_heads >= (1ll << 28)) return refuse("too many tokens and heads");
+    const SharePlan y = plan_share(pages, batch, prefixes, n_q_heads);
+    if (y.bytes && (!workspace || (uintptr_t)workspace % 16)) return refuse("null or misaligned (16 B) workspace");
+    if (workspace_bytes < y.bytes) return refuse("workspace too small", RIVER_ENOSPC);
+    if (y.tiles == 0) return RIVER_OK;
+    const Cache c = layer_cache(pages, layer);
+    const Batch b = device_batch(batch, pages->page_size);
+    const int rep = n_q_heads / pages->n_kv_heads;
+    auto turn = [](long long round) { int k = 0; while ((round << k) % 32) ++k; return k; };
+    const int turn_z = turn((long long)y.n_splits * c.n_kv_heads), turn_s = turn((long long)b.n_seq * y.n_splits * c.n_kv_heads);
+    const AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale2, 0, 0, y.n_splits, y.least, y.tiles, kAttnRows, turn_s, turn_z,
+                     y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), nullptr};
+    const Prefixes x{prefixes->table, prefixes->lens, prefixes->seq_start, prefixes->n_groups, prefixes->max_pages, prefixes->table_stride,
+                     (int)std::min<long long>((long long)prefixes->max_pages * pages->page_size, kMostPositions), std::max(1, y.p_tiles),
+                     std::max(1, y.p_splits), y.p_least, (unsigned)y.units};
+    const long long groups = y.units + (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
+    const int chunks_of = 256 / (pages->head_dim / 4), chunks = (n_q_heads + chunks_of - 1) / chunks_of;
+    if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * chunks * 256 >= (1ll << 32))
+      return refuse("too many sequences, groups, tokens and heads");
+    const hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
+      return launch(k_share_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups), dim3(kAttnThreads), 0, st, c, b, a, x);
+    });
+    if (e == hipSuccess && y.bytes)
+      e = by_types(pages, [&](auto t, auto, auto hd) {
+        constexpr int HD = decltype(hd)::v;
+        return launch(k_share_join<decltype(t), HD, 1024 / HD>, dim3((unsigned)(b.n_tokens * chunks)), dim3(256), 0, st, b, a, x, chunks);
+      });
+    return e == hipSuccess ? RIVER_OK : hip_failed("river_prefix_attention", e);
+  });
+}

@@ -1,0 +1,268 @@
+// Device code that lays a step out (gfx950): pages from a free list on the device, slot maps, keys and values stored by them.
+#pragma once
+#include "river_pages.h"
+
+namespace river {
+namespace pg {
+
+// ------------------------------------------------------------------ a step from the requests' lengths
+//
+// Sequence s has lens[s] positions and asks for n_new[s] more (gives back -n_new[s] where that is negative).  Everything follows from
+// running sums over the sequences in their order, tokens and pages asked for so far: who is served, where each one's tokens begin, which
+// pages of the free list it gets.  One workgroup keeps them in LDS (12 bytes a sequence); a thread has neighbouring sequences.
+
+constexpr int kBuildThreads = 1024, kBuildSeqs = 4096, kBuildEach = kBuildSeqs / kBuildThreads;
+
+struct BuildArgs {
+  int *table;
+  const int *lens, *n_new, *n_free, *n_shared;
+  int *lens_out, *free_pages, *n_free_out;
+  int n_seq, max_pages, table_stride, n_pages, page_size, n_tokens;
+  int cap;                                // positions that a row has entries for
+  Div by_page;
+  int *q_start;
+  long long *slots;
+  int *positions, *refused;
+};
+
+// Pages of n positions
+__device__ __forceinline__ int pages_of(const BuildArgs &a, int n) { return n > 0 ? a.by_page.quot(n - 1) + 1 : 0; }
+
+// Sums that stop at kMuch (more than there are tokens in a call, or pages): in any order the same, and no overflow.
+constexpr uint32_t kMuch = 1u << 30;
+struct Two { uint32_t x, y; };
+__device__ __forceinline__ Two add(Two a, Two b) { return {min(a.x + b.x, kMuch), min(a.y + b.y, kMuch)}; }
+// What the threads before this one have, and all of them; two barriers.
+__device__ __forceinline__ Two sum_before(Two mine, Two *waves, Two &all) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = blockDim.x / 64;
+  Two t = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const Two o = {__shfl_up(t.x, d), __shfl_up(t.y, d)};
+    if (lane >= d) t = add(t, o);
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = t;
+  Two before = {__shfl_up(t.x, 1), __shfl_up(t.y, 1)};
+  if (lane == 0) before = {0, 0};
+  __syncthreads();
+  all = {0, 0};
+  for (int w = 0; w < n; ++w) {
+    if (w == wave) before = add(all, before);
+    all = add(all, waves[w]);
+  }
+  return before;
+}
+
+// The first i of n with v[i] > x (v ascends).
+__device__ __forceinline__ int first_above(const int *v, int n, int x) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (v[mid] > x) hi = mid; else lo = mid + 1;
+  }
+  return lo;
+}
+
+// slots and positions of token t, which is at position p and has page `page`; p < 0: no token
+__device__ __forceinline__ void put_token(const BuildArgs &a, int t, int p, int page, int in_page) {
+  if (a.slots) a.slots[t] = p >= 0 && (unsigned)page < (unsigned)a.n_pages ? (long long)page * a.page_size + in_page : -1;
+  if (a.positions) a.positions[t] = max(p, 0);
+}
+
+template <bool TOKENS>
+__global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
+  extern __shared__ int sums[];
+  const int n = a.n_seq, nt = blockDim.x, tid = threadIdx.x, lane = tid % 64;
+  int *const len = sums, *const page_sum = sums + n, *const start = sums + 2 * n;     // [n], [n], [n + 1]
+  __shared__ Two waves[kBuildThreads / 64];
+  __shared__ int taken_;
+  const int each = (n + nt - 1) / nt, s0 = tid * each;
+  int free = min(max(*a.n_free, 0), a.n_pages);
+  int old[kBuildEach], d[kBuildEach], kept[kBuildEach];
+  bool back = false;
+#pragma unroll
+  for (int i = 0; i < kBuildEach; ++i) {
+    const int s = s0 + i;
+    old[i] = d[i] = kept[i] = 0;
+    if (i >= each || s >= n) continue;
+    kept[i] = a.lens[s];
+    d[i] = a.n_new[s];
+    old[i] = max(kept[i], 0);
+    if (d[i] < 0) kept[i] = (int)max(0ll, (long long)old[i] + d[i]);
+    back |= d[i] < 0;
+  }
+  if (tid == 0) taken_ = 0;
+  if (__syncthreads_or(back)) {
+    // Given back: entries from .. to - 1 of a row that name pages, the last one of the last sequence first onto the free list, so that
+    // pages that a call has given out come to lie as they lay before it.  A wavefront a row: how many, then where.
+#pragma unroll
+    for (int i = 0; i < kBuildEach; ++i) {
+      const int s = s0 + i;
+      if (i >= each || s >= n) continue;
+      const int from = max(pages_of(a, max(kept[i], 0)), a.n_shared ? a.n_shared[s] : 0);
+      start[s] = from;
+      page_sum[s] = d[i] < 0 ? min(pages_of(a, old[i]), a.max_pages) : from;
+    }
+    __syncthreads();
+    for (int s = tid / 64; s < n; s += nt / 64) {
+      const int *row = a.table + (long long)s * a.table_stride;
+      int count = 0;
+      for (int at = start[s]; at < page_sum[s]; at += 64)
+        count += __popcll(__ballot(at + lane < page_sum[s] && (unsigned)row[min(at + lane, a.max_pages - 1)] < (unsigned)a.n_pages));
+      if (lane == 0) len[s] = count;
+    }
+    __syncthreads();
+    Two mine = {0, 0}, all;
+#pragma unroll
+    for (int i = 0; i < kBuildEach; ++i)
+      if (i < each && s0 + i < n) mine.x += len[s0 + i];
+    const Two before = sum_before(mine, waves, all);
+    int behind = (int)(all.x - before.x);
+#pragma unroll
+    for (int i = 0; i < kBuildEach; ++i)
+      if (i < each && s0 + i < n) {
+        behind -= len[s0 + i];
+        len[s0 + i] = free + behind;
+      }
+    __syncthreads();
+    for (int s = tid / 64; s < n; s += nt / 64) {
+      int *row = a.table + (long long)s * a.table_stride;
+      int at = len[s];
+      for (int to = page_sum[s]; to > start[s]; to -= 64) {
+        const int i = to - 1 - lane;
+        const int page = i >= start[s] ? row[i] : -1;
+        const bool ok = (unsigned)page < (unsigned)a.n_pages;
+        const unsigned long long all_ok = __ballot(ok);
+        const int to_list = at + __popcll(all_ok & ((1ull << lane) - 1));
+        if (ok && to_list < a.n_pages) a.free_pages[to_list] = page;
+        if (i >= start[s]) row[i] = -1;
+        at += __popcll(all_ok);
+      }
+    }
+    free = (int)min((long long)a.n_pages, (long long)free + all.x);
+    __syncthreads();
+  }
+  // Asked for: tokens and pages, one after the other.  Who has no room in its row takes no part.
+  Two ask[kBuildEach], all;
+  Two sum = {0, 0};
+#pragma unroll
+  for (int i = 0; i < kBuildEach; ++i) {
+    const bool fits = d[i] > 0 && (long long)old[i] + d[i] <= a.cap;
+    ask[i].x = fits ? d[i] : 0;
+    ask[i].y = fits ? pages_of(a, old[i] + d[i]) - pages_of(a, old[i]) : 0;
+    sum = add(sum, ask[i]);
+  }
+  Two so_far = sum_before(sum, waves, all), given = {0, 0};
+  int taken = 0;
+#pragma unroll
+  for (int i = 0; i < kBuildEach; ++i) {
+    so_far = add(so_far, ask[i]);
+    const bool yes = so_far.x <= (uint32_t)a.n_tokens && (ask[i].y == 0 || so_far.y <= (uint32_t)free);
+    if (!yes) ask[i].x = 0;
+    else if (ask[i].y) taken = (int)so_far.y;
+    if (i < each && s0 + i < n) page_sum[s0 + i] = (int)so_far.y;
+    given.x += ask[i].x;
+    given.y += d[i] > 0 && ask[i].x == 0;
+  }
+  if (taken) atomicMax(&taken_, taken);
+  Two before = sum_before(given, waves, all);
+#pragma unroll
+  for (int i = 0; i < kBuildEach; ++i) {
+    const int s = s0 + i;
+    if (i >= each || s >= n) continue;
+    len[s] = old[i];
+    start[s] = a.q_start[s] = (int)before.x;
+    a.lens_out[s] = kept[i] + (int)ask[i].x + (ask[i].x ? old[i] - kept[i] : 0);
+    before.x += ask[i].x;
+  }
+  taken = taken_;
+  if (tid == 0) {
+    start[n] = a.q_start[n] = (int)all.x;
+    *a.n_free_out = free - taken;
+    if (a.refused) *a.refused = (int)all.y;
+  }
+  __syncthreads();
+  // Page j of those that are taken is the one that lies j below the top
+  for (int j = tid; j < taken; j += nt) {
+    const int s = first_above(page_sum, n, j), i = pages_of(a, len[s]) + j - (s ? page_sum[s - 1] : 0);
+    a.table[(long long)s * a.table_stride + i] = a.free_pages[free - 1 - j];
+  }
+  if constexpr (TOKENS) {
+    for (int t = tid; t < a.n_tokens; t += nt) {
+      int p = -1, page = -1, in_page = 0;
+      if (t < start[n]) {
+        const int s = first_above(start + 1, n, t);
+        p = len[s] + t - start[s];
+        const int i = a.by_page.quot(p), fresh = i - pages_of(a, len[s]);
+        in_page = p - i * a.page_size;
+        page = fresh < 0 ? a.table[(long long)s * a.table_stride + i] : a.free_pages[free - 1 - (s ? page_sum[s - 1] : 0) - fresh];
+      }
+      put_token(a, t, p, page, in_page);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ keys and values by a slot map
+//
+// Row t of keys and values goes to slot slots[t] = page * page_size + place in the page, rounded once to the pages' type; a slot that
+// no page has is left out.  Bound: memory.  A workgroup has a few whole tokens, a thread kStoreEach pieces (what makes 16 bytes in the
+// pages or, wider, in the rows) on their way at once.
+constexpr int kStoreThreads = 256, kStoreEach = 4;
+
+struct StoreArgs {
+  const long long *slots;
+  const void *k, *v;
+  long long k_stride, v_stride;
+  double by_page;                         // 1 / page_size
+  long long n_slots;                      // of the pages
+  int n_tokens, tokens;                   // of the call, of a workgroup
+  Div by_row;                             // pieces of a token: its keys, then its values
+};
+
+template <class T, class C, int HD, bool WIDE>
+__global__ __launch_bounds__(kStoreThreads) void k_store_slots(Cache c, StoreArgs a) {
+  constexpr int PER = 16 / sizeof(T), P = HD / PER;
+  const int first = blockIdx.x * a.tokens, pieces = min(a.tokens, a.n_tokens - first) * (int)a.by_row.d, half = a.by_row.d / 2;
+  for (int at = threadIdx.x; at < pieces; at += kStoreThreads * kStoreEach) {
+    u32x4 w[kStoreEach];
+    long long slot[kStoreEach];
+#pragma unroll
+    for (int n = 0; n < kStoreEach; ++n) {
+      const int i = at + n * kStoreThreads;
+      if (i >= pieces) continue;
+      const int t = a.by_row.quot(i), j = i - t * (int)a.by_row.d;
+      slot[n] = a.slots[first + t];
+      const T *from = j < half ? (const T *)a.k + (first + t) * a.k_stride + j * PER : (const T *)a.v + (first + t) * a.v_stride + (j - half) * PER;
+      if constexpr (WIDE) w[n] = *(const u32x4 *)from;
+      else {
+        T x[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] = from[e];
+        w[n] = *(const u32x4 *)x;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kStoreEach; ++n) {
+      const int i = at + n * kStoreThreads;
+      if (i >= pieces || slot[n] < 0 || slot[n] >= a.n_slots) continue;
+      const int t = a.by_row.quot(i), j = i - t * (int)a.by_row.d, jj = j < half ? j : j - half, h = jj / P, e = jj % P * PER;
+      // (slots are below 2^47: their product with 1 / page_size is off by less than one)
+      long long page = (long long)((double)slot[n] * a.by_page);
+      int place = (int)(slot[n] - page * c.page_size);
+      if (place < 0) { --page; place += c.page_size; }
+      if (place >= c.page_size) { ++page; place -= c.page_size; }
+      C *to = (C *)(j < half ? c.k : c.v) + page * c.page_stride + ((long long)h * c.page_size + place) * HD + e;
+      if constexpr (__is_same(T, C)) *(u32x4 *)to = w[n];
+      else {
+        C y[PER];
+#pragma unroll
+        for (int x = 0; x < PER; ++x) y[x] = (C)(float)((const T *)&w[n])[x];
+        *(u32x4 *)to = *(const u32x4 *)y;
+      }
+    }
+  }
+}
+
+}  // namespace pg
+}  // namespace river

@@ -1,0 +1,485 @@
+"""Attention with common prefixes against a plain 64-bit implementation of its definition, and steps of all operators of the paged cache
+together.  Tolerances: those of test_gpu_pages (its `attention` has them); the parts of a row that are joined add a rounding each, which its
+n 2^-24 for n positions covers, since a part has 128 positions or is one of two."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_18396_amd import binding as B
+from test_gpu_pages import DEV, TYPES, Setup, attention, check, freqs, half_step, turned
+
+pytestmark = pytest.mark.gpu
+
+
+class Shared(Setup):
+    """Sequences of `lens` positions, `new` of them new; group g has the next groups[g][1] sequences, behind the first `lonely` ones, and a
+    prefix of groups[g][0] positions.  The sequences' own entries of whole pages of a prefix name pages that do not exist."""
+
+    def __init__(self, kind, nkv, hd, ps, lens, new, groups, lonely=0, seed=0, layers=1, pad=0, ragged=True, room=0, bounds=True):
+        self.groups, self.of = groups, [-1] * lonely + [g for g, (_, n) in enumerate(groups) for _ in range(n)]
+        self.of += [-1] * (len(lens) - len(self.of))
+        self.common = [-(-p // ps) for p, _ in groups]
+        super().__init__(kind, nkv, hd, ps, lens, new, seed=seed, spare=2 + sum(self.common), layers=layers, pad=pad, ragged=ragged, room=room)
+        self.prefix_host = np.full((max(len(groups), 1), max(self.common + [1]) + 1), -1, dtype=np.int32)
+        at = 0
+        for g, n in enumerate(self.common):
+            self.prefix_host[g, :n] = self.spare[at:at + n]
+            at += n
+        for s, g in enumerate(self.of):
+            if g >= 0:
+                self.host[s, :min(groups[g][0] // ps, self.host.shape[1])] = (-1, 10**9, self.k.shape[1], -2**31)[s % 4]
+        self.table.copy_(torch.from_numpy(self.host))
+        start = lonely + np.concatenate([[0], np.cumsum([n for _, n in groups])]).astype(np.int32)
+        self.make(start, *((max([p for p, _ in groups] + [1]), max([n for _, n in groups] + [1])) if bounds else (None, None)))
+
+    def make(self, start, max_len=None, max_seqs=None):
+        n = len(self.groups)
+        self.prefix_table = torch.from_numpy(self.prefix_host[:n]).to(DEV) if n else torch.zeros(0, 1, dtype=torch.int32, device=DEV)
+        self.prefixes = B.Prefixes(self.prefix_table, torch.tensor([p for p, _ in self.groups], dtype=torch.int32, device=DEV),
+                                   torch.tensor(start, dtype=torch.int32, device=DEV), max_len, max_seqs)
+
+    def rows(self, s, layer=0):
+        k, v, there = super().rows(s, layer)
+        g = self.of[s]
+        if g >= 0:
+            p = np.arange(min(self.groups[g][0], len(k)))
+            entry = self.prefix_host[g][np.minimum(p // self.ps, self.prefix_host.shape[1] - 1)]
+            ok = (entry >= 0) & (entry < self.k.shape[1])
+            page, slot = torch.from_numpy(np.where(ok, entry, 0)).to(DEV).long(), torch.from_numpy(p % self.ps).to(DEV).long()
+            k[:len(p)], v[:len(p)] = self.k[layer][page, :, slot].double(), self.v[layer][page, :, slot].double()
+            there[:len(p)] = torch.from_numpy(ok).to(DEV)
+        return k, v, there
+
+
+def run(st, nq, scale=0.0, std=1.5, layer=0):
+    q = st.randn(st.tokens, nq, st.hd, std=std)
+    out = torch.full_like(q, 7.0)
+    B.river_prefix_attention(st.pages, layer, st.batch, st.prefixes, q, scale, out)
+    want, tol = attention(st, q, scale=scale or None, layer=layer)
+    n = int(st.start[-1])
+    check(out[:n], want[:n], tol[:n], (st.lens, st.new, st.groups))
+    assert bool((out[n:] == 7.0).all())                          # tokens of no sequence
+    return q, out
+
+
+def behind(groups, own, new, lonely=()):
+    """Lengths of the sequences: a prefix, then own[i] positions, then the new ones."""
+    before = [0] * len(lonely) + [p for p, n in groups for _ in range(n)]
+    own = list(lonely) + list(own)
+    before += [0] * (len(own) - len(before))
+    return [b + o + m for b, o, m in zip(before, own, new)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("nkv,rep", [(1, 1), (2, 4), (3, 7), (1, 24), (8, 4)])
+@pytest.mark.parametrize("groups,own", [([(200, 5)], [0, 3, 40, 170, 1]), ([(1000, 2), (64, 0), (17, 3), (513, 1)], [9, 300, 0, 31, 64, 128, 5, 0]),
+                                        ([(2500, 20)], list(range(0, 200, 10)))], ids=str)
+def test_single_tokens(kind, hd, nkv, rep, groups, own):
+    new = [1] * len(own)
+    run(Shared(kind, nkv, hd, 16, behind(groups, own, new), new, groups, ragged=False), nkv * rep)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("hd,nkv,rep", [(64, 2, 4), (128, 1, 8), (128, 2, 1), (64, 1, 3)])
+@pytest.mark.parametrize("groups,own,new,lonely", [([(100, 3)], [0, 7, 60], [2, 5, 1], ()), ([(300, 2), (40, 2)], [10, 200, 0, 5, 90], [4, 0, 9, 1, 2], (50, 3)),
+                                                   ([(700, 4)], [0, 0, 33, 129], [130, 64, 1, 300], ()), ([(4000, 3), (130, 6)], [5] * 9, [3] * 9, (700,))], ids=str)
+@pytest.mark.parametrize("bounds", [True, False])
+def test_several_tokens(kind, hd, nkv, rep, groups, own, new, lonely, bounds):
+    new = [1 + i for i in range(len(lonely))] + new
+    run(Shared(kind, nkv, hd, 16, behind(groups, own, new, lonely), new, groups, lonely=len(lonely), pad=3, bounds=bounds, room=0 if bounds else 300), nkv * rep)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("ps", [1, 7, 20, 64, 1000])
+@pytest.mark.parametrize("prefix", [1, 63, 64, 640, 1001])
+def test_page_sizes(kind, ps, prefix):
+    groups, own, new = [(prefix, 4)], [0, 1, 63, 200], [1, 2, 1, 40]
+    run(Shared(kind, 2, 64, ps, behind(groups, own, new), new, groups, seed=ps), 8)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_large_groups(kind, hd):
+    # several tiles of rows, several splits of keys, several of them the sequences'
+    groups, own = [(3000, 70), (800, 30)], [(i * 37) % 500 for i in range(101)]
+    new = [1] * 101
+    run(Shared(kind, 2, hd, 16, behind(groups, own, new), new, groups, ragged=False, seed=1), 16)
+    new = [1 + i % 6 for i in range(101)]
+    run(Shared(kind, 2, hd, 16, behind(groups, own, new), new, groups, seed=2), 8)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("groups,own,new", [([(20000, 2)], [100, 3000], [1, 1]), ([(50, 2)], [20000, 10], [1, 1]), ([(9000, 2)], [100, 5], [20, 33])], ids=str)
+def test_long_caches(kind, groups, own, new):
+    run(Shared(kind, 1, 128, 16, behind(groups, own, new), new, groups, seed=3), 4)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("max_len,max_seqs", [(1, 1), (1, 2), (64, 3), (10**6, 1000), (0, 0), (2000, 2)])
+def test_more_than_the_bounds_say(kind, max_len, max_seqs):
+    groups = [(1500, 40), (333, 5)]
+    for new in ([1] * 45, [1 + i % 4 for i in range(45)]):
+        st = Shared(kind, 1, 64, 16, behind(groups, [i * 9 for i in range(45)], new), new, groups, seed=4)
+        st.make([0, 40, 45], max_len, max_seqs)
+        run(st, 8)
+        st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=max(new), max_len=100)
+        run(st, 8)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("lens,new", [([0, 300, 5, 128, 129, 1], [1] * 6), ([0, 200, 3, 128, 0, 40], [3, 90, 3, 128, 0, 7]), ([-5, 2, 130, -2**31, 127, 300], [2, 6, 1, 1, 140, 1])],
+                         ids=str)
+def test_sequences_shorter_than_their_prefix(kind, lens, new):
+    """What is below a token's position counts, up to it; a token without a position is zero."""
+    for groups in ([(128, 6)], [(128, 2), (129, 3)], [(1000, 5)]):
+        st = Shared(kind, 2, 64, 16, lens, new, groups, seed=5)
+        q, out = run(st, 8)
+        for s, t, p in st.positions():
+            assert p >= 0 or not bool(out[t].any())
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_prefixes_of_no_positions_and_groups_of_no_sequences(kind):
+    lens = [50, 1, 300, 0, 77]
+    for new in ([1] * 5, [2, 1, 130, 0, 5]):
+        for groups in ([(0, 5)], [(0, 2), (0, 0), (0, 1)], [(5, 0), (100, 0)], []):
+            st = Shared(kind, 2, 64, 16, lens, new, groups, seed=6)
+            q, out = run(st, 8)
+            # nothing is shared: river_paged_attention's rows, up to what joining them in other parts rounds
+            want, tol = attention(st, q)
+            check(B.river_paged_attention(st.pages, 0, st.batch, q), want, tol)
+    st.groups = [(-7, 3)]
+    st.common, st.prefix_host = [0], np.full((1, 2), -1, dtype=np.int32)
+    st.make([1, 4], 64, 3)
+    run(st, 8)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_pages_that_are_not_there(kind):
+    groups, own = [(300, 3), (70, 2)], [40, 0, 200, 100, 3]
+    for new in ([1] * 5, [3, 1, 40, 2, 3]):
+        st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=7)
+        st.prefix_host[0, 3], st.prefix_host[0, 18] = -1, 2**31 - 1
+        st.prefix_host[1, :] = -5                                 # a prefix of which nothing is there
+        st.host[2, 25] = st.k.shape[1]
+        st.table.copy_(torch.from_numpy(st.host))
+        st.make([0, 3, 5], 300, 3)
+        run(st, 8)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("lens,new", [([130, 140, 200, 64, 33], [1] * 5), ([130, 300, 200, 64, 33], [2, 160, 60, 3, 1])], ids=str)
+def test_what_is_not_seen_has_no_influence(kind, bad, lens, new):
+    """Places behind a row's position, of pages that nobody has, and of the prefix's last page behind its end, hold what is not finite."""
+    st = Shared(kind, 2, 64, 16, lens, new, [(130, 4)], lonely=1, seed=8)
+    q = st.randn(st.tokens, 8, 64)
+    clean = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+    used = torch.zeros(st.k.shape[1], 16, dtype=torch.bool, device=DEV)
+    for s, n in enumerate(st.lens):
+        before = 130 if st.of[s] >= 0 else 0
+        for p in range(before, n):
+            used[int(st.host[s, p // 16]), p % 16] = True
+    for p in range(130):
+        used[int(st.prefix_host[0, p // 16]), p % 16] = True
+    for x in (st.k, st.v):
+        x[0] = torch.where(used[:, None, :, None], x[0], bad)
+    assert torch.equal(B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q), clean)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_later_position_is_no_part_of_an_earlier_row(kind, bad, where, hd):
+    """A position holds what is not finite: rows below it are as without, others are not finite where the formula has it."""
+    for lens, new, at in (([300, 320, 290], [40, 1, 3], 270), ([300, 90, 290], [290, 1, 3], 120), ([300, 300], [1, 1], 285), ([310, 300], [25, 1], 290)):
+        st = Shared(kind, 1, hd, 16, lens, new, [(280, len(lens))], seed=9)
+        q = st.randn(st.tokens, 4, hd)
+        clean = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+        x = st.k if where == "k" else st.v
+        in_prefix = at < 280
+        page = st.prefix_host[0, at // 16] if in_prefix else st.host[0, at // 16]
+        x[0, page, 0, at % 16, 5] = bad
+        got = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+        for s, t, p in st.positions():
+            if p < at or not (in_prefix or s == 0):
+                assert torch.equal(got[t], clean[t]), (s, t, p)
+            elif where == "v":
+                assert not bool(got[t, :, 5].isfinite().any()) and torch.equal(got[t, :, 6:], clean[t, :, 6:])
+            elif not math.isinf(bad):
+                assert bool(got[t].isnan().all())
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_rows_that_see_only_scores_of_minus_infinity(kind):
+    st = Shared(kind, 1, 64, 16, [140, 150, 141], [1, 1, 2], [(128, 3)], seed=10)
+    q = st.randn(4, 4, 64).abs() + 0.5
+    st.k[0, :, :, :, 0] = -math.inf
+    st.v[0, :, :, :, 3] = math.inf
+    assert not bool(B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q).any())
+    # one key of the prefix that counts, and is all that does
+    page = int(st.prefix_host[0, 2])
+    st.k[0, page, 0, 5] = 0.0
+    st.v[0, :, :, :, 3] = 1.0
+    got = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+    assert torch.equal(got, st.v[0, page, 0, 5].to(st.act).expand_as(got))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("std,scale", [(8.0, 0.0), (1.0, 3.0), (0.01, 0.05), (200.0, 0.0)])
+def test_scales(kind, std, scale):
+    groups, own = [(400, 6)], [0, 100, 250, 3, 60, 31]
+    for new in ([1] * 6, [3, 70, 1, 9, 40, 2]):
+        run(Shared(kind, 2, 128, 16, behind(groups, own, new), new, groups, seed=11), 8, scale=scale, std=std)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_new_tokens_beyond_their_bound_are_left_out(kind):
+    groups, own, new = [(200, 2), (90, 1)], [5, 60, 3], [7, 300, 40]
+    st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=12)
+    st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=33)
+    q = st.randn(st.tokens, 8, 64)
+    out = torch.full_like(q, 7.0)
+    B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q, out=out)
+    want, tol = attention(st, q)
+    for s, n in enumerate(new):
+        lo = int(st.start[s])
+        check(out[lo:lo + min(n, 33)], want[lo:lo + min(n, 33)], tol[lo:lo + min(n, 33)])
+        assert bool((out[lo + min(n, 33):lo + n] == 7.0).all())
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_strides_and_layers(kind):
+    groups, own = [(100, 2)], [45, 3]
+    for new in ([1, 1], [80, 45]):
+        st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=13, layers=3)
+        wide = st.randn(st.tokens, 8 * 64 * 3)
+        q = wide[:, 64 * 8:64 * 16].unflatten(1, (8, 64))
+        room = torch.full((st.tokens, 12, 64), 7.0, dtype=st.act, device=DEV)
+        out = room[:, 2:10]
+        for layer in range(3):
+            B.river_prefix_attention(st.pages, layer, st.batch, st.prefixes, q, out=out)
+            want, tol = attention(st, q, layer=layer)
+            check(out, want, tol)
+            assert bool((room[:, :2] == 7.0).all()) and bool((room[:, 10:] == 7.0).all())
+
+
+def test_pages_beyond_32_bits():
+    # 2^31 elements and 4 GiB into the pages; only the pages that are used are ever touched
+    stride = 3 * 2 ** 28
+    flat = torch.empty(6 * stride, dtype=torch.bfloat16, device=DEV)
+    k = flat.as_strided((1, 6, 1, 16, 64), (6 * stride, stride, 1024, 64, 1))
+    v = flat[stride // 2:].as_strided((1, 6, 1, 16, 64), (6 * stride, stride, 1024, 64, 1))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(17)
+    for x in (k, v):
+        for p in range(6):
+            x[0, p] = torch.randn(1, 16, 64, generator=g, device=DEV).to(torch.bfloat16)
+    for new in ([1, 1], [5, 30], [3, 20]):
+        st = Shared("bf16", 1, 64, 16, [45, 60], new, [(30, 2)], seed=17)
+        st.k, st.v, st.pages = k, v, B.Pages(k, v)
+        st.prefix_host = np.array([[5, 4]], dtype=np.int32)
+        st.host = np.array([[-1, 0, 3, -1], [-1, 1, 2, 5]], dtype=np.int32)
+        st.table = torch.from_numpy(st.host).to(DEV)
+        st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=max(new), max_len=60)
+        st.make([0, 2], 30, 2)
+        run(st, 32)
+
+
+def test_the_same_call_gives_the_same_bits():
+    for kind in TYPES:
+        for hd in (64, 128):
+            groups, own = [(3000, 20), (700, 12)], [(i * 53) % 400 for i in range(32)]
+            for new in ([1] * 32, [1 + i % 9 for i in range(32)]):
+                st = Shared(kind, 8, hd, 16, behind(groups, own, new), new, groups, seed=18)
+                q = st.randn(st.tokens, 32, hd)
+                first = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+                for _ in range(5):
+                    assert torch.equal(first, B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q))
+
+
+def test_calls_without_sequences_or_tokens():
+    st = Shared("bf16", 2, 64, 16, [40, 30], [1, 1], [(10, 2)], seed=19)
+    q = st.randn(0, 8, 64)
+    assert B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q).shape == (0, 8, 64)
+    nobody = B.Batch(torch.zeros(0, 3, dtype=torch.int32, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV),
+                     torch.zeros(1, dtype=torch.int32, device=DEV))
+    q = st.randn(3, 8, 64)
+    out = torch.full_like(q, 7.0)
+    B.river_prefix_attention(st.pages, 0, nobody, st.prefixes, q, out=out)
+    assert bool((out == 7.0).all())
+
+
+def test_on_another_stream_and_two_at_once():
+    groups = [(900, 6)]
+    st = Shared("bf16", 2, 64, 16, behind(groups, [0, 9, 90, 300, 31, 7], [1] * 6), [1] * 6, groups, ragged=False, seed=20)
+    qs = [st.randn(6, 8, 64) for _ in range(2)]
+    want = [B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q) for q in qs]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(sides[i]):
+                got[i].append(B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, qs[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i])
+
+
+def test_the_binding_refuses():
+    st = Shared("bf16", 2, 64, 16, [40, 30], [1, 1], [(10, 2)], seed=21)
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32, device=DEV)
+    for a in ((i32(2, 3), i32(1), i32(2)), (i32(1, 3), i32(1), i32(1)), (i32(1, 3).long(), i32(1), i32(2)), (i32(1, 3).cpu(), i32(1).cpu(), i32(2).cpu()),
+              (i32(1, 3), i32(1), i32(4)[::2]), (i32(3, 2).t(), i32(2), i32(3)), (i32(1, 0), i32(1), i32(2))):
+        with pytest.raises(ValueError):
+            B.Prefixes(*a)
+    with pytest.raises(AttributeError):
+        st.prefixes.max_len = 5
+    q = st.randn(2, 8, 64)
+    for bad in (q.float(), q[:, :, :32], q.transpose(0, 1), q.cpu()):
+        with pytest.raises(ValueError):
+            B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, bad)
+    for kw in (dict(scale=-1.0), dict(out=q)):
+        with pytest.raises(B.RiverError):
+            B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q, **kw)
+    with pytest.raises(B.RiverError):
+        B.river_prefix_attention(st.pages, 1, st.batch, st.prefixes, q)
+    with pytest.raises(B.RiverError):                             # heads that do not divide
+        B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, st.randn(2, 7, 64))
+
+
+# ------------------------------------------------------------------ all of them together
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rotary", [True, False])
+def test_steps_of_a_server(kind, rotary):
+    """Two system prompts are laid out, stored and read by sequences that come, grow, draft, give back and leave, layer by layer: the step
+    is captured once, every replay's rows are those of attention over the whole history of each sequence, and in the end every page is free."""
+    act, kvt = TYPES[kind]
+    nkv, nq, hd, ps, L, n_pages, n = 2, 8, 64, 8, 2, 90, 6
+    g = torch.Generator(device=DEV)
+    g.manual_seed(22)
+    r = np.random.default_rng(5)
+    k, v = (torch.full((L, n_pages, nkv, ps, hd), math.nan, dtype=kvt, device=DEV) for _ in range(2))
+    pages = B.Pages(k, v, act)
+    f, m = freqs(hd, "ramp")
+    rope = B.Rope(f, "half", m)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    # rows 0 and 1 are the prompts, the others sequences: 2, 3, 4 go on from the first, 5, 6 from the second, 7 from none
+    shared = torch.zeros(n + 2, dtype=torch.int32, device=DEV)
+    t = B.Tables.empty(n_pages, ps, n + 2, 16, n_shared=shared)
+    lens = [37, 16]
+    group = [0, 0, 0, 1, 1, -1]
+    history = [[] for _ in range(n + 2)]
+    T = 64
+    d, start = i32([0] * (n + 2)), i32([0] * (n + 3))
+    slots, positions, refused = torch.zeros(T, dtype=torch.int64, device=DEV), i32([0] * T), i32([0])
+    batch = B.Batch(t.table, t.lens, start, max_new=T, max_len=128)
+    prefixes = B.Prefixes(t.table[:2], t.lens[:2], i32([2, 5, 7]), max_len=40, max_seqs=3)
+    x = torch.zeros(L, T, nq + 2 * nkv, hd, dtype=act, device=DEV)
+    outs = [torch.full((T, nq, hd), 7.0, dtype=act, device=DEV) for _ in range(L)]
+
+    def step():
+        B.river_build_batch(t, d, start, slots, positions, refused)
+        for l in range(L):
+            q, kk, vv = x[l, :, :nq], x[l, :, nq:nq + nkv], x[l, :, nq + nkv:]
+            if rotary:
+                q = B.river_rope_store(pages, l, batch, q, kk, vv, rope, out=queries[l])
+            else:
+                B.river_store_slots(pages, l, slots, kk, vv)
+            B.river_prefix_attention(pages, l, batch, prefixes, q, out=outs[l])
+
+    queries = [torch.zeros(T, nq, hd, dtype=act, device=DEV) for _ in range(L)]
+    graph = None
+
+    def advance(want, expect_refused=0):
+        """want: new positions of every row of the table."""
+        nonlocal graph
+        d.copy_(i32(want))
+        x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        for o in outs:
+            o.fill_(7.0)
+        if graph is None and len(history[2]):
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                step()
+        graph.replay() if graph is not None else step()
+        assert refused.item() == expect_refused
+        at = start.tolist()
+        for s in range(n + 2):
+            got = at[s + 1] - at[s]
+            if want[s] < 0:
+                history[s] = history[s][:max(0, len(history[s]) + want[s])]
+                assert got == 0
+            if not got:
+                continue
+            have = len(history[s])
+            assert got == want[s] and positions[at[s]:at[s + 1]].tolist() == list(range(have, have + got))
+            new = slice(at[s], at[s + 1])
+            cols = []
+            for l in range(L):
+                kk, vv = x[l, new, nq:nq + nkv], x[l, new, nq + nkv:]
+                if rotary:
+                    kk = turned(kk, list(range(have, have + got)), f, m, "half")[0]
+                cols.append((kk.to(kvt).double(), vv.to(kvt).double()))
+            history[s] = history[s] + [[(cols[l][0][i], cols[l][1][i]) for l in range(L)] for i in range(got)]
+            for l in range(L):
+                K, V = (torch.stack([h[l][i] for h in history[s]]) for i in range(2))
+                q = (queries[l] if rotary else x[l, :, :nq])[new]
+                j, p = torch.arange(have + got, device=DEV), torch.arange(have, have + got, device=DEV)[:, None]
+                for h in range(nq):
+                    w = torch.where(j <= p, q[:, h].double() @ K[:, h // 4].t() / 8, -math.inf).softmax(-1)
+                    o, a = w @ V[:, h // 4], w @ V[:, h // 4].abs()
+                    # (rotated keys of the cache and of this oracle may round to neighbours: see test_gpu_pages.test_a_serving_loop)
+                    most = (q[:, h].double().abs() @ K[:, h // 4].abs().t()).amax(1, keepdim=True) / 8
+                    e = most * ((2 * half_step(kvt) if rotary else 0.0) + (hd + 8) * 2.0 ** -24) + 2.0 ** -20
+                    check(outs[l][new, h], o, half_step(act) * o.abs() + a * (half_step(kvt) + 2 * e + 200 * 2.0 ** -24), (s, l, h))
+        for o in outs:
+            assert bool((o[at[-1]:] == 7.0).all())
+
+    def join(s):
+        """A sequence goes on from its prompt: whole pages are the prompt's, the last, half full one is copied."""
+        p = group[s - 2]
+        whole = lens[p] // ps
+        t.table[s, :whole] = t.table[p, :whole]
+        shared[s] = whole
+        if lens[p] % ps:
+            t.lens[s] = whole * ps
+            d.copy_(i32([lens[p] % ps if i == s else 0 for i in range(n + 2)]))
+            B.river_build_batch(t, d, start)
+            src, dst = int(t.table[p, whole]), int(t.table[s, whole])
+            B.river_copy_pages(pages, [src], [dst])
+            assert t.lens[s].item() == lens[p]
+        else:
+            t.lens[s] = lens[p]
+        history[s] = list(history[p])
+
+    advance(lens + [0] * n)                                      # the prompts themselves, which are nobody's followers
+    for s in range(2, 7):
+        join(s)
+    advance([0, 0, 5, 1, 9, 2, 1, 20])
+    for i in range(3):
+        advance([0, 0, 1, 1, 1, 1, 1, 1])
+    advance([0, 0, 4, 4, 4, 4, 4, 4])                             # drafts, of which some are rejected
+    advance([0, 0, -4, -1, 0, -2, -3, -4])
+    advance([0, 0, 1, 1, 1, 1, 1, 1])
+    advance([0, 0, -2**31, 0, 0, -2**31, 0, 0])                   # two leave (their prompts' pages stay), and come again
+    history[2], history[5] = [], []
+    assert t.table[2].tolist() == t.table[0, :4].tolist() + [-1] * 12 and t.table[5].tolist() == t.table[1, :2].tolist() + [-1] * 14
+    for s in (2, 5):
+        join(s)
+    advance([0, 0, 7, 1, 1, 8, 1, 1])
+    advance([0, 0, 1, 1, 1, 1, 1, 200], expect_refused=1)         # one has no room in its row and waits
+    advance([0, 0, 1, 1, 1, 1, 1, 1])
+    advance([0, 0] + [-2**31] * n)
+    shared.zero_()
+    t.table[2:].fill_(-1)
+    advance([-2**31] * 2 + [0] * n)
+    assert sorted(t.free_pages.tolist()) == list(range(n_pages)) and t.n_free.item() == n_pages and not bool(t.lens.any())

@@ -1,0 +1,370 @@
+"""A step laid out on the device (river_build_batch, river_store_slots) against plain statements of what they do.  Whole numbers are equal;
+a stored element is off by half a step of the pages' type at most: it is torch's own rounding of the same number."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_18396_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": (torch.float32, torch.float32), "bf16": (torch.bfloat16, torch.bfloat16), "bf16-f16": (torch.bfloat16, torch.float16)}
+LOWEST = -2**31
+
+
+class Model:
+    """Table, lengths and free list as lists; step is what river_build_batch says it does, one sequence and page after the other."""
+
+    def __init__(self, table, lens, stack, n_pages, ps, shared=None):
+        self.table, self.lens, self.stack, self.n_pages, self.ps = [list(r) for r in table], list(lens), list(stack), n_pages, ps
+        self.shared = shared or [0] * len(lens)
+
+    def pages(self, n):
+        return -(-max(n, 0) // self.ps)
+
+    def step(self, d, n_tokens):
+        for s in reversed(range(len(d))):
+            if d[s] < 0:
+                n = max(self.lens[s], 0)
+                kept = max(0, n + d[s])
+                for i in reversed(range(max(self.pages(kept), self.shared[s]), min(self.pages(n), len(self.table[s])))):
+                    if 0 <= self.table[s][i] < self.n_pages:
+                        self.stack.append(self.table[s][i])
+                    self.table[s][i] = -1
+                self.lens[s] = kept
+        tokens = pages = refused = 0
+        start, slots, positions = [0], [], []
+        free = list(reversed(self.stack))
+        taken = 0
+        cap = min(2**30, len(self.table[0]) * self.ps) if self.table else 0
+        for s in range(len(d)):
+            n, got = max(self.lens[s], 0), 0
+            if d[s] > 0:
+                if n + d[s] <= cap:
+                    need = self.pages(n + d[s]) - self.pages(n)
+                    tokens, pages = tokens + d[s], pages + need
+                    if tokens <= n_tokens and (need == 0 or pages <= len(self.stack)):
+                        got = d[s]
+                        for i in range(need):
+                            self.table[s][self.pages(n) + i] = free[pages - need + i]
+                        taken = max(taken, pages) if need else taken
+                        for p in range(n, n + got):
+                            e = self.table[s][p // self.ps]
+                            slots.append(e * self.ps + p % self.ps if 0 <= e < self.n_pages else -1)
+                            positions.append(p)
+                        self.lens[s] = n + got
+                refused += got == 0
+            start.append(start[-1] + got)
+        self.stack = self.stack[:len(self.stack) - taken]
+        return start, slots, positions, refused
+
+
+class Device:
+    """The same on the device, among memory that must stay as it is."""
+
+    def __init__(self, m, room=0, extra=0, lens_out=False):
+        n, width = len(m.lens), len(m.table[0])
+        self.m = m
+        self.wide = torch.full((n, width + extra), 77, dtype=torch.int32, device=DEV)
+        self.table = self.wide[:, :width]
+        self.table.copy_(torch.tensor(m.table, dtype=torch.int32))
+        self.lens = torch.tensor(m.lens, dtype=torch.int32, device=DEV)
+        self.free = torch.full((m.n_pages,), -5, dtype=torch.int32, device=DEV)
+        self.free[:len(m.stack)] = torch.tensor(m.stack, dtype=torch.int32)
+        self.n_free = torch.tensor([len(m.stack)], dtype=torch.int32, device=DEV)
+        self.lens_out = torch.full_like(self.lens, -9) if lens_out else self.lens
+        self.n_free_out = torch.full_like(self.n_free, -9) if lens_out else self.n_free
+        self.tables = B.Tables(self.table, self.lens, self.free, self.n_free, m.ps, torch.tensor(m.shared, dtype=torch.int32, device=DEV),
+                               self.lens_out, self.n_free_out)
+        self.q_start = torch.full((n + 1,), -9, dtype=torch.int32, device=DEV)
+
+    def step(self, d, n_tokens, what=("slots", "positions", "refused")):
+        slots = torch.full((n_tokens,), 55, dtype=torch.int64, device=DEV) if "slots" in what else None
+        positions = torch.full((n_tokens,), 55, dtype=torch.int32, device=DEV) if "positions" in what else None
+        refused = torch.full((1,), 55, dtype=torch.int32, device=DEV) if "refused" in what else None
+        B.river_build_batch(self.tables, torch.tensor(d, dtype=torch.int32, device=DEV), self.q_start, slots, positions, refused, n_tokens)
+        start, want_slots, want_positions, want_refused = self.m.step(d, n_tokens)
+        assert self.q_start.tolist() == start
+        pad = n_tokens - len(want_slots)
+        if slots is not None:
+            assert slots.tolist() == want_slots + [-1] * pad
+        if positions is not None:
+            assert positions.tolist() == want_positions + [0] * pad
+        if refused is not None:
+            assert refused.item() == want_refused
+        self.check()
+        return start
+
+    def check(self):
+        assert self.lens_out.tolist() == self.m.lens
+        assert self.table.tolist() == self.m.table
+        assert self.n_free_out.item() == len(self.m.stack)
+        assert self.free[:len(self.m.stack)].tolist() == self.m.stack
+        assert bool((self.wide[:, self.table.shape[1]:] == 77).all())
+
+
+def fresh(seed, n, ps, most, spare, width=None, shared=False, holes=False):
+    """A model of n sequences of up to `most` positions, and `spare` free pages."""
+    r = np.random.default_rng(seed)
+    lens = [int(x) for x in r.integers(0, most + 1, n)]
+    need = [-(-x // ps) for x in lens]
+    width = width or max(need + [1]) + 4
+    order = [int(x) for x in r.permutation(sum(need) + spare)]
+    table = []
+    for x in need:
+        row, order = order[:x], order[x:]
+        if holes and x > 2:
+            row[1] = -1                          # given back behind a window, say
+        table.append(row + [-1] * (width - x))
+    return Model(table, lens, order[:spare], max(sum(need) + spare, 1), ps, [int(x) for x in r.integers(0, 3, n)] if shared else None), r
+
+
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 300, 1024, 1025, 4096])
+@pytest.mark.parametrize("ps", [1, 7, 16, 300])
+def test_build_steps(n, ps):
+    most = 500 if n < 300 else 40
+    m, r = fresh(n * 1000 + ps, n, ps, most, 3 * n * (1 + 20 // ps), width=most // ps + 60)
+    dev = Device(m, extra=3)
+    for i in range(6):
+        d = r.integers(-30, 21, n) if i % 2 else np.ones(n, dtype=int)
+        d[r.random(n) < 0.2] = 0
+        dev.step([int(x) for x in d], int(d.clip(0).sum()) + (0, 5, 300)[i % 3])
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_build_where_something_runs_out(seed):
+    r = np.random.default_rng(seed)
+    n, ps = int(r.integers(1, 200)), int(r.choice([1, 3, 16, 64]))
+    m, r = fresh(seed, n, ps, 200, int(r.integers(0, 30)), width=200 // ps + 2, shared=True, holes=True)
+    dev = Device(m, extra=seed % 2)
+    for i in range(8):
+        d = [int(x) for x in r.choice([0, 1, 1, 2, 17, 90, 5000, -1, -7, -100, LOWEST, 2**31 - 1], n)]
+        tokens = int(r.choice([0, 1, 10, 300, 5000]))
+        dev.step(d, tokens, (("slots", "positions", "refused"), ("slots",), ("positions",), ())[i % 4])
+
+
+def test_build_of_long_prompts():
+    # more tokens than a workgroup has threads, many of them in one sequence
+    for lens, d, ps in (([0], [100000], 16), ([5, 0, 70], [3, 70000, 9000], 7), ([0] * 200, [777] * 200, 64), ([1 << 20], [5], 1)):
+        need = sum(-(-(a + b) // ps) for a, b in zip(lens, d))
+        width, at = max(-(-(a + b) // ps) for a, b in zip(lens, d)), 0
+        table = []
+        for a in lens:
+            x = -(-a // ps)
+            table.append(list(range(at, at + x)) + [-1] * (width - x))
+            at += x
+        Device(Model(table, lens, list(range(at, need + 2)), need + 2, ps)).step(d, sum(d) + 3)
+
+
+def test_build_gives_back_what_it_gave():
+    m, r = fresh(3, 90, 16, 300, 900)
+    dev = Device(m)
+    free, table, lens = dev.free.clone(), dev.table.clone(), dev.lens.clone()
+    for _ in range(3):
+        d = [int(x) for x in r.integers(0, 100, 90)]
+        start = dev.step(d, sum(d))
+        dev.step([a - b for a, b in zip(start, start[1:])], 0, ())       # (some had no room in their rows)
+        assert torch.equal(dev.free, free) and torch.equal(dev.table, table) and torch.equal(dev.lens, lens)
+    # and all of it: every page is free again
+    dev.step([LOWEST] * 90, 0, ())
+    assert sorted(dev.free.tolist()) == list(range(m.n_pages)) and bool((dev.table == -1).all()) and not bool(dev.lens.any())
+
+
+def test_build_ahead_of_a_step():
+    m, r = fresh(4, 40, 16, 100, 200)
+    dev = Device(m, lens_out=True)
+    d = [int(x) for x in r.integers(0, 40, 40)]
+    before = dev.lens.clone(), dev.free.clone()
+    dev.step(d, sum(d))
+    assert torch.equal(dev.lens, before[0]) and torch.equal(dev.free, before[1])
+
+
+def test_build_of_far_lengths():
+    # the last positions that a row can have, and lengths that none has
+    ps, width = 65536, 1 << 14
+    top = 2**30
+    table = [[0] + [-1] * (width - 2) + [1], [-1] * width, [-1] * (width - 1) + [2], [-1] * width, [-1] * width]
+    m = Model(table, [top - 3, -7, top, 2**31 - 1, LOWEST], [5, 4, 3], 6, ps)
+    dev = Device(m)
+    dev.step([3, 2, 1, 1, 0], 10)
+    dev.step([1, 0, 0, -1, 70000], 70000)
+    dev.step([-5, -2**31, -(2**31 - 1), 2**31 - 1, -3], 10)
+
+
+def test_build_with_lists_that_hold_nonsense():
+    # counts out of range and pages that do not exist are kept within the arrays
+    for n_free in (-3, 1000):
+        table = torch.full((2, 4), -1, dtype=torch.int32, device=DEV)
+        table[0, 0] = 9999
+        lens, free = torch.tensor([3, 0], dtype=torch.int32, device=DEV), torch.tensor([7000, -2, 1], dtype=torch.int32, device=DEV)
+        t = B.Tables(table, lens, free, torch.tensor([n_free], dtype=torch.int32, device=DEV), 4)
+        start, slots = torch.zeros(3, dtype=torch.int32, device=DEV), torch.zeros(8, dtype=torch.int64, device=DEV)
+        B.river_build_batch(t, torch.tensor([1, 7], dtype=torch.int32, device=DEV), start, slots)
+        assert t.n_free.item() == (0 if n_free < 0 else 1)
+        # (page 1 is there, page -2 is not; the last entry of the first row names none)
+        assert slots.tolist() == [-1] * 8 if n_free < 0 else [-1, 4, 5, 6, 7, -1, -1, -1]
+
+
+def test_build_without_sequences():
+    t = B.Tables.empty(4, 16, 0, 3)
+    start, slots = torch.full((1,), 9, dtype=torch.int32, device=DEV), torch.zeros(5, dtype=torch.int64, device=DEV)
+    B.river_build_batch(t, torch.zeros(0, dtype=torch.int32, device=DEV), start, slots)
+    assert start.item() == 0 and slots.tolist() == [-1] * 5 and t.n_free.item() == 4
+
+
+def test_build_is_captured():
+    """One token more for every sequence that goes on, captured once and replayed: pages come and go with the lengths."""
+    n, ps = 20, 4
+    t = B.Tables.empty(200, ps, n, 12)
+    m = Model([[-1] * 12 for _ in range(n)], [0] * n, list(range(199, -1, -1)), 200, ps)
+    d, start = torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros(n + 1, dtype=torch.int32, device=DEV)
+    slots, positions, refused = (torch.zeros(k, dtype=x, device=DEV) for k, x in ((64, torch.int64), (64, torch.int32), (1, torch.int32)))
+    r = np.random.default_rng(1)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        B.river_build_batch(t, d, start, slots, positions, refused)
+    for i in range(30):
+        step = [int(x) for x in r.choice([0, 1, 1, 1, 3, 9, -2, -50], n)]
+        d.copy_(torch.tensor(step, dtype=torch.int32))
+        if i % 3 == 2:
+            B.river_build_batch(t, d, start, slots, positions, refused)
+        else:
+            graph.replay()
+        want = m.step(step, 64)
+        assert (start.tolist(), refused.item()) == (want[0], want[3])
+        assert slots.tolist() == want[1] + [-1] * (64 - len(want[1])) and positions.tolist() == want[2] + [0] * (64 - len(want[2]))
+        assert t.lens.tolist() == m.lens and t.table.tolist() == m.table and t.free_pages[:t.n_free.item()].tolist() == m.stack
+
+
+# ------------------------------------------------------------------ the store
+
+def slots_of(seed, n_pages, ps, n, holes):
+    r = np.random.default_rng(seed)
+    slots = r.permutation(n_pages * ps)[:n].astype(np.int64)
+    if holes:
+        slots[::3] = r.choice([-1, -2**63, n_pages * ps, 2**62, -ps], len(slots[::3]))
+    return torch.from_numpy(slots).to(DEV)
+
+
+def want_store(k, v, slots, new_k, new_v, layer, ps):
+    k, v = k.clone(), v.clone()
+    for t, x in enumerate(slots.tolist()):
+        if 0 <= x < k.shape[1] * ps:
+            k[layer, x // ps, :, x % ps] = new_k[t].float().to(k.dtype)
+            v[layer, x // ps, :, x % ps] = new_v[t].float().to(v.dtype)
+    return k, v
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("hd,nkv", [(64, 1), (64, 3), (128, 8), (128, 2), (64, 40)])
+@pytest.mark.parametrize("ps,n,pad", [(16, 1, 0), (1, 33, 8), (7, 100, 1), (300, 257, 5), (16, 0, 0)])
+def test_store(kind, hd, nkv, ps, n, pad):
+    act, kvt = TYPES[kind]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n + hd)
+    n_pages = n // ps * 2 + 3
+    both = torch.randn(3, 2, n_pages, nkv, ps, hd, generator=g, device=DEV).to(kvt)
+    k, v = both[:, 0], both[:, 1]
+    pages = B.Pages(k, v, act)
+    rows = torch.randn(n, 2 * nkv * hd + pad, generator=g, device=DEV).mul_(3).to(act)
+    new_k, new_v = rows[:, pad:nkv * hd + pad].unflatten(1, (nkv, hd)), rows[:, nkv * hd + pad:].unflatten(1, (nkv, hd))
+    for layer, holes in ((1, False), (2, True)):
+        slots = slots_of(n + ps, n_pages, ps, n, holes)
+        want = want_store(k, v, slots, new_k, new_v, layer, ps)
+        B.river_store_slots(pages, layer, slots, new_k, new_v)
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
+def test_store_keeps_bits():
+    # what a type has of infinities and NaN stays as it is; bf16 beyond fp16's range is infinite
+    x = torch.tensor([math.nan, math.inf, -math.inf, 1e30, -0.0, 1e-30, 65504.0, 70000.0] * 8, device=DEV)
+    for kind, (act, kvt) in TYPES.items():
+        k, v = (torch.zeros(1, 2, 1, 16, 64, dtype=kvt, device=DEV) for _ in range(2))
+        new = x.to(act).view(1, 1, 64)
+        B.river_store_slots(B.Pages(k, v, act), 0, torch.tensor([21], device=DEV), new, new)
+        want = new[0].float().to(kvt)
+        for pages in (k, v):
+            assert torch.equal(pages[0, 1, :, 5].nan_to_num(7.0), want.nan_to_num(7.0)) and torch.equal(pages[0, 1, :, 5].isnan(), want.isnan())
+            if act == kvt:
+                bits = torch.int32 if act == torch.float32 else torch.int16
+                assert torch.equal(pages[0, 1, :, 5].view(bits), new[0].view(bits))
+
+
+def test_store_beyond_32_bits():
+    # 2^31 elements and 4 GiB into the pages, slots beyond 2^32; only the pages that are used are ever touched
+    stride, ps = 3 * 2 ** 28, 16
+    flat = torch.empty(6 * stride, dtype=torch.bfloat16, device=DEV)
+    k = flat.as_strided((1, 6, 1, ps, 64), (6 * stride, stride, 1024, 64, 1))
+    v = flat[stride // 2:].as_strided((1, 6, 1, ps, 64), (6 * stride, stride, 1024, 64, 1))
+    new = torch.randn(4, 1, 64, device=DEV).to(torch.bfloat16)
+    B.river_store_slots(B.Pages(k, v), 0, torch.tensor([95, 80, 3, 96], device=DEV), new, -new)
+    for t, (page, slot) in enumerate([(5, 15), (5, 0), (0, 3)]):
+        assert torch.equal(k[0, page, :, slot], new[t]) and torch.equal(v[0, page, :, slot], -new[t])
+    del flat, k, v
+    # many small pages: 4.3 GiB of 512 bytes a slot
+    pages = torch.zeros(1, 140000, 1, 256, 64, dtype=torch.bfloat16, device=DEV)
+    got = B.Pages(pages, torch.zeros_like(pages))
+    last = pages.shape[1] * 256 - 1
+    slots = torch.tensor([last, last - 256, 255, 256], device=DEV)
+    B.river_store_slots(got, 0, slots, new, new)
+    for t, x in enumerate(slots.tolist()):
+        assert torch.equal(pages[0, x // 256, 0, x % 256], new[t, 0])
+    assert int(pages.any(-1).sum()) == 4
+
+
+def test_store_on_another_stream_and_captured():
+    k, v = (torch.zeros(1, 8, 2, 16, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    pages = B.Pages(k, v)
+    x, y = (torch.randn(20, 2, 64, device=DEV).to(torch.bfloat16) for _ in range(2))
+    slots = slots_of(1, 8, 16, 20, True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        B.river_store_slots(pages, 0, slots, x, y)
+    for i in range(4):
+        want = want_store(k, v, slots, x, y, 0, 16)
+        if i == 2:
+            with torch.cuda.stream(side):
+                side.wait_stream(torch.cuda.default_stream())
+                B.river_store_slots(pages, 0, slots, x, y)
+            torch.cuda.current_stream().wait_stream(side)
+        else:
+            graph.replay()
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+        x.copy_(torch.randn(20, 2, 64, device=DEV))
+        slots.copy_(slots_of(i + 5, 8, 16, 20, i % 2 == 0))
+
+
+def test_the_binding_refuses():
+    t = B.Tables.empty(8, 16, 3, 4)
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32, device=DEV)
+    for a in ((i32(2), i32(4)), (i32(3), i32(3)), (i32(3).long(), i32(4)), (i32(3).cpu(), i32(4)), (i32(6)[::2], i32(4)), (i32(3), i32(4), i32(5)),
+              (i32(3), i32(4), i32(5).long(), i32(4)), (i32(3), i32(4), None, None, i32(2))):
+        with pytest.raises(ValueError):
+            B.river_build_batch(t, *a)
+    with pytest.raises(B.RiverError):
+        B.river_build_batch(t, i32(3), i32(4), n_tokens=-1)
+    for kw in (dict(lens=i32(2)), dict(lens=i32(3).long()), dict(free_pages=i32(4, 2)), dict(n_free=i32(2)), dict(n_shared=i32(2)), dict(lens_out=i32(4)),
+               dict(table=i32(4, 3).t()), dict(table=i32(3, 4).cpu())):
+        d = dict(table=i32(3, 4), lens=i32(3), free_pages=i32(8), n_free=i32(1), page_size=16)
+        d.update(kw)
+        with pytest.raises(ValueError):
+            B.Tables(**d)
+    with pytest.raises(B.RiverError):
+        B.river_build_batch(B.Tables.empty(8, 0, 3, 4), i32(3), i32(4))
+    with pytest.raises(AttributeError):
+        t.lens = i32(3)
+    k = torch.zeros(1, 8, 2, 16, 64, device=DEV)
+    pages, rows = B.Pages(k, k.clone()), torch.zeros(5, 2, 64, device=DEV)
+    slots = torch.zeros(5, dtype=torch.int64, device=DEV)
+    for a in ((slots[:4], rows, rows), (slots.int(), rows, rows), (slots.cpu(), rows, rows), (slots, rows, rows[:4]), (slots, rows.bfloat16(), rows),
+              (slots, rows[:, :1], rows), (torch.zeros(10, dtype=torch.int64, device=DEV)[::2], rows, rows)):
+        with pytest.raises(ValueError):
+            B.river_store_slots(pages, 0, *a)
+    with pytest.raises(B.RiverError):
+        B.river_store_slots(pages, 1, slots, rows, rows)
