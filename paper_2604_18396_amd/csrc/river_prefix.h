@@ -15,8 +15,9 @@ struct Prefixes {
   const int *table, *lens, *seq_start;
   int n_groups, max_pages, table_stride;
   int cap;                                // positions that a row has entries for
-  int tiles, n_splits, least;             // tiles of a group's rows (further ones are taken in turn), splits of its keys at most, keys of a split at least
+  int tiles, n_splits, least;             // of all groups' rows at most, splits of a prefix at most, keys of a split at least
   unsigned units;                         // workgroups of the prefixes; 0: a sequence's rows go through its prefix too
+  float shift;                            // added to the prefixes' maxima: both kernels scale fp16 probabilities, by different powers of two
 };
 
 // How many of n ascending numbers are at most x.  All lanes of a wavefront ask alike.
@@ -67,16 +68,44 @@ __device__ __forceinline__ int my_row(int r0, int r1) {           // this lane's
   return min(r0 + (TR == kAttnRows ? (int)threadIdx.x % 16 : (int)threadIdx.x / 64 * 32 + (int)threadIdx.x % 32), r1);
 }
 
-// Tile `tile` of group g's rows with split z of its prefix.  A token without a position (it has no result) counts as one
-// that sees all, so that it costs the others nothing.
+// Tile `tile` of all groups' rows, one group after the other, with split z of its group's prefix.  A token without a position (it
+// has no result) counts as one that sees all, so that it costs the others nothing.
 template <int TR>
-__device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int g, int tile, int z, int head, Share &w) {
-  const int n = prefix_len(x, g), parts = split_count(n, x.n_splits, x.least), len = split_len(n, x.n_splits, x.least);
-  if (n == 0 || z >= parts) return false;
-  const int s0 = min(max(x.seq_start[g], 0), b.n_seq), s1 = min(max(x.seq_start[g + 1], s0), b.n_seq);
-  const int t0 = b.q_start ? min(max(b.q_start[s0], 0), b.n_tokens) : s0, t1 = b.q_start ? min(max(b.q_start[s1], t0), b.n_tokens) : s1;
-  const int rows = (t1 - t0) * a.rep, r0 = tile * TR;
-  if (r0 >= rows) return false;
+__device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int tile, int z, int head, Share &w) {
+  // a lane a group: where its tiles begin
+  const int lane = threadIdx.x % 64;
+  int g, s0, s1, t0, rows, n;
+  for (int g0 = 0;; g0 += 64) {
+    if (g0 >= x.n_groups) return false;
+    g = min(g0 + lane, x.n_groups - 1);
+    s0 = min(max(x.seq_start[g], 0), b.n_seq);
+    s1 = min(max(x.seq_start[g + 1], s0), b.n_seq);
+    n = prefix_len(x, g);
+    t0 = b.q_start ? min(max(b.q_start[s0], 0), b.n_tokens) : s0;
+    rows = ((b.q_start ? min(max(b.q_start[s1], t0), b.n_tokens) : s1) - t0) * a.rep;
+    const int tiles = g0 + lane < x.n_groups && n ? (rows + TR - 1) / TR : 0;
+    int upto = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    const unsigned long long behind = __ballot(tile < upto);
+    if (behind) {
+      const int it = __ffsll(behind) - 1;
+      tile -= __builtin_amdgcn_readlane(upto - tiles, it);
+      g = __builtin_amdgcn_readlane(g, it);
+      s0 = __builtin_amdgcn_readlane(s0, it);
+      s1 = __builtin_amdgcn_readlane(s1, it);
+      n = __builtin_amdgcn_readlane(n, it);
+      t0 = __builtin_amdgcn_readlane(t0, it);
+      rows = __builtin_amdgcn_readlane(rows, it);
+      break;
+    }
+    tile -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  const int parts = split_count(n, x.n_splits, x.least), len = split_len(n, x.n_splits, x.least), r0 = tile * TR;
+  if (z >= parts || (unsigned)tile >= (unsigned)((rows + TR - 1) / TR)) return false;
   w.r0 = r0;
   w.r1 = min(r0 + TR - 1, rows - 1);
   const int t = t0 + a.by_rep.quot(my_row<TR>(r0, w.r1));
@@ -145,30 +174,40 @@ __device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, cons
   return true;
 }
 
-// Sixteen rows a unit, of either kind.  Bound and layout: see k_attn_split.
-template <class T, class C, int HD>
-__global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share_split(Cache c, Batch b, AttnArgs a, Prefixes x) {
-  __shared__ __align__(16) char lds[kAttnWaves * SplitLds<C, HD>::AREA];
-  __shared__ float2 res_ml[kAttnWaves][16];
-  const bool common = blockIdx.x < x.units;
-  int tile, s, z, head;
-  if (common) {
-    const unsigned u = blockIdx.x / c.n_kv_heads, v = u / x.tiles;
-    head = blockIdx.x % c.n_kv_heads;
-    tile = u % x.tiles;
-    z = v % x.n_splits;
-    s = v / x.n_splits;
-  } else work_of(blockIdx.x - x.units, c, b, a, tile, s, z, head);
+// PM, OM: tiles of 128 rows (many_unit) of the groups, of the sequences; else of 16 (split_unit).  Bounds and layouts: see there.
+template <class T, class C, int HD, bool PM, bool OM>
+struct ShareLds {
+  static constexpr int SPLIT = kAttnWaves * SplitLds<C, HD>::AREA, RES = kAttnWaves * 16 * 8, MANY = PM || OM ? Many<C, HD>::LDS : 0;
+  static constexpr int BYTES = (PM && OM) || MANY > SPLIT + RES ? MANY : SPLIT + RES;
+};
+template <class T, class C, int HD, bool PM, bool OM>
+__global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share(Cache c, Batch b, AttnArgs a, Prefixes x) {
+  extern __shared__ __align__(1024) char lds[];
+  constexpr int PR = PM ? Many<C, HD>::ROWS : kAttnRows, OR = OM ? Many<C, HD>::ROWS : kAttnRows;
   Share w;
   w.n_parts = (x.units ? x.n_splits : 0) + a.n_splits;
-  for (;;) {
-    if (!(common ? prefix_unit<kAttnRows>(x, b, a, s, tile, z, head, w) : own_unit<kAttnRows>(x, b, a, s, tile, z, head, w))) return;
+  auto split = [&] {
     const int early[2][Tile<C, HD>::KB] = {};
     float v[RowPart<HD>::E];
-    split_unit<T, C, HD>(c, a, w, lds, res_ml, false, early, v);
-    if (!common) return;
-    tile += x.tiles;
-    __syncthreads();
+    split_unit<T, C, HD>(c, a, w, lds, (float2(*)[16])(lds + ShareLds<T, C, HD, PM, OM>::SPLIT), false, early, v);
+  };
+  int tile, s, z, head;
+  if constexpr (!OM) {                    // (sequences whose rows fill such tiles go through their prefixes themselves)
+    if (blockIdx.x < x.units) {
+      const unsigned u = blockIdx.x / c.n_kv_heads;
+      if (!prefix_unit<PR>(x, b, a, u % x.tiles, u / x.tiles, blockIdx.x % c.n_kv_heads, w)) return;
+      if constexpr (PM) {
+        many_unit<T, C, HD>(c, a, w, lds);
+        return;
+      }
+    } else {
+      work_of(blockIdx.x - x.units, c, b, a, tile, s, z, head);
+      if (!own_unit<OR>(x, b, a, s, tile, z, head, w)) return;
+    }
+    split();
+  } else {
+    work_of(blockIdx.x, c, b, a, tile, s, z, head);
+    if (own_unit<OR>(x, b, a, s, tile, z, head, w)) many_unit<T, C, HD>(c, a, w, lds);
   }
 }
 
@@ -200,7 +239,8 @@ __global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixe
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int y = 0; y < common + own; ++y) {
     const long long part = row + (y < common ? y : before + y - common);
-    const float2 ml = a.part_ml[part];
+    float2 ml = a.part_ml[part];
+    if (y < common) ml.x += x.shift;
     const f32x4 o = *(const f32x4 *)(a.part_o + part * HD + e0);
     const float now = fmaxf(big, ml.x), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(big - now), g = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - now);
     sum = sum * f + g * ml.y;

@@ -2,6 +2,7 @@
 #include "river.h"
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -26,8 +27,9 @@ const char *bad_prefixes(const river_prefixes *x) {
 
 // How a call is divided: units of a group's rows and its prefix, units of a sequence's rows and its own keys.
 struct SharePlan {
+  bool many, p_many;                                             // tiles of 128 rows: of the sequences, of the prefixes
   int max_new, tiles, n_splits, least;                           // of the sequences
-  int p_tiles, p_splits, p_least;                                // of the prefixes
+  int p_tiles, p_splits, p_least;                                // of the prefixes, of all groups
   long long units;                                               // workgroups of the prefixes
   size_t o_bytes, bytes;                                         // of the partial results
 };
@@ -36,23 +38,33 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
   SharePlan y{};
   const int rep = nq / p->n_kv_heads;
   y.max_new = b->q_start ? std::min(b->max_new, b->n_tokens) : 1;
-  // Both kinds: three workgroups a CU of at least 128 keys, eight where that leaves them 512 (see plan_attention)
-  auto splits = [&](long long groups, long long keys) {
-    auto by = [&](long long goal, long long least) { return std::min({goal / std::max(1ll, groups), (keys + least - 1) / least, 64ll}); };
-    return (int)std::max(1ll, std::max(by(768, 128), by(2048, 512)));
-  };
-  const long long rows = (long long)y.max_new * rep;
-  y.tiles = (int)((rows + kAttnRows - 1) / kAttnRows);
+  const long long rows = (long long)y.max_new * rep, group_rows = std::min<long long>(b->n_tokens, (long long)x->max_seqs * y.max_new) * rep;
   const long long common = x->n_groups ? std::min<long long>({x->max_len, (long long)x->max_pages * p->page_size, kMostPositions}) : 0;
   const long long keys = std::min<long long>({b->max_len, std::max<long long>((long long)b->max_pages * p->page_size, common), kMostPositions});
-  y.least = y.p_least = 128;
-  if (common && x->max_seqs > 1) {
-    const long long group_rows = std::min<long long>(b->n_tokens, (long long)x->max_seqs * y.max_new) * rep;
-    y.p_tiles = (int)((group_rows + kAttnRows - 1) / kAttnRows);
-    y.p_splits = splits((long long)x->n_groups * p->n_kv_heads * y.p_tiles, common);
-    y.units = (long long)x->n_groups * p->n_kv_heads * y.p_tiles * y.p_splits;
+  constexpr int kManyRows = Many<__bf16, 128>::ROWS;
+  if (!common || x->max_seqs <= 1 || (p->dtype == RIVER_BF16 && rows >= kManyRows)) {
+    const AttnPlan o = plan_attention(p, b, nq, 0, 0);
+    y.many = y.p_many = o.many;
+    y.tiles = o.tiles;
+    y.n_splits = o.n_splits;
+    y.least = o.split_len;
+  } else {
+    // Both kinds: three workgroups a CU of at least 128 keys, eight where that leaves them 512 (see plan_attention)
+    auto splits = [&](long long groups, long long keys) {
+      auto by = [&](long long goal, long long least) { return std::min({goal / std::max(1ll, groups), (keys + least - 1) / least, 64ll}); };
+      return (int)std::max(1ll, std::max(by(768, 128), by(2048, 512)));
+    };
+    y.p_many = p->dtype == RIVER_BF16 && group_rows > kAttnRows;
+    y.least = y.p_least = 128;
+    const int tile = y.p_many ? kManyRows : kAttnRows;
+    // (each group may have a tile that is not full)
+    y.p_tiles = (int)std::min<long long>(((long long)b->n_tokens * rep + tile - 1) / tile + x->n_groups - 1, INT_MAX);
+    const long long groups = std::min<long long>(y.p_tiles, x->n_groups * ((group_rows + tile - 1) / tile)) * p->n_kv_heads;
+    y.p_splits = y.p_many ? (int)std::max(1ll, std::min({512 / std::max(1ll, groups), (common + 255) / 256, 64ll})) : splits(groups, common);
+    y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;
+    y.tiles = (int)((rows + kAttnRows - 1) / kAttnRows);
+    y.n_splits = splits((long long)b->n_seq * p->n_kv_heads * y.tiles, std::max(1ll, keys - common));
   }
-  y.n_splits = splits((long long)b->n_seq * p->n_kv_heads * y.tiles, y.units ? std::max(1ll, keys - common) : keys);
   if (y.units || y.n_splits > 1) {
     const size_t parts = (size_t)b->n_tokens * nq * ((y.units ? y.p_splits : 0) + y.n_splits);
     y.o_bytes = parts * p->head_dim * 4;
@@ -105,18 +117,30 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
     const int rep = n_q_heads / pages->n_kv_heads;
     auto turn = [](long long round) { int k = 0; while ((round << k) % 32) ++k; return k; };
     const int turn_z = turn((long long)y.n_splits * c.n_kv_heads), turn_s = turn((long long)b.n_seq * y.n_splits * c.n_kv_heads);
-    const AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale2, 0, 0, y.n_splits, y.least, y.tiles, kAttnRows, turn_s, turn_z,
+    const AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale2, 0, 0, y.n_splits, y.least, y.tiles, y.many ? Many<__bf16, 128>::ROWS : kAttnRows, turn_s, turn_z,
                      y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), nullptr};
     const Prefixes x{prefixes->table, prefixes->lens, prefixes->seq_start, prefixes->n_groups, prefixes->max_pages, prefixes->table_stride,
                      (int)std::min<long long>((long long)prefixes->max_pages * pages->page_size, kMostPositions), std::max(1, y.p_tiles),
-                     std::max(1, y.p_splits), y.p_least, (unsigned)y.units};
+                     std::max(1, y.p_splits), y.p_least, (unsigned)y.units,
+                     y.p_many && !y.many && pages->kv_dtype == RIVER_KV_F16 ? Mat<_Float16>::kBias - Mat<_Float16>::kLazyBias : 0.f};
     const long long groups = y.units + (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
     const int chunks_of = 256 / (pages->head_dim / 4), chunks = (n_q_heads + chunks_of - 1) / chunks_of;
     if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * chunks * 256 >= (1ll << 32))
       return refuse("too many sequences, groups, tokens and heads");
     const hipStream_t st = (hipStream_t)hip_stream;
     hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
-      return launch(k_share_split<decltype(t), decltype(ct), decltype(hd)::v>, dim3((unsigned)groups), dim3(kAttnThreads), 0, st, c, b, a, x);
+      typedef decltype(t) T;
+      typedef decltype(ct) C;
+      constexpr int HD = decltype(hd)::v;
+      auto go = [&](auto pm, auto om) {
+        constexpr bool PM = decltype(pm)::value, OM = decltype(om)::value;
+        return launch_lds<k_share<T, C, HD, PM, OM>>(dim3((unsigned)groups), dim3(kAttnThreads), ShareLds<T, C, HD, PM, OM>::BYTES, st, c, b, a, x);
+      };
+      if constexpr (sizeof(T) == 2) {
+        if (y.many) return go(True{}, True{});
+        if (y.p_many) return go(True{}, False{});
+      }
+      return go(False{}, False{});
     });
     if (e == hipSuccess && y.bytes)
       e = by_types(pages, [&](auto t, auto, auto hd) {
