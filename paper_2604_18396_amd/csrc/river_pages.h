@@ -51,6 +51,19 @@ __device__ __forceinline__ int seq_of(const Batch &b, int t) {
   return lo < b.n_seq && t >= b.q_start[lo] ? lo : -1;
 }
 
+// How many of n ascending numbers are at most x.  All lanes of a wavefront ask alike.
+__device__ __forceinline__ int count_up_to(const int *v, int n, int x) {
+  const int lane = threadIdx.x % 64;
+  int lo = 0;
+  while (n > 64) {
+    const int step = (n + 63) / 64, c = __popcll(__ballot(lane * step < n && v[lo + min(lane * step, n - 1)] <= x));
+    if (c == 0) return lo;
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  return lo + __popcll(__ballot(lane < n && v[lo + min(lane, max(n - 1, 0))] <= x));
+}
+
 // The position of token t of sequence s, negative if it has none.
 __device__ __forceinline__ int position_of(const Batch &b, int s, int t) {
   int first, count;

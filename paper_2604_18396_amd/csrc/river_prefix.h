@@ -20,19 +20,6 @@ struct Prefixes {
   float shift;                            // added to the prefixes' maxima: both kernels scale fp16 probabilities, by different powers of two
 };
 
-// How many of n ascending numbers are at most x.  All lanes of a wavefront ask alike.
-__device__ __forceinline__ int count_up_to(const int *v, int n, int x) {
-  const int lane = threadIdx.x % 64;
-  int lo = 0;
-  while (n > 64) {
-    const int step = (n + 63) / 64, c = __popcll(__ballot(lane * step < n && v[lo + min(lane * step, n - 1)] <= x));
-    if (c == 0) return lo;
-    lo += (c - 1) * step;
-    n = min(step, n - (c - 1) * step);
-  }
-  return lo + __popcll(__ballot(lane < n && v[lo + min(lane, max(n - 1, 0))] <= x));
-}
-
 __device__ __forceinline__ int group_of(const Prefixes &x, int s) {      // or -1
   if (x.n_groups == 0) return -1;
   const int g = __builtin_amdgcn_readfirstlane(count_up_to(x.seq_start, x.n_groups + 1, s)) - 1;
@@ -211,12 +198,27 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share(Cache 
   }
 }
 
-// A row's parts, joined: those of its group's prefix, then its sequence's own.  A workgroup has RB heads of one token.
+// A row's parts, joined: those of its group's prefix, then its sequence's own.  A workgroup has RB heads of one token, and where a row has
+// many parts G groups of lanes that take other parts each; their sums are added in their order.  Bound: latency; so the first parts are on
+// their way before it is known which of them there are.
 template <class T, int HD, int RB>
 __global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixes x, int chunks) {
-  constexpr int LANES = HD / 4;
-  static_assert(RB * LANES == 256, "a thread has four elements of a row");
-  const int t = blockIdx.x / chunks, h = blockIdx.x % chunks * RB + threadIdx.x / LANES, e0 = threadIdx.x % LANES * 4;
+  constexpr int LANES = HD / 4, G = 256 / (RB * LANES), AT_ONCE = 8;
+  const int t = blockIdx.x / chunks, in = threadIdx.x / LANES % RB, group = threadIdx.x / (LANES * RB), e0 = threadIdx.x % LANES * 4;
+  const int h = min(blockIdx.x % chunks * RB + in, a.nq - 1);
+  const int before = x.units ? x.n_splits : 0, n_parts = before + a.n_splits;
+  const long long row = ((long long)t * a.nq + h) * n_parts;
+  float2 ml[AT_ONCE];
+  f32x4 o[AT_ONCE];
+  auto fetch = [&](int y0) {
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const long long part = row + min(y0 + k * G, n_parts - 1);
+      ml[k] = a.part_ml[part];
+      o[k] = *(const f32x4 *)(a.part_o + part * HD + e0);
+    }
+  };
+  fetch(group);
   int s = t;
   if (b.q_start) {
     s = __builtin_amdgcn_readfirstlane(count_up_to(b.q_start, b.n_seq + 1, t)) - 1;
@@ -228,25 +230,61 @@ __global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixe
   if (i >= min(count, a.max_new)) return;
   const int len = length_of(b, s), n = prefix_len(x, group_of(x, s)), low = x.units ? n : 0;
   const int common = low ? split_count(n, x.n_splits, x.least) : 0;
-  // the last row of this one's tile: see own_unit
+  // (the last row of this one's tile: see own_unit)
   const int r = i * a.rep + h % a.rep, r1 = min(r - r % a.tile_rows + a.tile_rows, min(count, a.max_new) * a.rep) - 1;
   const int keys = max(0, min(new_position(len, count, a.by_rep.quot(r1)) + 1, max(b.cap, n)) - low);
   const int own = split_count(keys, a.n_splits, a.split_len);
-  if (common + own == 1 || h >= a.nq) return;
-  const int before = x.units ? x.n_splits : 0, n_parts = before + a.n_splits;
-  const long long row = ((long long)t * a.nq + h) * n_parts;
   float big = -INFINITY, sum = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int y = 0; y < common + own; ++y) {
-    const long long part = row + (y < common ? y : before + y - common);
-    float2 ml = a.part_ml[part];
-    if (y < common) ml.x += x.shift;
-    const f32x4 o = *(const f32x4 *)(a.part_o + part * HD + e0);
-    const float now = fmaxf(big, ml.x), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(big - now), g = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - now);
-    sum = sum * f + g * ml.y;
-    v = v * f + g * o;
+  for (int y0 = group;;) {
+    float now = big;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const int y = y0 + k * G;
+      const bool there = y < common || (y >= before && y < before + own);
+      if (y < common) ml[k].x += x.shift;
+      if (!there) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      now = fmaxf(now, ml[k].x);
+    }
+    const float off = now == -INFINITY ? 0.f : now, f = __builtin_amdgcn_exp2f(big - off);
+    sum *= f;
+    v *= f;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const float p = __builtin_amdgcn_exp2f(ml[k].x - off);
+      sum += p * ml[k].y;
+      v += p * o[k];
+    }
     big = now;
+    y0 += AT_ONCE * G;
+    if (y0 - group >= before + own) break;
+    fetch(y0);
   }
+  if constexpr (G > 1) {
+    __shared__ f32x4 part_v[G][RB][LANES];
+    __shared__ float2 part_ml[G][RB];
+    part_v[group][in][threadIdx.x % LANES] = v;
+    if (e0 == 0) part_ml[group][in] = make_float2(big, sum);
+    __syncthreads();
+    if (group) return;
+    float top = big;
+#pragma unroll
+    for (int k = 1; k < G; ++k) top = fmaxf(top, part_ml[k][in].x);
+    const float off = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(big - off);
+    sum *= f;
+    v *= f;
+#pragma unroll
+    for (int k = 1; k < G; ++k) {
+      const float2 m = part_ml[k][in];
+      const float p = __builtin_amdgcn_exp2f(m.x - off);
+      sum += p * m.y;
+      v += p * part_v[k][in][threadIdx.x % LANES];
+    }
+  }
+  if (common + own == 1 || blockIdx.x % chunks * RB + in >= a.nq) return;          // (it is done already, or no row)
   if (new_position(len, count, i) < 0) sum = 0.f;                // (a token without a position sees nothing)
   const float out[4] = {v[0], v[1], v[2], v[3]};
   store_row<T, 4>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, out, sum);

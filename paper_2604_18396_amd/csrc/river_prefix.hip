@@ -124,7 +124,10 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
                      std::max(1, y.p_splits), y.p_least, (unsigned)y.units,
                      y.p_many && !y.many && pages->kv_dtype == RIVER_KV_F16 ? Mat<_Float16>::kBias - Mat<_Float16>::kLazyBias : 0.f};
     const long long groups = y.units + (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
-    const int chunks_of = 256 / (pages->head_dim / 4), chunks = (n_q_heads + chunks_of - 1) / chunks_of;
+    // (rows of a workgroup of the join: eight parts a thread, where there are more the lanes of several rows have one)
+    const int parts = (y.units ? y.p_splits : 0) + y.n_splits, fit = 1024 / pages->head_dim;
+    const int each = std::max(1, std::min(fit, fit * 8 / std::max(8, parts))), heads = each >= fit ? fit : each >= 4 ? 4 : each >= 2 ? 2 : 1;
+    const int chunks = (n_q_heads + heads - 1) / heads;
     if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * chunks * 256 >= (1ll << 32))
       return refuse("too many sequences, groups, tokens and heads");
     const hipStream_t st = (hipStream_t)hip_stream;
@@ -145,7 +148,12 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
     if (e == hipSuccess && y.bytes)
       e = by_types(pages, [&](auto t, auto, auto hd) {
         constexpr int HD = decltype(hd)::v;
-        return launch(k_share_join<decltype(t), HD, 1024 / HD>, dim3((unsigned)(b.n_tokens * chunks)), dim3(256), 0, st, b, a, x, chunks);
+        typedef decltype(t) T;
+        const dim3 grid((unsigned)(b.n_tokens * chunks)), block(256);
+        return heads == 1   ? launch(k_share_join<T, HD, 1>, grid, block, 0, st, b, a, x, chunks)
+               : heads == 2 ? launch(k_share_join<T, HD, 2>, grid, block, 0, st, b, a, x, chunks)
+               : heads == 4 ? launch(k_share_join<T, HD, 4>, grid, block, 0, st, b, a, x, chunks)
+                            : launch(k_share_join<T, HD, 1024 / HD>, grid, block, 0, st, b, a, x, chunks);
       });
     return e == hipSuccess ? RIVER_OK : hip_failed("river_prefix_attention", e);
   });

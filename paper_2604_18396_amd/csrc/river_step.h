@@ -95,7 +95,9 @@ __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
   if (tid == 0) taken_ = 0;
   if (__syncthreads_or(back)) {
     // Given back: entries from .. to - 1 of a row that name pages, the last one of the last sequence first onto the free list, so that
-    // pages that a call has given out come to lie as they lay before it.  A wavefront a row: how many, then where.
+    // pages that a call has given out come to lie as they lay before it.  Sixteen lanes a row: how many, then where.
+    const int sub = tid % 16, shift = lane / 16 * 16;
+    auto mine_of = [&](bool ok) { return (uint32_t)(__ballot(ok) >> shift) & 0xffffu; };
 #pragma unroll
     for (int i = 0; i < kBuildEach; ++i) {
       const int s = s0 + i;
@@ -105,12 +107,14 @@ __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
       page_sum[s] = d[i] < 0 ? min(pages_of(a, old[i]), a.max_pages) : from;
     }
     __syncthreads();
-    for (int s = tid / 64; s < n; s += nt / 64) {
+    for (int s = tid / 16; s < n; s += nt / 16) {
       const int *row = a.table + (long long)s * a.table_stride;
       int count = 0;
-      for (int at = start[s]; at < page_sum[s]; at += 64)
-        count += __popcll(__ballot(at + lane < page_sum[s] && (unsigned)row[min(at + lane, a.max_pages - 1)] < (unsigned)a.n_pages));
-      if (lane == 0) len[s] = count;
+      for (int i = start[s] + sub; i - sub < page_sum[s]; i += 16) {
+        const int page = i < page_sum[s] ? row[i] : -1;
+        count += __popc(mine_of((unsigned)page < (unsigned)a.n_pages));
+      }
+      if (sub == 0) len[s] = count;
     }
     __syncthreads();
     Two mine = {0, 0}, all;
@@ -126,18 +130,17 @@ __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
         len[s0 + i] = free + behind;
       }
     __syncthreads();
-    for (int s = tid / 64; s < n; s += nt / 64) {
+    for (int s = tid / 16; s < n; s += nt / 16) {
       int *row = a.table + (long long)s * a.table_stride;
       int at = len[s];
-      for (int to = page_sum[s]; to > start[s]; to -= 64) {
-        const int i = to - 1 - lane;
+      for (int i = page_sum[s] - 1 - sub; i + sub >= start[s]; i -= 16) {
         const int page = i >= start[s] ? row[i] : -1;
         const bool ok = (unsigned)page < (unsigned)a.n_pages;
-        const unsigned long long all_ok = __ballot(ok);
-        const int to_list = at + __popcll(all_ok & ((1ull << lane) - 1));
-        if (ok && to_list < a.n_pages) a.free_pages[to_list] = page;
+        const uint32_t all_ok = mine_of(ok);
+        const int to = at + __popc(all_ok & ((1u << sub) - 1));
+        if (ok && to < a.n_pages) a.free_pages[to] = page;
         if (i >= start[s]) row[i] = -1;
-        at += __popcll(all_ok);
+        at += __popc(all_ok);
       }
     }
     free = (int)min((long long)a.n_pages, (long long)free + all.x);
@@ -200,6 +203,35 @@ __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
       }
       put_token(a, t, p, page, in_page);
     }
+  }
+}
+
+// The tokens' slots and positions in a launch of their own, from what k_build has left: where there are more than a workgroup does
+// quickly.  A wavefront has 256 tokens.
+constexpr int kSlotsEach = 4;
+__global__ __launch_bounds__(256) void k_slots(BuildArgs a) {
+  const int lane = threadIdx.x % 64, t0 = (blockIdx.x * 4 + threadIdx.x / 64) * 64 * kSlotsEach, n = a.n_seq;
+  if (t0 >= a.n_tokens) return;
+  const int total = a.q_start[n];
+  // the sequences of the first token and of the last one
+  const int from = count_up_to(a.q_start, n + 1, t0) - 1, upto = count_up_to(a.q_start, n + 1, t0 + 64 * kSlotsEach - 1) - 1;
+#pragma unroll
+  for (int j = 0; j < kSlotsEach; ++j) {
+    const int t = t0 + j * 64 + lane;
+    if (t >= a.n_tokens) return;
+    int p = -1, page = -1, in_page = 0;
+    if (t < total) {
+      int s = from, hi = min(upto, n - 1) + 1;
+      while (s + 1 < hi) {
+        const int mid = (s + hi) >> 1;
+        if (a.q_start[mid] <= t) s = mid; else hi = mid;
+      }
+      p = a.lens_out[s] + t - a.q_start[s + 1];
+      const int i = a.by_page.quot(p);
+      page = a.table[(long long)s * a.table_stride + i];
+      in_page = p - i * a.page_size;
+    }
+    put_token(a, t, p, page, in_page);
   }
 }
 

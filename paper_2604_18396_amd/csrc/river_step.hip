@@ -12,6 +12,9 @@
 using namespace river;
 using namespace river::pg;
 
+// More tokens than these have a launch of their own
+constexpr int kTokensInOne = 4096;
+
 extern "C" int river_build_batch(const river_tables *t, const int32_t *n_new, int32_t n_tokens, int32_t *q_start, int64_t *slots,
                                  int32_t *positions, int32_t *refused, void *hip_stream) {
   return guarded([&]() -> int {
@@ -28,12 +31,15 @@ extern "C" int river_build_batch(const river_tables *t, const int32_t *n_new, in
     const BuildArgs a{t->table, t->lens, n_new, t->n_free, t->n_shared, t->lens_out, t->free_pages, t->n_free_out, t->n_seq, t->max_pages,
                       t->table_stride, t->n_pages, t->page_size, n_tokens, (int)std::min<long long>((long long)t->max_pages * t->page_size, kMostPositions),
                       div_by(t->page_size), q_start, (long long *)slots, positions, refused};
-    const bool tokens = slots || positions;
-    // a thread a sequence or a token, as far as one workgroup reaches
-    const int threads = std::min(kBuildThreads, std::max({64, t->n_seq, tokens ? n_tokens : 0}) + 63 & ~63);
+    const bool tokens = slots || positions, apart = tokens && n_tokens > kTokensInOne;
+    // Threads: sixteen a sequence, which may give pages back, and one a token, as far as one workgroup reaches
+    const int threads = std::min(kBuildThreads, std::max({64, 16 * t->n_seq, tokens ? n_tokens : 0}) + 63 & ~63);
     const size_t lds = (3 * (size_t)t->n_seq + 1) * 4;
-    const hipError_t e = tokens ? launch(k_build<true>, dim3(1), dim3(threads), lds, (hipStream_t)hip_stream, a)
-                                : launch(k_build<false>, dim3(1), dim3(threads), lds, (hipStream_t)hip_stream, a);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = tokens && !apart ? launch(k_build<true>, dim3(1), dim3(threads), lds, st, a)
+                                    : launch(k_build<false>, dim3(1), dim3(threads), lds, st, a);
+    if (e == hipSuccess && apart)
+      e = launch(k_slots, dim3((n_tokens + 256 * kSlotsEach - 1) / (256 * kSlotsEach)), dim3(256), 0, st, a);
     return e == hipSuccess ? RIVER_OK : hip_failed("river_build_batch", e);
   });
 }
