@@ -385,13 +385,13 @@ typedef struct {
  * of positions below lens[g] are not read (they may be -1: river_rope_store and river_store_slots do not need them for later positions
  * either).  A prefix need not end with a page: its last page and the sequence's own entry of the same positions are two pages then, each with
  * its own positions.  A token whose position is below the prefix's length sees what comes up to it.
- * Arguments, roundings and errors as in river_paged_attention; no tickets.  max_new: as there; further tokens are left out.
+ * Arguments, roundings and errors as in river_paged_attention, tickets and a max_new that leaves tokens out among them.
  * workspace: as there, of the bytes that river_prefix_attention_workspace gives. */
 int river_prefix_attention_workspace(const river_pages *pages, const river_batch *batch, const river_prefixes *prefixes,
                                      int32_t n_q_heads, size_t *bytes);
 int river_prefix_attention(const river_pages *pages, int32_t layer, const river_batch *batch, const river_prefixes *prefixes,
                            int32_t n_q_heads, const void *q, int64_t q_stride, float scale, void *out, int64_t out_stride,
-                           void *workspace, size_t workspace_bytes, void *hip_stream);
+                           void *workspace, size_t workspace_bytes, int32_t *tickets, void *hip_stream);
 
 /* Writes keys and values as they are (rounded once to the cache's type) to slots of `layer`: token t's to slot slots[t] % page_size of
  * page slots[t] / page_size.  A slot below 0, or of no page, is left out: a place of the batch without a token.  Two tokens

@@ -140,7 +140,7 @@ def load():
     L.river_build_batch.argtypes = [C.POINTER(river_tables), ptr, i32, ptr, ptr, ptr, ptr, ptr]
     L.river_store_slots.argtypes = [pages, i32, ptr, i32, ptr, i64, ptr, i64, ptr]
     L.river_prefix_attention_workspace.argtypes = [pages, batch, prefixes, i32, C.POINTER(C.c_size_t)]
-    L.river_prefix_attention.argtypes = [pages, i32, batch, prefixes, i32, ptr, i64, C.c_float, ptr, i64, ptr, C.c_size_t, ptr]
+    L.river_prefix_attention.argtypes = [pages, i32, batch, prefixes, i32, ptr, i64, C.c_float, ptr, i64, ptr, C.c_size_t, ptr, ptr]
     L.river_save_pages.argtypes = [ptr, i32, i32, i32, pages, ptr, i32]
     L.river_load_pages.argtypes = [ptr, i32, i32, i32, pages, ptr, i32]
     _lib = L
@@ -816,10 +816,12 @@ def river_prefix_attention(pages: Pages, layer: int, batch: Batch, prefixes: Pre
         if len(prefixes._bytes) >= 256:
             prefixes._bytes.clear()
         nbytes = prefixes._bytes[key] = got.value
-    # (from torch's allocator, call by call: see river_paged_attention)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=pages.device).data_ptr() if nbytes else None
+    stream, ws, tickets = _stream(pages.index), None, None
+    if nbytes:
+        memory = torch.empty(nbytes, dtype=torch.uint8, device=pages.device)        # (call by call: see river_paged_attention)
+        ws, tickets = memory.data_ptr(), _tickets(pages.index, stream)
     _check_call(L.river_prefix_attention(pages.ref, layer, ref, shared, heads, q.data_ptr(), qs, scale, out.data_ptr(), os_, ws, nbytes,
-                                         _stream(pages.index)))
+                                         tickets, stream))
     return out
 
 

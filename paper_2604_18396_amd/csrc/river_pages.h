@@ -804,10 +804,30 @@ __device__ __forceinline__ void split_unit(const Cache &c, const AttnArgs &a, co
   }
 }
 
+// The last workgroup of a tile joins its rows' parts, in their order.
+template <class T, int HD, class Keys, class Rows>
+__device__ __forceinline__ void join_last(const AttnArgs &a, const Unit<Keys, Rows> &w, int parts, long long ticket_) {
+  constexpr int E = RowPart<HD>::E, LANES = RowPart<HD>::LANES;
+  __shared__ unsigned int order;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  unsigned int *const ticket = a.tickets + ticket_;
+  if (threadIdx.x == 0) order = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (order != (unsigned)parts - 1) return;
+  if (threadIdx.x == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const int row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
+  if (w.r0 + row > w.r1) return;
+  const int to = a.by_rep.quot(w.r0 + row), oh = w.head * a.rep + (w.r0 + row - to * a.rep);
+  float v[E], sum;
+  join_parts<HD, E>(a, ((w.row0 + to) * a.nq + oh) * w.n_parts, parts, e0, v, sum);
+  store_row<T, E>((T *)a.out + (long long)(w.first_token + to) * a.out_stride + (long long)oh * HD + e0, v, sum);
+}
+
 template <class T, class C, int HD>
 __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(Cache c, Batch b, AttnArgs a) {
   typedef Mat<C> M;
-  constexpr int KB = Tile<C, HD>::KB, E = RowPart<HD>::E, LANES = RowPart<HD>::LANES;
+  constexpr int KB = Tile<C, HD>::KB, E = RowPart<HD>::E;
   __shared__ __align__(16) char lds[kAttnWaves * SplitLds<C, HD>::AREA];
   __shared__ float2 res_ml[kAttnWaves][16];
   int tile, s, z, head;
@@ -834,21 +854,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
   float v[E];
   split_unit<T, C, HD>(c, a, w, lds, res_ml, !a.window, early, v);
   if (parts == 1 || !a.tickets) return;
-  // The last workgroup of the tile joins the parts, in their order
-  __shared__ unsigned int order;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  unsigned int *const ticket = a.tickets + ((long long)s * c.n_kv_heads + head) * a.tiles + tile;
-  if (threadIdx.x == 0) order = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (order != (unsigned)parts - 1) return;
-  if (threadIdx.x == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const int row = threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
-  if (r0 + row > r1) return;
-  const int to = a.by_rep.quot(r0 + row), oh = head * a.rep + (r0 + row - to * a.rep);
-  float sum;
-  join_parts<HD, E>(a, ((w.row0 + to) * a.nq + oh) * a.n_splits, parts, e0, v, sum);
-  store_row<T, E>((T *)a.out + (long long)(first_token + to) * a.out_stride + (long long)oh * HD + e0, v, sum);
+  join_last<T, HD>(a, w, parts, (s * c.n_kv_heads + head) * a.tiles + tile);
 }
 
 // ------------------------------------------------------------------ attention of many rows (16-bit pages)

@@ -130,7 +130,7 @@ __device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, c
 
 // Tile `tile` of sequence s's rows with split z of its own keys (of all that it sees, where the prefixes have no units).
 template <int TR>
-__device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int s, int tile, int z, int head, Share &w) {
+__device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int s, int tile, int z, int head, Share &w, int &parts) {
   int first_token, count;
   seq_tokens(b, s, first_token, count);
   const int rows = min(count, a.max_new) * a.rep, r0 = tile * TR;
@@ -140,7 +140,8 @@ __device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, cons
   const int g = group_of(x, s), n = prefix_len(x, g), len = length_of(b, s);
   const int lo = new_position(len, count, a.by_rep.quot(r0)), hi = new_position(len, count, a.by_rep.quot(w.r1));
   const int low = x.units ? n : 0, keys = max(0, min(hi + 1, max(b.cap, n)) - low);
-  const int parts = split_count(keys, a.n_splits, a.split_len), each = split_len(keys, a.n_splits, a.split_len);
+  const int each = split_len(keys, a.n_splits, a.split_len);
+  parts = split_count(keys, a.n_splits, a.split_len);
   if (z >= parts) return false;
   w.sp = {lo, hi, 0, low, keys};
   if constexpr (TR == kAttnRows) w.rows = {new_position(len, count, a.by_rep.quot(my_row<TR>(r0, w.r1))), lo, hi};
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share(Cache 
     float v[RowPart<HD>::E];
     split_unit<T, C, HD>(c, a, w, lds, (float2(*)[16])(lds + ShareLds<T, C, HD, PM, OM>::SPLIT), false, early, v);
   };
-  int tile, s, z, head;
+  int tile, s, z, head, parts;
   if constexpr (!OM) {                    // (sequences whose rows fill such tiles go through their prefixes themselves)
     if (blockIdx.x < x.units) {
       const unsigned u = blockIdx.x / c.n_kv_heads;
@@ -189,12 +190,15 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share(Cache 
       }
     } else {
       work_of(blockIdx.x - x.units, c, b, a, tile, s, z, head);
-      if (!own_unit<OR>(x, b, a, s, tile, z, head, w)) return;
+      if (!own_unit<OR>(x, b, a, s, tile, z, head, w, parts)) return;
     }
     split();
+    if constexpr (!PM) {                  // (tickets: there are no prefixes' units)
+      if (a.tickets && parts > 1) join_last<T, HD>(a, w, parts, (s * c.n_kv_heads + head) * a.tiles + tile);
+    }
   } else {
     work_of(blockIdx.x, c, b, a, tile, s, z, head);
-    if (own_unit<OR>(x, b, a, s, tile, z, head, w)) many_unit<T, C, HD>(c, a, w, lds);
+    if (own_unit<OR>(x, b, a, s, tile, z, head, w, parts)) many_unit<T, C, HD>(c, a, w, lds);
   }
 }
 

@@ -31,8 +31,22 @@ struct SharePlan {
   int max_new, tiles, n_splits, least;                           // of the sequences
   int p_tiles, p_splits, p_least;                                // of the prefixes, of all groups
   long long units;                                               // workgroups of the prefixes
+  bool fused;                                                    // last workgroups join the splits, where they have tickets
   size_t o_bytes, bytes;                                         // of the partial results
 };
+
+// Prefixes have units of their own where that saves enough of reading them for each sequence: 24 MB, or 8 MB of a long one.  (A call then
+// takes two launches, and its parts are written and read.  us, apart / each sequence through its prefix, 8B shape, 64 positions of their own:
+// 2 sequences behind 1024 11.7 / 9.9, behind 4096 12.8 / 15.5; 8 behind 1024 12.1 / 11.9; 16 behind 256 11.8 / 9.8, behind 1024 12.9 / 19.7;
+// 64 behind 16384 40 / 472; 1B shape: 2 behind 4096 11.8 / 11.6, 16 behind 1024 11.8 / 11.6, 32 behind 1024 12.0 / 14.6.)  And not where a
+// sequence's own rows fill a tile of 128: it reads its prefix as often as a group's tile would.
+constexpr double kSaves = 24e6, kSavesLong = 8e6;
+constexpr int kLong = 4096;
+// By tiles of 128 rows (many_unit) where rows x keys x elements of a key head are more than these: they read a key once for 128 rows, those of 16 take
+// less time to begin and end (us, 128 / 16, 8B shape: 32 rows behind 4096 17.7 / 15.1, behind 16384 25.3 / 26.0; 128 behind 1024 17.0 / 15.8,
+// behind 4096 23.1 / 25.9; 256 behind 1024 18.2 / 21.5; 1B shape: 64 behind 16384 23.1 / 24.1, 128 behind 4096 16.9 / 16.7, 256
+// behind 4096 18.9 / 24.0)
+constexpr double kManyWork = 3e8;
 
 SharePlan plan_share(const river_pages *p, const river_batch *b, const river_prefixes *x, int nq) {
   SharePlan y{};
@@ -41,29 +55,38 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
   const long long rows = (long long)y.max_new * rep, group_rows = std::min<long long>(b->n_tokens, (long long)x->max_seqs * y.max_new) * rep;
   const long long common = x->n_groups ? std::min<long long>({x->max_len, (long long)x->max_pages * p->page_size, kMostPositions}) : 0;
   const long long keys = std::min<long long>({b->max_len, std::max<long long>((long long)b->max_pages * p->page_size, common), kMostPositions});
+  const double key_bytes = 2. * p->n_kv_heads * p->head_dim * (p->dtype == RIVER_F32 ? 4 : 2);
+  const long long in_group = std::min<long long>(x->max_seqs, b->n_seq), groups = std::min<long long>(x->n_groups, b->n_seq);
+  const double saves = std::min<double>(groups * (in_group - 1.), b->n_seq) * common * key_bytes;
   constexpr int kManyRows = Many<__bf16, 128>::ROWS;
-  if (!common || x->max_seqs <= 1 || (p->dtype == RIVER_BF16 && rows >= kManyRows)) {
+  if (saves < (common >= kLong ? kSavesLong : kSaves) || (p->dtype == RIVER_BF16 && rows >= kManyRows)) {
     const AttnPlan o = plan_attention(p, b, nq, 0, 0);
     y.many = y.p_many = o.many;
     y.tiles = o.tiles;
     y.n_splits = o.n_splits;
     y.least = o.split_len;
+    y.fused = o.fused;
   } else {
-    // Both kinds: three workgroups a CU of at least 128 keys, eight where that leaves them 512 (see plan_attention)
-    auto splits = [&](long long groups, long long keys) {
-      auto by = [&](long long goal, long long least) { return std::min({goal / std::max(1ll, groups), (keys + least - 1) / least, 64ll}); };
-      return (int)std::max(1ll, std::max(by(768, 128), by(2048, 512)));
-    };
-    y.p_many = p->dtype == RIVER_BF16 && group_rows > kAttnRows;
+    y.p_many = p->dtype == RIVER_BF16 && group_rows > kAttnRows && (double)groups * group_rows * common * p->n_kv_heads * p->head_dim >= kManyWork;
     y.least = y.p_least = 128;
     const int tile = y.p_many ? kManyRows : kAttnRows;
+    const long long full = (group_rows + tile - 1) / tile;
     // (each group may have a tile that is not full)
     y.p_tiles = (int)std::min<long long>(((long long)b->n_tokens * rep + tile - 1) / tile + x->n_groups - 1, INT_MAX);
-    const long long groups = std::min<long long>(y.p_tiles, x->n_groups * ((group_rows + tile - 1) / tile)) * p->n_kv_heads;
-    y.p_splits = y.p_many ? (int)std::max(1ll, std::min({512 / std::max(1ll, groups), (common + 255) / 256, 64ll})) : splits(groups, common);
+    const long long p_groups = std::max(1ll, std::min<long long>(y.p_tiles, groups * full) * p->n_kv_heads);
+    // Splits of the prefixes: a workgroup a CU, two where that leaves them 1024 keys (24 sequences behind 131071 positions 129 us, with one 142); the
+    // other places are the sequences'.  But no more than it takes to be done (20 ns a key) in half the time that all keys take to stream: every
+    // split is one more part of each row (64 sequences of 225 .. 900 own positions behind 8191, us by splits: 8 47.7, 16 52.6, 32 64.7)
+    const long long own = std::max(1ll, keys - common);
+    const double stream = (groups * (double)common + (double)b->n_seq * own) * key_bytes / 5e6;
+    const long long fit = common / 1024 * p_groups >= 512 ? 512 : 256, hide = (long long)(common * 0.02 / (0.45 * stream)) + 1;
+    y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, 64ll}));
     y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;
     y.tiles = (int)((rows + kAttnRows - 1) / kAttnRows);
-    y.n_splits = splits((long long)b->n_seq * p->n_kv_heads * y.tiles, std::max(1ll, keys - common));
+    // of the sequences' own keys: see plan_attention
+    const long long o_groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
+    auto by = [&](long long goal, long long least) { return std::min({goal / o_groups, (own + least - 1) / least, 64ll}); };
+    y.n_splits = (int)std::max(1ll, std::max(by(768, 128), by(2048, 512)));
   }
   if (y.units || y.n_splits > 1) {
     const size_t parts = (size_t)b->n_tokens * nq * ((y.units ? y.p_splits : 0) + y.n_splits);
@@ -89,7 +112,7 @@ extern "C" int river_prefix_attention_workspace(const river_pages *pages, const 
 
 extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, const river_batch *batch, const river_prefixes *prefixes,
                                       int32_t n_q_heads, const void *q, int64_t q_stride, float scale, void *out, int64_t out_stride,
-                                      void *workspace, size_t workspace_bytes, void *hip_stream) {
+                                      void *workspace, size_t workspace_bytes, int32_t *tickets, void *hip_stream) {
   return guarded([&]() -> int {
     std::string why;
     if (const char *m = bad_attention(pages, batch, n_q_heads, 0, 0, &why)) return refuse(m);
@@ -111,6 +134,7 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
     const SharePlan y = plan_share(pages, batch, prefixes, n_q_heads);
     if (y.bytes && (!workspace || (uintptr_t)workspace % 16)) return refuse("null or misaligned (16 B) workspace");
     if (workspace_bytes < y.bytes) return refuse("workspace too small", RIVER_ENOSPC);
+    if (tickets && (uintptr_t)tickets % 4) return refuse("misaligned tickets");
     if (y.tiles == 0) return RIVER_OK;
     const Cache c = layer_cache(pages, layer);
     const Batch b = device_batch(batch, pages->page_size);
@@ -118,17 +142,17 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
     auto turn = [](long long round) { int k = 0; while ((round << k) % 32) ++k; return k; };
     const int turn_z = turn((long long)y.n_splits * c.n_kv_heads), turn_s = turn((long long)b.n_seq * y.n_splits * c.n_kv_heads);
     const AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale2, 0, 0, y.n_splits, y.least, y.tiles, y.many ? Many<__bf16, 128>::ROWS : kAttnRows, turn_s, turn_z,
-                     y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), nullptr};
+                     y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), y.fused && tickets ? (unsigned int *)tickets : nullptr};
     const Prefixes x{prefixes->table, prefixes->lens, prefixes->seq_start, prefixes->n_groups, prefixes->max_pages, prefixes->table_stride,
                      (int)std::min<long long>((long long)prefixes->max_pages * pages->page_size, kMostPositions), std::max(1, y.p_tiles),
                      std::max(1, y.p_splits), y.p_least, (unsigned)y.units,
                      y.p_many && !y.many && pages->kv_dtype == RIVER_KV_F16 ? Mat<_Float16>::kBias - Mat<_Float16>::kLazyBias : 0.f};
-    const long long groups = y.units + (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
+    const long long workgroups = y.units + (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
     // (rows of a workgroup of the join: eight parts a thread, where there are more the lanes of several rows have one)
     const int parts = (y.units ? y.p_splits : 0) + y.n_splits, fit = 1024 / pages->head_dim;
     const int each = std::max(1, std::min(fit, fit * 8 / std::max(8, parts))), heads = each >= fit ? fit : each >= 4 ? 4 : each >= 2 ? 2 : 1;
     const int chunks = (n_q_heads + heads - 1) / heads;
-    if (groups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * chunks * 256 >= (1ll << 32))
+    if (workgroups * kAttnThreads >= (1ll << 32) || (long long)b.n_tokens * chunks * 256 >= (1ll << 32))
       return refuse("too many sequences, groups, tokens and heads");
     const hipStream_t st = (hipStream_t)hip_stream;
     hipError_t e = by_types(pages, [&](auto t, auto ct, auto hd) {
@@ -137,7 +161,7 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
       constexpr int HD = decltype(hd)::v;
       auto go = [&](auto pm, auto om) {
         constexpr bool PM = decltype(pm)::value, OM = decltype(om)::value;
-        return launch_lds<k_share<T, C, HD, PM, OM>>(dim3((unsigned)groups), dim3(kAttnThreads), ShareLds<T, C, HD, PM, OM>::BYTES, st, c, b, a, x);
+        return launch_lds<k_share<T, C, HD, PM, OM>>(dim3((unsigned)workgroups), dim3(kAttnThreads), ShareLds<T, C, HD, PM, OM>::BYTES, st, c, b, a, x);
       };
       if constexpr (sizeof(T) == 2) {
         if (y.many) return go(True{}, True{});
@@ -145,7 +169,7 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
       }
       return go(False{}, False{});
     });
-    if (e == hipSuccess && y.bytes)
+    if (e == hipSuccess && y.bytes && !a.tickets)
       e = by_types(pages, [&](auto t, auto, auto hd) {
         constexpr int HD = decltype(hd)::v;
         typedef decltype(t) T;

@@ -15,9 +15,13 @@ pytestmark = pytest.mark.gpu
 
 class Shared(Setup):
     """Sequences of `lens` positions, `new` of them new; group g has the next groups[g][1] sequences, behind the first `lonely` ones, and a
-    prefix of groups[g][0] positions.  The sequences' own entries of whole pages of a prefix name pages that do not exist."""
+    prefix of groups[g][0] positions.  The sequences' own entries of whole pages of a prefix name pages that do not exist.
+    how: the bounds that are given, by which a call is divided.  "through": those of what is there (each sequence goes through its prefix, unless
+    that is large); "rows" and "tiles": the prefixes' table has room for so many positions that prefixes have units of their own, of 16 rows, or of 128
+    where the type has them."""
 
-    def __init__(self, kind, nkv, hd, ps, lens, new, groups, lonely=0, seed=0, layers=1, pad=0, ragged=True, room=0, bounds=True):
+    def __init__(self, kind, nkv, hd, ps, lens, new, groups, lonely=0, seed=0, layers=1, pad=0, ragged=True, room=0, how="through"):
+        self.how = how
         self.groups, self.of = groups, [-1] * lonely + [g for g, (_, n) in enumerate(groups) for _ in range(n)]
         self.of += [-1] * (len(lens) - len(self.of))
         self.common = [-(-p // ps) for p, _ in groups]
@@ -32,11 +36,18 @@ class Shared(Setup):
                 self.host[s, :min(groups[g][0] // ps, self.host.shape[1])] = (-1, 10**9, self.k.shape[1], -2**31)[s % 4]
         self.table.copy_(torch.from_numpy(self.host))
         start = lonely + np.concatenate([[0], np.cumsum([n for _, n in groups])]).astype(np.int32)
-        self.make(start, *((max([p for p, _ in groups] + [1]), max([n for _, n in groups] + [1])) if bounds else (None, None)))
+        self.make(start, *((max([p for p, _ in groups] + [1]), max([n for _, n in groups] + [1])) if how == "through" else (None, None)))
 
     def make(self, start, max_len=None, max_seqs=None):
-        n = len(self.groups)
+        n, seqs = len(self.groups), len(self.lens)
         self.prefix_table = torch.from_numpy(self.prefix_host[:n]).to(DEV) if n else torch.zeros(0, 1, dtype=torch.int32, device=DEV)
+        if self.how != "through" and n:
+            # 26 MB that sharing saves, or 2^20 positions
+            key = 2 * self.nkv * self.hd * self.kvt.itemsize
+            room = 1 << 20 if self.how == "tiles" else 26e6 / (key * max(1, min(n * (seqs - 1), seqs)))
+            wide = torch.full((n, max(self.prefix_host.shape[1], int(room) // self.ps + 1)), -1, dtype=torch.int32, device=DEV)
+            wide[:, :self.prefix_host.shape[1]] = self.prefix_table
+            self.prefix_table = wide
         self.prefixes = B.Prefixes(self.prefix_table, torch.tensor([p for p, _ in self.groups], dtype=torch.int32, device=DEV),
                                    torch.tensor(start, dtype=torch.int32, device=DEV), max_len, max_seqs)
 
@@ -51,6 +62,9 @@ class Shared(Setup):
             k[:len(p)], v[:len(p)] = self.k[layer][page, :, slot].double(), self.v[layer][page, :, slot].double()
             there[:len(p)] = torch.from_numpy(ok).to(DEV)
         return k, v, there
+
+
+HOW = pytest.mark.parametrize("how", ["through", "rows", "tiles"])
 
 
 def run(st, nq, scale=0.0, std=1.5, layer=0):
@@ -77,52 +91,58 @@ def behind(groups, own, new, lonely=()):
 @pytest.mark.parametrize("nkv,rep", [(1, 1), (2, 4), (3, 7), (1, 24), (8, 4)])
 @pytest.mark.parametrize("groups,own", [([(200, 5)], [0, 3, 40, 170, 1]), ([(1000, 2), (64, 0), (17, 3), (513, 1)], [9, 300, 0, 31, 64, 128, 5, 0]),
                                         ([(2500, 20)], list(range(0, 200, 10)))], ids=str)
-def test_single_tokens(kind, hd, nkv, rep, groups, own):
+@HOW
+def test_single_tokens(kind, hd, nkv, rep, groups, own, how):
     new = [1] * len(own)
-    run(Shared(kind, nkv, hd, 16, behind(groups, own, new), new, groups, ragged=False), nkv * rep)
+    run(Shared(kind, nkv, hd, 16, behind(groups, own, new), new, groups, ragged=False, how=how), nkv * rep)
 
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("hd,nkv,rep", [(64, 2, 4), (128, 1, 8), (128, 2, 1), (64, 1, 3)])
 @pytest.mark.parametrize("groups,own,new,lonely", [([(100, 3)], [0, 7, 60], [2, 5, 1], ()), ([(300, 2), (40, 2)], [10, 200, 0, 5, 90], [4, 0, 9, 1, 2], (50, 3)),
                                                    ([(700, 4)], [0, 0, 33, 129], [130, 64, 1, 300], ()), ([(4000, 3), (130, 6)], [5] * 9, [3] * 9, (700,))], ids=str)
-@pytest.mark.parametrize("bounds", [True, False])
-def test_several_tokens(kind, hd, nkv, rep, groups, own, new, lonely, bounds):
+@HOW
+@pytest.mark.parametrize("room", [0, 300])
+def test_several_tokens(kind, hd, nkv, rep, groups, own, new, lonely, how, room):
     new = [1 + i for i in range(len(lonely))] + new
-    run(Shared(kind, nkv, hd, 16, behind(groups, own, new, lonely), new, groups, lonely=len(lonely), pad=3, bounds=bounds, room=0 if bounds else 300), nkv * rep)
+    run(Shared(kind, nkv, hd, 16, behind(groups, own, new, lonely), new, groups, lonely=len(lonely), pad=3, how=how, room=room), nkv * rep)
 
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("ps", [1, 7, 20, 64, 1000])
 @pytest.mark.parametrize("prefix", [1, 63, 64, 640, 1001])
-def test_page_sizes(kind, ps, prefix):
-    groups, own, new = [(prefix, 4)], [0, 1, 63, 200], [1, 2, 1, 40]
-    run(Shared(kind, 2, 64, ps, behind(groups, own, new), new, groups, seed=ps), 8)
+@HOW
+def test_page_sizes(kind, ps, prefix, how):
+    groups, own, new = [(prefix, 4)], [0, 1, 63, 200], [1, 2, 1, 20]
+    run(Shared(kind, 2, 64, ps, behind(groups, own, new), new, groups, seed=ps, how=how), 8)
 
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("hd", [64, 128])
-def test_large_groups(kind, hd):
+@HOW
+def test_large_groups(kind, hd, how):
     # several tiles of rows, several splits of keys, several of them the sequences'
     groups, own = [(3000, 70), (800, 30)], [(i * 37) % 500 for i in range(101)]
     new = [1] * 101
-    run(Shared(kind, 2, hd, 16, behind(groups, own, new), new, groups, ragged=False, seed=1), 16)
+    run(Shared(kind, 2, hd, 16, behind(groups, own, new), new, groups, ragged=False, seed=1, how=how), 16)
     new = [1 + i % 6 for i in range(101)]
-    run(Shared(kind, 2, hd, 16, behind(groups, own, new), new, groups, seed=2), 8)
+    run(Shared(kind, 2, hd, 16, behind(groups, own, new), new, groups, seed=2, how=how), 8)
 
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("groups,own,new", [([(20000, 2)], [100, 3000], [1, 1]), ([(50, 2)], [20000, 10], [1, 1]), ([(9000, 2)], [100, 5], [20, 33])], ids=str)
-def test_long_caches(kind, groups, own, new):
-    run(Shared(kind, 1, 128, 16, behind(groups, own, new), new, groups, seed=3), 4)
+@HOW
+def test_long_caches(kind, groups, own, new, how):
+    run(Shared(kind, 1, 128, 16, behind(groups, own, new), new, groups, seed=3, how=how), 4)
 
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("max_len,max_seqs", [(1, 1), (1, 2), (64, 3), (10**6, 1000), (0, 0), (2000, 2)])
-def test_more_than_the_bounds_say(kind, max_len, max_seqs):
+@HOW
+def test_more_than_the_bounds_say(kind, max_len, max_seqs, how):
     groups = [(1500, 40), (333, 5)]
     for new in ([1] * 45, [1 + i % 4 for i in range(45)]):
-        st = Shared(kind, 1, 64, 16, behind(groups, [i * 9 for i in range(45)], new), new, groups, seed=4)
+        st = Shared(kind, 1, 64, 16, behind(groups, [i * 9 for i in range(45)], new), new, groups, seed=4, how=how)
         st.make([0, 40, 45], max_len, max_seqs)
         run(st, 8)
         st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=max(new), max_len=100)
@@ -132,50 +152,54 @@ def test_more_than_the_bounds_say(kind, max_len, max_seqs):
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("lens,new", [([0, 300, 5, 128, 129, 1], [1] * 6), ([0, 200, 3, 128, 0, 40], [3, 90, 3, 128, 0, 7]), ([-5, 2, 130, -2**31, 127, 300], [2, 6, 1, 1, 140, 1])],
                          ids=str)
-def test_sequences_shorter_than_their_prefix(kind, lens, new):
+@HOW
+def test_sequences_shorter_than_their_prefix(kind, lens, new, how):
     """What is below a token's position counts, up to it; a token without a position is zero."""
     for groups in ([(128, 6)], [(128, 2), (129, 3)], [(1000, 5)]):
-        st = Shared(kind, 2, 64, 16, lens, new, groups, seed=5)
+        st = Shared(kind, 2, 64, 16, lens, new, groups, seed=5, how=how)
         q, out = run(st, 8)
         for s, t, p in st.positions():
             assert p >= 0 or not bool(out[t].any())
 
 
 @pytest.mark.parametrize("kind", TYPES)
-def test_prefixes_of_no_positions_and_groups_of_no_sequences(kind):
+@HOW
+def test_prefixes_of_no_positions_and_groups_of_no_sequences(kind, how):
     lens = [50, 1, 300, 0, 77]
     for new in ([1] * 5, [2, 1, 130, 0, 5]):
         for groups in ([(0, 5)], [(0, 2), (0, 0), (0, 1)], [(5, 0), (100, 0)], []):
-            st = Shared(kind, 2, 64, 16, lens, new, groups, seed=6)
+            st = Shared(kind, 2, 64, 16, lens, new, groups, seed=6, how=how)
             q, out = run(st, 8)
             # nothing is shared: river_paged_attention's rows, up to what joining them in other parts rounds
             want, tol = attention(st, q)
             check(B.river_paged_attention(st.pages, 0, st.batch, q), want, tol)
     st.groups = [(-7, 3)]
     st.common, st.prefix_host = [0], np.full((1, 2), -1, dtype=np.int32)
-    st.make([1, 4], 64, 3)
+    st.make([1, 4])
     run(st, 8)
 
 
 @pytest.mark.parametrize("kind", TYPES)
-def test_pages_that_are_not_there(kind):
+@HOW
+def test_pages_that_are_not_there(kind, how):
     groups, own = [(300, 3), (70, 2)], [40, 0, 200, 100, 3]
     for new in ([1] * 5, [3, 1, 40, 2, 3]):
-        st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=7)
+        st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=7, how=how)
         st.prefix_host[0, 3], st.prefix_host[0, 18] = -1, 2**31 - 1
         st.prefix_host[1, :] = -5                                 # a prefix of which nothing is there
         st.host[2, 25] = st.k.shape[1]
         st.table.copy_(torch.from_numpy(st.host))
-        st.make([0, 3, 5], 300, 3)
+        st.make([0, 3, 5], *((300, 3) if how == "through" else ()))
         run(st, 8)
 
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("lens,new", [([130, 140, 200, 64, 33], [1] * 5), ([130, 300, 200, 64, 33], [2, 160, 60, 3, 1])], ids=str)
-def test_what_is_not_seen_has_no_influence(kind, bad, lens, new):
+@HOW
+def test_what_is_not_seen_has_no_influence(kind, bad, lens, new, how):
     """Places behind a row's position, of pages that nobody has, and of the prefix's last page behind its end, hold what is not finite."""
-    st = Shared(kind, 2, 64, 16, lens, new, [(130, 4)], lonely=1, seed=8)
+    st = Shared(kind, 2, 64, 16, lens, new, [(130, 4)], lonely=1, seed=8, how=how)
     q = st.randn(st.tokens, 8, 64)
     clean = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
     used = torch.zeros(st.k.shape[1], 16, dtype=torch.bool, device=DEV)
@@ -194,10 +218,11 @@ def test_what_is_not_seen_has_no_influence(kind, bad, lens, new):
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("where", ["k", "v"])
 @pytest.mark.parametrize("hd", [64, 128])
-def test_a_later_position_is_no_part_of_an_earlier_row(kind, bad, where, hd):
+@HOW
+def test_a_later_position_is_no_part_of_an_earlier_row(kind, bad, where, hd, how):
     """A position holds what is not finite: rows below it are as without, others are not finite where the formula has it."""
     for lens, new, at in (([300, 320, 290], [40, 1, 3], 270), ([300, 90, 290], [290, 1, 3], 120), ([300, 300], [1, 1], 285), ([310, 300], [25, 1], 290)):
-        st = Shared(kind, 1, hd, 16, lens, new, [(280, len(lens))], seed=9)
+        st = Shared(kind, 1, hd, 16, lens, new, [(280, len(lens))], seed=9, how=how)
         q = st.randn(st.tokens, 4, hd)
         clean = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
         x = st.k if where == "k" else st.v
@@ -215,9 +240,10 @@ def test_a_later_position_is_no_part_of_an_earlier_row(kind, bad, where, hd):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-def test_rows_that_see_only_scores_of_minus_infinity(kind):
-    st = Shared(kind, 1, 64, 16, [140, 150, 141], [1, 1, 2], [(128, 3)], seed=10)
-    q = st.randn(4, 4, 64).abs() + 0.5
+@HOW
+def test_rows_that_see_only_scores_of_minus_infinity(kind, how):
+    st = Shared(kind, 1, 64, 16, [140, 150, 145], [1, 1, 6], [(128, 3)], seed=10, how=how)
+    q = st.randn(8, 4, 64).abs() + 0.5
     st.k[0, :, :, :, 0] = -math.inf
     st.v[0, :, :, :, 3] = math.inf
     assert not bool(B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q).any())
@@ -231,32 +257,37 @@ def test_rows_that_see_only_scores_of_minus_infinity(kind):
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("std,scale", [(8.0, 0.0), (1.0, 3.0), (0.01, 0.05), (200.0, 0.0)])
-def test_scales(kind, std, scale):
+@HOW
+def test_scales(kind, std, scale, how):
     groups, own = [(400, 6)], [0, 100, 250, 3, 60, 31]
-    for new in ([1] * 6, [3, 70, 1, 9, 40, 2]):
-        run(Shared(kind, 2, 128, 16, behind(groups, own, new), new, groups, seed=11), 8, scale=scale, std=std)
+    for new in ([1] * 6, [3, 30, 1, 9, 20, 2], [3, 70, 1, 9, 40, 2]):
+        run(Shared(kind, 2, 128, 16, behind(groups, own, new), new, groups, seed=11, how=how), 8, scale=scale, std=std)
 
 
 @pytest.mark.parametrize("kind", TYPES)
-def test_new_tokens_beyond_their_bound_are_left_out(kind):
+@HOW
+@pytest.mark.parametrize("most", [20, 33])
+def test_new_tokens_beyond_their_bound_are_left_out(kind, how, most):
     groups, own, new = [(200, 2), (90, 1)], [5, 60, 3], [7, 300, 40]
-    st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=12)
-    st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=33)
+    st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=12, how=how)
+    st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=most)
     q = st.randn(st.tokens, 8, 64)
     out = torch.full_like(q, 7.0)
     B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q, out=out)
     want, tol = attention(st, q)
     for s, n in enumerate(new):
         lo = int(st.start[s])
-        check(out[lo:lo + min(n, 33)], want[lo:lo + min(n, 33)], tol[lo:lo + min(n, 33)])
-        assert bool((out[lo + min(n, 33):lo + n] == 7.0).all())
+        m = min(n, most)
+        check(out[lo:lo + m], want[lo:lo + m], tol[lo:lo + m])
+        assert bool((out[lo + m:lo + n] == 7.0).all())
 
 
 @pytest.mark.parametrize("kind", TYPES)
-def test_strides_and_layers(kind):
+@HOW
+def test_strides_and_layers(kind, how):
     groups, own = [(100, 2)], [45, 3]
-    for new in ([1, 1], [80, 45]):
-        st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=13, layers=3)
+    for new in ([1, 1], [20, 3], [80, 45]):
+        st = Shared(kind, 2, 64, 16, behind(groups, own, new), new, groups, seed=13, layers=3, how=how)
         wide = st.randn(st.tokens, 8 * 64 * 3)
         q = wide[:, 64 * 8:64 * 16].unflatten(1, (8, 64))
         room = torch.full((st.tokens, 12, 64), 7.0, dtype=st.act, device=DEV)
@@ -268,7 +299,8 @@ def test_strides_and_layers(kind):
             assert bool((room[:, :2] == 7.0).all()) and bool((room[:, 10:] == 7.0).all())
 
 
-def test_pages_beyond_32_bits():
+@HOW
+def test_pages_beyond_32_bits(how):
     # 2^31 elements and 4 GiB into the pages; only the pages that are used are ever touched
     stride = 3 * 2 ** 28
     flat = torch.empty(6 * stride, dtype=torch.bfloat16, device=DEV)
@@ -280,22 +312,23 @@ def test_pages_beyond_32_bits():
         for p in range(6):
             x[0, p] = torch.randn(1, 16, 64, generator=g, device=DEV).to(torch.bfloat16)
     for new in ([1, 1], [5, 30], [3, 20]):
-        st = Shared("bf16", 1, 64, 16, [45, 60], new, [(30, 2)], seed=17)
+        st = Shared("bf16", 1, 64, 16, [45, 60], new, [(30, 2)], seed=17, how=how)
         st.k, st.v, st.pages = k, v, B.Pages(k, v)
         st.prefix_host = np.array([[5, 4]], dtype=np.int32)
         st.host = np.array([[-1, 0, 3, -1], [-1, 1, 2, 5]], dtype=np.int32)
         st.table = torch.from_numpy(st.host).to(DEV)
         st.batch = B.Batch(st.table, st.dlens, st.q_start, max_new=max(new), max_len=60)
-        st.make([0, 2], 30, 2)
+        st.make([0, 2], *((30, 2) if how == "through" else ()))
         run(st, 32)
 
 
-def test_the_same_call_gives_the_same_bits():
+@HOW
+def test_the_same_call_gives_the_same_bits(how):
     for kind in TYPES:
         for hd in (64, 128):
             groups, own = [(3000, 20), (700, 12)], [(i * 53) % 400 for i in range(32)]
             for new in ([1] * 32, [1 + i % 9 for i in range(32)]):
-                st = Shared(kind, 8, hd, 16, behind(groups, own, new), new, groups, seed=18)
+                st = Shared(kind, 8, hd, 16, behind(groups, own, new), new, groups, seed=18, how=how)
                 q = st.randn(st.tokens, 32, hd)
                 first = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
                 for _ in range(5):
@@ -314,9 +347,10 @@ def test_calls_without_sequences_or_tokens():
     assert bool((out == 7.0).all())
 
 
-def test_on_another_stream_and_two_at_once():
+@HOW
+def test_on_another_stream_and_two_at_once(how):
     groups = [(900, 6)]
-    st = Shared("bf16", 2, 64, 16, behind(groups, [0, 9, 90, 300, 31, 7], [1] * 6), [1] * 6, groups, ragged=False, seed=20)
+    st = Shared("bf16", 2, 64, 16, behind(groups, [0, 9, 90, 300, 31, 7], [1] * 6), [1] * 6, groups, ragged=False, seed=20, how=how)
     qs = [st.randn(6, 8, 64) for _ in range(2)]
     want = [B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q) for q in qs]
     sides = [torch.cuda.Stream() for _ in range(2)]
@@ -357,7 +391,8 @@ def test_the_binding_refuses():
 
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("rotary", [True, False])
-def test_steps_of_a_server(kind, rotary):
+@HOW
+def test_steps_of_a_server(kind, rotary, how):
     """Two system prompts are laid out, stored and read by sequences that come, grow, draft, give back and leave, layer by layer: the step
     is captured once, every replay's rows are those of attention over the whole history of each sequence, and in the end every page is free."""
     act, kvt = TYPES[kind]
@@ -373,6 +408,9 @@ def test_steps_of_a_server(kind, rotary):
     # rows 0 and 1 are the prompts, the others sequences: 2, 3, 4 go on from the first, 5, 6 from the second, 7 from none
     shared = torch.zeros(n + 2, dtype=torch.int32, device=DEV)
     t = B.Tables.empty(n_pages, ps, n + 2, 16, n_shared=shared)
+    # (rows of the prefixes with room for 2^20 positions, or what 26 MB are, and none: prefixes with units of their own or not, see Shared)
+    wide = {"through": 16, "rows": 26000000 // (2 * nkv * hd * kvt.itemsize * 8 * ps) + 1, "tiles": (1 << 20) // ps}[how]
+    prompts = torch.full((2, wide), -1, dtype=torch.int32, device=DEV)
     lens = [37, 16]
     group = [0, 0, 0, 1, 1, -1]
     history = [[] for _ in range(n + 2)]
@@ -380,12 +418,13 @@ def test_steps_of_a_server(kind, rotary):
     d, start = i32([0] * (n + 2)), i32([0] * (n + 3))
     slots, positions, refused = torch.zeros(T, dtype=torch.int64, device=DEV), i32([0] * T), i32([0])
     batch = B.Batch(t.table, t.lens, start, max_new=T, max_len=128)
-    prefixes = B.Prefixes(t.table[:2], t.lens[:2], i32([2, 5, 7]), max_len=40, max_seqs=3)
+    prefixes = B.Prefixes(prompts, t.lens[:2], i32([2, 5, 7]), *((40, 3) if how == "through" else ()))
     x = torch.zeros(L, T, nq + 2 * nkv, hd, dtype=act, device=DEV)
     outs = [torch.full((T, nq, hd), 7.0, dtype=act, device=DEV) for _ in range(L)]
 
     def step():
         B.river_build_batch(t, d, start, slots, positions, refused)
+        prompts[:, :16] = t.table[:2]
         for l in range(L):
             q, kk, vv = x[l, :, :nq], x[l, :, nq:nq + nkv], x[l, :, nq + nkv:]
             if rotary:

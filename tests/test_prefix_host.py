@@ -19,9 +19,9 @@ def tables(**kw):
     return B.river_tables(*(d[f] for f, _ in B.river_tables._fields_))
 
 
-def attend(pg=None, b=None, x=None, layer=0, nq=4, q=P, qs=256, scale=0.0, out=2 * P, os=256, ws=None, n=0):
+def attend(pg=None, b=None, x=None, layer=0, nq=4, q=P, qs=256, scale=0.0, out=2 * P, os=256, ws=None, n=0, tickets=None):
     return B.load().river_prefix_attention(C.byref(pg or pages()), layer, C.byref(b or batch()), C.byref(x or prefixes()), nq, q, qs, scale, out, os,
-                                           ws, n, None)
+                                           ws, n, tickets, None)
 
 
 def store(pg=None, layer=0, slots=P, n=4, k=P, ks=128, v=P, vs=128):
@@ -54,25 +54,30 @@ def test_bad_prefixes_are_refused(bad):
     assert attend(x=prefixes(**bad)) == workspace(x=prefixes(**bad)) == B.RIVER_EINVAL and text()
 
 
+BIG = prefixes(max_pages=1 << 20, table_stride=1 << 20, max_len=1 << 20)        # (a prefix that pays: it has parts, which need a workspace)
+
+
 @pytest.mark.parametrize("bad", [dict(layer=-1), dict(layer=2), dict(nq=0), dict(nq=3), dict(nq=65538), dict(q=0), dict(out=0), dict(q=P + 8), dict(out=P + 4),
                                  dict(qs=255), dict(qs=260), dict(os=128), dict(out=P), dict(scale=-1.0), dict(scale=float("nan")),
-                                 dict(scale=float("inf")), dict(scale=3e38), dict(ws=None, n=1 << 30), dict(ws=P + 8, n=1 << 30)], ids=str)
+                                 dict(scale=float("inf")), dict(scale=3e38), dict(x=BIG, ws=None, n=1 << 30), dict(x=BIG, ws=P + 8, n=1 << 30), dict(x=BIG, ws=P, n=1 << 30, tickets=P + 2)], ids=str)
 def test_attention_refuses(bad):
     assert attend(**bad) == B.RIVER_EINVAL and text()
 
 
 def test_a_workspace_that_is_too_small_is_refused():
-    n = workspace()
+    n = workspace(x=BIG)
     assert n > 0
-    assert attend(ws=P, n=n - 1) == B.RIVER_ENOSPC and "workspace" in text()
+    assert attend(x=BIG, ws=P, n=n - 1) == B.RIVER_ENOSPC and "workspace" in text()
 
 
 def test_workspaces():
-    # what nothing shares and nothing splits needs none; what is shared has a part of each row for the prefix and one of its own at least
+    # what nothing shares, or too little to pay, and nothing splits needs none; what is shared has a part of each row for the prefix and one of
+    # its own at least
     assert workspace(x=prefixes(n_groups=0, table=0, lens=0, seq_start=0)) == 0
     assert workspace(x=prefixes(max_seqs=1)) == 0
-    assert workspace() >= 4 * 4 * 2 * (64 * 4 + 8)
-    assert workspace(nq=8) == 2 * workspace()
+    assert workspace() == 0
+    assert workspace(x=BIG) >= 4 * 4 * 2 * (64 * 4 + 8)
+    assert workspace(x=BIG, nq=8) == 2 * workspace(x=BIG)
     assert workspace(b=batch(n_tokens=0)) >= 0
 
 
@@ -82,7 +87,8 @@ def test_calls_without_tokens_end_at_once():
 
 def test_calls_that_are_too_large_are_refused():
     assert attend(b=batch(n_tokens=1 << 22, max_new=1 << 22), nq=64, qs=4096, os=4096) == B.RIVER_EINVAL and "too many" in text()
-    assert attend(x=prefixes(n_groups=1 << 22), b=batch(n_tokens=1 << 14, max_new=1 << 14), ws=P, n=1 << 62) == B.RIVER_EINVAL and "too many" in text()
+    many = prefixes(n_groups=1 << 22, max_pages=1 << 20, table_stride=1 << 20, max_len=1 << 20)
+    assert attend(x=many, b=batch(n_tokens=4), ws=P, n=1 << 62) == B.RIVER_EINVAL and "too many" in text()
 
 
 @pytest.mark.parametrize("bad", [dict(layer=2), dict(layer=-1), dict(n=-1), dict(n=2**23), dict(slots=0), dict(k=0), dict(v=0), dict(slots=P + 4), dict(k=P + 1),
@@ -112,7 +118,7 @@ def test_null_structs_are_refused():
     L, n = B.load(), C.c_size_t()
     assert L.river_build_batch(None, P, 4, P, P, P, P, None) == B.RIVER_EINVAL
     assert L.river_store_slots(None, 0, P, 4, P, 128, P, 128, None) == B.RIVER_EINVAL
-    assert L.river_prefix_attention(C.byref(pages()), 0, C.byref(batch()), None, 4, P, 256, 0.0, 2 * P, 256, None, 0, None) == B.RIVER_EINVAL
-    assert L.river_prefix_attention(C.byref(pages()), 0, None, C.byref(prefixes()), 4, P, 256, 0.0, 2 * P, 256, None, 0, None) == B.RIVER_EINVAL
+    assert L.river_prefix_attention(C.byref(pages()), 0, C.byref(batch()), None, 4, P, 256, 0.0, 2 * P, 256, None, 0, None, None) == B.RIVER_EINVAL
+    assert L.river_prefix_attention(C.byref(pages()), 0, None, C.byref(prefixes()), 4, P, 256, 0.0, 2 * P, 256, None, 0, None, None) == B.RIVER_EINVAL
     assert L.river_prefix_attention_workspace(C.byref(pages()), C.byref(batch()), C.byref(prefixes()), 4, None) == B.RIVER_EINVAL
     assert L.river_prefix_attention_workspace(C.byref(pages()), C.byref(batch()), None, 4, C.byref(n)) == B.RIVER_EINVAL
