@@ -875,12 +875,12 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 // Keys and values go from memory straight into LDS (no registers, AHEAD steps in flight), in rings, one barrier a step; where a key's
 // row lies is looked up for CHUNK steps at once.
 // 8B shape, 4096 tokens: 148 .. 158 us by the box, 870 .. 930 TFLOP/s; 2048 behind 16384 615 us, 950; the largest matrix products of the library reach 1250.
-template <class C, int HD>
+template <class C, int HD, int AHEAD_ = 2>
 struct Many {
   typedef Mat<C> M;
   static constexpr int KEYS = 32, WROWS = 32, ROWS = 4 * WROWS;
-  static constexpr int AHEAD = 2, KRING = 2, VRING = 4;  // in steps
-  static constexpr int CHUNK = 16;                       // steps whose rows are looked up at once
+  static constexpr int AHEAD = AHEAD_, KRING = AHEAD, VRING = AHEAD + 2;          // in steps
+  static constexpr int CHUNK = AHEAD == 2 ? 16 : 8;      // steps whose rows are looked up at once
   static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
   static constexpr int KS = HD / 16, DB = HD / 32;
   static constexpr int STAGE = KEYS * ROW;
@@ -913,10 +913,21 @@ __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
   else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
 }
 
+// Entries of a unit's first keys, CHUNK steps of them, that were read before
+struct NoFirst {
+  static constexpr bool have = false;
+  int e[1];
+};
+template <int N>
+struct First {
+  static constexpr bool have = true;
+  int e[N];
+};
+
 // One unit of 128 rows at most: its result in the output, or as a part of it.
-template <class T, class C, int HD, class Keys, class Rows>
-__device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, const Unit<Keys, Rows> &w, char *lds) {
-  typedef Many<C, HD> W;
+template <class T, class C, int HD, int AHEAD, class First, class Keys, class Rows>
+__device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, const Unit<Keys, Rows> &w, const First &first, char *lds) {
+  typedef Many<C, HD, AHEAD> W;
   typedef Mat<C> M;
   constexpr int KS = W::KS, DB = W::DB, NL = W::NL, KEYS = W::KEYS;
   char *const vlds = lds + W::V;
@@ -930,8 +941,8 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
 
   // this wavefront's rows: rows behind the last repeat it
   const int w0 = min(r0 + wave * W::WROWS, r1), w1 = min(w0 + W::WROWS - 1, r1);
-  int first, last;                                       // positions of their first and last token
-  w.rows.reach(a.by_rep.quot(w0), a.by_rep.quot(w1), first, last);
+  int lowest, highest;                                   // positions of their first and last token
+  w.rows.reach(a.by_rep.quot(w0), a.by_rep.quot(w1), lowest, highest);
   const int my_slot = lane % W::PIECES;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   // Their queries in the operand's order.  (Through LDS, in whole rows of memory, they take as long: 4500 cycles, on the way with
@@ -963,13 +974,13 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
 
   const u32x4 *kp = (const u32x4 *)((const C *)c.k + (long long)head * c.page_size * HD), *vp = (const u32x4 *)((const C *)c.v + (long long)head * c.page_size * HD);
   constexpr int CK = W::CHUNK * KEYS;
-  // Where the rows of CHUNK steps lie, and a bit a key.  What has no row (no page, behind the end): keys of page 0, which no
+  // Where the rows of CHUNK steps lie, and a bit a key (the first steps' entries are here already, where `first` has them).  What has no row (no page, behind the end): keys of page 0, which no
   // score counts, and values of zeros, whatever the bits of the cache there
-  auto look_up = [&](int chunk) {
+  auto look_up_by = [&](int chunk, auto entry) {
 #pragma unroll
     for (int j = 0; j < CK / 256; ++j) {
       const int k = j * 256 + (int)threadIdx.x, i = chunk * CK + k, p = sp.pos(min(i0 + i, i1 - 1)), page = c.by_page.quot(p);
-      const int e = w.keys.entry(p, page);
+      const int e = entry(j, p, page);
       const bool ok = i0 + i < i1 && (unsigned)e < (unsigned)c.n_pages;
       const unsigned long long at = (unsigned long long)(uint32_t)e * c.page_pieces + (uint32_t)((p - page * c.page_size) * W::PIECES);
       places[(chunk & 1) * CK + k] = Place{(uintptr_t)(kp + (ok ? at : 0)), (uintptr_t)(ok ? vp + at : g_zero_row)};
@@ -977,6 +988,7 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
       if (lane < 2) there_of[(chunk & 1) * W::CHUNK + (j * 256 + wave * 64) / KEYS + lane] = (uint32_t)(all >> (32 * lane));
     }
   };
+  auto look_up = [&](int chunk) { look_up_by(chunk, [&](int, int p, int page) { return w.keys.entry(p, page); }); };
   // a lane's piece of a row: in LDS it lies where the swizzle puts it
   const int my_row = wave * 8 + lane / W::PIECES;
   int k_piece[NL], v_piece[NL];
@@ -1007,7 +1019,7 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
   bool pend;
   // Steps of which every row of this wavefront sees every key (where all pages are there): their last key is at most all_to,
   // and their first is at least all_from or their last below all_sinks, by index in the split
-  const int all_to = sp.at(first) - i0, all_from = (a.window ? max(0, sp.at(max(last, -1) - a.window + 1)) : 0) - i0, all_sinks = sight.sinks - i0;
+  const int all_to = sp.at(lowest) - i0, all_from = (a.window ? max(0, sp.at(max(highest, -1) - a.window + 1)) : 0) - i0, all_sinks = sight.sinks - i0;
 
   // Step n's scores as they count: what a row does not see is -infinity.  The maximum, where that moves it.
   auto settle = [&](int n, Scores &sx, uint32_t there_) {
@@ -1064,7 +1076,8 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
         for (int w = 0; w < 4; ++w) at[w] = finite_only<C>(at[w]);
       }
     };
-    look_up(0);
+    if (First::have && !careful) look_up_by(0, [&](int j, int, int) { return first.e[j]; });
+    else look_up(0);
     // the values of step -1 are zeros
     for (int i = threadIdx.x; i < W::STAGE / 16; i += 256) *(u32x4 *)(vlds + (W::VRING - 1) * W::STAGE + i * 16) = u32x4{0, 0, 0, 0};
     wait_and_meet<0>();
@@ -1291,8 +1304,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   const int parts = splits_of(a, sp.n);
   if (z >= parts) return;
   const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
-  many_unit<T, C, HD>(c, a, Unit<OneRow, OfSequence>{{b.table + (long long)s * b.table_stride}, {len, count}, sp, i0, i1, r0, r1, first_token, head,
-                                                     a.n_splits, z, (long long)s * a.max_new, parts == 1}, lds);
+  many_unit<T, C, HD, 2>(c, a, Unit<OneRow, OfSequence>{{b.table + (long long)s * b.table_stride}, {len, count}, sp, i0, i1, r0, r1, first_token, head,
+                                                        a.n_splits, z, (long long)s * a.max_new, parts == 1}, NoFirst{}, lds);
 }
 
 // Row w of the partial results: head h of new token i of sequence s.  Its number of splits (0: no row, 1: it is done already), and its

@@ -20,12 +20,25 @@ struct Prefixes {
   float shift;                            // added to the prefixes' maxima: both kernels scale fp16 probabilities, by different powers of two
 };
 
-__device__ __forceinline__ int group_of(const Prefixes &x, int s) {      // or -1
-  if (x.n_groups == 0) return -1;
-  const int g = __builtin_amdgcn_readfirstlane(count_up_to(x.seq_start, x.n_groups + 1, s)) - 1;
-  return g < x.n_groups ? g : -1;
+// The group of sequence s (-1: none) and its prefix's positions.
+__device__ __forceinline__ int cut_len(const Prefixes &x, int len) { return min(max(len, 0), x.cap); }
+__device__ __forceinline__ void find_group(const Prefixes &x, int s, int &g, int &n) {
+  g = -1;
+  n = 0;
+  if (x.n_groups == 0) return;
+  if (x.n_groups < 64) {                  // (a lane a group: both are read at once)
+    const int lane = threadIdx.x % 64, start = x.seq_start[min(lane, x.n_groups)], len = x.lens[min(lane, x.n_groups - 1)];
+    const int c = __popcll(__ballot(lane <= x.n_groups && start <= s)) - 1;
+    if (c < 0 || c >= x.n_groups) return;
+    g = c;
+    n = cut_len(x, __builtin_amdgcn_readlane(len, c));
+  } else {
+    const int c = __builtin_amdgcn_readfirstlane(count_up_to(x.seq_start, x.n_groups + 1, s)) - 1;
+    if (c < 0 || c >= x.n_groups) return;
+    g = c;
+    n = cut_len(x, x.lens[c]);
+  }
 }
-__device__ __forceinline__ int prefix_len(const Prefixes &x, int g) { return g < 0 ? 0 : min(max(x.lens[g], 0), x.cap); }
 
 // Splits of n keys: whole steps of 128 keys, `least` at least and no more splits than `most`; one if there are none.
 __device__ __forceinline__ int split_len(int n, int most, int least) { return max(least, ((n + most - 1) / most + 127) / 128 * 128); }
@@ -49,16 +62,36 @@ struct Found {
 typedef Unit<TwoRows, Found> Share;
 
 constexpr int kAttnRows = 16;              // of a tile of split_unit
+// Steps of a prefix's keys in flight (many_unit): three at head size 128, whose stream they hide better (64 sequences behind 8191 58.1 ->
+// 53.8 us, 24 behind 131071 133 -> 129; four leave one workgroup a CU: 68, 149); at 64 no more than the compute-bound calls have (88.6 us, three 92)
+template <int HD> constexpr int kAhead = HD == 128 ? 3 : 2;
 constexpr int kEverything = 1 << 30;       // a position that sees every key
 template <int TR>
 __device__ __forceinline__ int my_row(int r0, int r1) {           // this lane's row of a tile of TR
   return min(r0 + (TR == kAttnRows ? (int)threadIdx.x % 16 : (int)threadIdx.x / 64 * 32 + (int)threadIdx.x % 32), r1);
 }
 
+// The table's entries of a unit's first keys: those of the first two steps of a lane (split_unit), or CHUNK steps, a thread each (many_unit).
+template <class C, int HD, int TR>
+struct FirstOf {
+  static constexpr int N = TR == kAttnRows ? 2 * Tile<C, HD>::KB : Many<C, HD, kAhead<HD>>::CHUNK * 32 / 256;
+};
+template <class C, int HD, int TR>
+__device__ __forceinline__ void first_entries(const Cache &c, const Share &w, First<FirstOf<C, HD, TR>::N> &first) {
+#pragma unroll
+  for (int j = 0; j < FirstOf<C, HD, TR>::N; ++j) {
+    constexpr int KB = Tile<C, HD>::KB;
+    const int i = TR == kAttnRows ? (j / KB * kAttnWaves + (int)threadIdx.x / 64) * Mat<C>::kKeys + j % KB * 16 + (int)threadIdx.x % 16 : j * 256 + (int)threadIdx.x;
+    const int p = max(w.sp.pos(min(w.i0 + i, w.i1 - 1)), 0);     // (a unit of no keys: any entry)
+    first.e[j] = w.keys.entry(p, c.by_page.quot(p));
+  }
+}
+
 // Tile `tile` of all groups' rows, one group after the other, with split z of its group's prefix.  A token without a position (it
 // has no result) counts as one that sees all, so that it costs the others nothing.
-template <int TR>
-__device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int tile, int z, int head, Share &w) {
+template <class C, int HD, int TR>
+__device__ __forceinline__ bool prefix_unit(const Cache &c, const Prefixes &x, const Batch &b, const AttnArgs &a, int tile, int z, int head, Share &w,
+                                            First<FirstOf<C, HD, TR>::N> &first) {
   // a lane a group: where its tiles begin
   const int lane = threadIdx.x % 64;
   int g, s0, s1, t0, rows, n;
@@ -67,7 +100,7 @@ __device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, c
     g = min(g0 + lane, x.n_groups - 1);
     s0 = min(max(x.seq_start[g], 0), b.n_seq);
     s1 = min(max(x.seq_start[g + 1], s0), b.n_seq);
-    n = prefix_len(x, g);
+    n = cut_len(x, x.lens[g]);
     t0 = b.q_start ? min(max(b.q_start[s0], 0), b.n_tokens) : s0;
     rows = ((b.q_start ? min(max(b.q_start[s1], t0), b.n_tokens) : s1) - t0) * a.rep;
     const int tiles = g0 + lane < x.n_groups && n ? (rows + TR - 1) / TR : 0;
@@ -95,16 +128,30 @@ __device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, c
   if (z >= parts || (unsigned)tile >= (unsigned)((rows + TR - 1) / TR)) return false;
   w.r0 = r0;
   w.r1 = min(r0 + TR - 1, rows - 1);
+  const int *row = x.table + (long long)g * x.table_stride;
+  w.keys = {row, row, n};
+  w.sp = {0, 0, 0, 0, n};
+  w.i0 = z * len;
+  w.i1 = z == parts - 1 ? n : w.i0 + len;
+  first_entries<C, HD, TR>(c, w, first);
   const int t = t0 + a.by_rep.quot(my_row<TR>(r0, w.r1));
-  int s = t;
-  if (b.q_start) {                        // the last of the group's sequences that begins at or before the token
-    int hi = s1;
-    for (s = s0; s + 1 < hi;) {
+  int p;
+  if (!b.q_start) p = max(b.lens[t], 0) - 1;
+  else if (s1 - s0 <= 64) {               // (a lane a sequence: where it ends, and its length; the token's is the first that ends behind it)
+    const int ends = min(b.q_start[min(s0 + lane + 1, s1)], b.n_tokens), lens = b.lens[min(s0 + lane, s1 - 1)];
+    int k = 0;
+#pragma unroll
+    for (int d = 32; d; d >>= 1)
+      if (__shfl(ends, k + d - 1) <= t) k += d;
+    p = max(__shfl(lens, k), 0) - (__shfl(ends, k) - t);
+  } else {
+    int s = s0, hi = s1;
+    while (s + 1 < hi) {
       const int mid = (s + hi) >> 1;
       if (b.q_start[mid] <= t) s = mid; else hi = mid;
     }
+    p = position_of(b, s, t);
   }
-  int p = position_of(b, s, t);
   if (p < 0) p = kEverything;
   int lo = p, hi = p;
 #pragma unroll
@@ -116,10 +163,6 @@ __device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, c
   hi = __builtin_amdgcn_readfirstlane(hi);
   w.rows = {p, lo, hi};
   w.sp = {lo, hi, 0, 0, n};
-  const int *row = x.table + (long long)g * x.table_stride;
-  w.keys = {row, row, n};
-  w.i0 = z * len;
-  w.i1 = z == parts - 1 ? n : w.i0 + len;
   w.first_token = t0;
   w.row0 = t0;
   w.head = head;
@@ -129,15 +172,18 @@ __device__ __forceinline__ bool prefix_unit(const Prefixes &x, const Batch &b, c
 }
 
 // Tile `tile` of sequence s's rows with split z of its own keys (of all that it sees, where the prefixes have no units).
-template <int TR>
-__device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, const AttnArgs &a, int s, int tile, int z, int head, Share &w, int &parts) {
+template <class C, int HD, int TR, class F>
+__device__ __forceinline__ bool own_unit(const Cache &c, const Prefixes &x, const Batch &b, const AttnArgs &a, int s, int tile, int z, int head, Share &w,
+                                         F &first, int &parts) {
+  int g, n;
+  find_group(x, s, g, n);
   int first_token, count;
   seq_tokens(b, s, first_token, count);
   const int rows = min(count, a.max_new) * a.rep, r0 = tile * TR;
   if (r0 >= rows) return false;
   w.r0 = r0;
   w.r1 = min(r0 + TR - 1, rows - 1);
-  const int g = group_of(x, s), n = prefix_len(x, g), len = length_of(b, s);
+  const int len = length_of(b, s);
   const int lo = new_position(len, count, a.by_rep.quot(r0)), hi = new_position(len, count, a.by_rep.quot(w.r1));
   const int low = x.units ? n : 0, keys = max(0, min(hi + 1, max(b.cap, n)) - low);
   const int each = split_len(keys, a.n_splits, a.split_len);
@@ -153,6 +199,7 @@ __device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, cons
   w.keys = {x.table + (long long)max(g, 0) * x.table_stride, b.table + (long long)s * b.table_stride, n};
   w.i0 = z * each;
   w.i1 = z == parts - 1 ? keys : w.i0 + each;
+  if constexpr (F::have) first_entries<C, HD, TR>(c, w, first);
   w.first_token = first_token;
   w.row0 = first_token;
   w.head = head;
@@ -165,7 +212,7 @@ __device__ __forceinline__ bool own_unit(const Prefixes &x, const Batch &b, cons
 // PM, OM: tiles of 128 rows (many_unit) of the groups, of the sequences; else of 16 (split_unit).  Bounds and layouts: see there.
 template <class T, class C, int HD, bool PM, bool OM>
 struct ShareLds {
-  static constexpr int SPLIT = kAttnWaves * SplitLds<C, HD>::AREA, RES = kAttnWaves * 16 * 8, MANY = PM || OM ? Many<C, HD>::LDS : 0;
+  static constexpr int SPLIT = kAttnWaves * SplitLds<C, HD>::AREA, RES = kAttnWaves * 16 * 8, MANY = OM ? Many<C, HD>::LDS : PM ? Many<C, HD, kAhead<HD>>::LDS : 0;
   static constexpr int BYTES = (PM && OM) || MANY > SPLIT + RES ? MANY : SPLIT + RES;
 };
 template <class T, class C, int HD, bool PM, bool OM>
@@ -174,31 +221,33 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share(Cache 
   constexpr int PR = PM ? Many<C, HD>::ROWS : kAttnRows, OR = OM ? Many<C, HD>::ROWS : kAttnRows;
   Share w;
   w.n_parts = (x.units ? x.n_splits : 0) + a.n_splits;
-  auto split = [&] {
-    const int early[2][Tile<C, HD>::KB] = {};
-    float v[RowPart<HD>::E];
-    split_unit<T, C, HD>(c, a, w, lds, (float2(*)[16])(lds + ShareLds<T, C, HD, PM, OM>::SPLIT), false, early, v);
-  };
   int tile, s, z, head, parts;
   if constexpr (!OM) {                    // (sequences whose rows fill such tiles go through their prefixes themselves)
+    First<FirstOf<C, HD, OR>::N> first;
     if (blockIdx.x < x.units) {
       const unsigned u = blockIdx.x / c.n_kv_heads;
-      if (!prefix_unit<PR>(x, b, a, u % x.tiles, u / x.tiles, blockIdx.x % c.n_kv_heads, w)) return;
       if constexpr (PM) {
-        many_unit<T, C, HD>(c, a, w, lds);
+        First<FirstOf<C, HD, PR>::N> first;
+        if (prefix_unit<C, HD, PR>(c, x, b, a, u % x.tiles, u / x.tiles, blockIdx.x % c.n_kv_heads, w, first))
+          many_unit<T, C, HD, kAhead<HD>>(c, a, w, first, lds);
         return;
-      }
+      } else if (!prefix_unit<C, HD, PR>(c, x, b, a, u % x.tiles, u / x.tiles, blockIdx.x % c.n_kv_heads, w, first)) return;
     } else {
       work_of(blockIdx.x - x.units, c, b, a, tile, s, z, head);
-      if (!own_unit<OR>(x, b, a, s, tile, z, head, w, parts)) return;
+      if (!own_unit<C, HD, OR>(c, x, b, a, s, tile, z, head, w, first, parts)) return;
     }
-    split();
+    int early[2][Tile<C, HD>::KB];
+#pragma unroll
+    for (int j = 0; j < FirstOf<C, HD, OR>::N; ++j) early[j / Tile<C, HD>::KB][j % Tile<C, HD>::KB] = first.e[j];
+    float v[RowPart<HD>::E];
+    split_unit<T, C, HD>(c, a, w, lds, (float2(*)[16])(lds + ShareLds<T, C, HD, PM, OM>::SPLIT), true, early, v);
     if constexpr (!PM) {                  // (tickets: there are no prefixes' units)
       if (a.tickets && parts > 1) join_last<T, HD>(a, w, parts, (s * c.n_kv_heads + head) * a.tiles + tile);
     }
   } else {
+    NoFirst first;
     work_of(blockIdx.x, c, b, a, tile, s, z, head);
-    if (own_unit<OR>(x, b, a, s, tile, z, head, w, parts)) many_unit<T, C, HD>(c, a, w, lds);
+    if (own_unit<C, HD, OR>(c, x, b, a, s, tile, z, head, w, first, parts)) many_unit<T, C, HD, 2>(c, a, w, first, lds);
   }
 }
 
@@ -232,7 +281,9 @@ __global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixe
   seq_tokens(b, s, first, count);
   const int i = t - first;
   if (i >= min(count, a.max_new)) return;
-  const int len = length_of(b, s), n = prefix_len(x, group_of(x, s)), low = x.units ? n : 0;
+  int g, n;
+  find_group(x, s, g, n);
+  const int len = length_of(b, s), low = x.units ? n : 0;
   const int common = low ? split_count(n, x.n_splits, x.least) : 0;
   // (the last row of this one's tile: see own_unit)
   const int r = i * a.rep + h % a.rep, r1 = min(r - r % a.tile_rows + a.tile_rows, min(count, a.max_new) * a.rep) - 1;

@@ -74,19 +74,20 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     // (each group may have a tile that is not full)
     y.p_tiles = (int)std::min<long long>(((long long)b->n_tokens * rep + tile - 1) / tile + x->n_groups - 1, INT_MAX);
     const long long p_groups = std::max(1ll, std::min<long long>(y.p_tiles, groups * full) * p->n_kv_heads);
-    // Splits of the prefixes: a workgroup a CU, two where that leaves them 1024 keys (24 sequences behind 131071 positions 129 us, with one 142); the
-    // other places are the sequences'.  But no more than it takes to be done (20 ns a key) in half the time that all keys take to stream: every
-    // split is one more part of each row (64 sequences of 225 .. 900 own positions behind 8191, us by splits: 8 47.7, 16 52.6, 32 64.7)
+    // Splits of the prefixes: a workgroup a CU, at head size 64, where three have place, half as many more, and two where that leaves them 1024
+    // keys; the other places are the sequences'.  But no more than it takes to be done (20 ns a key) in half the time that all keys take to
+    // stream: every split is one more part of each row.  (us by splits: 64 sequences of 225 .. 900 own positions behind 8191, 16 tiles and heads:
+    // 8 53.8, 12 57.8, 16 59.1; 24 behind 131071, 8 tiles and heads: 32 128, 64 129, at head size 64 122 and 88)
     const long long own = std::max(1ll, keys - common);
     const double stream = (groups * (double)common + (double)b->n_seq * own) * key_bytes / 5e6;
-    const long long fit = common / 1024 * p_groups >= 512 ? 512 : 256, hide = (long long)(common * 0.02 / (0.45 * stream)) + 1;
+    const long long fit = p->head_dim == 128 ? 256 : common / 1024 * p_groups >= 512 ? 512 : 384, hide = (long long)(common * 0.02 / (0.4 * stream)) + 1;
     y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, 64ll}));
     y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;
     y.tiles = (int)((rows + kAttnRows - 1) / kAttnRows);
-    // of the sequences' own keys: see plan_attention
+    // of the sequences' own keys: see plan_attention; the places that are left
     const long long o_groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
     auto by = [&](long long goal, long long least) { return std::min({goal / o_groups, (own + least - 1) / least, 64ll}); };
-    y.n_splits = (int)std::max(1ll, std::max(by(768, 128), by(2048, 512)));
+    y.n_splits = (int)std::max(1ll, std::max(by(std::max(256ll, (p->head_dim == 128 ? 512 : 768) - p_groups * y.p_splits), 128), by(2048, 512)));
   }
   if (y.units || y.n_splits > 1) {
     const size_t parts = (size_t)b->n_tokens * nq * ((y.units ? y.p_splits : 0) + y.n_splits);

@@ -79,15 +79,16 @@ __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
   __shared__ int taken_;
   const int each = (n + nt - 1) / nt, s0 = tid * each;
   int free = min(max(*a.n_free, 0), a.n_pages);
-  int old[kBuildEach], d[kBuildEach], kept[kBuildEach];
+  int old[kBuildEach], d[kBuildEach], kept[kBuildEach], shared[kBuildEach];
   bool back = false;
 #pragma unroll
   for (int i = 0; i < kBuildEach; ++i) {
     const int s = s0 + i;
-    old[i] = d[i] = kept[i] = 0;
+    old[i] = d[i] = kept[i] = shared[i] = 0;
     if (i >= each || s >= n) continue;
     kept[i] = a.lens[s];
     d[i] = a.n_new[s];
+    if (a.n_shared) shared[i] = a.n_shared[s];
     old[i] = max(kept[i], 0);
     if (d[i] < 0) kept[i] = (int)max(0ll, (long long)old[i] + d[i]);
     back |= d[i] < 0;
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
     for (int i = 0; i < kBuildEach; ++i) {
       const int s = s0 + i;
       if (i >= each || s >= n) continue;
-      const int from = max(pages_of(a, max(kept[i], 0)), a.n_shared ? a.n_shared[s] : 0);
+      const int from = max(pages_of(a, max(kept[i], 0)), shared[i]);
       start[s] = from;
       page_sum[s] = d[i] < 0 ? min(pages_of(a, old[i]), a.max_pages) : from;
     }
