@@ -332,6 +332,7 @@ __device__ __forceinline__ void work_of(unsigned group, const Cache &c, const Ba
 // are the lowest and the highest of tokens i .. j (of a wavefront's rows, in k_attn_many).
 struct OneRow {
   const int *row;
+  __device__ __forceinline__ const int *place(int, int i) const { return row + i; }
   __device__ __forceinline__ int entry(int, int i) const { return row[i]; }
 };
 struct OfSequence {
@@ -879,13 +880,21 @@ template <class C, int HD, int AHEAD_ = 2>
 struct Many {
   typedef Mat<C> M;
   static constexpr int KEYS = 32, WROWS = 32, ROWS = 4 * WROWS;
-  static constexpr int AHEAD = AHEAD_, KRING = AHEAD, VRING = AHEAD + 2;          // in steps
+  // Steps in flight.  Values are needed two steps after their keys: from three steps on they are fetched two steps after them, which takes
+  // two stages less of LDS.
+  static constexpr int AHEAD = AHEAD_, LATER = AHEAD == 2 ? 0 : 2, KRING = AHEAD, VRING = AHEAD + 2 - LATER;
+  // loads that may be in flight behind a step: all but those of the keys n + 2 and values n, and what was issued before them
   static constexpr int CHUNK = AHEAD == 2 ? 16 : 8;      // steps whose rows are looked up at once
   static constexpr int ROW = HD * 2, PIECES = HD / 8;    // bytes and 16-byte pieces of a row
   static constexpr int KS = HD / 16, DB = HD / 32;
   static constexpr int STAGE = KEYS * ROW;
-  static constexpr int V = KRING * STAGE, PLACES = V + VRING * STAGE, THERE = PLACES + 2 * CHUNK * KEYS * 16, LDS = THERE + 2 * CHUNK * 4;
+  static constexpr int V = KRING * STAGE, PLACES = V + VRING * STAGE, THERE = PLACES + 2 * CHUNK * KEYS * 16, ENTRIES = THERE + 2 * CHUNK * 4;
+  // With more steps in flight the entries of a chunk come into LDS ahead too: a load whose result the compiler waits for would wait for all
+  // that is in flight.
+  static constexpr int LDS = ENTRIES + (LATER ? CHUNK * KEYS * 4 : 0);
+  static_assert(8 * STAGE <= THERE, "the results of four wavefronts lie over the rings and the places");
   static constexpr int PER = 64 / PIECES, NL = 8 / PER;  // a wavefront loads eight rows, PER of them at a time
+  static constexpr int IN_FLIGHT = (AHEAD - 2) * 2 * NL + (LATER ? 0 : NL);
   // Pieces of a row lie in an order by row: neighbouring rows of keys, and the four rows (of 64 bytes each) that half a wavefront's
   // transposing read of values takes, meet in different banks (conflicts: 1 % of LDS cycles; values in pairs of pieces 30 %)
   static __device__ __forceinline__ int k_swizzle(int row) { return HD == 128 ? row & 15 : row & 7; }
@@ -899,6 +908,9 @@ struct Many {
 // compiler keeps nothing in (it is reserved: it sets it in front of each use of its own, and takes no clobber of it).
 __device__ __forceinline__ void load_lds16(uint32_t lds, const void *from) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from));
+}
+__device__ __forceinline__ void load_lds4(uint32_t lds, const void *from) {           // the same with four bytes a lane
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from));
 }
 template <int N>
 __device__ __forceinline__ void wait_and_meet() {        // all but the last N loads done, by every wavefront
@@ -988,7 +1000,23 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
       if (lane < 2) there_of[(chunk & 1) * W::CHUNK + (j * 256 + wave * 64) / KEYS + lane] = (uint32_t)(all >> (32 * lane));
     }
   };
-  auto look_up = [&](int chunk) { look_up_by(chunk, [&](int, int p, int page) { return w.keys.entry(p, page); }); };
+  // A chunk's entries into LDS: a thread's are read by itself alone, CHUNK steps later
+  auto fetch_entries = [&](int chunk) {
+    if constexpr (W::LATER > 0)
+#pragma unroll
+    for (int j = 0; j < CK / 256; ++j) {
+      const int p = sp.pos(min(i0 + chunk * CK + j * 256 + (int)threadIdx.x, i1 - 1));
+      load_lds4(lds_base + W::ENTRIES + (j * 256 + wave * 64) * 4, w.keys.place(p, c.by_page.quot(p)));
+    }
+  };
+  auto look_up = [&](int chunk) {
+    if constexpr (W::LATER == 0) look_up_by(chunk, [&](int, int p, int page) { return w.keys.entry(p, page); });
+    else {
+      look_up_by(chunk, [&](int j, int, int) { return ((const volatile int *)(lds + W::ENTRIES))[j * 256 + threadIdx.x]; });
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (read before others come to their place)
+      fetch_entries(chunk + 1);
+    }
+  };
   // a lane's piece of a row: in LDS it lies where the swizzle puts it
   const int my_row = wave * 8 + lane / W::PIECES;
   int k_piece[NL], v_piece[NL];
@@ -1000,15 +1028,20 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
   const uint32_t lds0 = lds_base + wave * 8 * W::ROW;
   auto find = [&](int n, Place (&at)[NL]) {
 #pragma unroll
-    for (int j = 0; j < NL; ++j) at[j] = places[n % (2 * W::CHUNK) * KEYS + my_row + j * W::PER];
+    for (int j = 0; j < NL; ++j) {
+      const int row = my_row + j * W::PER;
+      if constexpr (W::LATER == 0) at[j] = places[n % (2 * W::CHUNK) * KEYS + row];
+      else at[j] = Place{places[n % (2 * W::CHUNK) * KEYS + row].x, places[(n + 2 * W::CHUNK - W::LATER) % (2 * W::CHUNK) * KEYS + row].y};
+    }
   };
-  // (a step's keys, then its values: they are needed a step later, and a wait may leave the last of them in flight)
+  // (a step's keys, then its values, or those of an earlier one: they are needed later, and a wait may leave the last of them in flight)
   auto fetch = [&](int n, const Place (&at)[NL]) {
 #pragma unroll
     for (int j = 0; j < NL; ++j) load_lds16(lds0 + n % W::KRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].x + k_piece[j]);
+    if (n < W::LATER) return;
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      load_lds16(lds0 + W::V + n % W::VRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].y + v_piece[j]);
+      load_lds16(lds0 + W::V + (n - W::LATER) % W::VRING * W::STAGE + j * W::PER * W::ROW, (const u32x4 *)at[j].y + v_piece[j]);
     }
   };
 
@@ -1077,10 +1110,11 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
       }
     };
     if (First::have && !careful) look_up_by(0, [&](int j, int, int) { return first.e[j]; });
-    else look_up(0);
+    else look_up_by(0, [&](int, int p, int page) { return w.keys.entry(p, page); });
     // the values of step -1 are zeros
     for (int i = threadIdx.x; i < W::STAGE / 16; i += 256) *(u32x4 *)(vlds + (W::VRING - 1) * W::STAGE + i * 16) = u32x4{0, 0, 0, 0};
     wait_and_meet<0>();
+    if constexpr (W::LATER > 0) fetch_entries(1);
 #pragma unroll
     for (int n = 0; n < W::AHEAD; ++n) {
       Place at[NL];
@@ -1089,11 +1123,11 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
     }
     if (careful) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      for (int n = 0; n < W::AHEAD; ++n) clean(n);
+      for (int n = 0; n < W::AHEAD - W::LATER; ++n) clean(n);
     } else {
       queries();
     }
-    wait_and_meet<(W::AHEAD - 2) * 2 * NL + NL>();
+    wait_and_meet<W::IN_FLIGHT>();
     // The operands of a step, one after the other: keys of S(n + 1), then values of step n - 1.  The swizzle's part that
     // depends on the operand is an exclusive or with a constant, the rest is the lane's.
     const uint32_t k0 = lds_base + W::k_at(col, h);
@@ -1175,9 +1209,9 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
       if ((n + W::AHEAD + 1) % W::CHUNK == 0) look_up((n + W::AHEAD + 1) / W::CHUNK);
       if (careful) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        clean(n + W::AHEAD);
+        clean(n + W::AHEAD - W::LATER);
       }
-      wait_and_meet<(W::AHEAD - 2) * 2 * NL + NL>();
+      wait_and_meet<W::IN_FLIGHT>();
     };
     Scores s0, s1;
     Probs p0, p1;
@@ -1195,7 +1229,7 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
       p0[0] = p0[1] = u32x4{0, 0, 0, 0};
     }
     settle(0, s0, there_of[0]);
-    wait_and_meet<(W::AHEAD - 2) * 2 * NL + NL>();               // (step 0 fetches over the keys of S(0))
+    wait_and_meet<W::IN_FLIGHT>();               // (step 0 fetches over the keys of S(0))
     // step `steps` only adds what the last one left
     for (int n = 0; n <= steps; n += 2) {
       step(n, s0, p0, s1, p1);

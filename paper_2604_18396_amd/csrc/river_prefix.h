@@ -51,7 +51,8 @@ __device__ __forceinline__ int split_count(int n, int most, int least) {
 struct TwoRows {
   const int *common, *own;
   int n;
-  __device__ __forceinline__ int entry(int p, int i) const { return (p < n ? common : own)[i]; }
+  __device__ __forceinline__ const int *place(int p, int i) const { return (p < n ? common : own) + i; }
+  __device__ __forceinline__ int entry(int p, int i) const { return *place(p, i); }
 };
 // Rows whose positions were found before: this lane's, and the lowest and highest of its wavefront's.
 struct Found {
@@ -62,9 +63,9 @@ struct Found {
 typedef Unit<TwoRows, Found> Share;
 
 constexpr int kAttnRows = 16;              // of a tile of split_unit
-// Steps of a prefix's keys in flight (many_unit): three at head size 128, whose stream they hide better (64 sequences behind 8191 58.1 ->
-// 53.8 us, 24 behind 131071 133 -> 129; four leave one workgroup a CU: 68, 149); at 64 no more than the compute-bound calls have (88.6 us, three 92)
-template <int HD> constexpr int kAhead = HD == 128 ? 3 : 2;
+// Steps of a prefix's keys in flight in many_unit: here they come from memory, where the prompts of k_attn_many read them again and again
+// (us with two / four: 64 sequences behind 8191 58.1 / 53.8, 24 behind 131071 133 / 125, at head size 64 92 / 87; five there 92, and no place at 128)
+constexpr int kAhead = 4;
 constexpr int kEverything = 1 << 30;       // a position that sees every key
 template <int TR>
 __device__ __forceinline__ int my_row(int r0, int r1) {           // this lane's row of a tile of TR
@@ -74,7 +75,7 @@ __device__ __forceinline__ int my_row(int r0, int r1) {           // this lane's
 // The table's entries of a unit's first keys: those of the first two steps of a lane (split_unit), or CHUNK steps, a thread each (many_unit).
 template <class C, int HD, int TR>
 struct FirstOf {
-  static constexpr int N = TR == kAttnRows ? 2 * Tile<C, HD>::KB : Many<C, HD, kAhead<HD>>::CHUNK * 32 / 256;
+  static constexpr int N = TR == kAttnRows ? 2 * Tile<C, HD>::KB : Many<C, HD, kAhead>::CHUNK * 32 / 256;
 };
 template <class C, int HD, int TR>
 __device__ __forceinline__ void first_entries(const Cache &c, const Share &w, First<FirstOf<C, HD, TR>::N> &first) {
@@ -212,7 +213,7 @@ __device__ __forceinline__ bool own_unit(const Cache &c, const Prefixes &x, cons
 // PM, OM: tiles of 128 rows (many_unit) of the groups, of the sequences; else of 16 (split_unit).  Bounds and layouts: see there.
 template <class T, class C, int HD, bool PM, bool OM>
 struct ShareLds {
-  static constexpr int SPLIT = kAttnWaves * SplitLds<C, HD>::AREA, RES = kAttnWaves * 16 * 8, MANY = OM ? Many<C, HD>::LDS : PM ? Many<C, HD, kAhead<HD>>::LDS : 0;
+  static constexpr int SPLIT = kAttnWaves * SplitLds<C, HD>::AREA, RES = kAttnWaves * 16 * 8, MANY = OM ? Many<C, HD>::LDS : PM ? Many<C, HD, kAhead>::LDS : 0;
   static constexpr int BYTES = (PM && OM) || MANY > SPLIT + RES ? MANY : SPLIT + RES;
 };
 template <class T, class C, int HD, bool PM, bool OM>
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share(Cache 
       if constexpr (PM) {
         First<FirstOf<C, HD, PR>::N> first;
         if (prefix_unit<C, HD, PR>(c, x, b, a, u % x.tiles, u / x.tiles, blockIdx.x % c.n_kv_heads, w, first))
-          many_unit<T, C, HD, kAhead<HD>>(c, a, w, first, lds);
+          many_unit<T, C, HD, kAhead>(c, a, w, first, lds);
         return;
       } else if (!prefix_unit<C, HD, PR>(c, x, b, a, u % x.tiles, u / x.tiles, blockIdx.x % c.n_kv_heads, w, first)) return;
     } else {
