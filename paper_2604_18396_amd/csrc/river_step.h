@@ -32,19 +32,25 @@ __device__ __forceinline__ int pages_of(const BuildArgs &a, int n) { return n > 
 constexpr uint32_t kMuch = 1u << 30;
 struct Two { uint32_t x, y; };
 __device__ __forceinline__ Two add(Two a, Two b) { return {min(a.x + b.x, kMuch), min(a.y + b.y, kMuch)}; }
-// What the threads before this one have, and all of them; two barriers.
-__device__ __forceinline__ Two sum_before(Two mine, Two *waves, Two &all) {
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = blockDim.x / 64;
+// What the lanes before this one have, and all of the wavefront
+__device__ __forceinline__ Two lanes_before(Two mine, Two &all) {
+  const int lane = threadIdx.x % 64;
   Two t = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const Two o = {__shfl_up(t.x, d), __shfl_up(t.y, d)};
     if (lane >= d) t = add(t, o);
   }
+  all = {(uint32_t)__builtin_amdgcn_readlane(t.x, 63), (uint32_t)__builtin_amdgcn_readlane(t.y, 63)};
+  const Two before = {__shfl_up(t.x, 1), __shfl_up(t.y, 1)};
+  return lane ? before : Two{0, 0};
+}
+// The same over the workgroup; two barriers.
+__device__ __forceinline__ Two threads_before(Two mine, Two *waves, Two &all) {
+  const int wave = threadIdx.x / 64, n = blockDim.x / 64;
+  Two sum, before = lanes_before(mine, sum);
   __syncthreads();
-  if (lane == 63) waves[wave] = t;
-  Two before = {__shfl_up(t.x, 1), __shfl_up(t.y, 1)};
-  if (lane == 0) before = {0, 0};
+  if (threadIdx.x % 64 == 0) waves[wave] = sum;
   __syncthreads();
   all = {0, 0};
   for (int w = 0; w < n; ++w) {
@@ -70,123 +76,133 @@ __device__ __forceinline__ void put_token(const BuildArgs &a, int t, int p, int 
   if (a.positions) a.positions[t] = max(p, 0);
 }
 
-template <bool TOKENS>
+// FEW: at most 64 sequences, a lane each, and every wavefront has all of them: its sums are its own, what it writes to LDS every other
+// writes too, and no barrier stands between.  Else a thread has EACH neighbouring ones, and the sums go through LDS.
+// Bound: latency, of the loads that need what others brought (lengths, the free list, the rows), and of the barriers.
+template <bool TOKENS, bool FEW>
 __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
   extern __shared__ int sums[];
-  const int n = a.n_seq, nt = blockDim.x, tid = threadIdx.x, lane = tid % 64;
+  constexpr int EACH = FEW ? 1 : kBuildEach;
+  const int n = a.n_seq, nt = blockDim.x, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   int *const len = sums, *const page_sum = sums + n, *const start = sums + 2 * n;     // [n], [n], [n + 1]
   __shared__ Two waves[kBuildThreads / 64];
+  __shared__ int gone[2][kBuildThreads / 64];
   __shared__ int taken_;
-  const int each = (n + nt - 1) / nt, s0 = tid * each;
+  auto sum_before = [&](Two mine, Two &all) { return FEW ? lanes_before(mine, all) : threads_before(mine, waves, all); };
+  const int each = FEW ? 1 : (n + nt - 1) / nt, s0 = FEW ? lane : tid * each;
+  auto mine = [&](int i) { return i < each && s0 + i < n; };      // is sequence s0 + i this thread's?
   int free = min(max(*a.n_free, 0), a.n_pages);
-  int old[kBuildEach], d[kBuildEach], kept[kBuildEach], shared[kBuildEach];
+  int old[EACH], d[EACH], kept[EACH], shared[EACH];
   bool back = false;
 #pragma unroll
-  for (int i = 0; i < kBuildEach; ++i) {
-    const int s = s0 + i;
+  for (int i = 0; i < EACH; ++i) {
     old[i] = d[i] = kept[i] = shared[i] = 0;
-    if (i >= each || s >= n) continue;
-    kept[i] = a.lens[s];
-    d[i] = a.n_new[s];
-    if (a.n_shared) shared[i] = a.n_shared[s];
+    if (!mine(i)) continue;
+    kept[i] = a.lens[s0 + i];
+    d[i] = a.n_new[s0 + i];
+    if (a.n_shared) shared[i] = a.n_shared[s0 + i];
+  }
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
     old[i] = max(kept[i], 0);
     if (d[i] < 0) kept[i] = (int)max(0ll, (long long)old[i] + d[i]);
     back |= d[i] < 0;
   }
   if (tid == 0) taken_ = 0;
-  if (__syncthreads_or(back)) {
-    // Given back: entries from .. to - 1 of a row that name pages, the last one of the last sequence first onto the free list, so that
-    // pages that a call has given out come to lie as they lay before it.  Sixteen lanes a row: how many, then where.
-    const int sub = tid % 16, shift = lane / 16 * 16;
-    auto mine_of = [&](bool ok) { return (uint32_t)(__ballot(ok) >> shift) & 0xffffu; };
+  if (__syncthreads_or(back)) {           // (and everything has been read that may be written over)
+    // Given back: entries of a row that name pages, from the last one on down to what is kept or shared, the last sequence's first, so that pages
+    // that a call has given out come to lie in the free list as they lay before it.  A thread an entry, in that order: sequence n - 1 - r has
+    // those below page_sum[r].
+    uint32_t to[EACH];
+    Two go[EACH], sum = {0, 0}, all;
 #pragma unroll
-    for (int i = 0; i < kBuildEach; ++i) {
-      const int s = s0 + i;
-      if (i >= each || s >= n) continue;
-      const int from = max(pages_of(a, max(kept[i], 0)), shared[i]);
-      start[s] = from;
-      page_sum[s] = d[i] < 0 ? min(pages_of(a, old[i]), a.max_pages) : from;
+    for (int i = 0; i < EACH; ++i) {
+      to[i] = min(pages_of(a, old[i]), a.max_pages);
+      go[i] = {(uint32_t)(d[i] < 0 ? max(0, (int)to[i] - max(pages_of(a, max(kept[i], 0)), shared[i])) : 0), 0};
+      sum = add(sum, go[i]);
     }
-    __syncthreads();
-    for (int s = tid / 16; s < n; s += nt / 16) {
-      const int *row = a.table + (long long)s * a.table_stride;
-      int count = 0;
-      for (int i = start[s] + sub; i - sub < page_sum[s]; i += 16) {
-        const int page = i < page_sum[s] ? row[i] : -1;
-        count += __popc(mine_of((unsigned)page < (unsigned)a.n_pages));
-      }
-      if (sub == 0) len[s] = count;
-    }
-    __syncthreads();
-    Two mine = {0, 0}, all;
+    Two before = sum_before(sum, all);
 #pragma unroll
-    for (int i = 0; i < kBuildEach; ++i)
-      if (i < each && s0 + i < n) mine.x += len[s0 + i];
-    const Two before = sum_before(mine, waves, all);
-    int behind = (int)(all.x - before.x);
-#pragma unroll
-    for (int i = 0; i < kBuildEach; ++i)
-      if (i < each && s0 + i < n) {
-        behind -= len[s0 + i];
-        len[s0 + i] = free + behind;
+    for (int i = 0; i < EACH; ++i)
+      if (mine(i)) {
+        page_sum[n - 1 - s0 - i] = (int)(all.x - before.x);
+        before = add(before, go[i]);
+        start[s0 + i] = (int)to[i];
       }
-    __syncthreads();
-    for (int s = tid / 16; s < n; s += nt / 16) {
-      int *row = a.table + (long long)s * a.table_stride;
-      int at = len[s];
-      for (int i = page_sum[s] - 1 - sub; i + sub >= start[s]; i -= 16) {
-        const int page = i >= start[s] ? row[i] : -1;
-        const bool ok = (unsigned)page < (unsigned)a.n_pages;
-        const uint32_t all_ok = mine_of(ok);
-        const int to = at + __popc(all_ok & ((1u << sub) - 1));
-        if (ok && to < a.n_pages) a.free_pages[to] = page;
-        if (i >= start[s]) row[i] = -1;
-        at += __popc(all_ok);
+    if (!FEW) __syncthreads();
+    int done = 0;
+    for (int j0 = 0, buf = 0; j0 < (int)all.x; j0 += nt, buf ^= 1) {
+      const int j = j0 + tid;
+      int *entry = nullptr, page = -1;
+      if (j < (int)all.x) {
+        const int r = first_above(page_sum, n, j), s = n - 1 - r;
+        entry = a.table + (long long)s * a.table_stride + start[s] - 1 - (j - (r ? page_sum[r - 1] : 0));
+        page = *entry;
       }
+      const bool ok = (unsigned)page < (unsigned)a.n_pages;
+      const unsigned long long oks = __ballot(ok);
+      if (lane == 0) gone[buf][wave] = __popcll(oks);
+      __syncthreads();
+      int at = free + done + __popcll(oks & ((1ull << lane) - 1));
+      for (int w = 0; w < nt / 64; ++w) {
+        if (w < wave) at += gone[buf][w];
+        done += gone[buf][w];
+      }
+      if (ok && at < a.n_pages) a.free_pages[at] = page;
+      if (entry) *entry = -1;
     }
-    free = (int)min((long long)a.n_pages, (long long)free + all.x);
+    free = min(a.n_pages, free + done);
     __syncthreads();
   }
   // Asked for: tokens and pages, one after the other.  Who has no room in its row takes no part.
-  Two ask[kBuildEach], all;
+  Two ask[EACH], all;
   Two sum = {0, 0};
 #pragma unroll
-  for (int i = 0; i < kBuildEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     const bool fits = d[i] > 0 && (long long)old[i] + d[i] <= a.cap;
     ask[i].x = fits ? d[i] : 0;
     ask[i].y = fits ? pages_of(a, old[i] + d[i]) - pages_of(a, old[i]) : 0;
     sum = add(sum, ask[i]);
   }
-  Two so_far = sum_before(sum, waves, all), given = {0, 0};
+  Two so_far = sum_before(sum, all), given = {0, 0};
   int taken = 0;
 #pragma unroll
-  for (int i = 0; i < kBuildEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     so_far = add(so_far, ask[i]);
     const bool yes = so_far.x <= (uint32_t)a.n_tokens && (ask[i].y == 0 || so_far.y <= (uint32_t)free);
     if (!yes) ask[i].x = 0;
     else if (ask[i].y) taken = (int)so_far.y;
-    if (i < each && s0 + i < n) page_sum[s0 + i] = (int)so_far.y;
+    if (mine(i)) page_sum[s0 + i] = (int)so_far.y;
     given.x += ask[i].x;
     given.y += d[i] > 0 && ask[i].x == 0;
   }
-  if (taken) atomicMax(&taken_, taken);
-  Two before = sum_before(given, waves, all);
+  if constexpr (FEW) {                    // (the sums ascend: the last that took any has the most)
+    const unsigned long long took = __ballot(taken > 0);
+    taken = took ? __builtin_amdgcn_readlane(taken, 63 - __clzll(took)) : 0;
+  } else if (taken) atomicMax(&taken_, taken);
+  Two before = sum_before(given, all);
+  const bool writes = !FEW || wave == 0;
 #pragma unroll
-  for (int i = 0; i < kBuildEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     const int s = s0 + i;
-    if (i >= each || s >= n) continue;
+    if (!mine(i)) continue;
     len[s] = old[i];
-    start[s] = a.q_start[s] = (int)before.x;
-    a.lens_out[s] = kept[i] + (int)ask[i].x + (ask[i].x ? old[i] - kept[i] : 0);
+    start[s] = (int)before.x;
+    if (writes) {
+      a.q_start[s] = (int)before.x;
+      a.lens_out[s] = ask[i].x ? old[i] + (int)ask[i].x : kept[i];
+    }
     before.x += ask[i].x;
   }
-  taken = taken_;
+  if (!FEW) taken = taken_;
+  if (FEW ? lane == 0 : tid == 0) start[n] = (int)all.x;
   if (tid == 0) {
-    start[n] = a.q_start[n] = (int)all.x;
+    a.q_start[n] = (int)all.x;
     *a.n_free_out = free - taken;
     if (a.refused) *a.refused = (int)all.y;
   }
-  __syncthreads();
+  if (FEW) __builtin_amdgcn_wave_barrier();
+  else __syncthreads();
   // Page j of those that are taken is the one that lies j below the top
   for (int j = tid; j < taken; j += nt) {
     const int s = first_above(page_sum, n, j), i = pages_of(a, len[s]) + j - (s ? page_sum[s - 1] : 0);

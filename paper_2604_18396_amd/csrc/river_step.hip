@@ -32,12 +32,13 @@ extern "C" int river_build_batch(const river_tables *t, const int32_t *n_new, in
                       t->table_stride, t->n_pages, t->page_size, n_tokens, (int)std::min<long long>((long long)t->max_pages * t->page_size, kMostPositions),
                       div_by(t->page_size), q_start, (long long *)slots, positions, refused};
     const bool tokens = slots || positions, apart = tokens && n_tokens > kTokensInOne;
-    // Threads: sixteen a sequence, which may give pages back, and one a token, as far as one workgroup reaches
-    const int threads = std::min(kBuildThreads, std::max({64, 16 * t->n_seq, tokens ? n_tokens : 0}) + 63 & ~63);
+    // Threads: one a token or a page, as far as one workgroup reaches, and one a sequence
+    const int threads = std::min(kBuildThreads, std::max({64, 4 * t->n_seq, tokens ? n_tokens : 0}) + 63 & ~63);
     const size_t lds = (3 * (size_t)t->n_seq + 1) * 4;
     const hipStream_t st = (hipStream_t)hip_stream;
-    hipError_t e = tokens && !apart ? launch(k_build<true>, dim3(1), dim3(threads), lds, st, a)
-                                    : launch(k_build<false>, dim3(1), dim3(threads), lds, st, a);
+    auto go = [&](auto k) { return launch(k, dim3(1), dim3(threads), lds, st, a); };
+    const bool few = t->n_seq <= 64;
+    hipError_t e = tokens && !apart ? (few ? go(k_build<true, true>) : go(k_build<true, false>)) : few ? go(k_build<false, true>) : go(k_build<false, false>);
     if (e == hipSuccess && apart)
       e = launch(k_slots, dim3((n_tokens + 256 * kSlotsEach - 1) / (256 * kSlotsEach)), dim3(256), 0, st, a);
     return e == hipSuccess ? RIVER_OK : hip_failed("river_build_batch", e);
