@@ -216,8 +216,10 @@ struct ShareLds {
   static constexpr int SPLIT = kAttnWaves * SplitLds<C, HD>::AREA, RES = kAttnWaves * 16 * 8, MANY = OM ? Many<C, HD>::LDS : PM ? Many<C, HD, kAhead>::LDS : 0;
   static constexpr int BYTES = (PM && OM) || MANY > SPLIT + RES ? MANY : SPLIT + RES;
 };
+// Both kinds in one kernel take more than the 168 registers that leave three workgroups a CU at head size 64: two (24 sequences behind
+// 131071 85 -> 75 us, without the 20 registers that were spilled).
 template <class T, class C, int HD, bool PM, bool OM>
-__global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_share(Cache c, Batch b, AttnArgs a, Prefixes x) {
+__global__ __launch_bounds__(kAttnThreads, HD == 64 && !(PM && !OM) ? 3 : 2) void k_share(Cache c, Batch b, AttnArgs a, Prefixes x) {
   extern __shared__ __align__(1024) char lds[];
   constexpr int PR = PM ? Many<C, HD>::ROWS : kAttnRows, OR = OM ? Many<C, HD>::ROWS : kAttnRows;
   Share w;

@@ -74,15 +74,16 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     // (each group may have a tile that is not full)
     y.p_tiles = (int)std::min<long long>(((long long)b->n_tokens * rep + tile - 1) / tile + x->n_groups - 1, INT_MAX);
     const long long p_groups = std::max(1ll, std::min<long long>(y.p_tiles, groups * full) * p->n_kv_heads);
-    // Splits of the prefixes, as workgroups: at head size 128 one a CU, or seven on four CUs (the eighth place is for the sequences) where that
-    // leaves them 1024 keys, at 64, where three have place on a CU, six on four, or two a CU where that leaves 512.  But no more than it takes to be
-    // done (20 ns a key) in two fifths of the time that all keys take to stream: every split is one more part of each row.
+    // Splits of the prefixes, as workgroups: one a CU, or seven on four CUs (the eighth place is for the sequences) where that leaves them 1024
+    // keys; six on four where three have place on a CU.  But no more than it takes to be done (20 ns a key) in two fifths of the time that
+    // all keys take to stream: every split is one more part of each row.
     // (us by splits: 24 sequences behind 131071 positions, 8 tiles and heads, 32 132, 48 128, 56 122, 64 125; 32 behind 65536 32 77.5, 56 77.6,
     // 64 83; 32 behind 32768 32 48, 56 53; 64 of 225 .. 900 own positions behind 8191, 16 tiles and heads, 6 58, 8 53.8, 12 57.4, 16 59;
-    // head size 64: 24 behind 65536 32 62, 48 58, 64 52; 48 behind 16384, 16 tiles and heads, 24 34.7, 32 32.6, 48 35.8)
+    // head size 64: 24 behind 131071 32 90, 48 79, 64 73 .. 77; 48 behind 16384, 16 tiles and heads, 16 29.8, 24 30.2, 32 31.1)
     const long long own = std::max(1ll, keys - common);
     const double stream = (groups * (double)common + (double)b->n_seq * own) * key_bytes / 5e6;
-    const long long fit = p->head_dim == 128 ? (common * p_groups >= 448 * 1024 ? 448 : 256) : common * p_groups >= 512 * 512 ? 512 : 384;
+    const bool three = p->head_dim == 64 && !y.p_many;           // (workgroups that have place on a CU: see k_share)
+    const long long places = three ? 768 : 512, fit = three ? 384 : common * p_groups >= 448 * 1024 ? 448 : 256;
     const long long hide = (long long)(common * 0.02 / (0.4 * stream)) + 1;
     y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, 64ll}));
     y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;
@@ -90,7 +91,7 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     // of the sequences' own keys: see plan_attention; the places that are left
     const long long o_groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
     auto by = [&](long long goal, long long least) { return std::min({goal / o_groups, (own + least - 1) / least, 64ll}); };
-    y.n_splits = (int)std::max(1ll, std::max(by(std::max(256ll, (p->head_dim == 128 ? 512 : 768) - p_groups * y.p_splits), 128), by(2048, 512)));
+    y.n_splits = (int)std::max(1ll, std::max(by(std::max(256ll, places - p_groups * y.p_splits), 128), by(2048, 512)));
   }
   if (y.units || y.n_splits > 1) {
     const size_t parts = (size_t)b->n_tokens * nq * ((y.units ? y.p_splits : 0) + y.n_splits);
