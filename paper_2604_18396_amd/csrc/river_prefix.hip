@@ -38,10 +38,22 @@ struct SharePlan {
 // Prefixes have units of their own where that saves enough of reading them for each sequence: 24 MB, or 8 MB of a long one.  (A call then
 // takes two launches, and its parts are written and read.  us, apart / each sequence through its prefix, 8B shape, 64 positions of their own:
 // 2 sequences behind 1024 11.7 / 9.9, behind 4096 12.8 / 15.5; 8 behind 1024 12.1 / 11.9; 16 behind 256 11.8 / 9.8, behind 1024 12.9 / 19.7;
-// 64 behind 16384 40 / 472; 1B shape: 2 behind 4096 11.8 / 11.6, 16 behind 1024 11.8 / 11.6, 32 behind 1024 12.0 / 14.6.)  And not where a
-// sequence's own rows fill a tile of 128: it reads its prefix as often as a group's tile would.
+// 64 behind 16384 40 / 472; 1B shape: 2 behind 4096 11.8 / 11.6, 16 behind 1024 11.8 / 11.6, 32 behind 1024 12.0 / 14.6.)
 constexpr double kSaves = 24e6, kSavesLong = 8e6;
 constexpr int kLong = 4096;
+// Several new tokens of 16-bit types: sequences whose rows nearly fill tiles of 128 read their prefixes hardly more often than a group's tiles do.
+// An estimate of both in us: what a tile of 128 rows or of 16 takes per key and key head on the whole card, parts written and read at 4 TB/s.
+// (us, apart / through, 8B shape, 300 own positions: 24 sequences of up to 8 new tokens behind 1024 31 / 35, behind 8192 45 / 128; of 24 46 / 42,
+// 91 / 136; of 48 73 / 46, 165 / 228; of 100 134 / 52, 318 / 415; 6 of 8 17.5 / 20.4, 27 / 39, of 48 36 / 32, 58 / 64; 1B shape: 24 of 24 27.9 / 29.8,
+// 66 / 97, of 48 47 / 33, 102 / 166)
+bool pays(const river_pages *p, const river_batch *b, int nq, long long rows, double groups, double common, double own) {
+  const int rep = nq / p->n_kv_heads;
+  const double all = (double)b->n_tokens * rep, n = b->n_seq, large = p->n_kv_heads * (p->head_dim == 128 ? 65e-6 : 50e-6),
+               small = p->n_kv_heads * (p->head_dim == 128 ? 80e-6 : 50e-6);
+  const double through = n * ((rows + 127) / 128) * (common + own) * large + 12;
+  const double apart = (all / 128 + groups) * common * large + (all / 16 + n / 2) * own * 0.6 * small + (double)b->n_tokens * nq * 2 * (p->head_dim * 4 + 8) * 2 / 4e6 + 10;
+  return apart < through;
+}
 // By tiles of 128 rows (many_unit) where rows x keys x elements of a key head are more than these: they read a key once for 128 rows, those of 16 take
 // less time to begin and end (us, 128 / 16, 8B shape: 32 rows behind 4096 17.7 / 15.1, behind 16384 25.3 / 26.0; 128 behind 1024 17.0 / 15.8,
 // behind 4096 23.1 / 25.9; 256 behind 1024 18.2 / 21.5; 1B shape: 64 behind 16384 23.1 / 24.1, 128 behind 4096 16.9 / 16.7, 256
@@ -58,8 +70,11 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
   const double key_bytes = 2. * p->n_kv_heads * p->head_dim * (p->dtype == RIVER_F32 ? 4 : 2);
   const long long in_group = std::min<long long>(x->max_seqs, b->n_seq), groups = std::min<long long>(x->n_groups, b->n_seq);
   const double saves = std::min<double>(groups * (in_group - 1.), b->n_seq) * common * key_bytes;
+  const long long own = std::max(1ll, keys - common);
+  const bool apart = p->dtype == RIVER_BF16 && rows > kAttnRows ? saves > 0 && pays(p, b, nq, rows, (double)groups, (double)common, (double)own)
+                                                                : saves >= (common >= kLong ? kSavesLong : kSaves);
   constexpr int kManyRows = Many<__bf16, 128>::ROWS;
-  if (saves < (common >= kLong ? kSavesLong : kSaves) || (p->dtype == RIVER_BF16 && rows >= kManyRows)) {
+  if (!apart) {
     const AttnPlan o = plan_attention(p, b, nq, 0, 0);
     y.many = y.p_many = o.many;
     y.tiles = o.tiles;
@@ -71,8 +86,8 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     y.least = y.p_least = 128;
     const int tile = y.p_many ? kManyRows : kAttnRows;
     const long long full = (group_rows + tile - 1) / tile;
-    // (each group may have a tile that is not full)
-    y.p_tiles = (int)std::min<long long>(((long long)b->n_tokens * rep + tile - 1) / tile + x->n_groups - 1, INT_MAX);
+    // (each group that has sequences may have a tile that is not full)
+    y.p_tiles = (int)std::min<long long>(((long long)b->n_tokens * rep + tile - 1) / tile + std::max(0ll, groups - 1), INT_MAX);
     const long long p_groups = std::max(1ll, std::min<long long>(y.p_tiles, groups * full) * p->n_kv_heads);
     // Splits of the prefixes, as workgroups: one a CU, or seven on four CUs (the eighth place is for the sequences) where that leaves them 1024
     // keys; six on four where three have place on a CU.  But no more than it takes to be done (20 ns a key) in two fifths of the time that
@@ -80,7 +95,6 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     // (us by splits: 24 sequences behind 131071 positions, 8 tiles and heads, 32 132, 48 128, 56 122, 64 125; 32 behind 65536 32 77.5, 56 77.6,
     // 64 83; 32 behind 32768 32 48, 56 53; 64 of 225 .. 900 own positions behind 8191, 16 tiles and heads, 6 58, 8 53.8, 12 57.4, 16 59;
     // head size 64: 24 behind 131071 32 90, 48 79, 64 73 .. 77; 48 behind 16384, 16 tiles and heads, 16 29.8, 24 30.2, 32 31.1)
-    const long long own = std::max(1ll, keys - common);
     const double stream = (groups * (double)common + (double)b->n_seq * own) * key_bytes / 5e6;
     const bool three = p->head_dim == 64 && !y.p_many;           // (workgroups that have place on a CU: see k_share)
     const long long places = three ? 768 : 512, fit = three ? 384 : common * p_groups >= 448 * 1024 ? 448 : 256;

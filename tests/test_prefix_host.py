@@ -87,8 +87,9 @@ def test_calls_without_tokens_end_at_once():
 
 def test_calls_that_are_too_large_are_refused():
     assert attend(b=batch(n_tokens=1 << 22, max_new=1 << 22), nq=64, qs=4096, os=4096) == B.RIVER_EINVAL and "too many" in text()
-    many = prefixes(n_groups=1 << 22, max_pages=1 << 20, table_stride=1 << 20, max_len=1 << 20)
-    assert attend(x=many, b=batch(n_tokens=4), ws=P, n=1 << 62) == B.RIVER_EINVAL and "too many" in text()
+    pg = pages(n_kv_heads=8, page_size=1, page_stride=512, layer_stride=8 * 512)
+    assert attend(pg, batch(n_seq=1 << 22, n_tokens=1 << 22, max_new=1), BIG, nq=8, qs=512, os=512, ws=P, n=1 << 62) == B.RIVER_EINVAL
+    assert "too many" in text()
 
 
 @pytest.mark.parametrize("bad", [dict(layer=2), dict(layer=-1), dict(n=-1), dict(n=2**23), dict(slots=0), dict(k=0), dict(v=0), dict(slots=P + 4), dict(k=P + 1),
