@@ -254,6 +254,41 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 && !(PM && !OM) ? 3 : 2) voi
   }
 }
 
+// Head h of token t: parts of its group's prefix, parts of its sequence's own, its position.  False: it has no row.
+__device__ __forceinline__ bool parts_of(const Batch &b, const AttnArgs &a, const Prefixes &x, int t, int h, int &common, int &own, int &p) {
+  int s = t;
+  if (b.q_start) {
+    s = __builtin_amdgcn_readfirstlane(count_up_to(b.q_start, b.n_seq + 1, t)) - 1;
+    if (s < 0 || s >= b.n_seq) return false;
+  }
+  int first, count;
+  seq_tokens(b, s, first, count);
+  const int i = t - first;
+  if (i >= min(count, a.max_new)) return false;
+  int g, n;
+  find_group(x, s, g, n);
+  const int len = length_of(b, s), low = x.units ? n : 0;
+  common = low ? split_count(n, x.n_splits, x.least) : 0;
+  // (the last row of this one's tile: see own_unit)
+  const int r = i * a.rep + h % a.rep, r1 = min(r - r % a.tile_rows + a.tile_rows, min(count, a.max_new) * a.rep) - 1;
+  const int keys = max(0, min(new_position(len, count, a.by_rep.quot(r1)) + 1, max(b.cap, n)) - low);
+  own = split_count(keys, a.n_splits, a.split_len);
+  p = new_position(len, count, i);
+  return true;
+}
+
+// Few parts where prefixes have no units: bit for bit what a tile's last workgroup does where it has tickets.  Sixteen heads of a token.
+template <class T, int HD>
+__global__ __launch_bounds__(256) void k_share_join_few(Batch b, AttnArgs a, Prefixes x, int chunks) {
+  constexpr int E = RowPart<HD>::E, LANES = RowPart<HD>::LANES;
+  const int t = blockIdx.x / chunks, h = blockIdx.x % chunks * 16 + threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
+  int common, own, p;
+  if (!parts_of(b, a, x, t, min(h, a.nq - 1), common, own, p) || own == 1 || h >= a.nq) return;
+  float v[E], sum;
+  join_parts<HD, E>(a, ((long long)t * a.nq + h) * a.n_splits, own, e0, v, sum);
+  store_row<T, E>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, v, sum);
+}
+
 // A row's parts, joined: those of its group's prefix, then its sequence's own.  A workgroup has RB heads of one token, and where a row has
 // many parts G groups of lanes that take other parts each; their sums are added in their order.  Bound: latency; so the first parts are on
 // their way before it is known which of them there are.
@@ -275,23 +310,8 @@ __global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixe
     }
   };
   fetch(group);
-  int s = t;
-  if (b.q_start) {
-    s = __builtin_amdgcn_readfirstlane(count_up_to(b.q_start, b.n_seq + 1, t)) - 1;
-    if (s < 0 || s >= b.n_seq) return;
-  }
-  int first, count;
-  seq_tokens(b, s, first, count);
-  const int i = t - first;
-  if (i >= min(count, a.max_new)) return;
-  int g, n;
-  find_group(x, s, g, n);
-  const int len = length_of(b, s), low = x.units ? n : 0;
-  const int common = low ? split_count(n, x.n_splits, x.least) : 0;
-  // (the last row of this one's tile: see own_unit)
-  const int r = i * a.rep + h % a.rep, r1 = min(r - r % a.tile_rows + a.tile_rows, min(count, a.max_new) * a.rep) - 1;
-  const int keys = max(0, min(new_position(len, count, a.by_rep.quot(r1)) + 1, max(b.cap, n)) - low);
-  const int own = split_count(keys, a.n_splits, a.split_len);
+  int common, own, p;
+  if (!parts_of(b, a, x, t, h, common, own, p)) return;
   float big = -INFINITY, sum = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int y0 = group;;) {
@@ -343,7 +363,7 @@ __global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixe
     }
   }
   if (common + own == 1 || blockIdx.x % chunks * RB + in >= a.nq) return;          // (it is done already, or no row)
-  if (new_position(len, count, i) < 0) sum = 0.f;                // (a token without a position sees nothing)
+  if (p < 0) sum = 0.f;                                          // (a token without a position sees nothing)
   const float out[4] = {v[0], v[1], v[2], v[3]};
   store_row<T, 4>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, out, sum);
 }

@@ -192,6 +192,10 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
       e = by_types(pages, [&](auto t, auto, auto hd) {
         constexpr int HD = decltype(hd)::v;
         typedef decltype(t) T;
+        if (y.fused) {
+          const int sixteens = (n_q_heads + 15) / 16;
+          return launch(k_share_join_few<T, HD>, dim3((unsigned)(b.n_tokens * sixteens)), dim3(256), 0, st, b, a, x, sixteens);
+        }
         const dim3 grid((unsigned)(b.n_tokens * chunks)), block(256);
         return heads == 1   ? launch(k_share_join<T, HD, 1>, grid, block, 0, st, b, a, x, chunks)
                : heads == 2 ? launch(k_share_join<T, HD, 2>, grid, block, 0, st, b, a, x, chunks)

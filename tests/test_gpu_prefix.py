@@ -130,6 +130,35 @@ def test_large_groups(kind, hd, how):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@HOW
+def test_many_groups(kind, how):
+    # more groups than a wavefront has lanes, some of them empty, some sequences in front of the first and behind the last
+    groups = [(1 + (i * 97) % 300, (i * 7) % 4) for i in range(150)]
+    n = 3 + sum(k for _, k in groups) + 2
+    lonely, own = (7, 130, 1), [(i * 11) % 90 for i in range(n - 3)]
+    for new in ([1] * n, [1 + i % 5 for i in range(n)]):
+        run(Shared(kind, 1, 64, 16, behind(groups, own, new, lonely), new, groups, lonely=3, seed=14, how=how), 4)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@HOW
+def test_queries_of_places_without_a_sequence(kind, bad, how):
+    """A padded batch: places whose sequence has no positions, with whatever bits in their queries, are zeros, and all others have the bits that they
+    have without them."""
+    for new in ([1] * 9, [1, 2, 3, 4, 5, 1, 2, 3, 4]):
+        lens = [260 + 9 * i + m for i, m in enumerate(new)]
+        lens[1] = lens[4] = lens[8] = 0
+        st = Shared(kind, 1, 64, 16, lens, new, [(250, 9)], seed=15, how=how)
+        q = st.randn(st.tokens, 8, 64)
+        places = torch.tensor([t for s, t, _ in st.positions() if s in (1, 4, 8)], device=DEV)
+        q[places] = 0.0
+        clean = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+        q[places] = bad
+        assert torch.equal(B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q), clean) and not bool(clean[places].any())
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("groups,own,new", [([(20000, 2)], [100, 3000], [1, 1]), ([(50, 2)], [20000, 10], [1, 1]), ([(9000, 2)], [100, 5], [20, 33])], ids=str)
 @HOW
 def test_long_caches(kind, groups, own, new, how):
@@ -333,6 +362,33 @@ def test_the_same_call_gives_the_same_bits(how):
                 first = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
                 for _ in range(5):
                     assert torch.equal(first, B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@HOW
+def test_a_captured_call_has_the_bits_of_an_eager_one(kind, how):
+    """(A captured call has no tickets: its splits are joined by a launch of their own.)  Replayed with eager calls and synchronizations between, while
+    lengths, prefixes and queries change."""
+    groups, own = [(700, 3), (90, 2)], [300, 0, 41, 5, 200]
+    for new in ([1] * 5, [2, 5, 1, 3, 4]):
+        lens = behind(groups, own, new)
+        st = Shared(kind, 2, 64, 16, lens, new, groups, ragged=new[1] > 1, seed=16, how=how)
+        q, out = st.randn(st.tokens, 8, 64), torch.zeros(st.tokens, 8, 64, dtype=st.act, device=DEV)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q, out=out)
+        for i in range(5):
+            q.copy_(st.randn(st.tokens, 8, 64))
+            st.dlens.copy_(torch.tensor([n - i for n in lens], dtype=torch.int32))
+            st.prefixes.lens.copy_(torch.tensor([700 - 32 * i, 90 - 7 * i], dtype=torch.int32))
+            if i != 3:
+                st.prefixes.seq_start.copy_(torch.tensor([0, 3 - i % 2, 5 - i % 2], dtype=torch.int32))
+            want = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+            torch.cuda.synchronize()
+            graph.replay()
+            assert torch.equal(out, want), i
 
 
 def test_calls_without_sequences_or_tokens():

@@ -1,5 +1,6 @@
 """The host side of a step laid out on the device and of attention with common prefixes: refused arguments, workspaces (no GPU)."""
 import ctypes as C
+import types
 
 import pytest
 
@@ -123,3 +124,18 @@ def test_null_structs_are_refused():
     assert L.river_prefix_attention(C.byref(pages()), 0, None, C.byref(prefixes()), 4, P, 256, 0.0, 2 * P, 256, None, 0, None, None) == B.RIVER_EINVAL
     assert L.river_prefix_attention_workspace(C.byref(pages()), C.byref(batch()), C.byref(prefixes()), 4, None) == B.RIVER_EINVAL
     assert L.river_prefix_attention_workspace(C.byref(pages()), C.byref(batch()), None, 4, C.byref(n)) == B.RIVER_EINVAL
+
+
+def test_the_binding_refuses_prefixes_of_another_device(monkeypatch):
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    with pytest.raises(ValueError, match="different devices"):
+        B.river_prefix_attention(types.SimpleNamespace(index=0), 0, None, types.SimpleNamespace(index=1), None)
+
+
+def test_handles_ask_for_device_tensors():
+    import torch
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        B.Prefixes(i32(2, 3), i32(2), i32(3))
+    with pytest.raises(ValueError):
+        B.Tables(i32(2, 3), i32(2), i32(8), i32(1), 16)
