@@ -778,7 +778,8 @@ class Prefixes(_Fixed):
             raise ValueError("seq_start [n_groups + 1]")
         self.table, self.lens, self.seq_start, self.index, self.n_groups = table, lens, seq_start, table.get_device(), n
         self.max_len, self.max_seqs = max_len, max_seqs
-        self._calls, self._bytes = {}, {}       # the C struct of a batch and page size, and the workspace's size of a shape of call
+        self.shape_key = (n, table.shape[1], max_len, max_seqs)
+        self._calls = {}                        # the C struct of a number of sequences and page size
         self._made = True
 
     def bind(self, n_seq: int, page_size: int):
@@ -787,7 +788,6 @@ class Prefixes(_Fixed):
             most = self.table.shape[1]
             if len(self._calls) >= 256:
                 self._calls.clear()
-                self._bytes.clear()
             got = self._calls[(n_seq, page_size)] = C.byref(river_prefixes(
                 self.table.data_ptr(), self.lens.data_ptr(), self.seq_start.data_ptr(), self.n_groups, most,
                 self.table.stride(0) if self.n_groups > 1 else most,
@@ -808,14 +808,14 @@ def river_prefix_attention(pages: Pages, layer: int, batch: Batch, prefixes: Pre
     out, os_ = _out(q, out, pages)
     L, (n, heads, _) = load(), q.shape
     ref, shared = batch.bind(n, pages), prefixes.bind(batch.n_seq, pages.page_size)
-    key = (pages.shape_key, n, heads, batch.n_seq, batch.q_start is None, batch.max_new, batch.max_len, batch.table.shape[1])
-    nbytes = prefixes._bytes.get(key)
+    key = (pages.shape_key, n, heads, prefixes.shape_key)
+    nbytes = batch._bytes.get(key)
     if nbytes is None:
         got = C.c_size_t()
         _check_call(L.river_prefix_attention_workspace(pages.ref, ref, shared, heads, C.byref(got)))
-        if len(prefixes._bytes) >= 256:
-            prefixes._bytes.clear()
-        nbytes = prefixes._bytes[key] = got.value
+        if len(batch._bytes) >= 256:
+            batch._bytes.clear()
+        nbytes = batch._bytes[key] = got.value
     stream, ws, tickets = _stream(pages.index), None, None
     if nbytes:
         memory = torch.empty(nbytes, dtype=torch.uint8, device=pages.device)        # (call by call: see river_paged_attention)

@@ -137,10 +137,6 @@ const char *river::pg::bad_attention(const river_pages *pages, const river_batch
 // sixteen, 16 behind 512 16.3 / 14.8, 32 behind 512 19.3 / 21.0.  One product does not part all of these: 256 behind none and eight sequences
 // of 8 behind 2048 lie above the limit and are 8 .. 10 % slower there)
 static double many_work(int head_dim) { return head_dim == 128 ? 1.3e8 : 3e8; }
-// Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a
-// second launch 6.4 + 3.8; 16 sequences of up to 1201 15.8, 14.3 + 3.9; 64 splits of 131072 105, 96 + 6)
-constexpr int kFewSplits = 16;
-
 AttnPlan river::pg::plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks) {
   AttnPlan y{};
   const int rep = nq / p->n_kv_heads;

@@ -105,6 +105,9 @@ struct AttnPlan {
   size_t o_bytes, bytes;                                         // of the partial results
 };
 constexpr int kSplitRows = 16;            // of a tile of k_attn_split
+// Up to 16 splits are joined by a row's last workgroup, where there are tickets (8B shape, one sequence of 512: 8.1 us, with a
+// second launch 6.4 + 3.8; 16 sequences of up to 1201 15.8, 14.3 + 3.9; 64 splits of 131072 105, 96 + 6)
+constexpr int kFewSplits = 16;
 AttnPlan plan_attention(const river_pages *p, const river_batch *b, int nq, int window, int sinks);
 
 }  // namespace pg

@@ -254,19 +254,8 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 && !(PM && !OM) ? 3 : 2) voi
   }
 }
 
-// Head h of token t: parts of its group's prefix, parts of its sequence's own, its position.  False: it has no row.
-__device__ __forceinline__ bool parts_of(const Batch &b, const AttnArgs &a, const Prefixes &x, int t, int h, int &common, int &own, int &p) {
-  int s = t;
-  if (b.q_start) {
-    s = __builtin_amdgcn_readfirstlane(count_up_to(b.q_start, b.n_seq + 1, t)) - 1;
-    if (s < 0 || s >= b.n_seq) return false;
-  }
-  int first, count;
-  seq_tokens(b, s, first, count);
-  const int i = t - first;
-  if (i >= min(count, a.max_new)) return false;
-  int g, n;
-  find_group(x, s, g, n);
+// Head h of new token i of sequence s, which has n positions of a prefix: parts of the prefix, parts of its own, its position.
+__device__ __forceinline__ void parts_of(const Batch &b, const AttnArgs &a, const Prefixes &x, int s, int count, int i, int h, int n, int &common, int &own, int &p) {
   const int len = length_of(b, s), low = x.units ? n : 0;
   common = low ? split_count(n, x.n_splits, x.least) : 0;
   // (the last row of this one's tile: see own_unit)
@@ -274,18 +263,34 @@ __device__ __forceinline__ bool parts_of(const Batch &b, const AttnArgs &a, cons
   const int keys = max(0, min(new_position(len, count, a.by_rep.quot(r1)) + 1, max(b.cap, n)) - low);
   own = split_count(keys, a.n_splits, a.split_len);
   p = new_position(len, count, i);
-  return true;
 }
 
-// Few parts where prefixes have no units: bit for bit what a tile's last workgroup does where it has tickets.  Sixteen heads of a token.
+// Few parts where prefixes have no units: bit for bit what a tile's last workgroup does where it has tickets.  Sixteen rows a workgroup, of any
+// tokens.  Bound: latency.
 template <class T, int HD>
-__global__ __launch_bounds__(256) void k_share_join_few(Batch b, AttnArgs a, Prefixes x, int chunks) {
+__global__ __launch_bounds__(256) void k_share_join_few(Batch b, AttnArgs a, Prefixes x) {
   constexpr int E = RowPart<HD>::E, LANES = RowPart<HD>::LANES;
-  const int t = blockIdx.x / chunks, h = blockIdx.x % chunks * 16 + threadIdx.x / LANES, e0 = threadIdx.x % LANES * E;
+  const int w = blockIdx.x * 16 + threadIdx.x / LANES, t = w / a.nq, h = w - t * a.nq, e0 = threadIdx.x % LANES * E;
+  if (t >= b.n_tokens) return;
+  const int s = seq_of(b, t);
+  if (s < 0) return;
+  int first, count;
+  seq_tokens(b, s, first, count);
+  if (t - first >= min(count, a.max_new)) return;
+  int n = 0;
+  if (x.n_groups && s >= x.seq_start[0]) {
+    int g = 0, hi = x.n_groups + 1;       // the last that begins at or before s
+    while (g + 1 < hi) {
+      const int mid = (g + hi) >> 1;
+      if (x.seq_start[mid] <= s) g = mid; else hi = mid;
+    }
+    if (g < x.n_groups) n = cut_len(x, x.lens[g]);
+  }
   int common, own, p;
-  if (!parts_of(b, a, x, t, min(h, a.nq - 1), common, own, p) || own == 1 || h >= a.nq) return;
+  parts_of(b, a, x, s, count, t - first, h, n, common, own, p);
+  if (own == 1) return;
   float v[E], sum;
-  join_parts<HD, E>(a, ((long long)t * a.nq + h) * a.n_splits, own, e0, v, sum);
+  join_parts<HD, E>(a, (long long)w * a.n_splits, own, e0, v, sum);
   store_row<T, E>((T *)a.out + (long long)t * a.out_stride + (long long)h * HD + e0, v, sum);
 }
 
@@ -310,8 +315,16 @@ __global__ __launch_bounds__(256) void k_share_join(Batch b, AttnArgs a, Prefixe
     }
   };
   fetch(group);
-  int common, own, p;
-  if (!parts_of(b, a, x, t, h, common, own, p)) return;
+  int s = t;
+  if (b.q_start) {
+    s = __builtin_amdgcn_readfirstlane(count_up_to(b.q_start, b.n_seq + 1, t)) - 1;
+    if (s < 0 || s >= b.n_seq) return;
+  }
+  int first, count, g, n, common, own, p;
+  seq_tokens(b, s, first, count);
+  if (t - first >= min(count, a.max_new)) return;
+  find_group(x, s, g, n);
+  parts_of(b, a, x, s, count, t - first, h, n, common, own, p);
   float big = -INFINITY, sum = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int y0 = group;;) {

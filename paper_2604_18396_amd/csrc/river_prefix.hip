@@ -71,8 +71,10 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
   const long long in_group = std::min<long long>(x->max_seqs, b->n_seq), groups = std::min<long long>(x->n_groups, b->n_seq);
   const double saves = std::min<double>(groups * (in_group - 1.), b->n_seq) * common * key_bytes;
   const long long own = std::max(1ll, keys - common);
-  const bool apart = p->dtype == RIVER_BF16 && rows > kAttnRows ? saves > 0 && pays(p, b, nq, rows, (double)groups, (double)common, (double)own)
-                                                                : saves >= (common >= kLong ? kSavesLong : kSaves);
+  bool apart = saves >= (common >= kLong ? kSavesLong : kSaves);
+  if (p->dtype == RIVER_BF16 && rows > kAttnRows) apart = saves >= kSavesLong && pays(p, b, nq, rows, (double)groups, (double)common, (double)own);
+  // (fp32 products take longer than their keys' way from the caches: what counts are tiles, which have to become fewer)
+  if (p->dtype == RIVER_F32) apart = apart && 2 * b->n_seq * ((rows + 15) / 16) >= 3 * ((long long)b->n_tokens * rep / 16 + groups);
   constexpr int kManyRows = Many<__bf16, 128>::ROWS;
   if (!apart) {
     const AttnPlan o = plan_attention(p, b, nq, 0, 0);
@@ -192,10 +194,8 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
       e = by_types(pages, [&](auto t, auto, auto hd) {
         constexpr int HD = decltype(hd)::v;
         typedef decltype(t) T;
-        if (y.fused) {
-          const int sixteens = (n_q_heads + 15) / 16;
-          return launch(k_share_join_few<T, HD>, dim3((unsigned)(b.n_tokens * sixteens)), dim3(256), 0, st, b, a, x, sixteens);
-        }
+        if (!y.units && y.n_splits <= kFewSplits)
+          return launch(k_share_join_few<T, HD>, dim3((unsigned)(((long long)b.n_tokens * n_q_heads + 15) / 16)), dim3(256), 0, st, b, a, x);
         const dim3 grid((unsigned)(b.n_tokens * chunks)), block(256);
         return heads == 1   ? launch(k_share_join<T, HD, 1>, grid, block, 0, st, b, a, x, chunks)
                : heads == 2 ? launch(k_share_join<T, HD, 2>, grid, block, 0, st, b, a, x, chunks)
