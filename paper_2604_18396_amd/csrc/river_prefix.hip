@@ -42,16 +42,19 @@ struct SharePlan {
 constexpr double kSaves = 24e6, kSavesLong = 8e6;
 constexpr int kLong = 4096;
 // Several new tokens of 16-bit types: sequences whose rows nearly fill tiles of 128 read their prefixes hardly more often than a group's tiles do.
-// An estimate of both in us: what a tile of 128 rows or of 16 takes per key and key head on the whole card, parts written and read at 4 TB/s.
+// An estimate of both in us: all tiles' work on the whole card (a tile of 128 rows, or of 16, per key and key head), or the keys of the longest
+// workgroup (20 ns each) where that is more, and what it takes to begin, to end and to write and read parts (4 TB/s).
 // (us, apart / through, 8B shape, 300 own positions: 24 sequences of up to 8 new tokens behind 1024 31 / 35, behind 8192 45 / 128; of 24 46 / 42,
 // 91 / 136; of 48 73 / 46, 165 / 228; of 100 134 / 52, 318 / 415; 6 of 8 17.5 / 20.4, 27 / 39, of 48 36 / 32, 58 / 64; 1B shape: 24 of 24 27.9 / 29.8,
 // 66 / 97, of 48 47 / 33, 102 / 166)
-bool pays(const river_pages *p, const river_batch *b, int nq, long long rows, double groups, double common, double own) {
-  const int rep = nq / p->n_kv_heads;
-  const double all = (double)b->n_tokens * rep, n = b->n_seq, large = p->n_kv_heads * (p->head_dim == 128 ? 65e-6 : 50e-6),
-               small = p->n_kv_heads * (p->head_dim == 128 ? 80e-6 : 50e-6);
-  const double through = n * ((rows + 127) / 128) * (common + own) * large + 12;
-  const double apart = (all / 128 + groups) * common * large + (all / 16 + n / 2) * own * 0.6 * small + (double)b->n_tokens * nq * 2 * (p->head_dim * 4 + 8) * 2 / 4e6 + 10;
+bool pays(const river_pages *p, const river_batch *b, int nq, const AttnPlan &o, double groups, double common, double own) {
+  const bool big = p->head_dim == 128;
+  const double heads = p->n_kv_heads, all = (double)b->n_tokens * (nq / p->n_kv_heads), n = b->n_seq, keys = common + own;
+  const double large = heads * (big ? 65e-6 : 50e-6), small = heads * (big ? 80e-6 : 50e-6);
+  const double through = std::max((all / 128 + n / 2) * keys * large * 1.15, keys / o.n_splits * 0.02) + (o.n_splits > 1 ? 13 : 10);
+  const double tiles = all / 128 + groups, splits = std::max(1., std::min(256 / (tiles * heads), common / 128));
+  const double apart = std::max(tiles * common * large + (all / 16 + n / 2) * own * 0.6 * small, common / splits * 0.02) +
+                       (double)b->n_tokens * nq * 2 * (p->head_dim * 4 + 8) * 2 / 4e6 + 14;
   return apart < through;
 }
 // By tiles of 128 rows (many_unit) where rows x keys x elements of a key head are more than these: they read a key once for 128 rows, those of 16 take
@@ -72,12 +75,12 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
   const double saves = std::min<double>(groups * (in_group - 1.), b->n_seq) * common * key_bytes;
   const long long own = std::max(1ll, keys - common);
   bool apart = saves >= (common >= kLong ? kSavesLong : kSaves);
-  if (p->dtype == RIVER_BF16 && rows > kAttnRows) apart = saves >= kSavesLong && pays(p, b, nq, rows, (double)groups, (double)common, (double)own);
+  const AttnPlan o = plan_attention(p, b, nq, 0, 0);
+  if (p->dtype == RIVER_BF16 && rows > kAttnRows) apart = saves >= kSavesLong && pays(p, b, nq, o, (double)groups, (double)common, (double)own);
   // (fp32 products take longer than their keys' way from the caches: what counts are tiles, which have to become fewer)
   if (p->dtype == RIVER_F32) apart = apart && 2 * b->n_seq * ((rows + 15) / 16) >= 3 * ((long long)b->n_tokens * rep / 16 + groups);
   constexpr int kManyRows = Many<__bf16, 128>::ROWS;
   if (!apart) {
-    const AttnPlan o = plan_attention(p, b, nq, 0, 0);
     y.many = y.p_many = o.many;
     y.tiles = o.tiles;
     y.n_splits = o.n_splits;
