@@ -410,9 +410,11 @@ typedef struct {
   int32_t *free_pages;      /* [n_pages] */
   const int32_t *n_free;    /* [1] before the call */
   int32_t *n_free_out;      /* [1] after it: may be n_free */
-  const int32_t *n_shared;  /* [n_seq], or NULL (0): entries at a row's beginning that are somebody else's (a prefix): they are never given back */
+  const int32_t *n_shared;  /* [n_seq], or NULL (0): entries at a row's beginning that are somebody else's (a prefix): they are never given back.
+                               A sequence that has given back positions in them writes over those entries, or into those pages, when it asks
+                               again: lower its n_shared and copy the page in which it ends first */
   int32_t n_seq;            /* at most 4096 */
-  int32_t max_pages, table_stride;
+  int32_t max_pages, table_stride;                 /* n_seq * max_pages: at most 2^30 */
   int32_t n_pages, page_size;
 } river_tables;
 

@@ -22,6 +22,7 @@ extern "C" int river_build_batch(const river_tables *t, const int32_t *n_new, in
     if (t->n_seq < 0 || t->n_seq > kBuildSeqs) return refuse("build: n_seq in [0, 4096]");
     if (t->n_pages < 1 || t->n_pages > (1 << 28) || t->page_size < 1 || t->page_size > 65536 || t->max_pages < 1 || t->table_stride < t->max_pages)
       return refuse("build: n_pages in [1, 2^28], page_size in [1, 65536], 1 <= max_pages <= table_stride");
+    if ((long long)t->n_seq * t->max_pages > (long long)kMuch) return refuse("build: more than 2^30 entries");      // (sums of pages given back end there)
     if (n_tokens < 0 || n_tokens > kMostTokens) return refuse("build: n_tokens in [0, 2^22]");
     if (!t->n_free || !t->n_free_out || !t->free_pages || !q_start) return refuse("build: null free list or q_start");
     if (t->n_seq && (!t->table || !t->lens || !t->lens_out || !n_new)) return refuse("build: null table, lengths or n_new");

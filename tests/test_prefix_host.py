@@ -139,3 +139,9 @@ def test_handles_ask_for_device_tensors():
         B.Prefixes(i32(2, 3), i32(2), i32(3))
     with pytest.raises(ValueError):
         B.Tables(i32(2, 3), i32(2), i32(8), i32(1), 16)
+
+
+def test_build_refuses_more_entries_than_it_counts():
+    # pages given back are counted up to 2^30: more of them would stay in their rows
+    assert build(tables(n_seq=4096, max_pages=2**18 + 1, table_stride=2**18 + 1)) == B.RIVER_EINVAL and "entries" in text()
+    assert build(tables(n_seq=2, max_pages=2**29 + 1, table_stride=2**29 + 1)) == B.RIVER_EINVAL and "entries" in text()
