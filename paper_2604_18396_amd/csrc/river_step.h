@@ -70,6 +70,14 @@ __device__ __forceinline__ int first_above(const int *v, int n, int x) {
   return lo;
 }
 
+// The same where a lane has one of the n numbers (at most 64) and they lie in LDS too: x is x0 and the lane, so that most wavefronts meet one or
+// two of them and need not search.
+__device__ __forceinline__ int first_above(const int *v, int mine, int n, int x0) {
+  const int lane = threadIdx.x % 64;
+  const int lo = __popcll(__ballot(lane < n && mine <= x0)), hi = __popcll(__ballot(lane < n && mine <= x0 + 63));
+  return lo + first_above(v + lo, hi - lo, x0 + lane);
+}
+
 // slots and positions of token t, which is at position p and has page `page`; p < 0: no token
 __device__ __forceinline__ void put_token(const BuildArgs &a, int t, int p, int page, int in_page) {
   if (a.slots) a.slots[t] = p >= 0 && (unsigned)page < (unsigned)a.n_pages ? (long long)page * a.page_size + in_page : -1;
@@ -204,15 +212,16 @@ __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
   if (FEW) __builtin_amdgcn_wave_barrier();
   else __syncthreads();
   // Page j of those that are taken is the one that lies j below the top
-  for (int j = tid; j < taken; j += nt) {
-    const int s = first_above(page_sum, n, j), i = pages_of(a, len[s]) + j - (s ? page_sum[s - 1] : 0);
-    a.table[(long long)s * a.table_stride + i] = a.free_pages[free - 1 - j];
+  for (int j0 = wave * 64; j0 < taken; j0 += nt) {
+    const int j = j0 + lane, s = FEW ? first_above(page_sum, (int)so_far.y, n, j0) : first_above(page_sum, n, j);
+    if (j < taken) a.table[(long long)s * a.table_stride + pages_of(a, len[s]) + j - (s ? page_sum[s - 1] : 0)] = a.free_pages[free - 1 - j];
   }
   if constexpr (TOKENS) {
-    for (int t = tid; t < a.n_tokens; t += nt) {
+    for (int t0 = wave * 64; t0 < a.n_tokens; t0 += nt) {
+      const int t = t0 + lane, s = FEW ? first_above(start + 1, (int)before.x, n, t0) : first_above(start + 1, n, t);
+      if (t >= a.n_tokens) break;
       int p = -1, page = -1, in_page = 0;
       if (t < start[n]) {
-        const int s = first_above(start + 1, n, t);
         p = len[s] + t - start[s];
         const int i = a.by_page.quot(p), fresh = i - pages_of(a, len[s]);
         in_page = p - i * a.page_size;
@@ -230,15 +239,15 @@ __global__ __launch_bounds__(256) void k_slots(BuildArgs a) {
   const int lane = threadIdx.x % 64, t0 = (blockIdx.x * 4 + threadIdx.x / 64) * 64 * kSlotsEach, n = a.n_seq;
   if (t0 >= a.n_tokens) return;
   const int total = a.q_start[n];
-  // the sequences of the first token and of the last one
-  const int from = count_up_to(a.q_start, n + 1, t0) - 1, upto = count_up_to(a.q_start, n + 1, t0 + 64 * kSlotsEach - 1) - 1;
+  // the sequences of the first token and of the last one (the last of those that begin there: for tokens below `total`, their own)
+  const int from = count_up_to(a.q_start, n, t0) - 1, upto = count_up_to(a.q_start, n, t0 + 64 * kSlotsEach - 1) - 1;
 #pragma unroll
   for (int j = 0; j < kSlotsEach; ++j) {
     const int t = t0 + j * 64 + lane;
     if (t >= a.n_tokens) return;
     int p = -1, page = -1, in_page = 0;
     if (t < total) {
-      int s = from, hi = min(upto, n - 1) + 1;
+      int s = from, hi = upto + 1;
       while (s + 1 < hi) {
         const int mid = (s + hi) >> 1;
         if (a.q_start[mid] <= t) s = mid; else hi = mid;
