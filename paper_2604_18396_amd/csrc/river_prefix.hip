@@ -107,10 +107,12 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, 64ll}));
     y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;
     y.tiles = (int)((rows + kAttnRows - 1) / kAttnRows);
-    // of the sequences' own keys: see plan_attention; the places that are left
+    // of the sequences' own keys: see plan_attention; the places that are left.  Several tiles of a sequence's rows are that many workgroups
+    // already: twice the keys in a split (us, 512 / 1024: 1B shape, half pages, four groups of up to 12 sequences behind 3000, drafts of five behind up to
+    // 700 own positions 32.8 / 29.9; bf16 pages, behind up to 1400 37.4 / 36.4, 2047 43.4 / 42.0; 8B shape, 12 tokens behind up to 700 69.9 / 65.3)
     const long long o_groups = std::max(1ll, (long long)b->n_seq * p->n_kv_heads * y.tiles);
     auto by = [&](long long goal, long long least) { return std::min({goal / o_groups, (own + least - 1) / least, 64ll}); };
-    y.n_splits = (int)std::max(1ll, std::max(by(std::max(256ll, places - p_groups * y.p_splits), 128), by(2048, 512)));
+    y.n_splits = (int)std::max(1ll, std::max(by(std::max(256ll, places - p_groups * y.p_splits), 128), by(2048, y.tiles > 1 ? 1024 : 512)));
   }
   if (y.units || y.n_splits > 1) {
     const size_t parts = (size_t)b->n_tokens * nq * ((y.units ? y.p_splits : 0) + y.n_splits);
