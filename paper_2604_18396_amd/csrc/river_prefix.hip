@@ -170,8 +170,8 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
     const AttnArgs a{q, out, q_stride, out_stride, n_q_heads, rep, div_by(rep), scale2, 0, 0, y.n_splits, y.least, y.tiles, y.many ? Many<__bf16, 128>::ROWS : kAttnRows, turn_s, turn_z,
                      y.max_new, (float *)workspace, (float2 *)((char *)workspace + y.o_bytes), y.fused && tickets ? (unsigned int *)tickets : nullptr};
     const Prefixes x{prefixes->table, prefixes->lens, prefixes->seq_start, prefixes->n_groups, prefixes->max_pages, prefixes->table_stride,
-                     (int)std::min<long long>((long long)prefixes->max_pages * pages->page_size, kMostPositions), std::max(1, y.p_tiles),
-                     std::max(1, y.p_splits), y.p_least, (unsigned)y.units,
+                     (int)std::min<long long>((long long)prefixes->max_pages * pages->page_size, kMostPositions), std::max(1, y.p_splits), y.p_least,
+                     (unsigned)y.units,
                      y.p_many && !y.many && pages->kv_dtype == RIVER_KV_F16 ? Mat<_Float16>::kBias - Mat<_Float16>::kLazyBias : 0.f};
     const long long workgroups = y.units + (long long)b.n_seq * c.n_kv_heads * y.n_splits * y.tiles;
     // (rows of a workgroup of the join: eight parts a thread, where there are more the lanes of several rows have one)
