@@ -47,15 +47,30 @@ constexpr int kLong = 4096;
 // (us, apart / through, 8B shape, 300 own positions: 24 sequences of up to 8 new tokens behind 1024 31 / 35, behind 8192 45 / 128; of 24 46 / 42,
 // 91 / 136; of 48 73 / 46, 165 / 228; of 100 134 / 52, 318 / 415; 6 of 8 17.5 / 20.4, 27 / 39, of 48 36 / 32, 58 / 64; 1B shape: 24 of 24 27.9 / 29.8,
 // 66 / 97, of 48 47 / 33, 102 / 166)
-bool pays(const river_pages *p, const river_batch *b, int nq, const AttnPlan &o, double groups, double common, double own) {
+// Rows of sequences without a prefix count for their own keys alone: `members` sequences have one, with at most `grouped` rows in all.
+// (us, apart / through, 8 .. 30 sequences without one: 8B shape, one of 100 tokens behind 20000 109 / 467, two of 8 behind 30000 67 / 390, one of 8
+// behind 5000 35 / 47; 1B shape, one of 24 behind 8000 72 / 145)
+bool pays(const river_pages *p, const river_batch *b, int nq, const AttnPlan &o, double groups, double members, double grouped, double common, double own) {
   const bool big = p->head_dim == 128;
   const double heads = p->n_kv_heads, all = (double)b->n_tokens * (nq / p->n_kv_heads), n = b->n_seq, keys = common + own;
   const double large = heads * (big ? 65e-6 : 50e-6), small = heads * (big ? 80e-6 : 50e-6);
-  const double through = std::max((all / 128 + n / 2) * keys * large * 1.15, keys / o.n_splits * 0.02) + (o.n_splits > 1 ? 13 : 10);
-  const double tiles = all / 128 + groups, splits = std::max(1., std::min(256 / (tiles * heads), common / 128));
+  const double lone = ((all - grouped) / 128 + (n - members) / 2) * own * large;
+  const double through = std::max((grouped / 128 + members / 2) * keys * large * 1.15 + lone, keys / o.n_splits * 0.02) + (o.n_splits > 1 ? 13 : 10);
+  const double tiles = grouped / 128 + groups, splits = std::max(1., std::min(256 / (tiles * heads), common / 128));
   const double apart = std::max(tiles * common * large + (all / 16 + n / 2) * own * 0.6 * small, common / splits * 0.02) +
                        (double)b->n_tokens * nq * 2 * (p->head_dim * 4 + 8) * 2 / 4e6 + 14;
   return apart < through;
+}
+// Splits of the prefixes, as workgroups: one a CU, or seven on four CUs (the eighth place is for the sequences) where that leaves them 1024
+// keys; six on four where three have place on a CU.
+long long prefix_places(bool three, double common, double tiles) { return three ? 384 : common * tiles >= 448 * 1024 ? 448 : 256; }
+// Single tokens, a few long prefixes beside sequences without one: keys are split by the number of all sequences, and the long ones' workgroups
+// go on alone.  Units of their own have more splits; 12 us less of the longest workgroup pay for the second launch.
+// (us, apart / through, 30 sequences without one: 8B shape, one behind 30000 34.6 / 62, of four tokens 49 / 64, behind 5000 20.9 / 17.9, four behind 30000
+// 47 / 63, one behind 100000 beside 60 104 / 353; 1B shape, one behind 30000 22.7 / 33.5, behind 6000 16.9 / 13.6)
+bool unequal(const river_pages *p, const AttnPlan &o, double tiles, double common) {
+  const double splits = std::max(1., std::min({(double)prefix_places(false, common, tiles) / tiles, common / 128, 64.}));
+  return common * (1. / o.n_splits - 1. / splits) * (p->head_dim == 128 ? 0.014 : 0.0063) > 12;
 }
 // By tiles of 128 rows (many_unit) where rows x keys x elements of a key head are more than these: they read a key once for 128 rows, those of 16 take
 // less time to begin and end (us, 128 / 16, 8B shape: 32 rows behind 4096 17.7 / 15.1, behind 16384 25.3 / 26.0; 128 behind 1024 17.0 / 15.8,
@@ -76,7 +91,12 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
   const long long own = std::max(1ll, keys - common);
   bool apart = saves >= (common >= kLong ? kSavesLong : kSaves);
   const AttnPlan o = plan_attention(p, b, nq, 0, 0);
-  if (p->dtype == RIVER_BF16 && rows > kAttnRows) apart = saves >= kSavesLong && pays(p, b, nq, o, (double)groups, (double)common, (double)own);
+  // (several tokens beside sequences without a prefix: the long ones may be too few to fill the card by themselves)
+  const double members = std::min<double>((double)groups * in_group, b->n_seq), grouped = std::min<double>((double)groups * group_rows, (double)b->n_tokens * rep);
+  if (p->dtype == RIVER_BF16 && rows > kAttnRows)
+    apart = (saves >= kSavesLong || (common >= kLong && members < b->n_seq)) && pays(p, b, nq, o, (double)groups, members, grouped, (double)common, (double)own);
+  else if (p->dtype == RIVER_BF16 && !apart && common >= kLong && members < b->n_seq)
+    apart = unequal(p, o, (double)groups * ((group_rows + kAttnRows - 1) / kAttnRows) * p->n_kv_heads, (double)common);
   // (fp32 products take longer than their keys' way from the caches: what counts are tiles, which have to become fewer)
   if (p->dtype == RIVER_F32) apart = apart && 2 * b->n_seq * ((rows + 15) / 16) >= 3 * ((long long)b->n_tokens * rep / 16 + groups);
   constexpr int kManyRows = Many<__bf16, 128>::ROWS;
@@ -94,15 +114,14 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     // (each group that has sequences may have a tile that is not full)
     y.p_tiles = (int)std::min<long long>(((long long)b->n_tokens * rep + tile - 1) / tile + std::max(0ll, groups - 1), INT_MAX);
     const long long p_groups = std::max(1ll, std::min<long long>(y.p_tiles, groups * full) * p->n_kv_heads);
-    // Splits of the prefixes, as workgroups: one a CU, or seven on four CUs (the eighth place is for the sequences) where that leaves them 1024
-    // keys; six on four where three have place on a CU.  But no more than it takes to be done (20 ns a key) in two fifths of the time that
+    // Splits of the prefixes: see prefix_places.  But no more than it takes to be done (20 ns a key) in two fifths of the time that
     // all keys take to stream: every split is one more part of each row.
     // (us by splits: 24 sequences behind 131071 positions, 8 tiles and heads, 32 132, 48 128, 56 122, 64 125; 32 behind 65536 32 77.5, 56 77.6,
     // 64 83; 32 behind 32768 32 48, 56 53; 64 of 225 .. 900 own positions behind 8191, 16 tiles and heads, 6 58, 8 53.8, 12 57.4, 16 59;
     // head size 64: 24 behind 131071 32 90, 48 79, 64 73 .. 77; 48 behind 16384, 16 tiles and heads, 16 29.8, 24 30.2, 32 31.1)
     const double stream = (groups * (double)common + (double)b->n_seq * own) * key_bytes / 5e6;
     const bool three = p->head_dim == 64 && !y.p_many;           // (workgroups that have place on a CU: see k_share)
-    const long long places = three ? 768 : 512, fit = three ? 384 : common * p_groups >= 448 * 1024 ? 448 : 256;
+    const long long places = three ? 768 : 512, fit = prefix_places(three, (double)common, (double)p_groups);
     const long long hide = (long long)(common * 0.02 / (0.4 * stream)) + 1;
     y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, 64ll}));
     y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;

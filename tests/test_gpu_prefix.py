@@ -166,6 +166,23 @@ def test_long_caches(kind, groups, own, new, how):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("hd,nkv,rep", [(64, 2, 4), (128, 1, 6)])
+@pytest.mark.parametrize("groups,own,new,lonely", [([(20000, 1)], [100], [50], (0, 3, 40, 8, 300, 1)), ([(6000, 1), (9000, 1)], [0, 33], [8, 17], (200,) * 20)], ids=str)
+def test_long_prefixes_beside_sequences_without_one(kind, hd, nkv, rep, groups, own, new, lonely):
+    # (few long sequences do not fill the card by themselves: 16-bit types give their prefixes units of their own, though nobody shares them)
+    new = [1 + i * 7 % 30 for i in range(len(lonely))] + new
+    run(Shared(kind, nkv, hd, 16, behind(groups, own, new, lonely), new, groups, lonely=len(lonely), pad=2, seed=6), nkv * rep)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("hd,rep,new", [(64, 4, 1), (128, 2, 1), (128, 3, 5)])
+def test_single_tokens_of_one_long_prefix_beside_sequences_without_one(kind, hd, rep, new):
+    lonely, groups = tuple(i * 5 % 90 for i in range(30)), [(30000, 1)]
+    tokens = [1 + i % new for i in range(30)] + [new]
+    run(Shared(kind, 8, hd, 32, behind(groups, [70], tokens, lonely), tokens, groups, lonely=30, seed=7, ragged=new > 1), 8 * rep)
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("max_len,max_seqs", [(1, 1), (1, 2), (64, 3), (10**6, 1000), (0, 0), (2000, 2)])
 @HOW
 def test_more_than_the_bounds_say(kind, max_len, max_seqs, how):
