@@ -52,12 +52,17 @@ __device__ __forceinline__ Two threads_before(Two mine, Two *waves, Two &all) {
   __syncthreads();
   if (threadIdx.x % 64 == 0) waves[wave] = sum;
   __syncthreads();
+  Two of[kBuildThreads / 64];             // (all at once: a read behind the other takes as long as the rest)
+#pragma unroll
+  for (int w = 0; w < kBuildThreads / 64; ++w) of[w] = waves[w];
   all = {0, 0};
-  for (int w = 0; w < n; ++w) {
-    if (w == wave) before = add(all, before);
-    all = add(all, waves[w]);
+  Two here = {0, 0};
+#pragma unroll
+  for (int w = 0; w < kBuildThreads / 64; ++w) {
+    if (w == wave) here = all;
+    if (w < n) all = add(all, of[w]);
   }
-  return before;
+  return add(here, before);
 }
 
 // The first i of n with v[i] > x (v ascends).
@@ -85,12 +90,12 @@ __device__ __forceinline__ void put_token(const BuildArgs &a, int t, int p, int 
 }
 
 // FEW: at most 64 sequences, a lane each, and every wavefront has all of them: its sums are its own, what it writes to LDS every other
-// writes too, and no barrier stands between.  Else a thread has EACH neighbouring ones, and the sums go through LDS.
+// writes too, and no barrier stands between.  Else a thread has EACH neighbouring ones at most (one, or four of more than 1024), and the sums go
+// through LDS.
 // Bound: latency, of the loads that need what others brought (lengths, the free list, the rows), and of the barriers.
-template <bool TOKENS, bool FEW>
+template <bool TOKENS, bool FEW, int EACH>
 __global__ __launch_bounds__(kBuildThreads) void k_build(BuildArgs a) {
   extern __shared__ int sums[];
-  constexpr int EACH = FEW ? 1 : kBuildEach;
   const int n = a.n_seq, nt = blockDim.x, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   int *const len = sums, *const page_sum = sums + n, *const start = sums + 2 * n;     // [n], [n], [n + 1]
   __shared__ Two waves[kBuildThreads / 64];

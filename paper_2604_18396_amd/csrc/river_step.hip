@@ -38,8 +38,11 @@ extern "C" int river_build_batch(const river_tables *t, const int32_t *n_new, in
     const size_t lds = (3 * (size_t)t->n_seq + 1) * 4;
     const hipStream_t st = (hipStream_t)hip_stream;
     auto go = [&](auto k) { return launch(k, dim3(1), dim3(threads), lds, st, a); };
-    const bool few = t->n_seq <= 64;
-    hipError_t e = tokens && !apart ? (few ? go(k_build<true, true>) : go(k_build<true, false>)) : few ? go(k_build<false, true>) : go(k_build<false, false>);
+    auto by_seqs = [&](auto with_tokens) {
+      constexpr bool TOKENS = decltype(with_tokens)::value;
+      return t->n_seq <= 64 ? go(k_build<TOKENS, true, 1>) : t->n_seq <= kBuildThreads ? go(k_build<TOKENS, false, 1>) : go(k_build<TOKENS, false, kBuildEach>);
+    };
+    hipError_t e = tokens && !apart ? by_seqs(True{}) : by_seqs(False{});
     if (e == hipSuccess && apart)
       e = launch(k_slots, dim3((n_tokens + 256 * kSlotsEach - 1) / (256 * kSlotsEach)), dim3(256), 0, st, a);
     return e == hipSuccess ? RIVER_OK : hip_failed("river_build_batch", e);
