@@ -62,14 +62,19 @@ bool pays(const river_pages *p, const river_batch *b, int nq, const AttnPlan &o,
   return apart < through;
 }
 // Splits of the prefixes, as workgroups: one a CU, or seven on four CUs (the eighth place is for the sequences) where that leaves them 1024
-// keys; six on four where three have place on a CU.
-long long prefix_places(bool three, double common, double tiles) { return three ? 384 : common * tiles >= 448 * 1024 ? 448 : 256; }
+// keys of head size 128, 512 of 64, and where the sequences have no more keys of their own than the prefixes; six on four where three have place on a CU.
+// (us, 256 / 448, 1B shape, up to 100 own positions: 24 sequences behind 30000 31.1 / 29.1, behind 40000 35.8 / 32.2, 32 behind 48000 42.1 / 38.5, 48 behind
+// 20000 33.9 / 32.1, 18 of 64 heads behind 20937 35.4 / 30.2; 64 of up to 900 behind 16384 43.4 / 46.8; 8B shape, 64 of up to 900 behind 30000 80.1 / 87.5,
+// 32 of up to 2047 behind 60000 95.9 / 102.2)
+long long prefix_places(int head_dim, bool three, double common, double tiles, double groups, double own_keys) {
+  return three ? 384 : common * tiles >= 3584 * head_dim && own_keys <= groups * common ? 448 : 256;
+}
 // Single tokens, a few long prefixes beside sequences without one: keys are split by the number of all sequences, and the long ones' workgroups
 // go on alone.  Units of their own have more splits; 12 us less of the longest workgroup pay for the second launch.
 // (us, apart / through, 30 sequences without one: 8B shape, one behind 30000 34.6 / 62, of four tokens 49 / 64, behind 5000 20.9 / 17.9, four behind 30000
 // 47 / 63, one behind 100000 beside 60 104 / 353; 1B shape, one behind 30000 22.7 / 33.5, behind 6000 16.9 / 13.6)
-bool unequal(const river_pages *p, const AttnPlan &o, double tiles, double common) {
-  const double splits = std::max(1., std::min({(double)prefix_places(false, common, tiles) / tiles, common / 128, 64.}));
+bool unequal(const river_pages *p, const AttnPlan &o, double tiles, double groups, double common, double own_keys) {
+  const double splits = std::max(1., std::min({(double)prefix_places(p->head_dim, false, common, tiles, groups, own_keys) / tiles, common / 128, 64.}));
   return common * (1. / o.n_splits - 1. / splits) * (p->head_dim == 128 ? 0.014 : 0.0063) > 12;
 }
 // By tiles of 128 rows (many_unit) where rows x keys x elements of a key head are more than these: they read a key once for 128 rows, those of 16 take
@@ -96,7 +101,8 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
   if (p->dtype == RIVER_BF16 && rows > kAttnRows)
     apart = (saves >= kSavesLong || (common >= kLong && members < b->n_seq)) && pays(p, b, nq, o, (double)groups, members, grouped, (double)common, (double)own);
   else if (p->dtype == RIVER_BF16 && !apart && common >= kLong && members < b->n_seq)
-    apart = unequal(p, o, (double)groups * ((group_rows + kAttnRows - 1) / kAttnRows) * p->n_kv_heads, (double)common);
+    apart = unequal(p, o, (double)groups * ((group_rows + kAttnRows - 1) / kAttnRows) * p->n_kv_heads, (double)groups, (double)common,
+                    (double)b->n_seq * own);
   // (fp32 products take longer than their keys' way from the caches: what counts are tiles, which have to become fewer)
   if (p->dtype == RIVER_F32) apart = apart && 2 * b->n_seq * ((rows + 15) / 16) >= 3 * ((long long)b->n_tokens * rep / 16 + groups);
   constexpr int kManyRows = Many<__bf16, 128>::ROWS;
@@ -121,7 +127,7 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     // head size 64: 24 behind 131071 32 90, 48 79, 64 73 .. 77; 48 behind 16384, 16 tiles and heads, 16 29.8, 24 30.2, 32 31.1)
     const double stream = (groups * (double)common + (double)b->n_seq * own) * key_bytes / 5e6;
     const bool three = p->head_dim == 64 && !y.p_many;           // (workgroups that have place on a CU: see k_share)
-    const long long places = three ? 768 : 512, fit = prefix_places(three, (double)common, (double)p_groups);
+    const long long places = three ? 768 : 512, fit = prefix_places(p->head_dim, three, (double)common, (double)p_groups, (double)groups, (double)b->n_seq * own);
     const long long hide = (long long)(common * 0.02 / (0.4 * stream)) + 1;
     y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, 64ll}));
     y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;
