@@ -61,6 +61,9 @@ bool pays(const river_pages *p, const river_batch *b, int nq, const AttnPlan &o,
                        (double)b->n_tokens * nq * 2 * (p->head_dim * 4 + 8) * 2 / 4e6 + 14;
   return apart < through;
 }
+// Splits of a prefix: more than a CU each under one key head have no place (us, at most 64 / 256, one key head of 128: 14 sequences behind 131071 59 / 32,
+// two key heads, 16 behind 100000 53 / 38; head size 64, 14 behind 62852 28.4 / 21.5)
+constexpr int kMostSplits = 256;
 // Splits of the prefixes, as workgroups: one a CU, or seven on four CUs (the eighth place is for the sequences) where that leaves them 1024
 // keys of head size 128, 512 of 64, and where the sequences have no more keys of their own than the prefixes; six on four where three have place on a CU.
 // (us, 256 / 448, 1B shape, up to 100 own positions: 24 sequences behind 30000 31.1 / 29.1, behind 40000 35.8 / 32.2, 32 behind 48000 42.1 / 38.5, 48 behind
@@ -74,7 +77,7 @@ long long prefix_places(int head_dim, bool three, double common, double tiles, d
 // (us, apart / through, 30 sequences without one: 8B shape, one behind 30000 34.6 / 62, of four tokens 49 / 64, behind 5000 20.9 / 17.9, four behind 30000
 // 47 / 63, one behind 100000 beside 60 104 / 353; 1B shape, one behind 30000 22.7 / 33.5, behind 6000 16.9 / 13.6)
 bool unequal(const river_pages *p, const AttnPlan &o, double tiles, double groups, double common, double own_keys) {
-  const double splits = std::max(1., std::min({(double)prefix_places(p->head_dim, false, common, tiles, groups, own_keys) / tiles, common / 128, 64.}));
+  const double splits = std::max(1., std::min({(double)prefix_places(p->head_dim, false, common, tiles, groups, own_keys) / tiles, common / 128, (double)kMostSplits}));
   return common * (1. / o.n_splits - 1. / splits) * (p->head_dim == 128 ? 0.014 : 0.0063) > 12;
 }
 // By tiles of 128 rows (many_unit) where rows x keys x elements of a key head are more than these: they read a key once for 128 rows, those of 16 take
@@ -129,7 +132,7 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     const bool three = p->head_dim == 64 && !y.p_many;           // (workgroups that have place on a CU: see k_share)
     const long long places = three ? 768 : 512, fit = prefix_places(p->head_dim, three, (double)common, (double)p_groups, (double)groups, (double)b->n_seq * own);
     const long long hide = (long long)(common * 0.02 / (0.4 * stream)) + 1;
-    y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, 64ll}));
+    y.p_splits = (int)std::max(1ll, std::min({fit / p_groups, (common + 127) / 128, hide, (long long)kMostSplits}));
     y.units = (long long)y.p_tiles * p->n_kv_heads * y.p_splits;
     y.tiles = (int)((rows + kAttnRows - 1) / kAttnRows);
     // of the sequences' own keys: see plan_attention; the places that are left.  Several tiles of a sequence's rows are that many workgroups

@@ -175,6 +175,15 @@ def test_long_prefixes_beside_sequences_without_one(kind, hd, nkv, rep, groups, 
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("hd,rep", [(64, 8), (128, 3), (128, 8)])
+@pytest.mark.parametrize("new", [1, 3])
+def test_prefixes_in_hundreds_of_splits(kind, hd, rep, new):
+    # (one key head: as many splits as there are CUs, the last of them short)
+    groups, own, tokens = [(45001, 9)], [0, 5, 130, 17, 300, 1, 2, 64, 33, 90], [1 + i % new for i in range(10)]
+    run(Shared(kind, 1, hd, 64, behind(groups, own, tokens), tokens, groups, seed=8, ragged=new > 1), rep)
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("hd,rep,new", [(64, 4, 1), (128, 2, 1), (128, 3, 5)])
 def test_single_tokens_of_one_long_prefix_beside_sequences_without_one(kind, hd, rep, new):
     lonely, groups = tuple(i * 5 % 90 for i in range(30)), [(30000, 1)]
