@@ -353,7 +353,7 @@ int river_rope_store(const river_pages *pages, int32_t layer, const river_batch 
  * out must not overlap q.  At most 2^22 tokens and sequences a call (river_rope_store too), and fewer than
  * 2^28 tokens x heads.
  * Scores, maxima and sums are fp32.  What values are multiplied with is rounded: probabilities to 2^-17 of themselves over bf16 pages,
- * but to bf16 where a sequence has many new tokens, and to half over half pages (bf16 queries too, scaled by row); fp32 pages: none.
+ * but to bf16 where a sequence has more than 16 rows under a key head (new tokens x query heads that share it) with enough to see, and to half over half pages (bf16 queries too, scaled by row); fp32 pages: none.
  * workspace: DEVICE, 16-byte aligned, of at least the bytes that river_paged_attention_workspace gives for the
  * same arguments (0 bytes: may be NULL); its contents mean nothing before and after the call.
  * tickets: DEVICE int32 [RIVER_TICKETS], 4-byte aligned, or NULL.  All zero before the first call that has them and left zero by every call;
@@ -385,7 +385,8 @@ typedef struct {
  * of positions below lens[g] are not read (they may be -1: river_rope_store and river_store_slots do not need them for later positions
  * either).  A prefix need not end with a page: its last page and the sequence's own entry of the same positions are two pages then, each with
  * its own positions.  A token whose position is below the prefix's length sees what comes up to it.
- * Arguments, roundings and errors as in river_paged_attention, tickets and a max_new that leaves tokens out among them.
+ * Arguments, errors and roundings as in river_paged_attention (which probabilities over bf16 pages are rounded to bf16 follows from a sequence's own
+ * rows, whatever its group has), tickets and a max_new that leaves tokens out among them.
  * workspace: as there, of the bytes that river_prefix_attention_workspace gives. */
 int river_prefix_attention_workspace(const river_pages *pages, const river_batch *batch, const river_prefixes *prefixes,
                                      int32_t n_q_heads, size_t *bytes);

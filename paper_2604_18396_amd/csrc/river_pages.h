@@ -873,6 +873,9 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 // what was the maximum (one of 32 rows has a new maximum in most steps, and rescaling takes half as long as the step).
 // A probability is rounded once to the pages' type, and the sum is of what is multiplied: over bf16 pages that leaves out up to half a step of the
 // result (4096 tokens: off by 2.1e-3 of the norm, 1.6e-3 with fp32 ones); a second product, as in k_attn_split, would cost a third of the time.
+// Rows of sequences that have few each have it all the same (TWO; common prefixes): it costs 2 .. 10 us of a stream that a few tiles read (8B shape,
+// 64 single tokens behind 8191 53.6 -> 56.1, 24 behind 131071 121 -> 132, with a clock 5 % lower), and would cost 20 if wavefronts without rows
+// took part in the products (24 behind 131071 141, 8 behind it 107 -> 131, as it is 113; 1B shape 67 -> 80, as it is 60).
 // Keys and values go from memory straight into LDS (no registers, AHEAD steps in flight), in rings, one barrier a step; where a key's
 // row lies is looked up for CHUNK steps at once.
 // 8B shape, 4096 tokens: 148 .. 158 us by the box, 870 .. 930 TFLOP/s; 2048 behind 16384 615 us, 950; the largest matrix products of the library reach 1250.
@@ -936,8 +939,8 @@ struct First {
   int e[N];
 };
 
-// One unit of 128 rows at most: its result in the output, or as a part of it.
-template <class T, class C, int HD, int AHEAD, class First, class Keys, class Rows>
+// One unit of 128 rows at most: its result in the output, or as a part of it.  TWO: a bf16 probability is multiplied as two numbers.
+template <class T, class C, int HD, int AHEAD, bool TWO, class First, class Keys, class Rows>
 __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, const Unit<Keys, Rows> &w, const First &first, char *lds) {
   typedef Many<C, HD, AHEAD> W;
   typedef Mat<C> M;
@@ -1046,7 +1049,7 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
   };
 
   typedef float Scores[16];
-  typedef u32x4 Probs[2];
+  typedef u32x4 Probs[TWO ? 4 : 2];                      // (what the first two round off is in the others)
   f32x16 o[DB];
   float m, lim, l, off, fac, top;
   bool pend;
@@ -1169,7 +1172,15 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
       };
       auto round_and_add = [&](int q) {
         uint32_t w = M::pack(y[q % 2][0], y[q % 2][1]);
-        l = M::add_pair(w, l);                                   // (the sum of what is multiplied: rounded alike)
+        if constexpr (TWO) {
+          l += y[q % 2][0];
+          l += y[q % 2][1];
+          uint32_t rest = M::pack(y[q % 2][0] - M::low(w), y[q % 2][1] - M::high(w));
+          asm volatile("" : "+v"(rest));
+          p1[2 + q / 4][q % 4] = rest;
+        } else {
+          l = M::add_pair(w, l);                                 // (the sum of what is multiplied: rounded alike)
+        }
         asm volatile("" : "+v"(w), "+v"(l));
         p1[q / 4][q % 4] = w;
       };
@@ -1180,7 +1191,10 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
         if (slot + PRE < SLOTS) f[(slot + PRE) % (PRE + 1)] = operand(slot + PRE, k_step, v_step);
         const u32x4 x0 = f[slot % (PRE + 1)];
         if (slot < KS) sn = mul32<C>(x0, qf[slot], slot ? sn : f32x16{});
-        else o[(slot - KS) % DB] = mul32<C>(x0, p[(slot - KS) / DB], o[(slot - KS) % DB]);
+        else {
+          o[(slot - KS) % DB] = mul32<C>(x0, p[(slot - KS) / DB], o[(slot - KS) % DB]);
+          if constexpr (TWO) o[(slot - KS) % DB] = mul32<C>(x0, p[2 + (slot - KS) / DB], o[(slot - KS) % DB]);
+        }
 #pragma unroll
         for (int e = slot * EACH; e < (slot + 1) * EACH; ++e) {
           const int q = e / 2;
@@ -1213,28 +1227,45 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
       }
       wait_and_meet<W::IN_FLIGHT>();
     };
-    Scores s0, s1;
-    Probs p0, p1;
-    {
-      f32x16 sn;
+    if (__builtin_expect(!TWO || r0 + wave * W::WROWS <= r1, true)) {
+      Scores s0, s1;
+      Probs p0, p1;
+      {
+        f32x16 sn;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sn = mul32<C>(operand(ks, k0, 0), qf[ks], ks ? sn : f32x16{});
+        for (int ks = 0; ks < KS; ++ks) sn = mul32<C>(operand(ks, k0, 0), qf[ks], ks ? sn : f32x16{});
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float v = sn[i];
-        asm volatile("" : "+v"(v));
-        s0[i] = v;
-        top = i ? __builtin_elementwise_maximum(top, v) : v;
+        for (int i = 0; i < 16; ++i) {
+          float v = sn[i];
+          asm volatile("" : "+v"(v));
+          s0[i] = v;
+          top = i ? __builtin_elementwise_maximum(top, v) : v;
+        }
+        for (u32x4 &p : p0) p = u32x4{0, 0, 0, 0};
       }
-      p0[0] = p0[1] = u32x4{0, 0, 0, 0};
-    }
-    settle(0, s0, there_of[0]);
-    wait_and_meet<W::IN_FLIGHT>();               // (step 0 fetches over the keys of S(0))
-    // step `steps` only adds what the last one left
-    for (int n = 0; n <= steps; n += 2) {
-      step(n, s0, p0, s1, p1);
-      if (n == steps) break;
-      step(n + 1, s1, p1, s0, p0);
+      settle(0, s0, there_of[0]);
+      wait_and_meet<W::IN_FLIGHT>();               // (step 0 fetches over the keys of S(0))
+      // step `steps` only adds what the last one left
+      for (int n = 0; n <= steps; n += 2) {
+        step(n, s0, p0, s1, p1);
+        if (n == steps) break;
+        step(n + 1, s1, p1, s0, p0);
+      }
+    } else {
+      // A wavefront without rows has its part of the loads alone (see above)
+      wait_and_meet<W::IN_FLIGHT>();
+#pragma nounroll
+      for (int n = 0; n <= steps; ++n) {
+        Place at[NL];
+        find(n + W::AHEAD, at);
+        fetch(n + W::AHEAD, at);
+        if ((n + W::AHEAD + 1) % W::CHUNK == 0) look_up((n + W::AHEAD + 1) / W::CHUNK);
+        if (careful) {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          clean(n + W::AHEAD - W::LATER);
+        }
+        wait_and_meet<W::IN_FLIGHT>();
+      }
     }
     wait_and_meet<0>();                                          // (nothing may land in LDS behind the end)
     if (careful) {
@@ -1338,7 +1369,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_attn_many(Cache c, Ba
   const int parts = splits_of(a, sp.n);
   if (z >= parts) return;
   const int i0 = z * a.split_len, i1 = z == parts - 1 ? sp.n : min(sp.n, i0 + a.split_len);
-  many_unit<T, C, HD, 2>(c, a, Unit<OneRow, OfSequence>{{b.table + (long long)s * b.table_stride}, {len, count}, sp, i0, i1, r0, r1, first_token, head,
+  many_unit<T, C, HD, 2, false>(c, a, Unit<OneRow, OfSequence>{{b.table + (long long)s * b.table_stride}, {len, count}, sp, i0, i1, r0, r1, first_token, head,
                                                         a.n_splits, z, (long long)s * a.max_new, parts == 1}, NoFirst{}, lds);
 }
 

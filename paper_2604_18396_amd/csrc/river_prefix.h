@@ -218,7 +218,7 @@ struct ShareLds {
 };
 // Both kinds in one kernel take more than the 168 registers that leave three workgroups a CU at head size 64: two (24 sequences behind
 // 131071 85 -> 75 us, without the 20 registers that were spilled).
-template <class T, class C, int HD, bool PM, bool OM>
+template <class T, class C, int HD, bool PM, bool OM, bool TWO>
 __global__ __launch_bounds__(kAttnThreads, HD == 64 && !(PM && !OM) ? 3 : 2) void k_share(Cache c, Batch b, AttnArgs a, Prefixes x) {
   extern __shared__ __align__(1024) char lds[];
   constexpr int PR = PM ? Many<C, HD>::ROWS : kAttnRows, OR = OM ? Many<C, HD>::ROWS : kAttnRows;
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 && !(PM && !OM) ? 3 : 2) voi
       if constexpr (PM) {
         First<FirstOf<C, HD, PR>::N> first;
         if (prefix_unit<C, HD, PR>(c, x, b, a, u / x.n_splits, u % x.n_splits, blockIdx.x % c.n_kv_heads, w, first))
-          many_unit<T, C, HD, kAhead>(c, a, w, first, lds);
+          many_unit<T, C, HD, kAhead, TWO>(c, a, w, first, lds);
         return;
       } else if (!prefix_unit<C, HD, PR>(c, x, b, a, u / x.n_splits, u % x.n_splits, blockIdx.x % c.n_kv_heads, w, first)) return;
     } else {
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 && !(PM && !OM) ? 3 : 2) voi
   } else {
     NoFirst first;
     work_of(blockIdx.x, c, b, a, tile, s, z, head);
-    if (own_unit<C, HD, OR>(c, x, b, a, s, tile, z, head, w, first, parts)) many_unit<T, C, HD, 2>(c, a, w, first, lds);
+    if (own_unit<C, HD, OR>(c, x, b, a, s, tile, z, head, w, first, parts)) many_unit<T, C, HD, 2, false>(c, a, w, first, lds);
   }
 }
 

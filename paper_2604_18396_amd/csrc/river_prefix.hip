@@ -28,6 +28,7 @@ const char *bad_prefixes(const river_prefixes *x) {
 // How a call is divided: units of a group's rows and its prefix, units of a sequence's rows and its own keys.
 struct SharePlan {
   bool many, p_many;                                             // tiles of 128 rows: of the sequences, of the prefixes
+  bool two;                                                      // of the prefixes: bf16 probabilities as two numbers
   int max_new, tiles, n_splits, least;                           // of the sequences
   int p_tiles, p_splits, p_least;                                // of the prefixes, of all groups
   long long units;                                               // workgroups of the prefixes
@@ -70,6 +71,10 @@ constexpr int kMostSplits = 256;
 // 20000 33.9 / 32.1, 18 of 64 heads behind 20937 35.4 / 30.2; 64 of up to 900 behind 16384 43.4 / 46.8; 8B shape, 64 of up to 900 behind 30000 80.1 / 87.5,
 // 32 of up to 2047 behind 60000 95.9 / 102.2)
 long long prefix_places(int head_dim, bool three, double common, double tiles, double groups, double own_keys) {
+  
+#ifdef FIT
+  return FIT;
+#endif
   return three ? 384 : common * tiles >= 3584 * head_dim && own_keys <= groups * common ? 448 : 256;
 }
 // Single tokens, a few long prefixes beside sequences without one: keys are split by the number of all sequences, and the long ones' workgroups
@@ -84,7 +89,10 @@ bool unequal(const river_pages *p, const AttnPlan &o, double tiles, double group
 // less time to begin and end (us, 128 / 16, 8B shape: 32 rows behind 4096 17.7 / 15.1, behind 16384 25.3 / 26.0; 128 behind 1024 17.0 / 15.8,
 // behind 4096 23.1 / 25.9; 256 behind 1024 18.2 / 21.5; 1B shape: 64 behind 16384 23.1 / 24.1, 128 behind 4096 16.9 / 16.7, 256
 // behind 4096 18.9 / 24.0)
-constexpr double kManyWork = 3e8;
+#ifndef KMANY
+#define KMANY 3e8
+#endif
+constexpr double kManyWork = KMANY;
 
 SharePlan plan_share(const river_pages *p, const river_batch *b, const river_prefixes *x, int nq) {
   SharePlan y{};
@@ -117,6 +125,8 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     y.fused = o.fused;
   } else {
     y.p_many = p->dtype == RIVER_BF16 && group_rows > kAttnRows && (double)groups * group_rows * common * p->n_kv_heads * p->head_dim >= kManyWork;
+    // river_paged_attention's roundings of the same batch: a sequence of few rows has two numbers for a probability, also where its group has many
+    y.two = y.p_many && !o.many && p->kv_dtype != RIVER_KV_F16;
     y.least = y.p_least = 128;
     const int tile = y.p_many ? kManyRows : kAttnRows;
     const long long full = (group_rows + tile - 1) / tile;
@@ -213,15 +223,17 @@ extern "C" int river_prefix_attention(const river_pages *pages, int32_t layer, c
       typedef decltype(t) T;
       typedef decltype(ct) C;
       constexpr int HD = decltype(hd)::v;
-      auto go = [&](auto pm, auto om) {
+      auto go = [&](auto pm, auto om, auto two) {
         constexpr bool PM = decltype(pm)::value, OM = decltype(om)::value;
-        return launch_lds<k_share<T, C, HD, PM, OM>>(dim3((unsigned)workgroups), dim3(kAttnThreads), ShareLds<T, C, HD, PM, OM>::BYTES, st, c, b, a, x);
+        return launch_lds<k_share<T, C, HD, PM, OM, decltype(two)::value>>(dim3((unsigned)workgroups), dim3(kAttnThreads), ShareLds<T, C, HD, PM, OM>::BYTES, st, c, b, a, x);
       };
       if constexpr (sizeof(T) == 2) {
-        if (y.many) return go(True{}, True{});
-        if (y.p_many) return go(True{}, False{});
+        if (y.many) return go(True{}, True{}, False{});
+        if constexpr (Mat<C>::kSplitP)
+          if (y.two) return go(True{}, False{}, True{});
+        if (y.p_many) return go(True{}, False{}, False{});
       }
-      return go(False{}, False{});
+      return go(False{}, False{}, False{});
     });
     if (e == hipSuccess && y.bytes && !a.tickets)
       e = by_types(pages, [&](auto t, auto, auto hd) {

@@ -319,6 +319,35 @@ def test_scales(kind, std, scale, how):
         run(Shared(kind, 2, 128, 16, behind(groups, own, new), new, groups, seed=11, how=how), 8, scale=scale, std=std)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [1, 3])
+@HOW
+def test_probabilities_of_few_tokens_are_more_than_their_type(kind, hd, new, how):
+    # As test_gpu_pages has it for single tokens, whose tolerance and its reasons hold here: two keys of the prefix with scores 0 and -d and values 1 and -1,
+    # o = tanh(d / 2).  A sequence's own keys have scores below -42 and values of 0: they are below 2^-60 of the sum
+    n, own = 64, 2.0 ** 21
+    st = Shared(kind, 1, hd, 16, [2 + new] * n, [new] * n, [(2, n)], seed=23, ragged=new > 1, how=how)
+    st.k[:, :, :, :, 0] = -own
+    st.k[:, :, :, :, 1:] = 0.0
+    st.v.zero_()
+    page = int(st.prefix_host[0, 0])
+    st.k[0, page, 0, 0, 0], st.k[0, page, 0, 1, 0] = 0.0, -1.0
+    st.v[0, page, 0, 0], st.v[0, page, 0, 1] = 1.0, -1.0
+    d = (torch.arange(n * new, device=DEV, dtype=torch.float64) + 0.5) / (n * new) * 2.0 ** -7
+    q = torch.zeros(n * new, 1, hd, dtype=st.act, device=DEV)
+    q[:, 0, 0] = d.to(st.act)
+    d = q[:, 0, 0].double()
+    assert float(d.min()) * own > 42
+    got = B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q, scale=1.0).double()[:, 0]
+    want = torch.tanh(d / 2)[:, None].expand(n * new, hd)
+    tol = half_step(st.act) * want + 2.0 ** -17 + 2.0 ** -19
+    p = (-d).exp()
+    once = (1 - p.to(torch.bfloat16).double()) / (1 + p)
+    assert int(((once - want[:, 0]).abs() > tol[:, 0]).sum()) > n * new // 2        # (a single rounding would be seen)
+    check(got, want, tol)
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @HOW
 @pytest.mark.parametrize("most", [20, 33])
