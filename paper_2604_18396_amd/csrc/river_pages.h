@@ -326,10 +326,13 @@ __device__ __forceinline__ void work_of(unsigned group, const Cache &c, const Ba
   tile = a.tiles - 1 - t;
 }
 
+static __device__ const u32x4 g_zero_row[32] = {};        // (128 numbers of 32 bits)
+
 // What a workgroup of an attention kernel works on: rows r0 .. r1 (counted from the first token on, see above) and the keys
 // i0 .. i1 - 1 of their span, under one key head.
 // Keys: entry(p, i) is the table's entry i, which has position p.  Rows: position(i) is that of token first_token + i; reach(i, j, ..)
-// are the lowest and the highest of tokens i .. j (of a wavefront's rows, in k_attn_many).
+// are the lowest and the highest of tokens i .. j (of a wavefront's rows, in k_attn_many); nobody() where this lane's row counts as one
+// that sees everything and has no result: its query counts as zeros, so that whatever its bits are no tile has to be computed twice for it.
 struct OneRow {
   const int *row;
   __device__ __forceinline__ const int *place(int, int i) const { return row + i; }
@@ -339,6 +342,7 @@ struct OfSequence {
   int len, count;
   __device__ __forceinline__ int position(int i) const { return new_position(len, count, i); }
   __device__ __forceinline__ void reach(int i, int j, int &first, int &last) const { first = position(i); last = position(j); }
+  static constexpr bool nobody() { return false; }
 };
 template <class Keys, class Rows>
 struct Unit {
@@ -540,7 +544,7 @@ __device__ __forceinline__ void split_unit(const Cache &c, const AttnArgs &a, co
   // this lane's row: its query in the order of the contraction, its position
   const int r = min(r0 + col, r1), tok = a.by_rep.quot(r), qh = w.head * a.rep + (r - tok * a.rep);
   const int mypos = w.rows.position(tok);
-  const T *qrow = (const T *)a.q + (long long)(w.first_token + tok) * a.q_stride + (long long)qh * HD;
+  const T *qrow = w.rows.nobody() ? (const T *)g_zero_row : (const T *)a.q + (long long)(w.first_token + tok) * a.q_stride + (long long)qh * HD;
   u32x4 qf[NP];
   float sc = a.scale2;
   if constexpr (sizeof(T) == sizeof(C) && !(sizeof(C) == 2 && M::kBias != 0.f)) {
@@ -919,7 +923,6 @@ template <int N>
 __device__ __forceinline__ void wait_and_meet() {        // all but the last N loads done, by every wavefront
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
-static __device__ const u32x4 g_zero_row[16] = {};
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <class C>
 __device__ __forceinline__ f32x16 mul32(u32x4 a, u32x4 b, f32x16 c) {
@@ -966,7 +969,8 @@ __device__ __forceinline__ void many_unit(const Cache &c, const AttnArgs &a, con
   float sc = a.scale2;
   const int r = min(r0 + wave * W::WROWS + col, r1), tok = a.by_rep.quot(r);
   const Sight sight = sight_of(a, sp, w.rows.position(tok));
-  const T *q = (const T *)a.q + (long long)(w.first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
+  const T *q = w.rows.nobody() ? (const T *)g_zero_row
+                               : (const T *)a.q + (long long)(w.first_token + tok) * a.q_stride + (long long)(head * a.rep + r - tok * a.rep) * HD;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const u32x4 *)(q + (2 * ks + h) * 8);
   auto queries = [&] {

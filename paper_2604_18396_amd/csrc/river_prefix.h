@@ -57,8 +57,10 @@ struct TwoRows {
 // Rows whose positions were found before: this lane's, and the lowest and highest of its wavefront's.
 struct Found {
   int mine, first, last;
+  bool none;                              // no position: see prefix_unit
   __device__ __forceinline__ int position(int) const { return mine; }
   __device__ __forceinline__ void reach(int, int, int &lo, int &hi) const { lo = first; hi = last; }
+  __device__ __forceinline__ bool nobody() const { return none; }
 };
 typedef Unit<TwoRows, Found> Share;
 
@@ -89,7 +91,8 @@ __device__ __forceinline__ void first_entries(const Cache &c, const Share &w, Fi
 }
 
 // Tile `tile` of all groups' rows, one group after the other, with split z of its group's prefix.  A token without a position (it
-// has no result) counts as one that sees all, so that it costs the others nothing.
+// has no result) counts as one that sees all, with a query of zeros, so that it costs the others nothing, whatever its bits: a NaN there made the
+// tile one of careful passes (64 single tokens behind 8191, one of them such a place, 36 us / 675).
 template <class C, int HD, int TR>
 __device__ __forceinline__ bool prefix_unit(const Cache &c, const Prefixes &x, const Batch &b, const AttnArgs &a, int tile, int z, int head, Share &w,
                                             First<FirstOf<C, HD, TR>::N> &first) {
@@ -153,7 +156,8 @@ __device__ __forceinline__ bool prefix_unit(const Cache &c, const Prefixes &x, c
     }
     p = position_of(b, s, t);
   }
-  if (p < 0) p = kEverything;
+  const bool none = p < 0;
+  if (none) p = kEverything;
   int lo = p, hi = p;
 #pragma unroll
   for (int d = 1; d < (TR == kAttnRows ? 16 : 32); d <<= 1) {
@@ -162,7 +166,7 @@ __device__ __forceinline__ bool prefix_unit(const Cache &c, const Prefixes &x, c
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   hi = __builtin_amdgcn_readfirstlane(hi);
-  w.rows = {p, lo, hi};
+  w.rows = {p, lo, hi, none};
   w.sp = {lo, hi, 0, 0, n};
   w.first_token = t0;
   w.row0 = t0;
@@ -191,11 +195,11 @@ __device__ __forceinline__ bool own_unit(const Cache &c, const Prefixes &x, cons
   parts = split_count(keys, a.n_splits, a.split_len);
   if (z >= parts) return false;
   w.sp = {lo, hi, 0, low, keys};
-  if constexpr (TR == kAttnRows) w.rows = {new_position(len, count, a.by_rep.quot(my_row<TR>(r0, w.r1))), lo, hi};
+  if constexpr (TR == kAttnRows) w.rows = {new_position(len, count, a.by_rep.quot(my_row<TR>(r0, w.r1))), lo, hi, false};
   else {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w0 = min(r0 + wave * 32, w.r1), w1 = min(w0 + 31, w.r1);
     w.rows = {new_position(len, count, a.by_rep.quot(my_row<TR>(r0, w.r1))), new_position(len, count, a.by_rep.quot(w0)),
-              new_position(len, count, a.by_rep.quot(w1))};
+              new_position(len, count, a.by_rep.quot(w1)), false};
   }
   w.keys = {x.table + (long long)max(g, 0) * x.table_stride, b.table + (long long)s * b.table_stride, n};
   w.i0 = z * each;

@@ -158,6 +158,40 @@ def test_queries_of_places_without_a_sequence(kind, bad, how):
         assert torch.equal(B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q), clean) and not bool(clean[places].any())
 
 
+def least_ms(f, calls=10):
+    f()
+    best = math.inf
+    for _ in range(7):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        for _ in range(calls):
+            f()
+        end.record()
+        end.synchronize()
+        best = min(best, begin.elapsed_time(end) / calls)
+    return best
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("prefix,n", [(30000, 24), (8191, 64), (8191, 6)])
+def test_queries_of_places_without_a_sequence_cost_nothing(kind, prefix, n):
+    """Not finite queries of such places leave the bits of all others (see above), and their time: a tile that is computed twice takes three to twenty
+    times as long, a call's best time over several tries differs by a few hundredths."""
+    for new in ([1] * n, [1 + i % 3 for i in range(n)]):
+        lens = [prefix + 9 + i + m for i, m in enumerate(new)]
+        lens[1] = lens[n - 2] = 0
+        st = Shared(kind, 8, 64, 16, lens, new, [(prefix, n)], ragged=max(new) > 1, seed=24)
+        q = st.randn(st.tokens, 32, 64)
+        call = lambda: B.river_prefix_attention(st.pages, 0, st.batch, st.prefixes, q)
+        places = torch.tensor([t for s, t, _ in st.positions() if s in (1, n - 2)], device=DEV)
+        q[places] = 0.0
+        clean, usual = call(), least_ms(call)
+        for bad in (math.nan, math.inf):
+            q[places] = bad
+            assert least_ms(call) < 1.5 * usual, (bad, usual)
+            assert torch.equal(call(), clean)
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("groups,own,new", [([(20000, 2)], [100, 3000], [1, 1]), ([(50, 2)], [20000, 10], [1, 1]), ([(9000, 2)], [100, 5], [20, 33])], ids=str)
 @HOW
