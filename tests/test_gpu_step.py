@@ -172,6 +172,36 @@ def test_build_gives_back_what_it_gave():
     assert sorted(dev.free.tolist()) == list(range(m.n_pages)) and bool((dev.table == -1).all()) and not bool(dev.lens.any())
 
 
+@pytest.mark.parametrize("ps,pages,n", [(16, 8192, 1), (1, 20000, 1), (16, 1875, 4), (4, 300, 70)])
+def test_build_of_long_sequences_that_come_and_leave(ps, pages, n):
+    """Thousands of pages at once, with and without a slot map: they take about as long (with a wavefront in place of a workgroup: two to eight times)."""
+    m = Model([[-1] * (pages + 2) for _ in range(n)], [0] * n, [int(x) for x in np.random.default_rng(7).permutation(n * pages)], n * pages, ps)
+    dev = Device(m)
+    most = [pages * ps - s % ps for s in range(n)]
+    dev.step(most, sum(most), ("refused",))
+    if n > 1:
+        dev.step([0, -most[1], 1] + [0] * (n - 3), 1)
+    dev.step([LOWEST] * n, 0, ())
+    assert dev.n_free.item() == n * pages
+    up, down = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (most, [LOWEST] * n))
+    slots = torch.zeros(1024, dtype=torch.int64, device=DEV)
+
+    def least_ms(slots):
+        best = math.inf
+        for _ in range(12):
+            B.river_build_batch(dev.tables, up, dev.q_start)
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            B.river_build_batch(dev.tables, down, dev.q_start, slots)
+            end.record()
+            end.synchronize()
+            best = min(best, begin.elapsed_time(end))
+        return best
+    if n * pages >= 7500:
+        assert least_ms(None) < 1.5 * least_ms(slots)
+        assert least_ms(slots[:4]) < 1.5 * least_ms(slots)
+
+
 def test_build_ahead_of_a_step():
     m, r = fresh(4, 40, 16, 100, 200)
     dev = Device(m, lens_out=True)
