@@ -397,7 +397,7 @@ int river_prefix_attention(const river_pages *pages, int32_t layer, const river_
 /* Writes keys and values as they are (rounded once to the cache's type) to slots of `layer`: token t's to slot slots[t] % page_size of
  * page slots[t] / page_size.  A slot below 0, or of no page, is left out: a place of the batch without a token.  Two tokens
  * must not have the same slot.
- * slots: DEVICE [n_tokens], 8-byte aligned.  k, v: as in river_rope_store. */
+ * slots: DEVICE [n_tokens], 8-byte aligned.  k, v: as in river_rope_store, rows of at most 2^18 elements. */
 int river_store_slots(const river_pages *pages, int32_t layer, const int64_t *slots, int32_t n_tokens, const void *k, int64_t k_stride,
                       const void *v, int64_t v_stride, void *hip_stream);
 

@@ -840,7 +840,9 @@ def river_store_slots(pages: Pages, layer: int, slots: torch.Tensor, k: torch.Te
 class Tables(_Fixed):
     """A page table that lives on the device alone, and its free list: table [n_seq, max_pages], lens [n_seq], free_pages [n_pages], n_free [1]
     and, where rows begin with pages of somebody else, n_shared [n_seq]; all int32, the caller's, and changed by river_build_batch.  lens_out
-    and n_free_out: where it writes lengths and count instead (a step laid out ahead of being taken)."""
+    and n_free_out: where it writes lengths and count instead (a step laid out ahead of being taken).  A sequence that has given back positions
+    in its first n_shared pages and asks again writes over those entries, or into those pages: lower its n_shared, and copy the page in which it ends,
+    before it does."""
 
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int,
                  n_shared: torch.Tensor | None = None, lens_out: torch.Tensor | None = None, n_free_out: torch.Tensor | None = None):

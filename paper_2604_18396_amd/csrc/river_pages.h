@@ -11,8 +11,9 @@ namespace pg {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-// n / d for 0 <= n < 2^31 and 1 <= d <= 2^16 as a product: with 2^s >= d and m = ceil(2^(31+s) / d) the error m d - 2^(31+s)
-// is below d <= 2^s, so (n m) >> (31+s) is exact (Granlund and Montgomery, 1994).
+// n / d for 0 <= n < 2^31 and 1 <= d < 2^31 as a product: with the least 2^s >= d and m = ceil(2^(31+s) / d) the error m d - 2^(31+s)
+// is below d <= 2^s, so (n m) >> (31+s) is exact (Granlund and Montgomery, 1994).  m has 32 bits: d is 1 or at least 2^(s-1) + 1, and 2^(31+s) / d at most
+// 2^32 - 2^32 / (2^(s-1) + 1), which is 2 and more below 2^32 as s <= 31.
 struct Div {
   uint32_t d, m, s;
   __device__ __forceinline__ int quot(int n) const { return (int)(__umulhi(2u * (uint32_t)n, m) >> s); }
@@ -274,8 +275,9 @@ struct AttnArgs {
   int n_splits, split_len, tiles, tile_rows;   // of the keys; tiles of rows per sequence and key head
   int turn_s, turn_z;                     // see work_of
   int max_new;                            // new tokens of a sequence beyond these are left out
-  float *part_o;                          // [n_seq][max_new][nq][n_splits][HD], where a tile has several splits
-  float2 *part_ml;                        // [n_seq][max_new][nq][n_splits] maximum (base 2) and sum
+  float *part_o;                          // [n_seq][max_new][nq][n_splits][HD], where a tile has several splits.  With common prefixes
+                                          // [n_tokens][nq][splits of a prefix + n_splits][HD]
+  float2 *part_ml;                        // the same without HD: maximum (base 2) and sum
   unsigned int *tickets;                  // [sequences x key heads x tiles] workgroups that are done; zero between calls (null: a
                                           // launch of its own joins the splits)
 };

@@ -66,7 +66,8 @@ typedef Unit<TwoRows, Found> Share;
 
 constexpr int kAttnRows = 16;              // of a tile of split_unit
 // Steps of a prefix's keys in flight in many_unit: here they come from memory, where the prompts of k_attn_many read them again and again
-// (us with two / four: 64 sequences behind 8191 58.1 / 53.8, 24 behind 131071 133 / 125, at head size 64 92 / 87; five there 92, and no place at 128)
+// (us with two / four: 64 sequences behind 8191 59.2 / 56.5, 24 behind 131071 133 / 133, at head size 64 84 / 81; with one product a probability 58.1 / 53.8,
+// 133 / 125, 92 / 87; five there 92, and no place at 128)
 constexpr int kAhead = 4;
 constexpr int kEverything = 1 << 30;       // a position that sees every key
 template <int TR>
@@ -221,7 +222,8 @@ struct ShareLds {
   static constexpr int BYTES = (PM && OM) || MANY > SPLIT + RES ? MANY : SPLIT + RES;
 };
 // Both kinds in one kernel take more than the 168 registers that leave three workgroups a CU at head size 64: two (24 sequences behind
-// 131071 85 -> 75 us, without the 20 registers that were spilled).
+// 131071 85 -> 75 us, without the 20 registers that were spilled).  What is still spilled: 11 registers of fp32 rows at head size 128, 3 of rows over half pages
+// there, 11 of tiles with two numbers a probability, 5 or 6 of tiles at 64: in front of a pass or of the results, and in careful passes.
 template <class T, class C, int HD, bool PM, bool OM, bool TWO>
 __global__ __launch_bounds__(kAttnThreads, HD == 64 && !(PM && !OM) ? 3 : 2) void k_share(Cache c, Batch b, AttnArgs a, Prefixes x) {
   extern __shared__ __align__(1024) char lds[];

@@ -39,7 +39,7 @@ struct SharePlan {
 // Prefixes have units of their own where that saves enough of reading them for each sequence: 24 MB, or 8 MB of a long one.  (A call then
 // takes two launches, and its parts are written and read.  us, apart / each sequence through its prefix, 8B shape, 64 positions of their own:
 // 2 sequences behind 1024 11.7 / 9.9, behind 4096 12.8 / 15.5; 8 behind 1024 12.1 / 11.9; 16 behind 256 11.8 / 9.8, behind 1024 12.9 / 19.7;
-// 64 behind 16384 40 / 472; 1B shape: 2 behind 4096 11.8 / 11.6, 16 behind 1024 11.8 / 11.6, 32 behind 1024 12.0 / 14.6.)
+// 64 behind 16384 48 / 471; 1B shape: 2 behind 4096 11.8 / 11.6, 16 behind 1024 11.8 / 11.6, 32 behind 1024 12.0 / 14.6.)
 constexpr double kSaves = 24e6, kSavesLong = 8e6;
 constexpr int kLong = 4096;
 // Several new tokens of 16-bit types: sequences whose rows nearly fill tiles of 128 read their prefixes hardly more often than a group's tiles do.
@@ -62,14 +62,14 @@ bool pays(const river_pages *p, const river_batch *b, int nq, const AttnPlan &o,
                        (double)b->n_tokens * nq * 2 * (p->head_dim * 4 + 8) * 2 / 4e6 + 14;
   return apart < through;
 }
-// Splits of a prefix: more than a CU each under one key head have no place (us, at most 64 / 256, one key head of 128: 14 sequences behind 131071 59 / 32,
-// two key heads, 16 behind 100000 53 / 38; head size 64, 14 behind 62852 28.4 / 21.5)
+// Splits of a prefix: more than a CU each under one key head have no place (us, at most 64 / 256, one key head of 128: 14 sequences behind 131071 67 / 37,
+// two key heads, 16 behind 100000 59 / 44; head size 64, 14 behind 62852 31.0 / 21.8)
 constexpr int kMostSplits = 256;
 // Splits of the prefixes, as workgroups: one a CU, or seven on four CUs (the eighth place is for the sequences) where that leaves them 1024
 // keys of head size 128, 512 of 64, and where the sequences have no more keys of their own than the prefixes; six on four where three have place on a CU.
-// (us, 256 / 448, 1B shape, up to 100 own positions: 24 sequences behind 30000 31.1 / 29.1, behind 40000 35.8 / 32.2, 32 behind 48000 42.1 / 38.5, 48 behind
-// 20000 33.9 / 32.1, 18 of 64 heads behind 20937 35.4 / 30.2; 64 of up to 900 behind 16384 43.4 / 46.8; 8B shape, 64 of up to 900 behind 30000 80.1 / 87.5,
-// 32 of up to 2047 behind 60000 95.9 / 102.2)
+// (us, 256 / 448, 1B shape, up to 100 own positions: 24 sequences behind 30000 33.4 / 32.2, behind 40000 38.1 / 35.5, 32 behind 48000 43.9 / 41.0, 48 behind
+// 20000 37.7 / 35.1, 18 of 64 heads behind 20937 39.7 / 34.7; 64 of up to 900 behind 16384 39.6 / 44.2; 8B shape, 64 of up to 900 behind 30000 84.6 / 86.3,
+// 32 of up to 2047 behind 60000 100.9 / 101.3)
 long long prefix_places(int head_dim, bool three, double common, double tiles, double groups, double own_keys) {
   
 #ifdef FIT
@@ -86,9 +86,9 @@ bool unequal(const river_pages *p, const AttnPlan &o, double tiles, double group
   return common * (1. / o.n_splits - 1. / splits) * (p->head_dim == 128 ? 0.014 : 0.0063) > 12;
 }
 // By tiles of 128 rows (many_unit) where rows x keys x elements of a key head are more than these: they read a key once for 128 rows, those of 16 take
-// less time to begin and end (us, 128 / 16, 8B shape: 32 rows behind 4096 17.7 / 15.1, behind 16384 25.3 / 26.0; 128 behind 1024 17.0 / 15.8,
-// behind 4096 23.1 / 25.9; 256 behind 1024 18.2 / 21.5; 1B shape: 64 behind 16384 23.1 / 24.1, 128 behind 4096 16.9 / 16.7, 256
-// behind 4096 18.9 / 24.0)
+// less time to begin and end (us, 128 / 16, single tokens, 8B shape: 32 rows behind 4096 19.1 / 15.8, behind 16384 28.6 / 26.7, behind 60000 51 / 86; 128
+// behind 1024 18.1 / 16.2, behind 4096 25.2 / 26.0; 256 behind 1024 19.6 / 22.0; 1B shape: 64 behind 16384 22.4 / 29.2, 128 behind 4096 18.7 / 20.5, 256
+// behind 4096 18.6 / 29.1)
 #ifndef KMANY
 #define KMANY 3e8
 #endif
@@ -135,9 +135,9 @@ SharePlan plan_share(const river_pages *p, const river_batch *b, const river_pre
     const long long p_groups = std::max(1ll, std::min<long long>(y.p_tiles, groups * full) * p->n_kv_heads);
     // Splits of the prefixes: see prefix_places.  But no more than it takes to be done (20 ns a key) in two fifths of the time that
     // all keys take to stream: every split is one more part of each row.
-    // (us by splits: 24 sequences behind 131071 positions, 8 tiles and heads, 32 132, 48 128, 56 122, 64 125; 32 behind 65536 32 77.5, 56 77.6,
-    // 64 83; 32 behind 32768 32 48, 56 53; 64 of 225 .. 900 own positions behind 8191, 16 tiles and heads, 6 58, 8 53.8, 12 57.4, 16 59;
-    // head size 64: 24 behind 131071 32 90, 48 79, 64 73 .. 77; 48 behind 16384, 16 tiles and heads, 16 29.8, 24 30.2, 32 31.1)
+    // (us by splits: 24 sequences behind 131071 positions, 8 tiles and heads, 32 142, 48 140, 56 132, 64 130; 32 behind 65536 32 80, 48 82, 56 82,
+    // 64 80; 32 behind 32768 32 47, 48 53, 56 51; 64 of 225 .. 900 own positions behind 8191, 16 tiles and heads, 6 64, 8 56.5, 12 60.2, 16 61;
+    // head size 64: 24 behind 131071 32 93, 48 89, 56 80, 64 75; 48 behind 16384, 16 tiles and heads, 16 33, 24 35, 28 32, 32 34)
     const double stream = (groups * (double)common + (double)b->n_seq * own) * key_bytes / 5e6;
     const bool three = p->head_dim == 64 && !y.p_many;           // (workgroups that have place on a CU: see k_share)
     const long long places = three ? 768 : 512, fit = prefix_places(p->head_dim, three, (double)common, (double)p_groups, (double)groups, (double)b->n_seq * own);

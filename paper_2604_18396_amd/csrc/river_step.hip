@@ -59,7 +59,7 @@ extern "C" int river_store_slots(const river_pages *pages, int32_t layer, const 
     if (layer < 0 || layer >= pages->n_layers) return refuse("layer out of range");
     if (n_tokens < 0 || n_tokens > kMostTokens) return refuse("more than 2^22 tokens in a call, or a negative number");
     const long long kw = (long long)pages->n_kv_heads * pages->head_dim;
-    if (kw > (1 << 18)) return refuse("too many key heads");
+    if (kw > (1 << 18)) return refuse("too many key heads");    // (2^17 pieces a token at most)
     if (k_stride < kw || v_stride < kw) return refuse("a stride is smaller than its row");
     const int es = elem_bytes(pages);
     if (((uintptr_t)k | (uintptr_t)v) % es || (uintptr_t)slots % 8) return refuse("misaligned keys, values or slots");

@@ -309,6 +309,21 @@ def test_store(kind, hd, nkv, ps, n, pad):
         assert torch.equal(k, want[0]) and torch.equal(v, want[1])
 
 
+@pytest.mark.parametrize("kind", TYPES)
+def test_store_of_the_widest_rows(kind):
+    # (2^18 elements of keys: pieces of a token are counted up to 2^17)
+    act, kvt = TYPES[kind]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    for nkv, hd in ((2048, 128), (2047, 128), (4096, 64)):
+        k, v = (torch.zeros(1, 3, nkv, 3, hd, dtype=kvt, device=DEV) for _ in range(2))
+        new_k, new_v = (torch.randn(7, nkv, hd, generator=g, device=DEV).to(act) for _ in range(2))
+        slots = torch.tensor([8, 0, -1, 4, 5, 9, 7], device=DEV)
+        want = want_store(k, v, slots, new_k, new_v, 0, 3)
+        B.river_store_slots(B.Pages(k, v, act), 0, slots, new_k, new_v)
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
 def test_store_keeps_bits():
     # what a type has of infinities and NaN stays as it is; bf16 beyond fp16's range is infinite
     x = torch.tensor([math.nan, math.inf, -math.inf, 1e30, -0.0, 1e-30, 65504.0, 70000.0] * 8, device=DEV)
