@@ -33,10 +33,12 @@ extern "C" int river_build_batch(const river_tables *t, const int32_t *n_new, in
                       t->table_stride, t->n_pages, t->page_size, n_tokens, (int)std::min<long long>((long long)t->max_pages * t->page_size, kMostPositions),
                       div_by(t->page_size), q_start, (long long *)slots, positions, refused};
     const bool tokens = slots || positions, apart = tokens && n_tokens > kTokensInOne;
-    // Threads: one a token or an entry of the table (any of which may come or go), as far as one workgroup reaches, and one a sequence.  (us, taken and given
-    // back, one a sequence / one an entry too: a sequence of 8192 pages 85 / 17.7, of 131072 1286 / 165, 64 of 188 60.6 / 27.2; a few pages the same)
-    const long long entries = (long long)t->n_seq * t->max_pages;
-    const int threads = (int)std::min<long long>(kBuildThreads, (std::max<long long>({64, 4 * t->n_seq, tokens ? n_tokens : 0, entries}) + 63) / 64 * 64);
+    // Threads: one a token or a sixteenth of the table's entries, as far as one workgroup reaches, and four a sequence.  Any entry may come or go, and most do not:
+    // a wavefront more takes longer to meet.  (us, taken and given back, without entries / a sixteenth / all: a sequence of 8192 pages 85 / 19.0 / 17.7, of 131072
+    // 1286 / 165 / 165, 64 of 188 60.6 / 27.2 / 27.2; drafts of 64 sequences that have 252 entries each
+    // 11.5 / 11.6 / 11.6, the kernel that gives them back 3.9 / 5.0 / 5.0; a token of four that have 77 the same)
+    const long long some = (long long)t->n_seq * t->max_pages / 16;
+    const int threads = (int)std::min<long long>(kBuildThreads, (std::max<long long>({64, 4 * t->n_seq, tokens ? n_tokens : 0, some}) + 63) / 64 * 64);
     const size_t lds = (3 * (size_t)t->n_seq + 1) * 4;
     const hipStream_t st = (hipStream_t)hip_stream;
     auto go = [&](auto k) { return launch(k, dim3(1), dim3(threads), lds, st, a); };
