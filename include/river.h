@@ -387,7 +387,8 @@ typedef struct {
  * its own positions.  A token whose position is below the prefix's length sees what comes up to it.
  * Arguments, errors and roundings as in river_paged_attention (which probabilities over bf16 pages are rounded to bf16 follows from a sequence's own
  * rows, whatever its group has), tickets and a max_new that leaves tokens out among them.
- * workspace: as there, of the bytes that river_prefix_attention_workspace gives. */
+ * workspace: as there, of the bytes that river_prefix_attention_workspace gives: parts of every token for as many splits as the longest prefix
+ * that the bounds allow may have (hundreds of MB where hundreds of tokens stand beside a prefix of 100000 positions). */
 int river_prefix_attention_workspace(const river_pages *pages, const river_batch *batch, const river_prefixes *prefixes,
                                      int32_t n_q_heads, size_t *bytes);
 int river_prefix_attention(const river_pages *pages, int32_t layer, const river_batch *batch, const river_prefixes *prefixes,

@@ -879,9 +879,9 @@ __global__ __launch_bounds__(kAttnThreads, HD == 64 ? 3 : 2) void k_attn_split(C
 // what was the maximum (one of 32 rows has a new maximum in most steps, and rescaling takes half as long as the step).
 // A probability is rounded once to the pages' type, and the sum is of what is multiplied: over bf16 pages that leaves out up to half a step of the
 // result (4096 tokens: off by 2.1e-3 of the norm, 1.6e-3 with fp32 ones); a second product, as in k_attn_split, would cost a third of the time.
-// Rows of sequences that have few each have it all the same (TWO; common prefixes): it costs 2 .. 10 us of a stream that a few tiles read (8B shape,
-// 64 single tokens behind 8191 53.6 -> 56.1, 24 behind 131071 121 -> 132, with a clock 5 % lower), and would cost 20 if wavefronts without rows
-// took part in the products (24 behind 131071 141, 8 behind it 107 -> 131, as it is 113; 1B shape 67 -> 80, as it is 60).
+// Rows of sequences that have few each have it all the same (TWO; common prefixes): it costs 5 .. 21 % of a stream (8B shape, 64 single
+// tokens behind 8191 53.6 -> 56.5 us, behind 100000 158 -> 192, 24 behind 131071 121 -> 133), and would cost more if
+// wavefronts without rows took part in the products (24 behind 131071 141, 8 behind it 107 -> 131, as it is 113; 1B shape 67 -> 80, as it is 60).
 // Keys and values go from memory straight into LDS (no registers, AHEAD steps in flight), in rings, one barrier a step; where a key's
 // row lies is looked up for CHUNK steps at once.
 // 8B shape, 4096 tokens: 148 .. 158 us by the box, 870 .. 930 TFLOP/s; 2048 behind 16384 615 us, 950; the largest matrix products of the library reach 1250.

@@ -45,3 +45,26 @@ def test_block_end_of_a_batched_step_takes_no_more_registers_than_it_did(tmp_pat
     this one 18 registers larger and slower, in every block of every batched step."""
     (f,) = [f for n, f in kernels(tmp_path).items() if "k_bd_block_end" in n]
     assert int(f["vgpr_count"]) <= 124 and int(f["private_segment_fixed_size"]) == 0, f
+
+
+def test_paged_kernels_spill_next_to_nothing(tmp_path):
+    """Kernels of the paged cache, of steps laid out on the device and of common prefixes: attention over tiles has a few registers in scratch memory, which lie
+    outside its steps; more of them would lie in them, behind the keys and values that a wavefront has in flight."""
+    kernels(tmp_path)                                            # (skips without the tools; the whole section lies in `bundle` then)
+    parts = (tmp_path / "bundle").read_bytes().split(b"__CLANG_OFFLOAD_BUNDLE__")[1:]
+    found = {}
+    for i, part in enumerate(parts):
+        bundle, code = str(tmp_path / f"bundle{i}"), str(tmp_path / f"code{i}")
+        with open(bundle, "wb") as f:
+            f.write(b"__CLANG_OFFLOAD_BUNDLE__" + part)
+        subprocess.run([f"{LLVM}/clang-offload-bundler", "--unbundle", "--type=o", f"--input={bundle}", f"--output={code}",
+                        "--targets=hipv4-amdgcn-amd-amdhsa--gfx950"], check=True)
+        notes = subprocess.run([f"{LLVM}/llvm-readelf", "--notes", code], check=True, capture_output=True, text=True).stdout
+        for entry in notes.split("  - .agpr_count")[1:]:
+            fields = dict(re.findall(r"^ {4}\.(\w+): +(\S+)$", entry, re.M))
+            found[fields["name"]] = fields
+    names = [n for n in found if re.search(r"k_share|k_attn_(split|many|join)|k_build|k_slots|k_store_slots", n)]
+    assert len(names) > 50
+    for n in names:
+        may = 48 if re.search(r"7k_shareI|k_attn_manyI", n) else 0
+        assert int(found[n]["private_segment_fixed_size"]) <= may, (n, found[n])
