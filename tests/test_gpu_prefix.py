@@ -175,8 +175,8 @@ def least_ms(f, calls=10):
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("prefix,n", [(30000, 24), (8191, 64), (8191, 6)])
 def test_queries_of_places_without_a_sequence_cost_nothing(kind, prefix, n):
-    """Not finite queries of such places leave the bits of all others (see above), and their time: a tile that is computed twice takes three to twenty
-    times as long, a call's best time over several tries differs by a few hundredths."""
+    """Not finite queries of such places leave the bits of all others (see above), and their time: a tile that is computed twice takes four to
+    nineteen times as long; a call's best time over several tries differs by a few hundredths, under a clock that falls meanwhile by up to 1.5."""
     for new in ([1] * n, [1 + i % 3 for i in range(n)]):
         lens = [prefix + 9 + i + m for i, m in enumerate(new)]
         lens[1] = lens[n - 2] = 0
@@ -188,7 +188,7 @@ def test_queries_of_places_without_a_sequence_cost_nothing(kind, prefix, n):
         clean, usual = call(), least_ms(call)
         for bad in (math.nan, math.inf):
             q[places] = bad
-            assert least_ms(call) < 1.5 * usual, (bad, usual)
+            assert least_ms(call) < 2 * usual, (bad, usual)
             assert torch.equal(call(), clean)
 
 
